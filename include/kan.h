@@ -5,7 +5,9 @@
  * truncated-power form (paper: Sec. 2 "Step 4", eq. truncated for cubics and
  * eq. general_truncated for other degrees, with the bounded coordinate of
  * eq. bounded) and contracts it with the spline coefficients plus the SiLU
- * base branch (eq. kan_forward); it also computes the layer's gradients.
+ * base branch (eq. kan_forward); it also computes the layer's gradients.  Beside the
+ * layer stand the operators of a training or serving step around it: layer norm, which
+ * holds a layer's inputs on its grid.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -461,6 +463,74 @@ kan_status kan_layer_forward_noalloc(const kan_grid* grid, kan_dtype dtype, int6
  * enough for the packed weights of a 784 -> 256 layer with G = 10 in fp32
  * (11.2 MB) or of a 128 -> 128 layer with G = 200 in fp32 (13.4 MB). */
 #define KAN_NOALLOC_SCRATCH_BYTES (16u << 20)
+
+/*
+ * kan_layer_norm -- layer norm of each row, with the residual sum before it:
+ *
+ *   h[b, i] = x[b, i] + residual[b, i]            (h = x without a residual)
+ *   mean[b] = mean_i h[b, i],  rstd[b] = 1 / sqrt(mean_i (h[b, i] - mean[b])^2 + eps)
+ *   y[b, i] = (h[b, i] - mean[b]) rstd[b] weight[i] + bias[i]
+ *
+ * Between KAN layers it holds the inputs on the grid; the residual stream goes on in h.
+ *
+ *   dtype        of x, residual, h and y
+ *   param_dtype  of weight and bias: KAN_F32, or dtype
+ *   x, residual  [rows, n]   residual NULL: none
+ *   weight, bias [n]         NULL: 1 and 0
+ *   h            [rows, n]   the sum, for the backward and the residual stream; NULL: not
+ *                            written (must be NULL without a residual)
+ *   y            [rows, n]
+ *   mean, rstd   [rows] fp32, for the backward; both NULL: not written
+ *
+ * Statistics and arithmetic are binary32: the mean corrected by the mean difference from
+ * it, the variance from squared differences; in bf16 y comes from the sum before its
+ * rounding to h.  A NaN or infinity in a row gives NaN in that row's y alone.  With eps = 0
+ * a constant row gives NaN.
+ *
+ * Outputs must not overlap each other or an input.  Returns KAN_OK, KAN_ERR_INVALID_ARG
+ * (rows < 0, n < 1, n > 2^24, rows * n > 2^48, eps negative or not finite, NULL,
+ * misaligned or overlapping pointers with rows > 0), KAN_ERR_UNSUPPORTED (unknown dtype,
+ * bf16 weights with fp32 rows) or KAN_ERR_DEVICE.
+ */
+kan_status kan_layer_norm(kan_dtype dtype, kan_dtype param_dtype, int64_t rows, int32_t n,
+                          const void* x, const void* residual, const void* weight,
+                          const void* bias, float eps, void* h, void* y, float* mean, float* rstd,
+                          void* stream);
+
+/*
+ * kan_layer_norm_backward -- gradients of kan_layer_norm for dy = dL/dy:
+ *
+ *   xh = (h - mean) rstd,  g = dy weight
+ *   dx[b, i]   = rstd[b] (g[b, i] - mean_i g[b, :] - xh[b, i] mean_i (g xh)[b, :]) + dh[b, i]
+ *   dweight[i] = sum_b dy[b, i] xh[b, i],  dbias[i] = sum_b dy[b, i]
+ *
+ * dx is the gradient of x and of the residual alike (both enter as their sum).
+ *
+ *   h            [rows, n]   the sum that the forward normalised (x without a residual)
+ *   mean, rstd   [rows] fp32, the forward's
+ *   weight       [n]         NULL: 1
+ *   dy           [rows, n]
+ *   dh           [rows, n]   gradient that reaches h on the residual stream, added to dx;
+ *                            NULL: none (must be NULL without dx)
+ *   dx           [rows, n]   output, or NULL to skip it
+ *   dweight, dbias  [n] in param_dtype, outputs, either or both NULL to skip them
+ *   workspace    caller-owned, workspace_bytes >= kan_layer_norm_backward_workspace_bytes
+ *                (...), 16-byte aligned, overlapping no other argument: the fp32 partial
+ *                sums of dweight and dbias, added in a fixed order (deterministic).  May be
+ *                NULL without dweight and dbias.
+ *
+ * With rows == 0 the weight gradients are written as 0.  Returns as kan_layer_norm;
+ * KAN_ERR_INVALID_ARG also without any output.
+ */
+kan_status kan_layer_norm_backward(kan_dtype dtype, kan_dtype param_dtype, int64_t rows,
+                                   int32_t n, const void* h, const float* mean, const float* rstd,
+                                   const void* weight, const void* dy, const void* dh, void* dx,
+                                   void* dweight, void* dbias, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* Size in bytes of kan_layer_norm_backward's workspace for rows of this dtype and shape. */
+kan_status kan_layer_norm_backward_workspace_bytes(kan_dtype dtype, int64_t rows, int32_t n,
+                                                   size_t* bytes);
 
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char* kan_status_string(kan_status status);

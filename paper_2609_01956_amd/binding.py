@@ -35,7 +35,9 @@ EXPORTED_SYMBOLS = ("kan_basis_eval", "kan_basis_eval_cdb", "kan_layer_forward",
                     "kan_layer_forward_packed_full_workspace_bytes",
                     "kan_layer_plan", "kan_layer_forward_noalloc", "kan_layer_backward",
                     "kan_layer_backward_workspace_bytes", "kan_layer_forward_span",
-                    "kan_layer_forward_span_workspace_bytes", "kan_status_string",
+                    "kan_layer_forward_span_workspace_bytes", "kan_layer_norm",
+                    "kan_layer_norm_backward", "kan_layer_norm_backward_workspace_bytes",
+                    "kan_status_string",
                     "kan_abi_version")
 
 _VP = ctypes.c_void_p
@@ -117,6 +119,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
             lib.kan_layer_forward_span_workspace_bytes.argtypes = \
                 lib.kan_layer_forward_workspace_bytes.argtypes
             lib.kan_layer_forward_span_workspace_bytes.restype = ctypes.c_int
+            lib.kan_layer_norm.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_int64,
+                                           ctypes.c_int32, _VP, _VP, _VP, _VP, ctypes.c_float, _VP,
+                                           _VP, _VP, _VP, _VP]
+            lib.kan_layer_norm.restype = ctypes.c_int
+            lib.kan_layer_norm_backward.argtypes = [
+                ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.c_int32, _VP, _VP, _VP, _VP, _VP,
+                _VP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]
+            lib.kan_layer_norm_backward.restype = ctypes.c_int
+            lib.kan_layer_norm_backward_workspace_bytes.argtypes = [
+                ctypes.c_int, ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+            lib.kan_layer_norm_backward_workspace_bytes.restype = ctypes.c_int
             lib.kan_status_string.argtypes = [ctypes.c_int]
             lib.kan_status_string.restype = ctypes.c_char_p
             lib.kan_abi_version.argtypes = []
@@ -299,6 +312,34 @@ def kan_layer_forward_packed_full_workspace_bytes(grid: kan_grid, dtype: int, ba
         ctypes.byref(grid), int(dtype), int(batch), int(in_features), int(out_features),
         ctypes.byref(n)))
     return st, int(n.value)
+
+
+def kan_layer_norm(dtype: int, param_dtype: int, rows: int, n: int, x: int, residual: int,
+                   weight: int, bias: int, eps: float, h: int, y: int, mean: int, rstd: int,
+                   stream: int = 0) -> int:
+    """Raw call: device addresses as integers (0 for NULL); returns the kan_status code."""
+    return int(load_library().kan_layer_norm(
+        int(dtype), int(param_dtype), int(rows), int(n), _VP(x), _VP(residual), _VP(weight),
+        _VP(bias), float(eps), _VP(h), _VP(y), _VP(mean), _VP(rstd), _VP(stream)))
+
+
+def kan_layer_norm_backward(dtype: int, param_dtype: int, rows: int, n: int, h: int, mean: int,
+                            rstd: int, weight: int, dy: int, dh: int, dx: int, dweight: int,
+                            dbias: int, workspace: int, workspace_bytes: int,
+                            stream: int = 0) -> int:
+    """Raw call: device addresses as integers (0 for NULL); returns the kan_status code."""
+    return int(load_library().kan_layer_norm_backward(
+        int(dtype), int(param_dtype), int(rows), int(n), _VP(h), _VP(mean), _VP(rstd),
+        _VP(weight), _VP(dy), _VP(dh), _VP(dx), _VP(dweight), _VP(dbias), _VP(workspace),
+        ctypes.c_size_t(workspace_bytes), _VP(stream)))
+
+
+def kan_layer_norm_backward_workspace_bytes(dtype: int, rows: int, n: int) -> Tuple[int, int]:
+    """Raw call: returns (kan_status, bytes)."""
+    size = ctypes.c_size_t(0)
+    st = int(load_library().kan_layer_norm_backward_workspace_bytes(
+        int(dtype), int(rows), int(n), ctypes.byref(size)))
+    return st, int(size.value)
 
 
 def check(status: int) -> None:
@@ -602,3 +643,113 @@ def layer_forward_span(x, coef, base_w, grid_size: int, grid_lo: float = -1.0,
                 x.data_ptr(), coef.data_ptr(), base_w.data_ptr(), workspace.data_ptr(),
                 workspace.numel(), out.data_ptr(), _stream(x.device)))
     return out
+
+
+# ------------------------------------------------- the step around the layers
+
+def _ptr(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _same(what: str, like, *ts) -> None:
+    """Tensors (or None) of one shape, dtype and device, contiguous."""
+    for t in ts:
+        if t is not None and (t.shape != like.shape or t.dtype != like.dtype or
+                              t.device != like.device or not t.is_contiguous()):
+            raise ValueError(f"{what} must match each other in shape, dtype and device and be "
+                             "contiguous")
+
+
+def _norm_params(x, *ts) -> int:
+    """Checks a norm's parameters (or None) against x [..., n]: their dtype code."""
+    given = [t for t in ts if t is not None]
+    if not given:
+        return _dtype_code(x)
+    _require_device(x, *given)
+    for t in given:
+        if tuple(t.shape) != (x.shape[-1],) or t.dtype != given[0].dtype:
+            raise ValueError("the norm's parameters must be [n] of one dtype for rows of n")
+    return _dtype_code(given[0])
+
+
+def _rows(x) -> Tuple[int, int]:
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("expected rows [..., n] with n >= 1")
+    return x.numel() // x.shape[-1], x.shape[-1]
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None,
+               need_stats: bool = True, out=None):
+    """kan_layer_norm over the last dimension of x [..., n], with `residual` (shaped like x)
+    added first -> (y, h, mean, rstd): h = x + residual (x itself without one), mean and rstd
+    [...] fp32 for layer_norm_backward (None without need_stats).  weight and bias [n] are
+    fp32 or of x's dtype.  `out`, a (y, h) tuple (h None without a residual), receives the
+    results instead of fresh tensors."""
+    torch = _torch()
+    _require_device(x)
+    rows, n = _rows(x)
+    pdt = _norm_params(x, weight, bias)
+    _same("x and residual", x, residual)
+    if out is None:
+        y = torch.empty_like(x)
+        h = None if residual is None else torch.empty_like(x)
+    else:
+        y, h = out
+        if (h is None) != (residual is None) or y is None:
+            raise ValueError("out is (y, h), h with a residual only")
+        _same("x and out", x, y, h)
+    mean = rstd = None
+    if need_stats:
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
+    check(_call(x.device, _library().kan_layer_norm, _dtype_code(x), pdt, rows, n, x.data_ptr(),
+                _ptr(residual), _ptr(weight), _ptr(bias), eps, _ptr(h), y.data_ptr(), _ptr(mean),
+                _ptr(rstd), _stream(x.device)))
+    return y, x if residual is None else h, mean, rstd
+
+
+def layer_norm_backward(h, mean, rstd, weight, dy, dh=None, need_dx: bool = True,
+                        need_dw: bool = True, workspace=None, out=None):
+    """Gradients of layer_norm (kan_layer_norm_backward): h, mean and rstd as it returned
+    them, weight as it was given (None: 1), dy like h, dh (like h, or None) the gradient that
+    reaches h on the residual stream -> (dx or None, dweight or None, dbias or None); dx is
+    the gradient of x and of the residual.  dweight and dbias have weight's dtype (h's
+    without a weight).  `workspace` (a uint8 device tensor) is used when large enough, else a
+    fresh one is taken; `out`, a (dx, dweight, dbias) tuple, receives the gradients."""
+    torch = _torch()
+    _require_device(h, dy)
+    rows, n = _rows(h)
+    pdt = _norm_params(h, weight)
+    _same("h, dy and dh", h, dy, dh)
+    _require_device(h, mean, rstd)
+    for t in (mean, rstd):
+        if t.dtype != torch.float32 or t.shape != h.shape[:-1]:
+            raise ValueError("mean and rstd are fp32, one value per row")
+    if not (need_dx or need_dw):
+        raise ValueError("nothing to compute")
+    dw_dtype = h.dtype if weight is None else weight.dtype
+    if out is not None:
+        dx, dw, db = out
+        dx = dx if need_dx else None
+        dw, db = (dw, db) if need_dw else (None, None)
+        _same("h and dx", h, dx)
+        for t in (dw, db):
+            if t is not None and (tuple(t.shape) != (n,) or t.dtype != dw_dtype or
+                                  t.device != h.device or not t.is_contiguous()):
+                raise ValueError("dweight and dbias must be [n] with the weight's dtype")
+    else:
+        dx = torch.empty_like(h) if need_dx else None
+        dw = torch.empty((n,), dtype=dw_dtype, device=h.device) if need_dw else None
+        db = torch.empty_like(dw) if need_dw else None
+    lib, dt = _library(), _dtype_code(h)
+    ws, nbytes = None, 0
+    if dw is not None or db is not None:
+        size = ctypes.c_size_t(0)
+        check(lib.kan_layer_norm_backward_workspace_bytes(dt, rows, n, ctypes.byref(size)))
+        nbytes, ws = size.value, workspace
+        if ws is None or ws.numel() < nbytes or ws.device != h.device:
+            ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=h.device)
+    check(_call(h.device, lib.kan_layer_norm_backward, dt, pdt, rows, n, h.data_ptr(),
+                mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dy.data_ptr(), _ptr(dh), _ptr(dx),
+                _ptr(dw), _ptr(db), _ptr(ws), nbytes, _stream(h.device)))
+    return dx, dw, db

@@ -371,4 +371,39 @@ struct SpanArgs {
 hipError_t launch_span(bool bf16, const SpanGeom& g, const SpanArgs& a, const void* coef,
                        const void* bw, hipStream_t s);
 
+// ---------------------------------------------------------------- layer norm
+
+struct NormArgs {
+    const void *x, *res, *w, *b;  // res, w, b may be null
+    void *h, *y;                  // h may be null
+    float *mean, *rstd;           // both null or both not
+    int64_t rows;
+    int n;
+    float eps;
+    int shift;  // log2 of the lanes that share a row (one unit per lane)
+};
+struct NormGradArgs {
+    const void *h, *w, *dy, *dh;  // w, dh may be null
+    const float *mean, *rstd;
+    void* dx;     // may be null
+    float* part;  // [2][parts][n] partial weight gradients; null: none wanted
+    int64_t rows;
+    int n;
+    int shift;
+};
+// Longest row that stays in registers.
+constexpr int kNormRegRow = 16384;
+struct NormPlan {
+    int waves;   // waves per row (1, 4, 8), 0: rows longer than kNormRegRow
+    int units;   // 16-byte units per lane
+    int shift;   // log2 of the lanes of a row within a wave (one unit per lane)
+    int blocks;  // workgroups
+    int parts;   // partial weight gradients (backward)
+};
+// es: bytes per element of the rows.
+NormPlan norm_plan(int64_t rows, int32_t n, int es, bool grad);
+hipError_t launch_norm(bool bf16, bool bf16_params, const NormPlan& p, NormArgs a, hipStream_t s);
+hipError_t launch_norm_grad(bool bf16, bool bf16_params, const NormPlan& p, NormGradArgs a,
+                            void* dw, void* db, hipStream_t s);
+
 }  // namespace kan

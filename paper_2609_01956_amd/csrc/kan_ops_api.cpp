@@ -1,0 +1,127 @@
+// kan_ops_api.cpp -- the C ABI of the operators around the layer (layer norm, log
+// probabilities, gradient clipping) declared in include/kan.h: argument validation (host
+// only, before any HIP call), launch planning and dispatch onto the caller's stream.
+#include "kan.h"
+
+#include <cmath>
+#include <cstdint>
+#include <initializer_list>
+
+#include "kan_internal.h"
+
+namespace {
+
+size_t dtype_size(kan_dtype dt) { return dt == KAN_BF16 ? 2 : 4; }
+bool known(kan_dtype dt) { return dt == KAN_F32 || dt == KAN_BF16; }
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+kan_status device_status(hipError_t e) { return e == hipSuccess ? KAN_OK : KAN_ERR_DEVICE; }
+
+// `n` bytes at p (p NULL: not given), of elements of `a` bytes.
+struct Buf {
+    const void* p;
+    size_t n;
+    size_t a;
+};
+
+bool overlap(const Buf& x, const Buf& y) {
+    if (x.p == nullptr || y.p == nullptr || x.n == 0 || y.n == 0) return false;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+    return a < b + y.n && b < a + x.n;
+}
+
+// Every buffer aligned to its elements, no output over another output or an input.
+bool placed(std::initializer_list<Buf> ins, std::initializer_list<Buf> outs) {
+    for (const Buf& i : ins)
+        if (!aligned(i.p, i.a)) return false;
+    for (const Buf* o = outs.begin(); o != outs.end(); ++o) {
+        if (!aligned(o->p, o->a)) return false;
+        for (const Buf& i : ins)
+            if (overlap(*o, i)) return false;
+        for (const Buf* q = outs.begin(); q != o; ++q)
+            if (overlap(*o, *q)) return false;
+    }
+    return true;
+}
+
+// Rows of n elements: sizes that the kernels' indexes hold.
+kan_status check_rows(int64_t rows, int32_t n, int32_t most) {
+    if (rows < 0 || n < 1 || n > most) return KAN_ERR_INVALID_ARG;
+    if (rows > (INT64_C(1) << 48) / n) return KAN_ERR_INVALID_ARG;
+    return KAN_OK;
+}
+
+constexpr int32_t kMaxNormRow = 1 << 24;
+
+kan_status check_norm(kan_dtype dtype, kan_dtype param_dtype, int64_t rows, int32_t n) {
+    if (!known(dtype) || !known(param_dtype)) return KAN_ERR_UNSUPPORTED;
+    if (dtype == KAN_F32 && param_dtype != KAN_F32) return KAN_ERR_UNSUPPORTED;
+    return check_rows(rows, n, kMaxNormRow);
+}
+
+size_t norm_part_bytes(const kan::NormPlan& p, int32_t n) {
+    return (size_t)2 * p.parts * n * sizeof(float);
+}
+
+}  // namespace
+
+extern "C" {
+
+kan_status kan_layer_norm(kan_dtype dtype, kan_dtype param_dtype, int64_t rows, int32_t n,
+                          const void* x, const void* residual, const void* weight,
+                          const void* bias, float eps, void* h, void* y, float* mean, float* rstd,
+                          void* stream) {
+    const kan_status st = check_norm(dtype, param_dtype, rows, n);
+    if (st != KAN_OK) return st;
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return KAN_ERR_INVALID_ARG;
+    if (rows == 0) return KAN_OK;
+    if (x == nullptr || y == nullptr || (h != nullptr && residual == nullptr) ||
+        (mean == nullptr) != (rstd == nullptr))
+        return KAN_ERR_INVALID_ARG;
+    const size_t es = dtype_size(dtype), ps = dtype_size(param_dtype);
+    const size_t t = (size_t)rows * n * es, w = (size_t)n * ps, s = (size_t)rows * 4;
+    if (!placed({{x, t, es}, {residual, t, es}, {weight, w, ps}, {bias, w, ps}},
+                {{h, t, es}, {y, t, es}, {mean, s, 4}, {rstd, s, 4}}))
+        return KAN_ERR_INVALID_ARG;
+    const kan::NormArgs a = {x, residual, weight, bias, h, y, mean, rstd, rows, n, eps, 0};
+    return device_status(kan::launch_norm(dtype == KAN_BF16, param_dtype == KAN_BF16,
+                                          kan::norm_plan(rows, n, (int)es, false), a,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+kan_status kan_layer_norm_backward_workspace_bytes(kan_dtype dtype, int64_t rows, int32_t n,
+                                                   size_t* bytes) {
+    if (bytes == nullptr) return KAN_ERR_INVALID_ARG;
+    const kan_status st = check_norm(dtype, KAN_F32, rows, n);
+    if (st != KAN_OK) return st;
+    *bytes = norm_part_bytes(kan::norm_plan(rows, n, (int)dtype_size(dtype), true), n);
+    return KAN_OK;
+}
+
+kan_status kan_layer_norm_backward(kan_dtype dtype, kan_dtype param_dtype, int64_t rows,
+                                   int32_t n, const void* h, const float* mean, const float* rstd,
+                                   const void* weight, const void* dy, const void* dh, void* dx,
+                                   void* dweight, void* dbias, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+    const kan_status st = check_norm(dtype, param_dtype, rows, n);
+    if (st != KAN_OK) return st;
+    const bool params = dweight != nullptr || dbias != nullptr;
+    if (dx == nullptr && (!params || dh != nullptr)) return KAN_ERR_INVALID_ARG;
+    const size_t es = dtype_size(dtype), ps = dtype_size(param_dtype);
+    const size_t t = (size_t)rows * n * es, w = (size_t)n * ps, s = (size_t)rows * 4;
+    const kan::NormPlan p = kan::norm_plan(rows, n, (int)es, true);
+    const size_t need = params ? norm_part_bytes(p, n) : 0;
+    if (rows > 0 && (h == nullptr || mean == nullptr || rstd == nullptr || dy == nullptr))
+        return KAN_ERR_INVALID_ARG;
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return KAN_ERR_INVALID_ARG;
+    if (!placed({{h, t, es}, {mean, s, 4}, {rstd, s, 4}, {weight, w, ps}, {dy, t, es}, {dh, t, es}},
+                {{dx, t, es}, {dweight, w, ps}, {dbias, w, ps},
+                 {need > 0 ? workspace : nullptr, need, 16}}))
+        return KAN_ERR_INVALID_ARG;
+    if (rows == 0 && !params) return KAN_OK;
+    const kan::NormGradArgs a = {h, weight, dy, dh, mean, rstd, dx,
+                                 need > 0 ? static_cast<float*>(workspace) : nullptr, rows, n, 0};
+    return device_status(kan::launch_norm_grad(dtype == KAN_BF16, param_dtype == KAN_BF16, p, a,
+                                               dweight, dbias, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,56 @@
+"""Host checks of the operators around the layer, without a GPU: every invalid argument is
+rejected with the documented status before the device is touched (fake addresses, never
+dereferenced)."""
+import math
+
+import pytest
+
+from paper_2609_01956_amd import binding as kb
+
+F32, BF16, BAD, OK = kb.KAN_F32, kb.KAN_BF16, kb.KAN_ERR_INVALID_ARG, kb.KAN_OK
+X, R, W, B, H, Y, M, S = (0x100000000 * (i + 1) for i in range(8))
+DY, DH, DX, DW, DB, WS = (0x100000000 * (i + 16) for i in range(6))
+
+
+def test_layer_norm_host_checks():
+    def call(dtype=F32, pdtype=F32, rows=16, n=32, x=X, res=R, w=W, b=B, eps=1e-5, h=H, y=Y, m=M,
+             s=S):
+        return kb.kan_layer_norm(dtype, pdtype, rows, n, x, res, w, b, eps, h, y, m, s)
+    for kw in (dict(rows=-1), dict(n=0), dict(n=(1 << 24) + 1), dict(rows=1 << 48), dict(eps=-1e-9),
+               dict(eps=math.nan), dict(eps=math.inf), dict(x=0), dict(y=0), dict(res=0),
+               dict(m=0), dict(s=0), dict(x=X + 2), dict(w=W + 1), dict(m=M + 2), dict(y=X + 64),
+               dict(y=R), dict(y=W - 4), dict(h=X), dict(h=Y + 8), dict(m=Y), dict(s=M + 4),
+               dict(m=B + 4)):
+        assert call(**kw) == BAD, kw
+    for kw in (dict(dtype=2), dict(pdtype=-1), dict(pdtype=BF16)):
+        assert call(**kw) == kb.KAN_ERR_UNSUPPORTED, kw
+    assert call(dtype=BF16, y=Y + 1) == BAD
+    # an empty problem: pointers unchecked, nothing launched
+    assert call(rows=0, x=0, res=0, w=0, b=0, h=0, y=0, m=0, s=0) == OK
+
+
+def test_layer_norm_backward_host_checks():
+    st, need = kb.kan_layer_norm_backward_workspace_bytes(F32, 16, 32)
+    assert st == OK and need > 0 and need % (2 * 32 * 4) == 0
+
+    def call(dtype=F32, pdtype=F32, rows=16, n=32, h=H, m=M, s=S, w=W, dy=DY, dh=DH, dx=DX, dw=DW,
+             db=DB, ws=WS, nb=need):
+        return kb.kan_layer_norm_backward(dtype, pdtype, rows, n, h, m, s, w, dy, dh, dx, dw, db,
+                                          ws, nb)
+    for kw in (dict(rows=-1), dict(n=0), dict(h=0), dict(m=0), dict(s=0), dict(dy=0), dict(dx=0),
+               dict(dx=0, dh=0, dw=0, db=0), dict(ws=0), dict(nb=need - 1), dict(ws=WS + 8),
+               dict(ws=DX - 16), dict(dx=H), dict(dx=DY + 4), dict(dw=W), dict(db=DW + 4),
+               dict(dw=DX), dict(h=H + 2), dict(dw=DW + 2)):
+        assert call(**kw) == BAD, kw
+    assert call(pdtype=BF16) == kb.KAN_ERR_UNSUPPORTED
+    # an empty batch that wants dx alone: nothing to do
+    assert call(rows=0, h=0, m=0, s=0, dy=0, dh=0, dw=0, db=0, ws=0, nb=0) == OK
+    assert kb.kan_layer_norm_backward_workspace_bytes(F32, -1, 32)[0] == BAD
+    assert kb.kan_layer_norm_backward_workspace_bytes(F32, 16, 0)[0] == BAD
+    assert kb.kan_layer_norm_backward_workspace_bytes(3, 16, 4)[0] == kb.KAN_ERR_UNSUPPORTED
+    assert kb.load_library().kan_layer_norm_backward_workspace_bytes(F32, 16, 32, None) == BAD
+    assert kb.kan_layer_norm_backward_workspace_bytes(F32, 0, 32) == (OK, 0)
+    for rows, n in [(1, 1), (65536, 784), (16384, 8192), (100, 20000)]:
+        for dt in (F32, BF16):
+            st, nb = kb.kan_layer_norm_backward_workspace_bytes(dt, rows, n)
+            assert st == OK and 8 * n <= nb <= 8 * n * min(rows, 1024)

@@ -7,7 +7,8 @@
  * eq. bounded) and contracts it with the spline coefficients plus the SiLU
  * base branch (eq. kan_forward); it also computes the layer's gradients.  Beside the
  * layer stand the operators of a training or serving step around it: layer norm, which
- * holds a layer's inputs on its grid.
+ * holds a layer's inputs on its grid, and the log probabilities of given
+ * classes (tokens) under the logits that the last layer gives, with their gradient.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -531,6 +532,76 @@ kan_status kan_layer_norm_backward(kan_dtype dtype, kan_dtype param_dtype, int64
 /* Size in bytes of kan_layer_norm_backward's workspace for rows of this dtype and shape. */
 kan_status kan_layer_norm_backward_workspace_bytes(kan_dtype dtype, int64_t rows, int32_t n,
                                                    size_t* bytes);
+
+/*
+ * kan_token_logprobs -- log probabilities of given classes (tokens) under the softmax of
+ * each row's logits, with the entropy and the top_k most probable classes:
+ *
+ *   m[b] = max_v z[b, v],  logs[b] = log sum_v exp(z[b, v] - m[b])
+ *   logp[b]    = z[b, targets[b]] - m[b] - logs[b]
+ *   entropy[b] = logs[b] - sum_v p[b, v] (z[b, v] - m[b]),  p = exp(z - m - logs)
+ *   top_index[b, :], top_logp[b, :]  the classes by falling logit, equal ones by rising
+ *                                    index (-0 equals 0), and their log probabilities
+ *
+ *   logits      [rows, classes] of dtype, rows row_stride >= classes elements apart (what
+ *               lies between is not read)
+ *   targets     [rows] int64; ignore_index gives logp 0, another value outside
+ *               [0, classes) gives NaN (entropy and top classes as for any row)
+ *   top_k       0 .. min(64, classes)
+ *   logp        [rows] fp32
+ *   stats       [rows, 2] fp32: m and logs, for the backward
+ *   entropy     [rows] fp32, or NULL
+ *   top_logp    [rows, top_k] fp32, top_index [rows, top_k] int64: both NULL if top_k is 0
+ *   workspace   caller-owned, workspace_bytes >= kan_token_logprobs_workspace_bytes(...),
+ *               16-byte aligned, overlapping no other argument (0 bytes unless few long
+ *               rows are split over workgroups).
+ *
+ * A masked class holds -infinity (or so low a value that its weight is 0).  A row with no
+ * class left (all -infinity) gives logp and top_logp -infinity and entropy 0; a row whose
+ * classes all hold one finite value, however low, is uniform.  A NaN or +infinity makes its
+ * row's logp, entropy and top_logp NaN; top_index then ranks NaN after every number.
+ * Arithmetic is binary32; results do not depend on what other rows hold.
+ *
+ * Outputs must not overlap each other or an input.  Returns KAN_OK, KAN_ERR_INVALID_ARG
+ * (rows < 0, classes < 1, classes > 2^30, rows * row_stride > 2^48, a bad top_k, NULL,
+ * misaligned or overlapping pointers or a short workspace with rows > 0),
+ * KAN_ERR_UNSUPPORTED (unknown dtype) or KAN_ERR_DEVICE.
+ */
+kan_status kan_token_logprobs(kan_dtype dtype, int64_t rows, int32_t classes, const void* logits,
+                              int64_t row_stride, const int64_t* targets, int64_t ignore_index,
+                              int32_t top_k, float* logp, float* stats, float* entropy,
+                              float* top_logp, int64_t* top_index, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Size in bytes of kan_token_logprobs's workspace for logits of this dtype and shape. */
+kan_status kan_token_logprobs_workspace_bytes(kan_dtype dtype, int64_t rows, int32_t classes,
+                                              int32_t top_k, size_t* bytes);
+
+/*
+ * kan_token_logprobs_backward -- the gradient of kan_token_logprobs for dlogp = dL/dlogp
+ * and dentropy = dL/dentropy:
+ *
+ *   dlogits[b, v] = dlogp[b] ([v = targets[b]] - p[b, v])
+ *                   - dentropy[b] p[b, v] (log p[b, v] + entropy[b])
+ *
+ *   logits, row_stride, targets, ignore_index, stats, entropy   as in the forward; the
+ *                      dlogp of an ignored row counts as 0
+ *   dlogp              [rows] fp32
+ *   entropy, dentropy  [rows] fp32, both NULL: no gradient of the entropy
+ *   dlogits            [rows, classes] of dtype, rows dlogits_stride >= classes elements
+ *                      apart (what lies between is not written).  May be the logits
+ *                      themselves (same address and stride): in place.
+ *
+ * Masked classes (-infinity) get 0, and so does a row with no class left; a target outside
+ * the classes that is not ignore_index makes its row's gradient NaN.  Otherwise overlap and
+ * return codes as in kan_token_logprobs.
+ */
+kan_status kan_token_logprobs_backward(kan_dtype dtype, int64_t rows, int32_t classes,
+                                       const void* logits, int64_t row_stride,
+                                       const int64_t* targets, int64_t ignore_index,
+                                       const float* stats, const float* dlogp,
+                                       const float* entropy, const float* dentropy, void* dlogits,
+                                       int64_t dlogits_stride, void* stream);
 
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char* kan_status_string(kan_status status);

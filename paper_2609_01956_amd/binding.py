@@ -37,7 +37,8 @@ EXPORTED_SYMBOLS = ("kan_basis_eval", "kan_basis_eval_cdb", "kan_layer_forward",
                     "kan_layer_backward_workspace_bytes", "kan_layer_forward_span",
                     "kan_layer_forward_span_workspace_bytes", "kan_layer_norm",
                     "kan_layer_norm_backward", "kan_layer_norm_backward_workspace_bytes",
-                    "kan_status_string",
+                    "kan_token_logprobs", "kan_token_logprobs_workspace_bytes",
+                    "kan_token_logprobs_backward", "kan_status_string",
                     "kan_abi_version")
 
 _VP = ctypes.c_void_p
@@ -130,6 +131,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
             lib.kan_layer_norm_backward_workspace_bytes.argtypes = [
                 ctypes.c_int, ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
             lib.kan_layer_norm_backward_workspace_bytes.restype = ctypes.c_int
+            lib.kan_token_logprobs.argtypes = [
+                ctypes.c_int, ctypes.c_int64, ctypes.c_int32, _VP, ctypes.c_int64, _VP,
+                ctypes.c_int64, ctypes.c_int32, _VP, _VP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]
+            lib.kan_token_logprobs.restype = ctypes.c_int
+            lib.kan_token_logprobs_workspace_bytes.argtypes = [
+                ctypes.c_int, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                ctypes.POINTER(ctypes.c_size_t)]
+            lib.kan_token_logprobs_workspace_bytes.restype = ctypes.c_int
+            lib.kan_token_logprobs_backward.argtypes = [
+                ctypes.c_int, ctypes.c_int64, ctypes.c_int32, _VP, ctypes.c_int64, _VP,
+                ctypes.c_int64, _VP, _VP, _VP, _VP, _VP, ctypes.c_int64, _VP]
+            lib.kan_token_logprobs_backward.restype = ctypes.c_int
             lib.kan_status_string.argtypes = [ctypes.c_int]
             lib.kan_status_string.restype = ctypes.c_char_p
             lib.kan_abi_version.argtypes = []
@@ -340,6 +353,37 @@ def kan_layer_norm_backward_workspace_bytes(dtype: int, rows: int, n: int) -> Tu
     st = int(load_library().kan_layer_norm_backward_workspace_bytes(
         int(dtype), int(rows), int(n), ctypes.byref(size)))
     return st, int(size.value)
+
+
+def kan_token_logprobs(dtype: int, rows: int, classes: int, logits: int, row_stride: int,
+                       targets: int, ignore_index: int, top_k: int, logp: int, stats: int,
+                       entropy: int, top_logp: int, top_index: int, workspace: int,
+                       workspace_bytes: int, stream: int = 0) -> int:
+    """Raw call: device addresses as integers (0 for NULL); returns the kan_status code."""
+    return int(load_library().kan_token_logprobs(
+        int(dtype), int(rows), int(classes), _VP(logits), int(row_stride), _VP(targets),
+        int(ignore_index), int(top_k), _VP(logp), _VP(stats), _VP(entropy), _VP(top_logp),
+        _VP(top_index), _VP(workspace), ctypes.c_size_t(workspace_bytes), _VP(stream)))
+
+
+def kan_token_logprobs_workspace_bytes(dtype: int, rows: int, classes: int,
+                                       top_k: int) -> Tuple[int, int]:
+    """Raw call: returns (kan_status, bytes)."""
+    size = ctypes.c_size_t(0)
+    st = int(load_library().kan_token_logprobs_workspace_bytes(
+        int(dtype), int(rows), int(classes), int(top_k), ctypes.byref(size)))
+    return st, int(size.value)
+
+
+def kan_token_logprobs_backward(dtype: int, rows: int, classes: int, logits: int, row_stride: int,
+                                targets: int, ignore_index: int, stats: int, dlogp: int,
+                                entropy: int, dentropy: int, dlogits: int, dlogits_stride: int,
+                                stream: int = 0) -> int:
+    """Raw call: device addresses as integers (0 for NULL); returns the kan_status code."""
+    return int(load_library().kan_token_logprobs_backward(
+        int(dtype), int(rows), int(classes), _VP(logits), int(row_stride), _VP(targets),
+        int(ignore_index), _VP(stats), _VP(dlogp), _VP(entropy), _VP(dentropy), _VP(dlogits),
+        int(dlogits_stride), _VP(stream)))
 
 
 def check(status: int) -> None:
@@ -753,3 +797,87 @@ def layer_norm_backward(h, mean, rstd, weight, dy, dh=None, need_dx: bool = True
                 mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dy.data_ptr(), _ptr(dh), _ptr(dx),
                 _ptr(dw), _ptr(db), _ptr(ws), nbytes, _stream(h.device)))
     return dx, dw, db
+
+
+def _logits(z) -> Tuple[int, int, int]:
+    """Checks logits [rows, classes]: (rows, classes, elements from row to row)."""
+    if not z.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    if z.dim() != 2 or z.shape[1] < 1:
+        raise ValueError("logits must be [rows, classes]")
+    rows, classes = z.shape
+    stride = z.stride(0) if rows > 1 else classes
+    if (classes > 1 and z.stride(1) != 1) or stride < classes:
+        raise ValueError("a row of logits must be contiguous, and rows must not overlap")
+    return rows, classes, stride
+
+
+def _row_values(what: str, z, *ts) -> None:
+    """fp32 values (or None), one per row of the logits."""
+    torch = _torch()
+    for t in ts:
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (z.shape[0],) or
+                              t.device != z.device or not t.is_contiguous()):
+            raise ValueError(f"{what} must be fp32 [rows], contiguous, on the logits' device")
+
+
+def _check_targets(z, targets) -> None:
+    if targets.dtype != _torch().int64 or tuple(targets.shape) != (z.shape[0],) or \
+            targets.device != z.device or not targets.is_contiguous():
+        raise ValueError("targets must be int64 [rows], contiguous, on the logits' device")
+
+
+def token_logprobs(logits, targets, top_k: int = 0, entropy: bool = False,
+                   ignore_index: int = -100, workspace=None):
+    """kan_token_logprobs: logits [rows, classes] (rows may be padded: any row stride of at
+    least classes), targets [rows] int64 -> (logp [rows], stats [rows, 2], entropy [rows] or
+    None, top_logp [rows, top_k] or None, top_index [rows, top_k] int64 or None), all values
+    fp32.  stats goes to token_logprobs_backward.  `workspace` (a uint8 device tensor) is used
+    when large enough, else a fresh one is taken."""
+    torch = _torch()
+    rows, classes, stride = _logits(logits)
+    _check_targets(logits, targets)
+    dt, k, dev, lib = _dtype_code(logits), int(top_k), logits.device, _library()
+    size = ctypes.c_size_t(0)
+    check(lib.kan_token_logprobs_workspace_bytes(dt, rows, classes, k, ctypes.byref(size)))
+    logp = torch.empty((rows,), dtype=torch.float32, device=dev)
+    stats = torch.empty((rows, 2), dtype=torch.float32, device=dev)
+    ent = torch.empty_like(logp) if entropy else None
+    top = torch.empty((rows, k), dtype=torch.float32, device=dev) if k else None
+    idx = torch.empty((rows, k), dtype=torch.int64, device=dev) if k else None
+    ws = None
+    if size.value:
+        ws = workspace
+        if ws is None or ws.numel() < size.value or ws.device != dev:
+            ws = torch.empty(size.value, dtype=torch.uint8, device=dev)
+    check(_call(dev, lib.kan_token_logprobs, dt, rows, classes, logits.data_ptr(), stride,
+                targets.data_ptr(), int(ignore_index), k, logp.data_ptr(), stats.data_ptr(),
+                _ptr(ent), _ptr(top), _ptr(idx), _ptr(ws), size.value, _stream(dev)))
+    return logp, stats, ent, top, idx
+
+
+def token_logprobs_backward(logits, targets, stats, dlogp, entropy=None, dentropy=None,
+                            ignore_index: int = -100, out=None):
+    """The gradient of token_logprobs with respect to the logits
+    (kan_token_logprobs_backward) for dlogp [rows] fp32, and for dentropy [rows] fp32 given
+    the forward's entropy; stats as token_logprobs returned them.  `out` (like the logits; the
+    logits themselves: in place) receives the gradient instead of a fresh tensor."""
+    torch = _torch()
+    rows, classes, stride = _logits(logits)
+    _check_targets(logits, targets)
+    if stats.dtype != torch.float32 or tuple(stats.shape) != (rows, 2) or \
+            stats.device != logits.device or not stats.is_contiguous():
+        raise ValueError("stats must be fp32 [rows, 2], contiguous, on the logits' device")
+    _row_values("dlogp, entropy and dentropy", logits, dlogp, entropy, dentropy)
+    if dlogp is None or (entropy is None) != (dentropy is None):
+        raise ValueError("dlogp is needed, and entropy and dentropy go together")
+    if out is None:
+        out = torch.empty((rows, classes), dtype=logits.dtype, device=logits.device)
+    _, _, ostride = _logits(out)
+    if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device:
+        raise ValueError("out must match the logits in shape, dtype and device")
+    check(_call(logits.device, _library().kan_token_logprobs_backward, _dtype_code(logits), rows,
+                classes, logits.data_ptr(), stride, targets.data_ptr(), int(ignore_index),
+                stats.data_ptr(), dlogp.data_ptr(), _ptr(entropy), _ptr(dentropy), out.data_ptr(),
+                ostride, _stream(logits.device)))
+    return out

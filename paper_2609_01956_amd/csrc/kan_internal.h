@@ -406,4 +406,40 @@ hipError_t launch_norm(bool bf16, bool bf16_params, const NormPlan& p, NormArgs 
 hipError_t launch_norm_grad(bool bf16, bool bf16_params, const NormPlan& p, NormGradArgs a,
                             void* dw, void* db, hipStream_t s);
 
+// ---------------------------------------------------------------- log probabilities
+
+struct LogprobArgs {
+    const void* z;
+    const int64_t* targets;
+    int64_t rows, stride;  // elements from row to row
+    int64_t ignore;
+    int classes, k;
+    float *logp, *stats, *entropy;  // entropy may be null
+    float* top_logp;
+    int64_t* top_index;
+    int shift;      // short rows: log2 of the lanes of a row
+    int parts;      // workgroups (of one wave) that share a row
+    float4* part;   // [rows][parts] sums of the parts
+    uint64_t* keys; // [rows][parts][k] their best classes
+};
+struct LogprobGradArgs {
+    const void* z;
+    const int64_t* targets;
+    const float *stats, *dlogp, *entropy, *dentropy;  // the last two both null or both not
+    void* dz;
+    int64_t rows, stride, dstride, ignore;
+    int classes;
+    int shift;     // short rows
+    int segments;  // workgroups per row
+};
+constexpr int kMaxTop = 64;
+struct LogprobPlan {
+    int waves;  // per (row, part), 0: rows that share a wave
+    int shift, parts;
+    size_t bytes;  // workspace
+};
+LogprobPlan logprob_plan(int64_t rows, int32_t classes, int es, int k);
+hipError_t launch_logprob(bool bf16, const LogprobPlan& p, LogprobArgs a, void* ws, hipStream_t s);
+hipError_t launch_logprob_grad(bool bf16, LogprobGradArgs a, hipStream_t s);
+
 }  // namespace kan

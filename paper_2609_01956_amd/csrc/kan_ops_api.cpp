@@ -58,6 +58,20 @@ kan_status check_norm(kan_dtype dtype, kan_dtype param_dtype, int64_t rows, int3
     return check_rows(rows, n, kMaxNormRow);
 }
 
+constexpr int32_t kMaxClasses = 1 << 30;
+
+kan_status check_logits(kan_dtype dtype, int64_t rows, int32_t classes) {
+    if (!known(dtype)) return KAN_ERR_UNSUPPORTED;
+    return check_rows(rows, classes, kMaxClasses);
+}
+
+// Bytes from the first to past the last logit of rows `stride` elements apart; 0 for
+// strides that rows of `classes` elements do not fit or that pass the indexes.
+size_t logits_bytes(int64_t rows, int32_t classes, int64_t stride, size_t es) {
+    if (stride < classes || rows > (INT64_C(1) << 48) / stride) return 0;
+    return ((size_t)(rows - 1) * stride + classes) * es;
+}
+
 size_t norm_part_bytes(const kan::NormPlan& p, int32_t n) {
     return (size_t)2 * p.parts * n * sizeof(float);
 }
@@ -122,6 +136,92 @@ kan_status kan_layer_norm_backward(kan_dtype dtype, kan_dtype param_dtype, int64
                                  need > 0 ? static_cast<float*>(workspace) : nullptr, rows, n, 0};
     return device_status(kan::launch_norm_grad(dtype == KAN_BF16, param_dtype == KAN_BF16, p, a,
                                                dweight, dbias, static_cast<hipStream_t>(stream)));
+}
+
+kan_status kan_token_logprobs_workspace_bytes(kan_dtype dtype, int64_t rows, int32_t classes,
+                                              int32_t top_k, size_t* bytes) {
+    if (bytes == nullptr) return KAN_ERR_INVALID_ARG;
+    const kan_status st = check_logits(dtype, rows, classes);
+    if (st != KAN_OK) return st;
+    if (top_k < 0 || top_k > kan::kMaxTop || top_k > classes) return KAN_ERR_INVALID_ARG;
+    *bytes = kan::logprob_plan(rows, classes, (int)dtype_size(dtype), top_k).bytes;
+    return KAN_OK;
+}
+
+kan_status kan_token_logprobs(kan_dtype dtype, int64_t rows, int32_t classes, const void* logits,
+                              int64_t row_stride, const int64_t* targets, int64_t ignore_index,
+                              int32_t top_k, float* logp, float* stats, float* entropy,
+                              float* top_logp, int64_t* top_index, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+    const kan_status st = check_logits(dtype, rows, classes);
+    if (st != KAN_OK) return st;
+    if (top_k < 0 || top_k > kan::kMaxTop || top_k > classes) return KAN_ERR_INVALID_ARG;
+    if (rows == 0) return KAN_OK;
+    const size_t es = dtype_size(dtype), z = logits_bytes(rows, classes, row_stride, es);
+    if (z == 0 || logits == nullptr || targets == nullptr || logp == nullptr || stats == nullptr)
+        return KAN_ERR_INVALID_ARG;
+    if ((top_logp != nullptr) != (top_k > 0) || (top_index != nullptr) != (top_k > 0))
+        return KAN_ERR_INVALID_ARG;
+    const kan::LogprobPlan p = kan::logprob_plan(rows, classes, (int)es, top_k);
+    if (p.bytes > 0 && (workspace == nullptr || workspace_bytes < p.bytes))
+        return KAN_ERR_INVALID_ARG;
+    const size_t s = (size_t)rows * 4;
+    if (!placed({{logits, z, es}, {targets, 2 * s, 8}},
+                {{logp, s, 4}, {stats, 2 * s, 4}, {entropy, s, 4}, {top_logp, s * top_k, 4},
+                 {top_index, 2 * s * top_k, 8}, {p.bytes > 0 ? workspace : nullptr, p.bytes, 16}}))
+        return KAN_ERR_INVALID_ARG;
+    kan::LogprobArgs a = {};
+    a.z = logits;
+    a.targets = targets;
+    a.rows = rows;
+    a.stride = row_stride;
+    a.ignore = ignore_index;
+    a.classes = classes;
+    a.k = top_k;
+    a.logp = logp;
+    a.stats = stats;
+    a.entropy = entropy;
+    a.top_logp = top_logp;
+    a.top_index = top_index;
+    return device_status(kan::launch_logprob(dtype == KAN_BF16, p, a, workspace,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+kan_status kan_token_logprobs_backward(kan_dtype dtype, int64_t rows, int32_t classes,
+                                       const void* logits, int64_t row_stride,
+                                       const int64_t* targets, int64_t ignore_index,
+                                       const float* stats, const float* dlogp,
+                                       const float* entropy, const float* dentropy, void* dlogits,
+                                       int64_t dlogits_stride, void* stream) {
+    const kan_status st = check_logits(dtype, rows, classes);
+    if (st != KAN_OK) return st;
+    if (rows == 0) return KAN_OK;
+    const size_t es = dtype_size(dtype), z = logits_bytes(rows, classes, row_stride, es);
+    const size_t dz = logits_bytes(rows, classes, dlogits_stride, es), s = (size_t)rows * 4;
+    if (z == 0 || dz == 0 || logits == nullptr || targets == nullptr || stats == nullptr ||
+        dlogp == nullptr || dlogits == nullptr || (entropy == nullptr) != (dentropy == nullptr))
+        return KAN_ERR_INVALID_ARG;
+    // (in place: each gradient over its own logit)
+    const bool in_place = dlogits == logits && dlogits_stride == row_stride;
+    if (!placed({{in_place ? nullptr : logits, z, es}, {targets, 2 * s, 8}, {stats, 2 * s, 4},
+                 {dlogp, s, 4}, {entropy, s, 4}, {dentropy, s, 4}},
+                {{dlogits, dz, es}}))
+        return KAN_ERR_INVALID_ARG;
+    kan::LogprobGradArgs a = {};
+    a.z = logits;
+    a.targets = targets;
+    a.stats = stats;
+    a.dlogp = dlogp;
+    a.entropy = entropy;
+    a.dentropy = dentropy;
+    a.dz = dlogits;
+    a.rows = rows;
+    a.stride = row_stride;
+    a.dstride = dlogits_stride;
+    a.ignore = ignore_index;
+    a.classes = classes;
+    return device_status(kan::launch_logprob_grad(dtype == KAN_BF16, a,
+                                                  static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -54,3 +54,44 @@ def test_layer_norm_backward_host_checks():
         for dt in (F32, BF16):
             st, nb = kb.kan_layer_norm_backward_workspace_bytes(dt, rows, n)
             assert st == OK and 8 * n <= nb <= 8 * n * min(rows, 1024)
+
+
+Z, T, L, ST, E, TL, TI, DZ = (0x100000000 * (i + 32) for i in range(8))
+
+
+def test_token_logprobs_host_checks():
+    st, need = kb.kan_token_logprobs_workspace_bytes(F32, 2, 100000, 5)
+    assert st == OK and need > 0  # (few long rows are split)
+    assert kb.kan_token_logprobs_workspace_bytes(F32, 65536, 10, 5) == (OK, 0)
+
+    def call(dtype=F32, rows=2, classes=100000, z=Z, stride=100000, t=T, k=5, logp=L, stats=ST,
+             ent=E, top=TL, idx=TI, ws=WS, nb=need):
+        return kb.kan_token_logprobs(dtype, rows, classes, z, stride, t, -100, k, logp, stats, ent,
+                                     top, idx, ws, nb)
+    for kw in (dict(rows=-1), dict(classes=0), dict(classes=(1 << 30) + 1), dict(stride=99999),
+               dict(stride=1 << 62), dict(k=-1), dict(k=65), dict(classes=4, k=5), dict(z=0),
+               dict(t=0), dict(logp=0), dict(stats=0), dict(top=0), dict(idx=0), dict(k=0),
+               dict(ws=0), dict(nb=need - 1), dict(ws=WS + 8), dict(z=Z + 2), dict(t=T + 4),
+               dict(idx=TI + 4), dict(logp=Z + 4), dict(stats=L + 4), dict(ent=T), dict(ws=Z),
+               dict(top=E + 4)):
+        assert call(**kw) == BAD, kw
+    assert call(dtype=2) == kb.KAN_ERR_UNSUPPORTED
+    assert call(rows=0, z=0, t=0, logp=0, stats=0, ent=0, top=0, idx=0, ws=0, nb=0) == OK
+    assert kb.kan_token_logprobs_workspace_bytes(F32, 2, 4, 5)[0] == BAD
+    assert kb.kan_token_logprobs_workspace_bytes(F32, 2, 100, 65)[0] == BAD
+    assert kb.kan_token_logprobs_workspace_bytes(F32, -1, 4, 0)[0] == BAD
+    assert kb.kan_token_logprobs_workspace_bytes(7, 1, 4, 0)[0] == kb.KAN_ERR_UNSUPPORTED
+    assert kb.load_library().kan_token_logprobs_workspace_bytes(F32, 2, 4, 0, None) == BAD
+
+
+def test_token_logprobs_backward_host_checks():
+    def call(dtype=F32, rows=16, classes=100, z=Z, stride=104, t=T, stats=ST, dl=L, ent=E, de=TL,
+             dz=DZ, ds=100):
+        return kb.kan_token_logprobs_backward(dtype, rows, classes, z, stride, t, -100, stats, dl,
+                                              ent, de, dz, ds)
+    for kw in (dict(rows=-1), dict(classes=0), dict(stride=99), dict(ds=99), dict(z=0), dict(t=0),
+               dict(stats=0), dict(dl=0), dict(ent=0), dict(de=0), dict(dz=0), dict(dz=DZ + 2),
+               dict(dz=Z), dict(dz=Z + 4, ds=104), dict(dz=T), dict(dz=ST - 4), dict(dz=E)):
+        assert call(**kw) == BAD, kw
+    assert call(dtype=-1) == kb.KAN_ERR_UNSUPPORTED
+    assert call(rows=0, z=0, t=0, stats=0, dl=0, ent=0, de=0, dz=0) == OK

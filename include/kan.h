@@ -8,7 +8,8 @@
  * base branch (eq. kan_forward); it also computes the layer's gradients.  Beside the
  * layer stand the operators of a training or serving step around it: layer norm, which
  * holds a layer's inputs on its grid, and the log probabilities of given
- * classes (tokens) under the logits that the last layer gives, with their gradient.
+ * classes (tokens) under the logits that the last layer gives, with their gradient,
+ * and the clipping of all gradients by their global norm.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -602,6 +603,45 @@ kan_status kan_token_logprobs_backward(kan_dtype dtype, int64_t rows, int32_t cl
                                        const float* stats, const float* dlogp,
                                        const float* entropy, const float* dentropy, void* dlogits,
                                        int64_t dlogits_stride, void* stream);
+
+/*
+ * kan_grad_norm -- the global 2-norm of many tensors (the gradients of a stack of layers):
+ *
+ *   norm = sqrt(sum_t sum_i grads[t][i]^2)
+ *
+ * kan_clip_grad_norm -- the same, and the tensors scaled to a bound on it:
+ *
+ *   out[t][i] = c grads[t][i],  c = min(1, max_norm / (norm + eps))
+ *
+ *   count      number of tensors, 0 .. 16384
+ *   grads      HOST array of `count` device pointers (one whose size is 0 is not looked at)
+ *   sizes      HOST array: elements of each, 2^40 in all at most
+ *   dtypes     HOST array: the kan_dtype of each; they may differ
+ *   max_norm   at least 0 (infinity: no bound);  eps  at least 0, finite
+ *   out        HOST array of `count` device pointers: grads[t] itself (in place) or a tensor
+ *              that overlaps no gradient and no other output
+ *   workspace  caller-owned, workspace_bytes >= kan_grad_norm_workspace_bytes(count),
+ *              16-byte aligned, overlapping no other argument
+ *   norm       one fp32 value on the device
+ *
+ * The host arrays are read before the call returns and not kept.  Squares are summed in
+ * binary64 in a fixed order (deterministic; no overflow, no underflow).  With c = 1 a tensor
+ * scaled in place is not written.  A NaN gradient makes norm and every scaled gradient NaN;
+ * an infinite one makes norm infinite, c 0 and its own product NaN: test norm first.
+ *
+ * Returns KAN_OK, KAN_ERR_INVALID_ARG, KAN_ERR_UNSUPPORTED (unknown dtype) or
+ * KAN_ERR_DEVICE.
+ */
+kan_status kan_grad_norm(int32_t count, const void* const* grads, const int64_t* sizes,
+                         const int32_t* dtypes, void* workspace, size_t workspace_bytes,
+                         float* norm, void* stream);
+kan_status kan_clip_grad_norm(int32_t count, const void* const* grads, const int64_t* sizes,
+                              const int32_t* dtypes, float max_norm, float eps, void* const* out,
+                              void* workspace, size_t workspace_bytes, float* norm,
+                              void* stream);
+
+/* Size in bytes of the workspace of kan_grad_norm and kan_clip_grad_norm. */
+kan_status kan_grad_norm_workspace_bytes(int32_t count, size_t* bytes);
 
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char* kan_status_string(kan_status status);

@@ -11,6 +11,7 @@ loading raises if it is missing.  There is no fallback of any kind.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 import threading
@@ -38,7 +39,8 @@ EXPORTED_SYMBOLS = ("kan_basis_eval", "kan_basis_eval_cdb", "kan_layer_forward",
                     "kan_layer_forward_span_workspace_bytes", "kan_layer_norm",
                     "kan_layer_norm_backward", "kan_layer_norm_backward_workspace_bytes",
                     "kan_token_logprobs", "kan_token_logprobs_workspace_bytes",
-                    "kan_token_logprobs_backward", "kan_status_string",
+                    "kan_token_logprobs_backward", "kan_grad_norm", "kan_clip_grad_norm",
+                    "kan_grad_norm_workspace_bytes", "kan_status_string",
                     "kan_abi_version")
 
 _VP = ctypes.c_void_p
@@ -143,6 +145,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                 ctypes.c_int, ctypes.c_int64, ctypes.c_int32, _VP, ctypes.c_int64, _VP,
                 ctypes.c_int64, _VP, _VP, _VP, _VP, _VP, ctypes.c_int64, _VP]
             lib.kan_token_logprobs_backward.restype = ctypes.c_int
+            lib.kan_grad_norm.argtypes = [ctypes.c_int32, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP,
+                                          _VP]
+            lib.kan_grad_norm.restype = ctypes.c_int
+            lib.kan_clip_grad_norm.argtypes = [ctypes.c_int32, _VP, _VP, _VP, ctypes.c_float,
+                                               ctypes.c_float, _VP, _VP, ctypes.c_size_t, _VP, _VP]
+            lib.kan_clip_grad_norm.restype = ctypes.c_int
+            lib.kan_grad_norm_workspace_bytes.argtypes = [ctypes.c_int32,
+                                                          ctypes.POINTER(ctypes.c_size_t)]
+            lib.kan_grad_norm_workspace_bytes.restype = ctypes.c_int
             lib.kan_status_string.argtypes = [ctypes.c_int]
             lib.kan_status_string.restype = ctypes.c_char_p
             lib.kan_abi_version.argtypes = []
@@ -384,6 +395,43 @@ def kan_token_logprobs_backward(dtype: int, rows: int, classes: int, logits: int
         int(dtype), int(rows), int(classes), _VP(logits), int(row_stride), _VP(targets),
         int(ignore_index), _VP(stats), _VP(dlogp), _VP(entropy), _VP(dentropy), _VP(dlogits),
         int(dlogits_stride), _VP(stream)))
+
+
+def _host(kind: str, values):
+    """A host array and its address (0 for None)."""
+    if values is None:
+        return None, 0
+    a = array.array(kind, values)
+    return a, a.buffer_info()[0]
+
+
+def kan_grad_norm(grads: Sequence[int], sizes: Sequence[int], dtypes: Sequence[int],
+                  workspace: int, workspace_bytes: int, norm: int, stream: int = 0) -> int:
+    """Raw call: device addresses as integers, the host arrays as sequences; returns the
+    kan_status code."""
+    (g, pg), (n, pn), (d, pd) = _host("Q", grads), _host("q", sizes), _host("i", dtypes)
+    return int(load_library().kan_grad_norm(len(g), pg, pn, pd, _VP(workspace),
+                                            ctypes.c_size_t(workspace_bytes), _VP(norm),
+                                            _VP(stream)))
+
+
+def kan_clip_grad_norm(grads: Sequence[int], sizes: Sequence[int], dtypes: Sequence[int],
+                       max_norm: float, eps: float, out: Optional[Sequence[int]], workspace: int,
+                       workspace_bytes: int, norm: int, stream: int = 0) -> int:
+    """Raw call: device addresses as integers, the host arrays as sequences (out None: NULL);
+    returns the kan_status code."""
+    (g, pg), (n, pn), (d, pd) = _host("Q", grads), _host("q", sizes), _host("i", dtypes)
+    o, po = _host("Q", out)
+    return int(load_library().kan_clip_grad_norm(
+        len(g), pg, pn, pd, float(max_norm), float(eps), po, _VP(workspace),
+        ctypes.c_size_t(workspace_bytes), _VP(norm), _VP(stream)))
+
+
+def kan_grad_norm_workspace_bytes(count: int) -> Tuple[int, int]:
+    """Raw call: returns (kan_status, bytes)."""
+    size = ctypes.c_size_t(0)
+    st = int(load_library().kan_grad_norm_workspace_bytes(int(count), ctypes.byref(size)))
+    return st, int(size.value)
 
 
 def check(status: int) -> None:
@@ -881,3 +929,67 @@ def token_logprobs_backward(logits, targets, stats, dlogp, entropy=None, dentrop
                 stats.data_ptr(), dlogp.data_ptr(), _ptr(entropy), _ptr(dentropy), out.data_ptr(),
                 ostride, _stream(logits.device)))
     return out
+
+
+def _many(grads):
+    """Checks a list of tensors: host arrays of their addresses, sizes and dtypes."""
+    torch = _torch()
+    devices = set(map(torch.Tensor.get_device, grads))
+    if len(devices) > 1 or -1 in devices:
+        raise ValueError("tensors must live on one GPU")
+    if not all(map(torch.Tensor.is_contiguous, grads)):
+        raise ValueError("tensors must be contiguous")
+    codes = {torch.float32: KAN_F32, torch.bfloat16: KAN_BF16}
+    try:
+        dtypes = array.array("i", [codes[g.dtype] for g in grads])
+    except KeyError as e:
+        raise NotImplementedError(f"dtype {e.args[0]} is not supported (float32 or bfloat16)")
+    return (array.array("Q", map(torch.Tensor.data_ptr, grads)),
+            array.array("q", map(torch.Tensor.numel, grads)), dtypes)
+
+
+def _norm_buffers(count: int, device, workspace):
+    torch = _torch()
+    size = ctypes.c_size_t(0)
+    check(_library().kan_grad_norm_workspace_bytes(count, ctypes.byref(size)))
+    if workspace is None or workspace.numel() < size.value or workspace.device != device:
+        workspace = torch.empty(size.value, dtype=torch.uint8, device=device)
+    return torch.empty((), dtype=torch.float32, device=device), workspace
+
+
+def grad_norm(grads: Iterable, workspace=None):
+    """The global 2-norm of a list of tensors (fp32 or bf16, of any shapes, on one device):
+    a scalar fp32 tensor on the device (kan_grad_norm; nothing is copied to the host)."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("no tensors")
+    ptrs, sizes, dtypes = _many(grads)
+    dev = grads[0].device
+    norm, ws = _norm_buffers(len(grads), dev, workspace)
+    check(_call(dev, _library().kan_grad_norm, len(grads), ptrs.buffer_info()[0],
+                sizes.buffer_info()[0], dtypes.buffer_info()[0], ws.data_ptr(), ws.numel(),
+                norm.data_ptr(), _stream(dev)))
+    return norm
+
+
+def clip_grad_norm(grads: Iterable, max_norm: float, eps: float = 1e-6, out=None,
+                   workspace=None):
+    """Scales the tensors by min(1, max_norm / (norm + eps)) with their global 2-norm
+    (kan_clip_grad_norm), in place, or into `out`, a list of tensors like them -> the norm
+    before scaling, a scalar fp32 tensor on the device (nothing is copied to the host)."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("no tensors")
+    ptrs, sizes, dtypes = _many(grads)
+    optrs = ptrs
+    if out is not None:
+        out = list(out)
+        optrs, osizes, odtypes = _many(out)
+        if osizes != sizes or odtypes != dtypes or out[0].device != grads[0].device:
+            raise ValueError("out must match the gradients in sizes, dtypes and device")
+    dev = grads[0].device
+    norm, ws = _norm_buffers(len(grads), dev, workspace)
+    check(_call(dev, _library().kan_clip_grad_norm, len(grads), ptrs.buffer_info()[0],
+                sizes.buffer_info()[0], dtypes.buffer_info()[0], float(max_norm), float(eps),
+                optrs.buffer_info()[0], ws.data_ptr(), ws.numel(), norm.data_ptr(), _stream(dev)))
+    return norm

@@ -442,4 +442,36 @@ LogprobPlan logprob_plan(int64_t rows, int32_t classes, int es, int k);
 hipError_t launch_logprob(bool bf16, const LogprobPlan& p, LogprobArgs a, void* ws, hipStream_t s);
 hipError_t launch_logprob_grad(bool bf16, LogprobGradArgs a, hipStream_t s);
 
+// ---------------------------------------------------------------- gradient clipping
+
+// Tensors of one launch, by value: 20 bytes each and 8 for the outputs, within the 4 KB of a
+// kernel's arguments.
+constexpr int kClipTensors = 128;
+constexpr int kClipChunk = 1 << 14;  // elements
+struct ClipArgs {
+    const void* in[kClipTensors];
+    int64_t size[kClipTensors];  // elements, times 2, plus 1 for bf16
+    int first[kClipTensors];     // a tensor's first chunk
+    int count, chunks;
+};
+struct ClipOuts {
+    void* out[kClipTensors];
+};
+static_assert(sizeof(ClipArgs) + sizeof(ClipOuts) + 64 <= 4096, "kernel arguments");
+struct ClipList {
+    int64_t count;
+    const void* const* in;
+    void* const* out;  // null: the norm alone
+    const int64_t* sizes;
+    const int32_t* dtypes;  // kan_dtype
+    bool bf16(int64_t t) const { return dtypes[t] == 1; }
+};
+// Most tensors and elements of a call (the check for overlaps sorts on the stack, chunks
+// are counted in 32 bits).
+constexpr int kClipMaxTensors = 1 << 14;
+constexpr int64_t kClipMaxElements = INT64_C(1) << 40;
+size_t clip_workspace(int64_t count);
+hipError_t launch_clip(const ClipList& l, float max_norm, float eps, float* norm, void* ws,
+                       hipStream_t s);
+
 }  // namespace kan

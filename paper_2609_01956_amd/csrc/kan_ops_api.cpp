@@ -3,6 +3,7 @@
 // only, before any HIP call), launch planning and dispatch onto the caller's stream.
 #include "kan.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <initializer_list>
@@ -70,6 +71,67 @@ kan_status check_logits(kan_dtype dtype, int64_t rows, int32_t classes) {
 size_t logits_bytes(int64_t rows, int32_t classes, int64_t stride, size_t es) {
     if (stride < classes || rows > (INT64_C(1) << 48) / stride) return 0;
     return ((size_t)(rows - 1) * stride + classes) * es;
+}
+
+// Shared validation of the calls on many tensors.
+kan_status check_clip(const kan::ClipList& l, const void* workspace, size_t workspace_bytes,
+                      const float* norm) {
+    if (l.count < 0 || l.count > kan::kClipMaxTensors) return KAN_ERR_INVALID_ARG;
+    if (l.count > 0 && (l.in == nullptr || l.sizes == nullptr || l.dtypes == nullptr))
+        return KAN_ERR_INVALID_ARG;
+    const size_t need = kan::clip_workspace(l.count);
+    if (norm == nullptr || !aligned(norm, 4) || workspace == nullptr || !aligned(workspace, 16) ||
+        workspace_bytes < need)
+        return KAN_ERR_INVALID_ARG;
+    const Buf own[] = {{norm, 4, 4}, {workspace, need, 16}};
+    if (overlap(own[0], own[1])) return KAN_ERR_INVALID_ARG;
+    int64_t total = 0;
+    for (int64_t t = 0; t < l.count; ++t) {
+        if (l.dtypes[t] != KAN_F32 && l.dtypes[t] != KAN_BF16) return KAN_ERR_UNSUPPORTED;
+        const int64_t n = l.sizes[t];
+        if (n < 0 || n > kan::kClipMaxElements - total) return KAN_ERR_INVALID_ARG;
+        total += n;
+        if (n == 0) continue;
+        const size_t es = l.bf16(t) ? 2 : 4;
+        const Buf in = {l.in[t], (size_t)n * es, es};
+        if (in.p == nullptr || !aligned(in.p, es) || overlap(in, own[0]) || overlap(in, own[1]))
+            return KAN_ERR_INVALID_ARG;
+        if (l.out == nullptr || l.out[t] == in.p) continue;
+        const Buf out = {l.out[t], in.n, es};
+        if (out.p == nullptr || !aligned(out.p, es) || overlap(out, own[0]) ||
+            overlap(out, own[1]))
+            return KAN_ERR_INVALID_ARG;
+    }
+    return KAN_OK;
+}
+
+// Does any output overlap another output, or an input that is not its own in place?
+bool clip_outputs_clash(const kan::ClipList& l) {
+    // Item 2 t: output t (also its input, in place); 2 t + 1: input t, where it is another.
+    static_assert(kan::kClipMaxTensors <= 1 << 14, "128 KB of stack");
+    uint32_t items[2 * kan::kClipMaxTensors];
+    size_t count = 0;
+    auto start = [&](uint32_t i) {
+        return reinterpret_cast<uintptr_t>(i & 1 ? l.in[i >> 1] : l.out[i >> 1]);
+    };
+    auto end = [&](uint32_t i) {
+        return start(i) + (size_t)l.sizes[i >> 1] * (l.bf16(i >> 1) ? 2 : 4);
+    };
+    for (int64_t t = 0; t < l.count; ++t) {
+        if (l.sizes[t] == 0) continue;
+        items[count++] = (uint32_t)(2 * t);
+        if (l.in[t] != l.out[t]) items[count++] = (uint32_t)(2 * t + 1);
+    }
+    auto before = [&](uint32_t a, uint32_t b) { return start(a) < start(b); };
+    if (!std::is_sorted(items, items + count, before)) std::sort(items, items + count, before);
+    uintptr_t outs = 0, all = 0;  // ends of what starts earlier: outputs, anything
+    for (size_t k = 0; k < count; ++k) {
+        const uint32_t i = items[k];
+        if (start(i) < (i & 1 ? outs : all)) return true;
+        all = std::max(all, end(i));
+        if (!(i & 1)) outs = std::max(outs, end(i));
+    }
+    return false;
 }
 
 size_t norm_part_bytes(const kan::NormPlan& p, int32_t n) {
@@ -222,6 +284,37 @@ kan_status kan_token_logprobs_backward(kan_dtype dtype, int64_t rows, int32_t cl
     a.classes = classes;
     return device_status(kan::launch_logprob_grad(dtype == KAN_BF16, a,
                                                   static_cast<hipStream_t>(stream)));
+}
+
+kan_status kan_grad_norm_workspace_bytes(int32_t count, size_t* bytes) {
+    if (bytes == nullptr || count < 0 || count > kan::kClipMaxTensors) return KAN_ERR_INVALID_ARG;
+    *bytes = kan::clip_workspace(count);
+    return KAN_OK;
+}
+
+kan_status kan_grad_norm(int32_t count, const void* const* grads, const int64_t* sizes,
+                         const int32_t* dtypes, void* workspace, size_t workspace_bytes,
+                         float* norm, void* stream) {
+    const kan::ClipList l = {count, grads, nullptr, sizes, dtypes};
+    const kan_status st = check_clip(l, workspace, workspace_bytes, norm);
+    if (st != KAN_OK) return st;
+    return device_status(
+        kan::launch_clip(l, 0.0f, 0.0f, norm, workspace, static_cast<hipStream_t>(stream)));
+}
+
+kan_status kan_clip_grad_norm(int32_t count, const void* const* grads, const int64_t* sizes,
+                              const int32_t* dtypes, float max_norm, float eps, void* const* out,
+                              void* workspace, size_t workspace_bytes, float* norm,
+                              void* stream) {
+    if (!(max_norm >= 0.0f) || !(eps >= 0.0f) || !std::isfinite(eps)) return KAN_ERR_INVALID_ARG;
+    if (count > 0 && out == nullptr) return KAN_ERR_INVALID_ARG;
+    void* const none = nullptr;
+    const kan::ClipList l = {count, grads, count > 0 ? out : &none, sizes, dtypes};
+    const kan_status st = check_clip(l, workspace, workspace_bytes, norm);
+    if (st != KAN_OK) return st;
+    if (clip_outputs_clash(l)) return KAN_ERR_INVALID_ARG;
+    return device_status(kan::launch_clip(l, max_norm, eps, norm, workspace,
+                                          static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

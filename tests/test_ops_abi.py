@@ -95,3 +95,46 @@ def test_token_logprobs_backward_host_checks():
         assert call(**kw) == BAD, kw
     assert call(dtype=-1) == kb.KAN_ERR_UNSUPPORTED
     assert call(rows=0, z=0, t=0, stats=0, dl=0, ent=0, de=0, dz=0) == OK
+
+
+G0, G1, O0, O1, NM = (0x100000000 * (i + 48) for i in range(5))
+
+
+def test_clip_grad_norm_host_checks():
+    st, need = kb.kan_grad_norm_workspace_bytes(2)
+    assert st == OK and need > 0
+
+    def call(g=(G0, G1), n=(100, 7), d=(F32, BF16), mx=1.0, eps=1e-6, o=(O0, O1), ws=WS, nb=need,
+             nm=NM):
+        return kb.kan_clip_grad_norm(g, n, d, mx, eps, o, ws, nb, nm)
+    for kw in (dict(g=(0, G1)), dict(o=(0, O1)), dict(n=(-1, 7)), dict(n=(1 << 40, 1)),
+               dict(mx=-1.0), dict(mx=math.nan), dict(eps=-1.0), dict(eps=math.inf), dict(o=None),
+               dict(ws=0), dict(ws=WS + 8), dict(nb=need - 1), dict(nm=0), dict(nm=NM + 2),
+               dict(nm=WS + 4), dict(nm=G0 + 4), dict(nm=O1), dict(ws=G1), dict(ws=O0),
+               dict(g=(G0 + 2, G1)), dict(g=(G0, G1 + 1)), dict(o=(O0, O1 + 1)),
+               dict(o=(G0 + 4, O1)), dict(o=(G1, O1)), dict(o=(O0, O0)), dict(o=(O0, O0 + 396)),
+               dict(o=(O0, G0)), dict(g=(G0, G0), d=(F32, F32), o=(G0, G0)),
+               dict(g=(G0, G0 + 396), d=(F32, F32), o=(G0, G0 + 396))):
+        assert call(**kw) == BAD, kw
+    assert call(d=(F32, 2)) == kb.KAN_ERR_UNSUPPORTED
+    def norm(g=(G0, G1), n=(100, 7), d=(F32, BF16), ws=WS, nb=need, nm=NM):
+        return kb.kan_grad_norm(g, n, d, ws, nb, nm)
+    for kw in (dict(g=(0, G1)), dict(n=(100, -7)), dict(ws=0), dict(nb=need - 1), dict(nm=0),
+               dict(nm=G1), dict(ws=G0 - 16)):
+        assert norm(**kw) == BAD, kw
+    assert norm(d=(-1, F32)) == kb.KAN_ERR_UNSUPPORTED
+    assert kb.kan_grad_norm_workspace_bytes(-1)[0] == BAD
+    assert kb.kan_grad_norm_workspace_bytes(16385)[0] == BAD
+    assert kb.load_library().kan_grad_norm_workspace_bytes(1, None) == BAD
+
+
+def test_clip_outputs_of_many_tensors():
+    """The overlap check over thousands of tensors in any order (no device: an invalid dtype
+    is found first, an overlap last, so both orders of 5000 end in the code asked for)."""
+    count = 5000
+    st, need = kb.kan_grad_norm_workspace_bytes(count)
+    order = [(i * 1237) % count for i in range(count)]
+    g = [G0 + 64 * i for i in order]
+    bad = g[:-1] + [g[0] + 4]
+    assert kb.kan_clip_grad_norm(bad, [16] * count, [F32] * count, 1.0, 1e-6, bad, WS, need,
+                                 NM) == BAD

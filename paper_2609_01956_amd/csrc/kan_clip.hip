@@ -47,7 +47,7 @@ __device__ __forceinline__ double chunk_squares(const T* p, int n) {
     double s = 0.0;
     for (int i = threadIdx.x * V; i < n; i += 256 * V) {
         float v[V];
-        load_unit<false>(p, i, n, 0.0f, v);
+        load_unit(p, i, n, 0u, v);
 #pragma unroll
         for (int k = 0; k < V; ++k) s = __builtin_fma((double)v[k], (double)v[k], s);
     }
@@ -92,7 +92,7 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* q, int n, double c) {
     constexpr int V = kVec<T>;
     for (int i = threadIdx.x * V; i < n; i += 256 * V) {
         float v[V];
-        load_unit<false>(p, i, n, 0.0f, v);
+        load_unit(p, i, n, 0u, v);
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = (float)((double)v[k] * c);
         store_unit<false>(q, i, n, v);

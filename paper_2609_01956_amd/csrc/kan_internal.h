@@ -381,6 +381,7 @@ struct NormArgs {
     int n;
     float eps;
     int shift;  // log2 of the lanes that share a row (one unit per lane)
+    int waves;  // waves that share a row
 };
 struct NormGradArgs {
     const void *h, *w, *dy, *dh;  // w, dh may be null
@@ -389,16 +390,18 @@ struct NormGradArgs {
     float* part;  // [2][parts][n] partial weight gradients; null: none wanted
     int64_t rows;
     int n;
-    int shift;
+    int shift, waves;
 };
 // Longest row that stays in registers.
 constexpr int kNormRegRow = 16384;
 struct NormPlan {
-    int waves;   // waves per row (1, 4, 8), 0: rows longer than kNormRegRow
-    int units;   // 16-byte units per lane
-    int shift;   // log2 of the lanes of a row within a wave (one unit per lane)
-    int blocks;  // workgroups
-    int parts;   // partial weight gradients (backward)
+    int waves;    // per row; 0: rows longer than kNormRegRow
+    int units;    // 16-byte units per lane
+    int shift;    // log2 of the lanes of a row within a wave (one unit per lane)
+    int threads;  // of a workgroup
+    size_t lds;   // bytes (backward)
+    int blocks;   // workgroups
+    int parts;    // partial weight gradients (backward)
 };
 // es: bytes per element of the rows.
 NormPlan norm_plan(int64_t rows, int32_t n, int es, bool grad);

@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(256) logprob_short_kernel(LogprobArgs a) {
         const bool live = row < a.rows;
         const int n = live ? a.classes : 0;
         float v[V];
-        load_unit<false>(static_cast<const T*>(a.z) + (live ? row * a.stride : 0), slot * V, n,
-                         kNegInf, v);
+        load_unit(static_cast<const T*>(a.z) + (live ? row * a.stride : 0), slot * V, n,
+                  kNegInfBits<T>, v);
         Sums r = {kNegInf, 0.0f, 0.0f};
         add_values<true>(r, v, max_of(v));
         join_lanes(r, lanes);
@@ -216,17 +216,28 @@ __global__ void __launch_bounds__(256) logprob_short_kernel(LogprobArgs a) {
 constexpr int kTileElems = 32;  // per lane
 constexpr int kTile = 64 * kTileElems;
 
+template <typename T> constexpr int kTileUnits = kTileElems / kVec<T>;
+
 // One tile of a row into registers, 16-byte units interleaved over the lanes.
 template <typename T>
 __device__ __forceinline__ void load_tile(const T* row, int base, int n, int lane,
-                                          float (&v)[kTileElems]) {
+                                          u32x4 (&raw)[kTileUnits<T>]) {
     constexpr int V = kVec<T>;
-    StaticFor<0, kTileElems / V>::run([&](auto u) {
+    issue_units<0, false>(row, base + lane * V, 64 * V, n, 0u, raw);
+    if (base + kTile > n) settle_units<0, false, T>(base + lane * V, 64 * V, n, kNegInfBits<T>, raw);
+}
+
+template <typename T>
+__device__ __forceinline__ void widen_tile(const u32x4 (&raw)[kTileUnits<T>],
+                                           float (&v)[kTileElems]) {
+    constexpr int V = kVec<T>;
+#pragma unroll
+    for (int u = 0; u < kTileUnits<T>; ++u) {
         float unit[V];
-        load_unit<false>(row, base + (u * 64 + lane) * V, n, kNegInf, unit);
+        widen(raw[u], unit);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[u * V + i] = unit[i];
-    });
+    }
 }
 
 // Offers a tile's elements that can enter the best k (see the file's comment); `vm` is the
@@ -265,8 +276,10 @@ __global__ void __launch_bounds__(256) logprob_kernel(LogprobArgs a) {
         Best best(TOP ? a.k : 1);
         const int tiles = (a.classes + kTile - 1) / kTile;
         for (int t = p * W + (W == 1 ? 0 : wave); t < tiles; t += a.parts * W) {
+            u32x4 raw[kTileUnits<T>];
+            load_tile(z, t * kTile, a.classes, lane, raw);
             float v[kTileElems];
-            load_tile(z, t * kTile, a.classes, lane, v);
+            widen_tile<T>(raw, v);
             const float vm = max_of(v);
             add_values<ENT>(r, v, vm);
             if (TOP) offer_tile<T>(best, v, vm, t * kTile, a.classes, lane);
@@ -363,7 +376,7 @@ __global__ void __launch_bounds__(256) logprob_grad_short_kernel(LogprobGradArgs
         if (slot * V >= a.classes) continue;
         const RowGrad g = row_grad(a, row);
         float v[V];
-        load_unit<false>(static_cast<const T*>(a.z) + row * a.stride, slot * V, a.classes, 0.0f, v);
+        load_unit(static_cast<const T*>(a.z) + row * a.stride, slot * V, a.classes, 0u, v);
         unit_grad(g, slot * V, v);
         store_unit<false>(static_cast<T*>(a.dz) + row * a.dstride, slot * V, a.classes, v);
     }
@@ -381,15 +394,17 @@ __global__ void __launch_bounds__(256) logprob_grad_kernel(LogprobGradArgs a) {
         const RowGrad g = row_grad(a, row);
         const T* z = static_cast<const T*>(a.z) + row * a.stride;
         T* dz = static_cast<T*>(a.dz) + row * a.dstride;
-        float v[kGradUnits][V];
-#pragma unroll
-        for (int u = 0; u < kGradUnits; ++u)
-            load_unit<false>(z, base + (u * 256 + (int)threadIdx.x) * V, a.classes, 0.0f, v[u]);
+        const int first = base + (int)threadIdx.x * V;
+        u32x4 raw[kGradUnits];
+        issue_units<0, false>(z, first, 256 * V, a.classes, 0u, raw);
+        if (base + 256 * kGradUnits * V > a.classes)
+            settle_units<0, false, T>(first, 256 * V, a.classes, 0u, raw);
 #pragma unroll
         for (int u = 0; u < kGradUnits; ++u) {
-            const int col = base + (u * 256 + (int)threadIdx.x) * V;
-            unit_grad(g, col, v[u]);
-            store_unit<false>(dz, col, a.classes, v[u]);
+            float v[V];
+            widen(raw[u], v);
+            unit_grad(g, first + u * 256 * V, v);
+            store_unit<false>(dz, first + u * 256 * V, a.classes, v);
         }
     }
 }

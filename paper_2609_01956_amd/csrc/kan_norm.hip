@@ -26,23 +26,66 @@ namespace kan {
 
 namespace {
 
-// Sums a and b over the W waves of a workgroup (all waves call; `red` is a buffer that
-// no wave still reads: the callers alternate two).
-template <int W>
-__device__ __forceinline__ void wave_join(float& a, float& b, float (*red)[2], int wave, int lane) {
-    if (W == 1) return;
-    if (lane == 0) {
-        red[wave][0] = a;
-        red[wave][1] = b;
+constexpr int kMaxWaves = 8;
+
+// How a workgroup takes rows.
+enum Mode {
+    kShared,  // four waves, 64 >> shift rows in each, one unit per lane (32 lanes a row at most)
+    kWave,    // four waves, a row each (33 units or more)
+    kGroup,   // a.waves waves a row, as many rows as eight waves take
+};
+
+// Where a lane works.
+template <int M>
+struct Place {
+    int lane, wave;
+    int first, waves;  // kGroup: the waves of the row
+    int lanes;         // lanes that share a row, within the wave
+    int slot;          // this lane's place among all lanes of the row
+    int stride;        // lanes of the row, over all waves
+    int rows;          // rows a workgroup takes at a time
+    int sub;           // this lane's row among them
+    __device__ __forceinline__ Place(int shift, int waves_) : waves(waves_) {
+        lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        lanes = M == kShared ? 1 << shift : 64;
+        if (M == kGroup) {
+            rows = (int)(blockDim.x >> 6) / waves;
+            sub = wave / waves;
+        } else {
+            rows = M == kShared ? 256 >> shift : 4;
+            sub = M == kShared ? (int)threadIdx.x >> shift : wave;
+        }
+        first = M == kGroup ? sub * waves : 0;
+        stride = M == kGroup ? 64 * waves : lanes;
+        slot = M == kShared ? lane & (lanes - 1)
+               : M == kWave ? lane
+                            : (wave - first) * 64 + lane;
     }
-    __syncthreads();
-    a = b = 0.0f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-        a += red[w][0];
-        b += red[w][1];
+
+    // Sums over the lanes of a row (all lanes of the workgroup call).  kGroup: `red` is a
+    // buffer that no wave still reads (the callers alternate two).
+    __device__ __forceinline__ void sum(float& a, float& b, float (*red)[2]) const {
+        if (M == kShared) {
+            a = group_sum(a, lanes);
+            b = group_sum(b, lanes);
+            return;
+        }
+        a = wave_sum(a);
+        b = wave_sum(b);
+        if (M == kWave) return;
+        if (lane == 0) {
+            red[wave][0] = a;
+            red[wave][1] = b;
+        }
+        __syncthreads();
+        a = b = 0.0f;
+        for (int w = 0; w < waves; ++w) {
+            a += red[first + w][0];
+            b += red[first + w][1];
+        }
     }
-}
+};
 
 // The variance from the mean square q around a rounded mean that is e off: q - e^2, which
 // takes away next to nothing (and never all but rounding: e is a rounding of the mean).
@@ -50,107 +93,96 @@ __device__ __forceinline__ float spread(float q, float e) {
     return q - __builtin_fminf(e * e, q);
 }
 
-// Where a lane works.  W waves take a row (W = 1: each wave of the four its own row, or,
-// with one unit per lane, 64 >> shift rows).
-template <int W, int C>
-struct Place {
-    static constexpr bool kSub = W == 1 && C == 1;
-    int lane, wave;
-    int lanes;   // lanes that share a row, within the wave
-    int slot;    // this lane's place among all lanes of the row
-    int stride;  // lanes of the row, over all waves
-    int rows;    // rows a workgroup takes at a time
-    int sub;     // this lane's row among them
-    __device__ __forceinline__ explicit Place(int shift) {
-        lane = threadIdx.x & 63;
-        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        lanes = kSub ? 1 << shift : 64;
-        slot = kSub ? lane & (lanes - 1) : W == 1 ? lane : (int)threadIdx.x;
-        stride = kSub ? lanes : 64 * W;
-        rows = kSub ? 256 >> shift : W == 1 ? 4 : 1;
-        sub = kSub ? (int)threadIdx.x >> shift : W == 1 ? wave : 0;
-    }
-};
+// (the instruction is good to one unit in the last place)
+__device__ __forceinline__ float inverse_root(float v) { return __builtin_amdgcn_rsqf(v); }
 
-template <int W> constexpr int kThreads = W == 8 ? 512 : 256;
+template <int N>
+__device__ __forceinline__ void clear_units(u32x4 (&raw)[N]) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) raw[u] = u32x4{0u, 0u, 0u, 0u};
+}
+
+template <int M> constexpr int kThreads = M == kGroup ? 64 * kMaxWaves : 256;
 
 // C units per lane, of which the first FC are full in every lane.
-template <typename T, typename TP, int W, int C, int FC>
-__global__ void __launch_bounds__(kThreads<W>) norm_kernel(NormArgs a) {
+template <typename T, typename TP, int M, int C, int FC>
+__global__ void __launch_bounds__(kThreads<M>) norm_kernel(NormArgs a) {
     constexpr int V = kVec<T>;
-    __shared__ float red[2][W][2];
-    const Place<W, C> p(a.shift);
-    const int n = a.n;
+    constexpr bool kSub = M == kShared;
+    __shared__ float red[2][kMaxWaves][2];
+    const Place<M> p(a.shift, a.waves);
+    const int n = a.n, col0 = p.slot * V, step = p.stride * V;
     const float inv_n = 1.0f / (float)n;
     float w[C][V], b[C][V];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int col = (p.slot + c * p.stride) * V;
-        load_params(static_cast<const TP*>(a.w), col, n, 1.0f, w[c]);
-        load_params(static_cast<const TP*>(a.b), col, n, 0.0f, b[c]);
+        load_params<kSub>(static_cast<const TP*>(a.w), col0 + c * step, n, 1.0f, w[c]);
+        load_params<kSub>(static_cast<const TP*>(a.b), col0 + c * step, n, 0.0f, b[c]);
     }
     for (int64_t r0 = (int64_t)blockIdx.x * p.rows; r0 < a.rows;
          r0 += (int64_t)gridDim.x * p.rows) {
         const int64_t row = r0 + p.sub;
-        if (W == 1 && !Place<W, C>::kSub && row >= a.rows) break;
-        // (rows that share a wave: no loads or stores past the last one)
-        const bool live = !Place<W, C>::kSub || row < a.rows;
+        if (M == kWave && row >= a.rows) break;
+        // (past the last row nothing is stored; the first row's values stand in)
+        const bool live = M == kWave || row < a.rows;
         const int nl = live ? n : 0;
         const int64_t at = live ? row * n : 0;
         float v[C][V];
-        StaticFor<0, C>::run([&](auto c) {
-            load_unit<(c < FC)>(static_cast<const T*>(a.x) + at,
-                                          (p.slot + c * p.stride) * V, nl, 0.0f, v[c]);
-        });
-        if (a.res != nullptr) {
-            StaticFor<0, C>::run([&](auto c) {
-                float r[V];
-                load_unit<(c < FC)>(static_cast<const T*>(a.res) + at,
-                                              (p.slot + c * p.stride) * V, nl, 0.0f, r);
+        u32x4 rx[C], rr[C];
+        issue_units<FC, kSub>(static_cast<const T*>(a.x) + at, col0, step, n, 0u, rx);
+        if (a.res != nullptr)
+            issue_units<FC, kSub>(static_cast<const T*>(a.res) + at, col0, step, n, 0u, rr);
+        else
+            clear_units(rr);
+        settle_units<FC, kSub, T>(col0, step, n, 0u, rx);
+        settle_units<FC, kSub, T>(col0, step, n, 0u, rr);
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[c][i] += r[i];
-            });
+        for (int c = 0; c < C; ++c) {
+            float r[V];
+            widen(rx[c], v[c]);
+            widen(rr[c], r);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[c][i] += r[i];
         }
-        if (a.h != nullptr) {
-            StaticFor<0, C>::run([&](auto c) {
-                store_unit<(c < FC)>(static_cast<T*>(a.h) + at,
-                                               (p.slot + c * p.stride) * V, nl, v[c]);
-            });
+        if (a.h != nullptr && live) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if (c < FC) store_unit<true>(static_cast<T*>(a.h) + at, col0 + c * step, n, v[c]);
+                else store_unit<false>(static_cast<T*>(a.h) + at, col0 + c * step, n, v[c]);
+            }
         }
-        float s = 0.0f, none = 0.0f;
+        float s = 0.0f, q = 0.0f, e = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int i = 0; i < V; ++i) s += v[c][i];
-        s = group_sum(s, p.lanes);
-        wave_join<W>(s, none, red[0], p.wave, p.lane);
+        p.sum(s, e, red[0]);
         const float mu = s * inv_n;
-        float q = 0.0f, e = 0.0f;
+        e = 0.0f;
         StaticFor<0, C>::run([&](auto c) {
-            const int col = (p.slot + c * p.stride) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float d = (c < FC) || col + i < n ? v[c][i] - mu : 0.0f;
+                const float d = (c < FC) || col0 + c * step + i < n ? v[c][i] - mu : 0.0f;
                 v[c][i] = d;
                 e += d;
                 q = __builtin_fmaf(d, d, q);
             }
         });
-        q = group_sum(q, p.lanes);
-        e = group_sum(e, p.lanes);
-        wave_join<W>(q, e, red[1], p.wave, p.lane);
+        p.sum(q, e, red[1]);
         // what the rounding of the sum left out of the mean
         e *= inv_n;
-        const float rstd = 1.0f / __builtin_sqrtf(spread(q * inv_n, e) + a.eps);
+        const float rstd = inverse_root(spread(q * inv_n, e) + a.eps);
         if (a.mean != nullptr && live && p.slot == 0) {
             a.mean[row] = mu + e;
             a.rstd[row] = rstd;
         }
         StaticFor<0, C>::run([&](auto c) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[c][i] = __builtin_fmaf((v[c][i] - e) * rstd, w[c][i], b[c][i]);
-            store_unit<(c < FC)>(static_cast<T*>(a.y) + at, (p.slot + c * p.stride) * V,
-                                           nl, v[c]);
+            for (int i = 0; i < V; ++i)
+                v[c][i] = __builtin_fmaf((v[c][i] - e) * rstd, w[c][i], b[c][i]);
+            if (M == kGroup && !live) return;
+            store_unit<(c < FC) && M != kShared>(static_cast<T*>(a.y) + at, col0 + c * step, nl,
+                                                 v[c]);
         });
     }
 }
@@ -158,30 +190,28 @@ __global__ void __launch_bounds__(kThreads<W>) norm_kernel(NormArgs a) {
 // Rows that do not fit in registers: one workgroup per row, read three times.
 template <typename T, typename TP>
 __global__ void __launch_bounds__(512) norm_long_kernel(NormArgs a) {
-    __shared__ float red[2][8][2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n;
+    __shared__ float red[2][kMaxWaves][2];
+    const Place<kGroup> p(0, 8);
+    const int n = a.n;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + row * n;
         const T* res = a.res ? static_cast<const T*>(a.res) + row * n : nullptr;
         auto value = [&](int i) {
             return Storage<T>::load(x + i) + (res ? Storage<T>::load(res + i) : 0.0f);
         };
-        float s = 0.0f, q = 0.0f, none = 0.0f;
+        float s = 0.0f, q = 0.0f, e = 0.0f;
         for (int i = threadIdx.x; i < n; i += 512) s += value(i);
-        s = group_sum(s, 64);
-        wave_join<8>(s, none, red[0], wave, lane);
+        p.sum(s, e, red[0]);
         const float mu = s / (float)n;
-        float e = 0.0f;
+        e = 0.0f;
         for (int i = threadIdx.x; i < n; i += 512) {
             const float d = value(i) - mu;
             e += d;
             q = __builtin_fmaf(d, d, q);
         }
-        q = group_sum(q, 64);
-        e = group_sum(e, 64);
-        wave_join<8>(q, e, red[1], wave, lane);
+        p.sum(q, e, red[1]);
         e /= (float)n;
-        const float rstd = 1.0f / __builtin_sqrtf(spread(q / (float)n, e) + a.eps);
+        const float rstd = inverse_root(spread(q / (float)n, e) + a.eps);
         if (a.mean != nullptr && threadIdx.x == 0) {
             a.mean[row] = mu + e;
             a.rstd[row] = rstd;
@@ -197,114 +227,155 @@ __global__ void __launch_bounds__(512) norm_long_kernel(NormArgs a) {
     }
 }
 
-template <typename T, typename TP, int W, int C, int FC>
-__global__ void __launch_bounds__(kThreads<W>) norm_grad_kernel(NormGradArgs a) {
+// What a row's gradient reads.
+template <typename T, int C>
+struct GradRow {
+    u32x4 h[C], dy[C], dh[C];
+    float mu, rstd;
+    template <int FC, bool TINY>
+    __device__ __forceinline__ void issue(const NormGradArgs& a, int64_t row, int col0, int step) {
+        const int64_t at = row * a.n;
+        issue_units<FC, TINY>(static_cast<const T*>(a.h) + at, col0, step, a.n, 0u, h);
+        issue_units<FC, TINY>(static_cast<const T*>(a.dy) + at, col0, step, a.n, 0u, dy);
+        if (a.dh != nullptr)
+            issue_units<FC, TINY>(static_cast<const T*>(a.dh) + at, col0, step, a.n, 0u, dh);
+        else
+            clear_units(dh);
+        mu = a.mean[row];
+        rstd = a.rstd[row];
+    }
+    // What stands in for a row past the last one adds nothing to the sums.
+    __device__ __forceinline__ void keep(bool live) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                h[c][i] = live ? h[c][i] : 0u;
+                dy[c][i] = live ? dy[c][i] : 0u;
+            }
+        mu = live ? mu : 0.0f;
+        rstd = live ? rstd : 0.0f;
+    }
+};
+
+template <typename T, typename TP, int M, int C, int FC>
+__global__ void __launch_bounds__(kThreads<M>) norm_grad_kernel(NormGradArgs a) {
     constexpr int V = kVec<T>;
-    __shared__ float red[2][W][2];
-    __shared__ float join[W == 1 ? 4 * 64 * C * V : 1];
-    const Place<W, C> p(a.shift);
-    const int n = a.n;
+    constexpr bool kSub = M == kShared;
+    __shared__ float red[2][kMaxWaves][2];
+    extern __shared__ float join[];  // where a workgroup takes several rows
+    const Place<M> p(a.shift, a.waves);
+    const int n = a.n, col0 = p.slot * V, step = p.stride * V;
     const float inv_n = 1.0f / (float)n;
     float w[C][V], dw[C][V], db[C][V];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        load_params(static_cast<const TP*>(a.w), (p.slot + c * p.stride) * V, n, 1.0f, w[c]);
+        load_params<kSub>(static_cast<const TP*>(a.w), col0 + c * step, n, 1.0f, w[c]);
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[c][i] = db[c][i] = 0.0f;
     }
+    const int64_t stride = (int64_t)gridDim.x * p.rows;
     int turn = 0;
-    for (int64_t r0 = (int64_t)blockIdx.x * p.rows; r0 < a.rows;
-         r0 += (int64_t)gridDim.x * p.rows, turn ^= 1) {
+    for (int64_t r0 = (int64_t)blockIdx.x * p.rows; r0 < a.rows; r0 += stride, turn ^= 1) {
         const int64_t row = r0 + p.sub;
-        if (W == 1 && !Place<W, C>::kSub && row >= a.rows) break;
-        const bool live = !Place<W, C>::kSub || row < a.rows;
-        const int nl = live ? n : 0;
-        const int64_t at = live ? row * n : 0;
-        float h[C][V], dy[C][V];
-        StaticFor<0, C>::run([&](auto c) {
-            const int col = (p.slot + c * p.stride) * V;
-            load_unit<(c < FC)>(static_cast<const T*>(a.h) + at, col, nl, 0.0f, h[c]);
-            load_unit<(c < FC)>(static_cast<const T*>(a.dy) + at, col, nl, 0.0f, dy[c]);
-        });
-        const float mu = live ? a.mean[row] : 0.0f, rstd = live ? a.rstd[row] : 0.0f;
+        if (M == kWave && row >= a.rows) break;
+        const bool live = M == kWave || row < a.rows;
+        GradRow<T, C> cur;
+        cur.template issue<FC, kSub>(a, live ? row : 0, col0, step);
+        settle_units<FC, kSub, T>(col0, step, n, 0u, cur.h);
+        settle_units<FC, kSub, T>(col0, step, n, 0u, cur.dy);
+        if (M != kWave) cur.keep(live);
+        const float mu = cur.mu, rstd = cur.rstd;
         float s1 = 0.0f, s2 = 0.0f;
-        // (dy is 0 past the row's end, and so is all that is summed of it, as long as xh is
-        // finite there: h takes the row's mean)
-        StaticFor<0, C>::run([&](auto c) {
-            const int col = (p.slot + c * p.stride) * V;
+        // (past the row's end dy is 0, and with it all that is summed)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float h[V], dy[V];
+            widen(cur.h[c], h);
+            widen(cur.dy[c], dy);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const bool in = (c < FC) || col + i < nl;
-                const float xh = in ? (h[c][i] - mu) * rstd : 0.0f;
-                const float g = dy[c][i] * w[c][i];
-                dw[c][i] = __builtin_fmaf(dy[c][i], xh, dw[c][i]);
-                db[c][i] += dy[c][i];
-                s1 += in ? g : 0.0f;
+                const float xh = (h[i] - mu) * rstd;
+                const float g = dy[i] * w[c][i];
+                dw[c][i] = __builtin_fmaf(dy[i], xh, dw[c][i]);
+                db[c][i] += dy[i];
+                s1 += g;
                 s2 = __builtin_fmaf(g, xh, s2);
-                h[c][i] = xh;
-                dy[c][i] = g;
             }
-        });
-        if (a.dx == nullptr) continue;
-        s1 = group_sum(s1, p.lanes);
-        s2 = group_sum(s2, p.lanes);
-        wave_join<W>(s1, s2, red[turn], p.wave, p.lane);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        p.sum(s1, s2, red[turn]);
         s1 *= inv_n;
         s2 *= inv_n;
-        StaticFor<0, C>::run([&](auto c) {
-            const int col = (p.slot + c * p.stride) * V;
-            float d[V];
-            if (a.dh != nullptr)
-                load_unit<(c < FC)>(static_cast<const T*>(a.dh) + at, col, nl, 0.0f, d);
-            else
+        settle_units<FC, kSub, T>(col0, step, n, 0u, cur.dh);
+        // xh and g are formed again from the 16-byte units, which take half or less of the
+        // registers that they would take as fp32
 #pragma unroll
-                for (int i = 0; i < V; ++i) d[i] = 0.0f;
+        for (int c = 0; c < C; ++c) {
+            asm volatile("" : "+v"(cur.h[c]), "+v"(cur.dy[c]), "+v"(cur.dh[c]));
+            float h[V], dy[V], d[V];
+            widen(cur.h[c], h);
+            widen(cur.dy[c], dy);
+            widen(cur.dh[c], d);
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                d[i] = __builtin_fmaf(rstd, dy[c][i] - s1 - h[c][i] * s2, d[i]);
-            store_unit<(c < FC)>(static_cast<T*>(a.dx) + at, col, nl, d);
-        });
+            for (int i = 0; i < V; ++i) {
+                const float xh = (h[i] - mu) * rstd, g = dy[i] * w[c][i];
+                d[i] = __builtin_fmaf(rstd, g - s1 - xh * s2, d[i]);
+            }
+            if (a.dx != nullptr && live) {
+                T* dx = static_cast<T*>(a.dx) + row * n;
+                if (c < FC) store_unit<true>(dx, col0 + c * step, n, d);
+                else store_unit<false>(dx, col0 + c * step, n, d);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     if (a.part == nullptr) return;
-    // this workgroup's sums: [2][workgroups][n]
-    float* out = a.part + (int64_t)blockIdx.x * n;
-    const int64_t half = (int64_t)gridDim.x * n;
+    // This workgroup's sums, [2][workgroups][n]: over the rows of a wave by lanes, over the
+    // rows of the workgroup through LDS, [rows][columns of the lanes].
+    const int rows = M == kGroup ? p.rows : 4, mine = M == kGroup ? p.sub : p.wave;
+    const int span = C * step;
     for (int k = 0; k < 2; ++k) {
         float(&acc)[C][V] = k == 0 ? dw : db;
-        if (W > 1) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int col = (p.slot + c * p.stride) * V;
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (col + i < n) out[k * half + col + i] = acc[c][i];
-            }
-            continue;
-        }
-        if (Place<W, C>::kSub)
+        float* out = a.part + ((int64_t)k * gridDim.x + blockIdx.x) * n;
+        if (M == kShared)
             for (int o = p.lanes; o < 64; o *= 2)
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[0][i] += __shfl_xor(acc[0][i], o);
-        __syncthreads();
-        const int span = p.stride * C * V;  // columns of a wave's sums, at least n
+        if (rows == 1) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < V; i += 4) {
+                    const float u[4] = {acc[c][i], acc[c][i + 1], acc[c][i + 2], acc[c][i + 3]};
+                    store_unit<false>(out, col0 + c * step + i, n, u);
+                }
+            continue;
+        }
+        if (k == 1) __syncthreads();
         if (p.lane < p.lanes) {
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    join[p.wave * span + (p.slot + c * p.stride) * V + i] = acc[c][i];
+                for (int i = 0; i < V; i += 4)
+                    *reinterpret_cast<floatx4*>(join + mine * span + col0 + c * step + i) =
+                        floatx4{acc[c][i], acc[c][i + 1], acc[c][i + 2], acc[c][i + 3]};
         }
         __syncthreads();
-        for (int j = threadIdx.x; j < n; j += 256)
-            out[k * half + j] = (join[j] + join[span + j]) + (join[2 * span + j] + join[3 * span + j]);
+        for (int j = threadIdx.x; j < n; j += blockDim.x) {
+            float t = join[j];
+            for (int r = 1; r < rows; ++r) t += join[r * span + j];
+            out[j] = t;
+        }
     }
 }
 
 // dx of rows that do not fit in registers: one workgroup per row, read twice.
 template <typename T, typename TP>
 __global__ void __launch_bounds__(512) norm_grad_long_kernel(NormGradArgs a) {
-    __shared__ float red[2][8][2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n;
+    __shared__ float red[2][kMaxWaves][2];
+    const Place<kGroup> p(0, 8);
+    const int n = a.n;
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         const T* h = static_cast<const T*>(a.h) + row * n;
@@ -320,9 +391,7 @@ __global__ void __launch_bounds__(512) norm_grad_long_kernel(NormGradArgs a) {
             s1 += g;
             s2 = __builtin_fmaf(g, (Storage<T>::load(h + i) - mu) * rstd, s2);
         }
-        s1 = group_sum(s1, 64);
-        s2 = group_sum(s2, 64);
-        wave_join<8>(s1, s2, red[turn], wave, lane);
+        p.sum(s1, s2, red[turn]);
         s1 /= (float)n;
         s2 /= (float)n;
         for (int i = threadIdx.x; i < n; i += 512) {
@@ -354,25 +423,33 @@ __global__ void __launch_bounds__(256) norm_grad_columns_kernel(NormGradArgs a) 
     a.part[((int64_t)gridDim.y + blockIdx.y) * a.n + col] = db;
 }
 
-// dw (blockIdx.y 0) and db (1) from the workgroups' sums, in a fixed order: 32 columns
-// per workgroup, 32 lanes of each column over the parts.
+// dw (blockIdx.y 0) and db (1) from the workgroups' sums, in a fixed order: 16 columns
+// per workgroup, 64 lanes of each column over the parts, eight loads in flight.
 template <typename TP>
 __global__ void __launch_bounds__(1024) norm_params_kernel(const float* part, int parts, int n,
                                                            TP* dw, TP* db) {
-    __shared__ float sums[32][33];
+    __shared__ float sums[16][65];
     TP* out = blockIdx.y == 0 ? dw : db;
     if (out == nullptr) return;
-    const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
-    const int col = blockIdx.x * 32 + c;
+    const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const int col = blockIdx.x * 16 + c;
     const float* src = part + (int64_t)blockIdx.y * parts * n;
-    float s = 0.0f;
-    if (col < n)
-        for (int k = g; k < parts; k += 32) s += src[(int64_t)k * n + col];
+    float s = 0.0f, t[8] = {};
+    if (col < n) {
+        int k = g;
+        for (; k + 7 * 64 < parts; k += 8 * 64)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] += src[(int64_t)(k + j * 64) * n + col];
+        for (; k < parts; k += 64) s += src[(int64_t)k * n + col];
+    }
+    s += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
     sums[c][g] = s;
     __syncthreads();
-    // (lane g of column c: 32 neighbouring lanes add one column)
-    s = group_sum(sums[g][c], 32);
-    if (c == 0 && blockIdx.x * 32 + g < n) Storage<TP>::store(out + blockIdx.x * 32 + g, s);
+    // (a wave adds one column)
+    const int wave = threadIdx.x >> 6;
+    s = wave_sum(sums[wave][threadIdx.x & 63]);
+    if ((threadIdx.x & 63) == 0 && blockIdx.x * 16 + wave < n)
+        Storage<TP>::store(out + blockIdx.x * 16 + wave, s);
 }
 
 constexpr int kLongParts = 64;
@@ -380,31 +457,35 @@ constexpr int kLongParts = 64;
 }  // namespace
 
 NormPlan norm_plan(int64_t rows, int32_t n, int es, bool grad) {
-    NormPlan p;
+    NormPlan p = {};
     const int V = 16 / es;
-    p.shift = 6;
-    p.waves = 1;
-    p.units = 1;
-    int64_t per = 4;
+    int64_t per = 1, most = 2048;
+    p.threads = 512;
     if (n > kNormRegRow) {
         p.waves = 0;
-        p.units = 0;
-        per = 1;
-    } else if (n <= 64 * V) {
-        p.shift = 0;
-        while (V << p.shift < n) ++p.shift;
+    } else if (n <= 1024) {
+        p.waves = 1;
+        p.threads = 256;
+        while (V << p.shift < n && p.shift < 6) ++p.shift;
         per = 256 >> p.shift;
+        p.units = p.shift < 6 || n <= 64 * V ? 1 : (n <= 512 ? 8 : 16) / V;
     } else {
-        // 32 elements per lane at most, in steps of 8 (at fewer than two units: 4-byte
-        // types only)
-        const int e = n <= 512 ? 8 : n <= 1024 ? 16 : n <= 1536 ? 24 : n <= 2048 ? 32
-                      : n <= 4096 ? 16 : n <= 6144 ? 24 : n <= 8192 ? 32 : n <= 12288 ? 24 : 32;
-        p.waves = n <= 2048 ? 1 : n <= 8192 ? 4 : 8;
-        p.units = e / V;
-        if (p.waves > 1) per = 1;
+        // 16 elements per lane, 32 where eight waves need them
+        p.units = (n <= 8192 ? 16 : 32) / V;
+        p.waves = (n + 64 * V * p.units - 1) / (64 * V * p.units);
+        per = 8 / p.waves;
+        p.threads = (int)(64 * p.waves * per);
     }
+    // Workgroups of the gradient: each leaves a row of partial sums, so no more than keep the
+    // memory busy (16384 x 1024 fp32: 512 43 us, 768 45, 1024 47; one unit per lane, 65536 x
+    // 300 bf16: 512 50 us, 768 41, 1024 38).
+    if (grad) most = p.units == 1 ? 1024 : n <= 8192 ? 512 : 256;
+    // (the weight gradients' join: the columns of all lanes of the workgroup's waves that take
+    // different rows)
+    if (grad && per > 1 && p.waves > 0)
+        p.lds = sizeof(float) * p.units * V *
+                (p.waves > 1 ? p.threads : p.units > 1 ? 256 : 4 << p.shift);
     const int64_t need = (rows + per - 1) / per;
-    const int64_t most = grad ? (p.waves == 8 ? 256 : 512) : 2048;
     p.blocks = (int)(need < most ? need : most);
     p.parts = p.waves == 0 ? (int)(rows < kLongParts ? rows : kLongParts) : p.blocks;
     return p;
@@ -412,33 +493,29 @@ NormPlan norm_plan(int64_t rows, int32_t n, int es, bool grad) {
 
 namespace {
 
-// f(integral constants W, C, FC) for a plan's kernel.
+// f(integral constants M, C, FC) for a plan's kernel.  At more than one unit per lane a row
+// has more than half of the lanes' columns (whole waves share it): the first half of the
+// units is full.
 template <typename T, typename F>
 void norm_dispatch(const NormPlan& p, F&& f) {
     constexpr int V = kVec<T>;
-    auto at = [&](auto w, auto e) {
-        // the units before the last eight elements are full in every lane
-        constexpr int C = decltype(e)::value / V;
-        f(w, std::integral_constant<int, C>{},
-          std::integral_constant<int, C - 8 / V>{});
+    auto go = [&](auto mode, auto units) {
+        constexpr int C = decltype(units)::value;
+        f(mode, units, std::integral_constant<int, C / 2>{});
     };
     using std::integral_constant;
-    const int e = p.units * V;
-    if (p.units == 1)
-        f(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 0>{});
-    else if (p.waves == 1) {
-        if (V == 4 && e == 8) at(integral_constant<int, 1>{}, integral_constant<int, V == 4 ? 8 : 16>{});
-        else if (e == 16) at(integral_constant<int, 1>{}, integral_constant<int, 16>{});
-        else if (e == 24) at(integral_constant<int, 1>{}, integral_constant<int, 24>{});
-        else at(integral_constant<int, 1>{}, integral_constant<int, 32>{});
-    } else if (p.waves == 4) {
-        if (e == 16) at(integral_constant<int, 4>{}, integral_constant<int, 16>{});
-        else if (e == 24) at(integral_constant<int, 4>{}, integral_constant<int, 24>{});
-        else at(integral_constant<int, 4>{}, integral_constant<int, 32>{});
-    } else {
-        if (e == 24) at(integral_constant<int, 8>{}, integral_constant<int, 24>{});
-        else at(integral_constant<int, 8>{}, integral_constant<int, 32>{});
-    }
+    if (p.shift < 6 && p.waves == 1)
+        go(integral_constant<int, kShared>{}, integral_constant<int, 1>{});
+    else if (p.units == 1)
+        go(integral_constant<int, kWave>{}, integral_constant<int, 1>{});
+    else if (p.waves > 1 && p.units == 32 / V)
+        go(integral_constant<int, kGroup>{}, integral_constant<int, 32 / V>{});
+    else if (p.waves > 1)
+        go(integral_constant<int, kGroup>{}, integral_constant<int, 16 / V>{});
+    else if (p.units == 16 / V)
+        go(integral_constant<int, kWave>{}, integral_constant<int, 16 / V>{});
+    else if constexpr (V == 4)
+        go(integral_constant<int, kWave>{}, integral_constant<int, 2>{});
 }
 
 template <typename T, typename TP>
@@ -447,10 +524,9 @@ hipError_t norm_forward(const NormPlan& p, const NormArgs& a, hipStream_t s) {
         norm_long_kernel<T, TP><<<p.blocks, 512, 0, s>>>(a);
         return hipGetLastError();
     }
-    norm_dispatch<T>(p, [&](auto w, auto c, auto fc) {
-        constexpr int W = decltype(w)::value;
-        norm_kernel<T, TP, W, decltype(c)::value, decltype(fc)::value>
-            <<<p.blocks, kThreads<W>, 0, s>>>(a);
+    norm_dispatch<T>(p, [&](auto m, auto c, auto fc) {
+        norm_kernel<T, TP, decltype(m)::value, decltype(c)::value, decltype(fc)::value>
+            <<<p.blocks, p.threads, 0, s>>>(a);
     });
     return hipGetLastError();
 }
@@ -467,14 +543,13 @@ hipError_t norm_backward(const NormPlan& p, const NormGradArgs& a, void* dw, voi
         if (a.part != nullptr)
             norm_grad_columns_kernel<T><<<dim3((a.n + 255) / 256, p.parts), 256, 0, s>>>(a);
     } else if (a.rows > 0) {
-        norm_dispatch<T>(p, [&](auto w, auto c, auto fc) {
-            constexpr int W = decltype(w)::value;
-            norm_grad_kernel<T, TP, W, decltype(c)::value, decltype(fc)::value>
-                <<<p.blocks, kThreads<W>, 0, s>>>(a);
+        norm_dispatch<T>(p, [&](auto m, auto c, auto fc) {
+            norm_grad_kernel<T, TP, decltype(m)::value, decltype(c)::value, decltype(fc)::value>
+                <<<p.blocks, p.threads, p.lds, s>>>(a);
         });
     }
     if ((e = hipGetLastError()) != hipSuccess || (dw == nullptr && db == nullptr)) return e;
-    norm_params_kernel<TP><<<dim3((a.n + 31) / 32, 2), 1024, 0, s>>>(
+    norm_params_kernel<TP><<<dim3((a.n + 15) / 16, 2), 1024, 0, s>>>(
         a.part, p.parts, a.n, static_cast<TP*>(dw), static_cast<TP*>(db));
     return hipGetLastError();
 }
@@ -483,6 +558,7 @@ hipError_t norm_backward(const NormPlan& p, const NormGradArgs& a, void* dw, voi
 
 hipError_t launch_norm(bool bf16, bool bf16_params, const NormPlan& p, NormArgs a, hipStream_t s) {
     a.shift = p.shift;
+    a.waves = p.waves;
     if (!bf16) return norm_forward<float, float>(p, a, s);
     if (bf16_params) return norm_forward<uint16_t, uint16_t>(p, a, s);
     return norm_forward<uint16_t, float>(p, a, s);
@@ -491,6 +567,7 @@ hipError_t launch_norm(bool bf16, bool bf16_params, const NormPlan& p, NormArgs 
 hipError_t launch_norm_grad(bool bf16, bool bf16_params, const NormPlan& p, NormGradArgs a,
                             void* dw, void* db, hipStream_t s) {
     a.shift = p.shift;
+    a.waves = p.waves;
     if (!bf16) return norm_backward<float, float>(p, a, dw, db, s);
     if (bf16_params) return norm_backward<uint16_t, uint16_t>(p, a, dw, db, s);
     return norm_backward<uint16_t, float>(p, a, dw, db, s);

@@ -158,7 +158,7 @@ kan_status kan_layer_norm(kan_dtype dtype, kan_dtype param_dtype, int64_t rows, 
     if (!placed({{x, t, es}, {residual, t, es}, {weight, w, ps}, {bias, w, ps}},
                 {{h, t, es}, {y, t, es}, {mean, s, 4}, {rstd, s, 4}}))
         return KAN_ERR_INVALID_ARG;
-    const kan::NormArgs a = {x, residual, weight, bias, h, y, mean, rstd, rows, n, eps, 0};
+    const kan::NormArgs a = {x, residual, weight, bias, h, y, mean, rstd, rows, n, eps, 0, 0};
     return device_status(kan::launch_norm(dtype == KAN_BF16, param_dtype == KAN_BF16,
                                           kan::norm_plan(rows, n, (int)es, false), a,
                                           static_cast<hipStream_t>(stream)));
@@ -195,7 +195,7 @@ kan_status kan_layer_norm_backward(kan_dtype dtype, kan_dtype param_dtype, int64
         return KAN_ERR_INVALID_ARG;
     if (rows == 0 && !params) return KAN_OK;
     const kan::NormGradArgs a = {h, weight, dy, dh, mean, rstd, dx,
-                                 need > 0 ? static_cast<float*>(workspace) : nullptr, rows, n, 0};
+                                 need > 0 ? static_cast<float*>(workspace) : nullptr, rows, n, 0, 0};
     return device_status(kan::launch_norm_grad(dtype == KAN_BF16, param_dtype == KAN_BF16, p, a,
                                                dweight, dbias, static_cast<hipStream_t>(stream)));
 }

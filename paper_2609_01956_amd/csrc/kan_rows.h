@@ -42,34 +42,132 @@ __device__ __forceinline__ u32x4 narrow(const float (&v)[4]) {
     return r;
 }
 
-// Elements col .. col + V - 1 of a row of n elements as fp32, V = one 16-byte unit; past
-// the row's end `fill`.  FULL: the unit is known to lie within the row.
-template <bool FULL, typename T, int V>
-__device__ __forceinline__ void load_unit(const T* row, int col, int n, float fill, float (&v)[V]) {
-    static_assert(V == kVec<T>, "one unit");
-    if (FULL || col + V <= n) {
-        widen(*reinterpret_cast<const u32x4_any*>(row + col), v);
+// The unit from column c >= 0 on (a 32-bit byte offset from the row: one register, where
+// the row is the wave's).
+template <typename T>
+__device__ __forceinline__ u32x4_any* unit_at(T* row, int c) {
+    return reinterpret_cast<u32x4_any*>(reinterpret_cast<char*>(row) + (uint32_t)c * (uint32_t)sizeof(T));
+}
+template <typename T>
+__device__ __forceinline__ const u32x4_any* unit_at(const T* row, int c) {
+    return unit_at(const_cast<T*>(row), c);
+}
+
+// A unit's elements moved down by `bits` (16 .. 112), with those of `fill` (a pattern that
+// repeats every 32 bits) above them.
+__device__ __forceinline__ u32x4 shift_down(u32x4 r, int bits, uint32_t fill) {
+    const uint64_t f = (uint64_t)fill << 32 | fill;
+    const uint64_t lo = (uint64_t)r[1] << 32 | r[0], hi = (uint64_t)r[3] << 32 | r[2];
+    const int s = bits & 63;
+    // (twice by half of 64 - s, so that a shift by 64 is none: s may be 0)
+    const uint64_t up = (hi >> s) | (f << 1 << (63 - s));
+    const uint64_t low = (lo >> s) | (hi << 1 << (63 - s));
+    const uint64_t l = bits >= 64 ? up : low, h = bits >= 64 ? f : up;
+    return u32x4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+}
+
+// Rows as 16-byte units in registers.  A lane's N units of a row of n elements start at
+// columns col + u step; the first FULL are known to lie within the row.  They come in two
+// calls, so that loads can be in flight while other work goes on:
+//
+// issue_units loads.  A unit that ends past the row's end is loaded where it ends with it,
+// and one that starts past it is too: one 16-byte load each, under no condition.  Rows
+// shorter than a unit (TINY: there may be such) are loaded by elements.
+//
+// settle_units, before the units are used, moves the former into place and puts `fill` (bits
+// of T) past the row's end.  There n may be 0 for lanes without a row, whatever they loaded.
+template <int FULL, bool TINY, typename T, int N>
+__device__ __forceinline__ void issue_units(const T* row, int col, int step, int n, uint32_t fill,
+                                            u32x4 (&raw)[N]) {
+    constexpr int V = kVec<T>;
+    if (TINY && n < V) {
+        const uint32_t f = sizeof(T) == 2 ? fill << 16 | fill : fill;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            raw[u] = u32x4{f, f, f, f};
+            const int c = col + u * step;
+#pragma unroll
+            for (int i = 0; i + 1 < V; ++i) {
+                if (c + i >= n) continue;
+                if constexpr (sizeof(T) == 2)
+                    raw[u][i / 2] = i % 2 ? (raw[u][i / 2] & 0xffffu) | (uint32_t)row[c + i] << 16
+                                          : (raw[u][i / 2] & 0xffff0000u) | row[c + i];
+                else
+                    raw[u][i] = __float_as_uint(row[c + i]);
+            }
+        }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = col + i < n ? Storage<T>::load(row + col + i) : fill;
+    for (int u = 0; u < N; ++u) {
+        const int c = col + u * step;
+        raw[u] = *unit_at(row, u < FULL ? c : min(c, n - V));
+    }
 }
 
+template <int FULL, bool TINY, typename T, int N>
+__device__ __forceinline__ void settle_units(int col, int step, int n, uint32_t fill,
+                                             u32x4 (&raw)[N]) {
+    constexpr int V = kVec<T>;
+    const uint32_t f = sizeof(T) == 2 ? fill << 16 | fill : fill;
+    if (n % V != 0 && !(TINY && n < V)) {
+        const int bits = (V - n % V) * 8 * (int)sizeof(T);
+#pragma unroll
+        for (int u = FULL; u < N; ++u) {
+            const u32x4 moved = shift_down(raw[u], bits, f);
+            const bool ends = col + u * step + V > n;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[u][i] = ends ? moved[i] : raw[u][i];
+        }
+    }
+#pragma unroll
+    for (int u = FULL; u < N; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[u][i] = col + u * step < n ? raw[u][i] : f;
+}
+
+// One unit as fp32, of a row of any length.
+template <typename T, int V>
+__device__ __forceinline__ void load_unit(const T* row, int col, int n, uint32_t fill,
+                                          float (&v)[V]) {
+    static_assert(V == kVec<T>, "one unit");
+    u32x4 raw[1];
+    issue_units<0, true>(row, col, 0, n, fill, raw);
+    settle_units<0, true, T>(col, 0, n, fill, raw);
+    widen(raw[0], v);
+}
+
+// Bits of -infinity.
+template <typename T> constexpr uint32_t kNegInfBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
+
+// One unit of a row of n elements, those within the row: the last unit's n % V elements as
+// 8, 4 and 2 bytes.
 template <bool FULL, typename T, int V>
 __device__ __forceinline__ void store_unit(T* row, int col, int n, const float (&v)[V]) {
     static_assert(V == kVec<T>, "one unit");
+    typedef uint32_t u32_any __attribute__((aligned(2)));
+    typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+    const u32x4 r = narrow(v);
     if (FULL || col + V <= n) {
-        *reinterpret_cast<u32x4_any*>(row + col) = narrow(v);
+        *unit_at(row, col) = r;
         return;
     }
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (col + i < n) Storage<T>::store(row + col + i, v[i]);
+    if (col >= n) return;
+    const int left = n - col;
+    constexpr int W = 4 / (int)sizeof(T);  // elements per word
+    T* p = row + col;
+    if (left & (2 * W)) *reinterpret_cast<u32x2_any*>(p) = (u32x2_any){r[0], r[1]};
+    if (left & W)
+        *reinterpret_cast<u32_any*>(p + (left & (2 * W))) = left & (2 * W) ? r[2] : r[0];
+    if (W == 2 && (left & 1)) {
+        const uint32_t w = left & 4 ? (left & 2 ? r[3] : r[2]) : left & 2 ? r[1] : r[0];
+        p[left & 6] = (T)w;
+    }
 }
 
-// V parameters (of T's own type or fp32) from column col on, `fill` past the end or
+// V parameters (of the rows' own type or fp32) from column col on, `fill` past the end or
 // where there are none (p == nullptr).
-template <typename TP, int V>
+template <bool TINY, typename TP, int V>
 __device__ __forceinline__ void load_params(const TP* p, int col, int n, float fill,
                                             float (&v)[V]) {
     if (p == nullptr) {
@@ -78,10 +176,14 @@ __device__ __forceinline__ void load_params(const TP* p, int col, int n, float f
         return;
     }
     constexpr int U = kVec<TP>;
+    u32x4 raw[V / U];
+    const uint32_t f = sizeof(TP) == 2 ? __float_as_uint(fill) >> 16 : __float_as_uint(fill);
+    issue_units<0, TINY>(p, col, U, n, f, raw);
+    settle_units<0, TINY, TP>(col, U, n, f, raw);
 #pragma unroll
     for (int k = 0; k < V / U; ++k) {
         float u[U];
-        load_unit<false>(p, col + k * U, n, fill, u);
+        widen(raw[k], u);
 #pragma unroll
         for (int i = 0; i < U; ++i) v[k * U + i] = u[i];
     }
@@ -122,6 +224,30 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
 }
 __device__ __forceinline__ float group_max(float v, int lanes) {
     return group_reduce(v, lanes, [](float a, float b) { return __builtin_fmaxf(a, b); });
+}
+
+// The same over all 64 lanes, in fewer steps: the last two rows of 16 are reached by
+// broadcasts, and the last lane's value is read (uniform over the wave).
+template <typename Op>
+__device__ __forceinline__ float wave_reduce(float v, float none, Op op) {
+    v = op(v, dppf<kDppXor1>(v));
+    v = op(v, dppf<kDppXor2>(v));
+    v = op(v, dppf<kDppHalfMirror>(v));
+    v = op(v, dppf<kDppMirror>(v));
+    const int z = (int)__float_as_uint(none);
+    // row 0 to row 1 and row 2 to row 3, then row 1 to rows 2 and 3
+    v = op(v, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(
+                  z, (int)__float_as_uint(v), 0x142, 0xa, 0xf, false)));
+    v = op(v, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(
+                  z, (int)__float_as_uint(v), 0x143, 0xc, 0xf, false)));
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    return wave_reduce(v, 0.0f, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v) {
+    return wave_reduce(v, -__builtin_huge_valf(),
+                       [](float a, float b) { return __builtin_fmaxf(a, b); });
 }
 
 }  // namespace kan

@@ -432,12 +432,14 @@ struct LogprobGradArgs {
     void* dz;
     int64_t rows, stride, dstride, ignore;
     int classes;
-    int shift;     // short rows
-    int segments;  // workgroups per row
+    int shift;       // short rows
+    uint32_t items;  // (row, tile)
+    uint32_t tiles;  // per row
 };
 constexpr int kMaxTop = 64;
 struct LogprobPlan {
     int waves;  // per (row, part), 0: rows that share a wave
+    int elems;  // of a tile, per lane
     int shift, parts;
     size_t bytes;  // workspace
 };

@@ -14,16 +14,17 @@
 // 0.  Everything is fp32; a masked class is -infinity (or so low that its weight is 0).
 //
 // Rows of at most one 16-byte unit per lane of half a wave share a wave.  Longer rows are
-// taken by one wave, or four where rows are long and many, or by several workgroups where
-// rows are few (each leaves its sums and its best k in the workspace and a second launch
-// joins them).
+// taken in tiles of up to 32 elements per lane, the next tile's loads in flight, by one wave,
+// or four where rows are long and many, or by several workgroups where rows are few (each
+// leaves its sums and its best k in the workspace and a second launch joins them).
 //
 // The best k of a wave stand sorted across its lanes, one 64-bit key per lane (the value's
 // bits in order, then the complement of the index, so that keys are distinct and ties go
 // to the lowest index).  A tile is looked at again only if some lane's largest value
-// reaches the k-th best so far; then only its elements that reach the k-th largest of the
-// lanes' own maxima can enter (k lanes hold one at least as large), so that few of a first
-// tile's elements are inserted, one after the other.
+// reaches the k-th best so far.  Then every such lane offers its largest: many at once (the
+// first tile) are sorted across the lanes and merged, few are inserted one after the
+// other; those lanes' next largest are compared again, until none reaches the k-th best.
+// The waves of a row share the k-th best that any of them has.
 #include "kan_internal.h"
 #include "kan_rows.h"
 
@@ -61,7 +62,14 @@ __device__ __forceinline__ void join_lanes(Sums& a, int lanes) {
     a.q = group_sum(a.q, lanes);
 }
 
-// Adds the N values (maximum vm among them) to a lane's sums.
+// Joined over the wave.
+__device__ __forceinline__ void join_wave(Sums& a) {
+    rescale(a, wave_max(a.m));
+    a.s = wave_sum(a.s);
+    a.q = wave_sum(a.q);
+}
+
+// Adds the N values (vm = max_of(v)) to a lane's sums.
 template <bool ENT, int N>
 __device__ __forceinline__ void add_values(Sums& a, const float (&v)[N], float vm) {
     rescale(a, __builtin_fmaxf(a.m, vm));
@@ -77,12 +85,13 @@ __device__ __forceinline__ void add_values(Sums& a, const float (&v)[N], float v
     a.q += q;
 }
 
+// The largest of the values that are numbers (NaN if none is).
 template <int N>
 __device__ __forceinline__ float max_of(const float (&v)[N]) {
     float m = v[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) m = __builtin_fmaxf(m, v[i]);
-    return __builtin_fmaxf(m, kNegInf);  // (of NaN alone: -infinity)
+    return m;
 }
 
 // (-infinity for a row without any class)
@@ -109,58 +118,113 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t key, int lane) {
     return (uint64_t)hi << 32 | lo;
 }
 
+// The key of lane `lane` ^ S.
+template <int S>
+__device__ __forceinline__ uint64_t key_xor(uint64_t key) {
+    const uint32_t lo = (uint32_t)key, hi = (uint32_t)(key >> 32);
+    if constexpr (S == 1) return (uint64_t)dpp<kDppXor1>(hi, hi) << 32 | dpp<kDppXor1>(lo, lo);
+    if constexpr (S == 2) return (uint64_t)dpp<kDppXor2>(hi, hi) << 32 | dpp<kDppXor2>(lo, lo);
+    if constexpr (S == 4) {
+        const uint32_t l = dpp<kDppHalfMirror>(lo, lo), h = dpp<kDppHalfMirror>(hi, hi);
+        return (uint64_t)dpp<kDppFlip4>(h, h) << 32 | dpp<kDppFlip4>(l, l);
+    }
+    if constexpr (S == 8) return (uint64_t)dpp<kDppRor8>(hi, hi) << 32 | dpp<kDppRor8>(lo, lo);
+    if constexpr (S >= 16) return __shfl_xor((unsigned long long)key, S);
+}
+
+// Lanes that keep the larger key in a step of a bitonic sort (largest first) of groups of
+// `size`: those whose bit `step` agrees with the order of their group.
+constexpr uint64_t keep_larger(int size, int step) {
+    uint64_t m = 0;
+    for (int l = 0; l < 64; ++l)
+        if (((l & step) == 0) == ((l & size) == 0)) m |= UINT64_C(1) << l;
+    return m;
+}
+template <int SIZE, int STEP>
+__device__ __forceinline__ uint64_t sort_step(uint64_t key) {
+    const uint64_t other = key_xor<STEP>(key);
+    const bool larger = __builtin_amdgcn_inverse_ballot_w64(keep_larger(SIZE, STEP));
+    return (other > key) == larger ? other : key;
+}
+// Steps STEP, STEP / 2 .. 1.
+template <int SIZE, int STEP>
+__device__ __forceinline__ uint64_t sort_steps(uint64_t key) {
+    key = sort_step<SIZE, STEP>(key);
+    if constexpr (STEP > 1) key = sort_steps<SIZE, STEP / 2>(key);
+    return key;
+}
+// The keys of a wave in falling order over its lanes.
+__device__ __forceinline__ uint64_t sort_keys(uint64_t key) {
+    key = sort_steps<2, 1>(key);
+    key = sort_steps<4, 2>(key);
+    key = sort_steps<8, 4>(key);
+    key = sort_steps<16, 8>(key);
+    key = sort_steps<32, 16>(key);
+    return sort_steps<64, 32>(key);
+}
+
 // The best k <= 64 keys of a wave: lane i holds the i-th best.  All lanes call.
 struct Best {
     uint64_t mine;  // this lane's key
-    uint64_t last;  // the k-th best (0: not full yet)
+    uint64_t bar;   // what a key has to pass: the k-th best (0: not full yet)
     int k;
 
-    __device__ __forceinline__ explicit Best(int k_) : mine(0), last(0), k(k_) {}
+    __device__ __forceinline__ explicit Best(int k_) : mine(0), bar(0), k(k_) {}
+
+    __device__ __forceinline__ void raise(uint64_t b) { bar = b > bar ? b : bar; }
+
+    // Merges 64 keys in falling order.
+    __device__ __forceinline__ void merge(uint64_t sorted, int lane) {
+        const uint64_t other = __shfl((unsigned long long)sorted, 63 - lane);
+        mine = sort_steps<64, 32>(other > mine ? other : mine);
+        raise(lane_key(mine, k - 1));
+    }
 
     // Offers one key per lane (0: none).
     __device__ __forceinline__ void offer(uint64_t key, int lane) {
-        uint64_t todo = __ballot(key > last);
+        uint64_t todo = __ballot(key > bar);
+        // (an insertion takes about a seventh of sorting and merging)
+        if (__popcll(todo) > 7) {
+            merge(sort_keys(key > bar ? key : 0), lane);
+            return;
+        }
         while (todo != 0) {
             const uint64_t one = lane_key(key, __builtin_ctzll(todo));
             const int at = __popcll(__ballot(mine > one));
             const uint32_t lo = dpp<kDppWaveShr1>((uint32_t)mine, (uint32_t)mine);
             const uint32_t hi = dpp<kDppWaveShr1>((uint32_t)(mine >> 32), (uint32_t)(mine >> 32));
             mine = lane < at ? mine : lane == at ? one : (uint64_t)hi << 32 | lo;
-            last = lane_key(mine, k - 1);
+            raise(lane_key(mine, k - 1));
             todo &= todo - 1;
-            todo &= __ballot(key > last);
+            todo &= __ballot(key > bar);
         }
     }
 };
 
-// The k-th largest of the lanes' values (k <= 64).
-__device__ __forceinline__ float kth_of_lanes(float v, int k) {
-    int above = 0;
-    for (int l = 0; l < 64; ++l)
-        above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)) > v;
-    // the smallest value with fewer than k above it
-    return -group_max(above < k ? -v : kNegInf, 64);
-}
-
 // ------------------------------------------------------------------ outputs of a row
 
-// z_target - m - log s of a row: NaN for a target outside the classes, 0 for one that is
-// ignored, -infinity where no class is left.
-__device__ __forceinline__ float target_logp(const LogprobArgs& a, int64_t target, float z,
-                                             const Sums& r, float logs) {
-    if (target == a.ignore) return 0.0f;
-    if (target < 0 || target >= a.classes) return __builtin_nanf("");
-    return r.s == 0.0f ? kNegInf : z - r.m - logs;
+// A row's target and its logit, read ahead of the sums.
+struct Target {
+    int64_t index;
+    float z;
+};
+template <typename T>
+__device__ __forceinline__ Target target_of(const LogprobArgs& a, int64_t row) {
+    Target t;
+    t.index = a.targets[row];
+    const bool in = t.index >= 0 && t.index < a.classes;
+    t.z = Storage<T>::load(static_cast<const T*>(a.z) + row * a.stride + (in ? t.index : 0));
+    return t;
 }
 
-template <typename T>
-__device__ __forceinline__ void store_row(const LogprobArgs& a, int64_t row, const Sums& r) {
-    const int64_t target = a.targets[row];
-    float z = 0.0f;
-    if (target >= 0 && target < a.classes)
-        z = Storage<T>::load(static_cast<const T*>(a.z) + row * a.stride + target);
+__device__ __forceinline__ void store_row(const LogprobArgs& a, int64_t row, const Target& t,
+                                          const Sums& r) {
     const float logs = log_sum(r);
-    a.logp[row] = target_logp(a, target, z, r, logs);
+    const bool in = t.index >= 0 && t.index < a.classes;
+    a.logp[row] = t.index == a.ignore ? 0.0f
+                  : !in               ? __builtin_nanf("")
+                  : r.s == 0.0f       ? kNegInf
+                                      : t.z - r.m - logs;
     a.stats[2 * row] = r.m;
     a.stats[2 * row + 1] = logs;
     if (a.entropy != nullptr) a.entropy[row] = r.s == 0.0f ? 0.0f : logs - r.q / r.s;
@@ -190,7 +254,7 @@ __global__ void __launch_bounds__(256) logprob_short_kernel(LogprobArgs a) {
         Sums r = {kNegInf, 0.0f, 0.0f};
         add_values<true>(r, v, max_of(v));
         join_lanes(r, lanes);
-        if (live && slot == 0) store_row<T>(a, row, r);
+        if (live && slot == 0) store_row(a, row, target_of<T>(a, row), r);
         if (a.k == 0) continue;
         uint64_t key[V];
 #pragma unroll
@@ -213,58 +277,81 @@ __global__ void __launch_bounds__(256) logprob_short_kernel(LogprobArgs a) {
 
 // ------------------------------------------------------------------ long rows
 
-constexpr int kTileElems = 32;  // per lane
-constexpr int kTile = 64 * kTileElems;
-
-template <typename T> constexpr int kTileUnits = kTileElems / kVec<T>;
-
-// One tile of a row into registers, 16-byte units interleaved over the lanes.
-template <typename T>
-__device__ __forceinline__ void load_tile(const T* row, int base, int n, int lane,
-                                          u32x4 (&raw)[kTileUnits<T>]) {
-    constexpr int V = kVec<T>;
-    issue_units<0, false>(row, base + lane * V, 64 * V, n, 0u, raw);
-    if (base + kTile > n) settle_units<0, false, T>(base + lane * V, 64 * V, n, kNegInfBits<T>, raw);
-}
-
-template <typename T>
-__device__ __forceinline__ void widen_tile(const u32x4 (&raw)[kTileUnits<T>],
-                                           float (&v)[kTileElems]) {
-    constexpr int V = kVec<T>;
+// One tile of a row, E elements per lane, in 16-byte units interleaved over the lanes.
+template <typename T, int E>
+struct Tile {
+    static constexpr int V = kVec<T>, U = E / V, kElems = 64 * E;
+    u32x4 raw[U];
+    __device__ __forceinline__ void issue(const T* row, int base, int n, int lane) {
+        issue_units<0, false>(row, base + lane * V, 64 * V, n, 0u, raw);
+    }
+    __device__ __forceinline__ void values(int base, int n, int lane, float (&v)[E]) {
+        if (base + kElems > n)
+            settle_units<0, false, T>(base + lane * V, 64 * V, n, kNegInfBits<T>, raw);
 #pragma unroll
-    for (int u = 0; u < kTileUnits<T>; ++u) {
-        float unit[V];
-        widen(raw[u], unit);
+        for (int u = 0; u < U; ++u) {
+            float unit[V];
+            widen(raw[u], unit);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[u * V + i] = unit[i];
+            for (int i = 0; i < V; ++i) v[u * V + i] = unit[i];
+        }
+    }
+    // The class of a lane's element e.
+    static __device__ __forceinline__ int index(int base, int lane, int e) {
+        return base + ((e / V) * 64 + lane) * V + e % V;
+    }
+};
+
+// Offers a tile's elements to the best k (see the file's comment; vm = max_of(v)).  The elements are used up: an offered one becomes NaN.
+template <typename T, int E>
+__device__ __forceinline__ void offer_tile(Best& best, float (&v)[E], float vm, int base, int n,
+                                           int lane) {
+    while (true) {
+        const bool reach = vm >= key_value(best.bar);
+        if (__ballot(reach) == 0) return;
+        int at = 0;
+#pragma unroll
+        for (int e = E - 1; e >= 0; --e) at = v[e] == vm ? e : at;
+        const int index = Tile<T, E>::index(base, lane, at);
+        const uint64_t key = reach && index < n ? key_of(vm, index) : 0;
+        const bool use = key > best.bar;
+        // (only ties are left, of a higher index: the first of a lane's equal elements is its
+        // lowest)
+        if (__ballot(use) == 0) return;
+        best.offer(key, lane);
+        vm = __builtin_nanf("");
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[e] = use && at == e ? __builtin_nanf("") : v[e];
+            vm = __builtin_fmaxf(vm, v[e]);
+        }
     }
 }
 
-// Offers a tile's elements that can enter the best k (see the file's comment); `vm` is the
-// lane's largest.
+// Where a row has fewer than k classes that are numbers: its NaN classes, lowest index
+// first.
 template <typename T>
-__device__ __forceinline__ void offer_tile(Best& best, const float (&v)[kTileElems], float vm,
-                                           int base, int n, int lane) {
-    constexpr int V = kVec<T>;
-    float floor = key_value(best.last);
-    const int lanes = __popcll(__ballot(vm >= floor));
-    if (lanes == 0) return;
-    if (lanes > best.k) floor = __builtin_fmaxf(floor, kth_of_lanes(vm, best.k));
-    StaticFor<0, kTileElems>::run([&](auto e) {
-        const int index = base + ((e / V) * 64 + lane) * V + e % V;
-        const bool in = index < n && !(v[e] < floor);
-        best.offer(in ? key_of(v[e], index) : 0, lane);
-    });
+__device__ __forceinline__ void offer_nan(Best& best, const T* z, int n, int lane) {
+    for (int base = 0; base < n; base += 64) {
+        const float v = base + lane < n ? Storage<T>::load(z + base + lane) : 0.0f;
+        best.offer(v != v ? key_of(v, base + lane) : 0, lane);
+    }
 }
 
 // W waves per (row, part): W = 1, four of them per workgroup, or W = 4.
-template <typename T, int W, bool ENT, bool TOP>
+template <typename T, int W, int E, bool ENT, bool TOP>
 __global__ void __launch_bounds__(256) logprob_kernel(LogprobArgs a) {
     __shared__ Sums part[W];
     __shared__ uint64_t keys[W][64];
-    const int lane = threadIdx.x & 63;
+    __shared__ unsigned long long bar;  // the highest k-th best of the waves of a row
+    constexpr int kTile = Tile<T, E>::kElems;
+    const int lane = threadIdx.x & 63, n = a.classes;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t items = a.rows * a.parts;
+    if (W > 1 && TOP) {
+        bar = 0;
+        __syncthreads();
+    }
     for (int64_t i0 = (int64_t)blockIdx.x * (4 / W); i0 < items;
          i0 += (int64_t)gridDim.x * (4 / W)) {
         const int64_t item = i0 + (W == 1 ? wave : 0);
@@ -274,26 +361,44 @@ __global__ void __launch_bounds__(256) logprob_kernel(LogprobArgs a) {
         const T* z = static_cast<const T*>(a.z) + row * a.stride;
         Sums r = {kNegInf, 0.0f, 0.0f};
         Best best(TOP ? a.k : 1);
-        const int tiles = (a.classes + kTile - 1) / kTile;
-        for (int t = p * W + (W == 1 ? 0 : wave); t < tiles; t += a.parts * W) {
-            u32x4 raw[kTileUnits<T>];
-            load_tile(z, t * kTile, a.classes, lane, raw);
-            float v[kTileElems];
-            widen_tile<T>(raw, v);
+        int base = (W == 1 ? p : p * W + wave) * kTile;
+        const int step = a.parts * W * kTile;
+        Tile<T, E> next;
+        next.issue(z, base, n, lane);
+        const Target target = target_of<T>(a, row);
+        // (kMaxClasses and a step stay below 2^31)
+        for (; base < n; base += step) {
+            Tile<T, E> tile = next;
+            if (base + step < n) next.issue(z, base + step, n, lane);
+            float v[E];
+            tile.values(base, n, lane, v);
             const float vm = max_of(v);
             add_values<ENT>(r, v, vm);
-            if (TOP) offer_tile<T>(best, v, vm, t * kTile, a.classes, lane);
+            if (TOP) {
+                if (W > 1)
+                    best.raise(__hip_atomic_load(&bar, __ATOMIC_RELAXED,
+                                                 __HIP_MEMORY_SCOPE_WORKGROUP));
+                const uint64_t had = best.bar;
+                offer_tile<T>(best, v, vm, base, n, lane);
+                if (W > 1 && best.bar > had && lane == 0)
+                    __hip_atomic_fetch_max(&bar, best.bar, __ATOMIC_RELAXED,
+                                           __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
         }
-        join_lanes(r, 64);
+        join_wave(r);
         if (W > 1) {
             if (lane == 0) part[wave] = r;
-            if (TOP) keys[wave][lane] = lane < a.k ? best.mine : 0;
+            if (TOP) keys[wave][lane] = best.mine;
             __syncthreads();
             if (wave == 0) {
                 r = lane < W ? part[lane] : Sums{kNegInf, 0.0f, 0.0f};
-                join_lanes(r, 64);
-                if (TOP)
-                    for (int w = 1; w < W; ++w) best.offer(keys[w][lane], lane);
+                join_wave(r);
+                if (TOP) {
+                    best.bar = 0;
+                    for (int w = 1; w < W; ++w) best.merge(keys[w][lane], lane);
+                }
+            } else if (TOP) {
+                bar = 0;
             }
             __syncthreads();
             if (wave != 0) continue;
@@ -301,32 +406,43 @@ __global__ void __launch_bounds__(256) logprob_kernel(LogprobArgs a) {
         if (a.parts > 1) {
             if (lane == 0) a.part[item] = make_float4(r.m, r.s, r.q, 0.0f);
             if (TOP && lane < a.k) a.keys[item * a.k + lane] = best.mine;
-        } else {
-            if (lane == 0) store_row<T>(a, row, r);
-            if (TOP && lane < a.k) store_top(a, row * a.k + lane, best.mine, r);
+            continue;
         }
+        if (lane == 0) store_row(a, row, target, r);
+        if (!TOP) continue;
+        if (r.s != r.s && best.bar == 0) offer_nan(best, z, n, lane);
+        if (lane < a.k) store_top(a, row * a.k + lane, best.mine, r);
     }
 }
 
 // Joins the parts (at most 64) of each row: one wave per row.
 template <typename T>
-__global__ void __launch_bounds__(256) logprob_join_kernel(LogprobArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t row = (int64_t)blockIdx.x * 4 + wave;
-    if (row >= a.rows) return;
+__global__ void __launch_bounds__(64) logprob_join_kernel(LogprobArgs a) {
+    const int lane = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const bool on = lane < a.parts;
     Sums r = {kNegInf, 0.0f, 0.0f};
-    if (lane < a.parts) {
+    if (on) {
         const float4 f = a.part[row * a.parts + lane];
         r = {f.x, f.y, f.z};
     }
-    join_lanes(r, 64);
-    if (lane == 0) store_row<T>(a, row, r);
-    if (a.k == 0) return;
-    // (each part's keys are sorted: the lanes offer theirs rank by rank)
-    Best best(a.k);
+    // (each part's keys are sorted: the lanes offer theirs rank by rank, the next one
+    // loaded ahead, until none passes)
     const uint64_t* keys = a.keys + (row * a.parts + lane) * a.k;
-    for (int j = 0; j < a.k; ++j) best.offer(lane < a.parts ? keys[j] : 0, lane);
+    uint64_t next = on && a.k > 0 ? keys[0] : 0;
+    const Target target = target_of<T>(a, row);
+    join_wave(r);
+    if (lane == 0) store_row(a, row, target, r);
+    if (a.k == 0) return;
+    Best best(a.k);
+    for (int j = 0; j < a.k; ++j) {
+        const uint64_t key = next;
+        next = on && j + 1 < a.k ? keys[j + 1] : 0;
+        if (__ballot(key > best.bar) == 0) break;
+        best.offer(key, lane);
+    }
+    const T* z = static_cast<const T*>(a.z) + row * a.stride;
+    if (r.s != r.s && best.bar == 0) offer_nan(best, z, a.classes, lane);
     if (lane < a.k) store_top(a, row * a.k + lane, best.mine, r);
 }
 
@@ -382,45 +498,50 @@ __global__ void __launch_bounds__(256) logprob_grad_short_kernel(LogprobGradArgs
     }
 }
 
-constexpr int kGradUnits = 4;  // per lane
-
-template <typename T>
+// One wave per (row, tile).
+template <typename T, int E>
 __global__ void __launch_bounds__(256) logprob_grad_kernel(LogprobGradArgs a) {
     constexpr int V = kVec<T>;
-    const int64_t items = a.rows * a.segments;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int64_t row = item / a.segments;
-        const int base = (int)(item - row * a.segments) * (256 * kGradUnits * V);
-        const RowGrad g = row_grad(a, row);
-        const T* z = static_cast<const T*>(a.z) + row * a.stride;
-        T* dz = static_cast<T*>(a.dz) + row * a.dstride;
-        const int first = base + (int)threadIdx.x * V;
-        u32x4 raw[kGradUnits];
-        issue_units<0, false>(z, first, 256 * V, a.classes, 0u, raw);
-        if (base + 256 * kGradUnits * V > a.classes)
-            settle_units<0, false, T>(first, 256 * V, a.classes, 0u, raw);
+    const int lane = threadIdx.x & 63, n = a.classes;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t item = blockIdx.x * 4 + wave;
+    if (item >= a.items) return;
+    const uint32_t row = a.tiles == 1 ? item : item / a.tiles;
+    const int base = (int)(item - row * a.tiles) * Tile<T, E>::kElems;
+    Tile<T, E> tile;
+    tile.issue(static_cast<const T*>(a.z) + row * a.stride, base, n, lane);
+    const RowGrad g = row_grad(a, row);
+    float v[E];
+    tile.values(base, n, lane, v);
+    T* dz = static_cast<T*>(a.dz) + row * a.dstride;
 #pragma unroll
-        for (int u = 0; u < kGradUnits; ++u) {
-            float v[V];
-            widen(raw[u], v);
-            unit_grad(g, first + u * 256 * V, v);
-            store_unit<false>(dz, first + u * 256 * V, a.classes, v);
-        }
+    for (int u = 0; u < E / V; ++u) {
+        const int col = base + (u * 64 + lane) * V;
+        float d[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) d[i] = v[u * V + i];
+        unit_grad(g, col, d);
+        if (base + Tile<T, E>::kElems <= n) store_unit<true>(dz, col, n, d);
+        else store_unit<false>(dz, col, n, d);
     }
 }
+
+// Elements per lane of a tile: a row of one tile leaves few lanes idle.
+int tile_elems(int32_t classes) { return classes <= 512 ? 8 : classes <= 1024 ? 16 : 32; }
 
 int grid_of(int64_t n, int64_t most) { return (int)(n < most ? n : most); }
 
 }  // namespace
 
 LogprobPlan logprob_plan(int64_t rows, int32_t classes, int es, int k) {
-    LogprobPlan p = {0, 0, 1, 0};
+    LogprobPlan p = {0, 0, 0, 1, 0};
     const int V = 16 / es;
     if (classes <= 32 * V) {
         while (V << p.shift < classes) ++p.shift;
         return p;
     }
-    const int64_t tiles = (classes + kTile - 1) / kTile;
+    p.elems = tile_elems(classes);
+    const int64_t tiles = (classes + 64 * p.elems - 1) / (64 * p.elems);
     // four waves a row where rows alone fill the GPU with such workgroups and are long
     // enough that each wave gets a tile; below that, parts of rows to 16 waves per CU
     p.waves = rows >= 1024 && tiles >= 4 ? 4 : 1;
@@ -446,37 +567,63 @@ hipError_t run_logprob(const LogprobPlan& p, const LogprobArgs& a, hipStream_t s
     const int64_t items = a.rows * p.parts, per = 4 / p.waves;
     const int grid = grid_of((items + per - 1) / per, 1 << 30);
     const bool ent = a.entropy != nullptr, top = a.k > 0;
-    auto go = [&](auto w, auto e, auto t) {
-        logprob_kernel<T, decltype(w)::value, decltype(e)::value, decltype(t)::value>
-            <<<grid, 256, 0, s>>>(a);
+    using std::false_type;
+    using std::integral_constant;
+    using std::true_type;
+    auto go = [&](auto w, auto e, auto ent_, auto top_) {
+        logprob_kernel<T, decltype(w)::value, decltype(e)::value, decltype(ent_)::value,
+                       decltype(top_)::value><<<grid, 256, 0, s>>>(a);
     };
-    auto pick = [&](auto w) {
-        if (ent && top) go(w, std::true_type{}, std::true_type{});
-        else if (ent) go(w, std::true_type{}, std::false_type{});
-        else if (top) go(w, std::false_type{}, std::true_type{});
-        else go(w, std::false_type{}, std::false_type{});
+    auto pick = [&](auto w, auto e) {
+        if (ent && top) go(w, e, true_type{}, true_type{});
+        else if (ent) go(w, e, true_type{}, false_type{});
+        else if (top) go(w, e, false_type{}, true_type{});
+        else go(w, e, false_type{}, false_type{});
     };
-    if (p.waves == 4) pick(std::integral_constant<int, 4>{});
-    else pick(std::integral_constant<int, 1>{});
+    if (p.waves == 4) pick(integral_constant<int, 4>{}, integral_constant<int, 32>{});
+    else if (p.elems == 8) pick(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+    else if (p.elems == 16) pick(integral_constant<int, 1>{}, integral_constant<int, 16>{});
+    else pick(integral_constant<int, 1>{}, integral_constant<int, 32>{});
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
-    logprob_join_kernel<T><<<(int)((a.rows + 3) / 4), 256, 0, s>>>(a);
+    logprob_join_kernel<T><<<(int)a.rows, 64, 0, s>>>(a);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t run_logprob_grad(LogprobGradArgs a, hipStream_t s) {
     constexpr int V = kVec<T>;
-    if (a.classes <= 64 * V) {
+    if (a.classes <= 32 * V) {
         a.shift = 0;
         while (V << a.shift < a.classes) ++a.shift;
         const int64_t per = 256 >> a.shift;
         logprob_grad_short_kernel<T><<<grid_of((a.rows + per - 1) / per, 8192), 256, 0, s>>>(a);
         return hipGetLastError();
     }
-    a.segments = (a.classes + 256 * kGradUnits * V - 1) / (256 * kGradUnits * V);
-    logprob_grad_kernel<T><<<grid_of(a.rows * a.segments, 1 << 30), 256, 0, s>>>(a);
-    return hipGetLastError();
+    const int elems = tile_elems(a.classes);
+    a.tiles = (a.classes + 64 * elems - 1) / (64 * elems);
+    // (items are counted in 32 bits: rows in pieces, one but for 2^30 and more tiles)
+    const int64_t most = (1 << 30) / a.tiles;
+    for (int64_t rows = a.rows; rows > 0; rows -= most) {
+        const int64_t now = rows < most ? rows : most;
+        a.items = (uint32_t)(now * a.tiles);
+        const int grid = (int)((a.items + 3) / 4);
+        if (elems == 8) logprob_grad_kernel<T, 8><<<grid, 256, 0, s>>>(a);
+        else if (elems == 16) logprob_grad_kernel<T, 16><<<grid, 256, 0, s>>>(a);
+        else logprob_grad_kernel<T, 32><<<grid, 256, 0, s>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.z = static_cast<const T*>(a.z) + now * a.stride;
+        a.dz = static_cast<T*>(a.dz) + now * a.dstride;
+        a.targets += now;
+        a.stats += 2 * now;
+        a.dlogp += now;
+        if (a.dentropy != nullptr) {
+            a.entropy += now;
+            a.dentropy += now;
+        }
+    }
+    return hipSuccess;
 }
 
 }  // namespace

@@ -199,6 +199,8 @@ __device__ __forceinline__ float dppf(float v) {
     const uint32_t u = __float_as_uint(v);
     return __uint_as_float(dpp<CTRL>(u, u));
 }
+constexpr int kDppFlip4 = 0x1B;        // quad_perm [3, 2, 1, 0]
+constexpr int kDppRor8 = 0x128;        // lane i of 16 <- (i + 8) % 16
 constexpr int kDppXor1 = 0xB1;         // quad_perm [1, 0, 3, 2]
 constexpr int kDppXor2 = 0x4E;         // quad_perm [2, 3, 0, 1]
 constexpr int kDppHalfMirror = 0x141;  // lane i of 8 <-> 7 - i

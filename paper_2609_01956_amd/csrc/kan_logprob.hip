@@ -122,13 +122,13 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t key, int lane) {
 template <int S>
 __device__ __forceinline__ uint64_t key_xor(uint64_t key) {
     const uint32_t lo = (uint32_t)key, hi = (uint32_t)(key >> 32);
-    if constexpr (S == 1) return (uint64_t)dpp<kDppXor1>(hi, hi) << 32 | dpp<kDppXor1>(lo, lo);
-    if constexpr (S == 2) return (uint64_t)dpp<kDppXor2>(hi, hi) << 32 | dpp<kDppXor2>(lo, lo);
+    if constexpr (S == 1) return (uint64_t)dpp<kDppXor1>(hi) << 32 | dpp<kDppXor1>(lo);
+    if constexpr (S == 2) return (uint64_t)dpp<kDppXor2>(hi) << 32 | dpp<kDppXor2>(lo);
     if constexpr (S == 4) {
-        const uint32_t l = dpp<kDppHalfMirror>(lo, lo), h = dpp<kDppHalfMirror>(hi, hi);
-        return (uint64_t)dpp<kDppFlip4>(h, h) << 32 | dpp<kDppFlip4>(l, l);
+        const uint32_t l = dpp<kDppHalfMirror>(lo), h = dpp<kDppHalfMirror>(hi);
+        return (uint64_t)dpp<kDppFlip4>(h) << 32 | dpp<kDppFlip4>(l);
     }
-    if constexpr (S == 8) return (uint64_t)dpp<kDppRor8>(hi, hi) << 32 | dpp<kDppRor8>(lo, lo);
+    if constexpr (S == 8) return (uint64_t)dpp<kDppRor8>(hi) << 32 | dpp<kDppRor8>(lo);
     if constexpr (S >= 16) return __shfl_xor((unsigned long long)key, S);
 }
 
@@ -175,8 +175,12 @@ struct Best {
 
     // Merges 64 keys in falling order.
     __device__ __forceinline__ void merge(uint64_t sorted, int lane) {
-        const uint64_t other = __shfl((unsigned long long)sorted, 63 - lane);
-        mine = sort_steps<64, 32>(other > mine ? other : mine);
+        if (lane_key(mine, 0) == 0) {
+            mine = sorted;
+        } else {
+            const uint64_t other = __shfl((unsigned long long)sorted, 63 - lane);
+            mine = sort_steps<64, 32>(other > mine ? other : mine);
+        }
         raise(lane_key(mine, k - 1));
     }
 
@@ -191,8 +195,7 @@ struct Best {
         while (todo != 0) {
             const uint64_t one = lane_key(key, __builtin_ctzll(todo));
             const int at = __popcll(__ballot(mine > one));
-            const uint32_t lo = dpp<kDppWaveShr1>((uint32_t)mine, (uint32_t)mine);
-            const uint32_t hi = dpp<kDppWaveShr1>((uint32_t)(mine >> 32), (uint32_t)(mine >> 32));
+            const uint32_t lo = dpp_shr((uint32_t)mine), hi = dpp_shr((uint32_t)(mine >> 32));
             mine = lane < at ? mine : lane == at ? one : (uint64_t)hi << 32 | lo;
             raise(lane_key(mine, k - 1));
             todo &= todo - 1;
@@ -302,7 +305,8 @@ struct Tile {
     }
 };
 
-// Offers a tile's elements to the best k (see the file's comment; vm = max_of(v)).  The elements are used up: an offered one becomes NaN.
+// Offers a tile's elements to the best k (see the file's comment; vm = max_of(v)).  The
+// elements are used up: an offered one becomes NaN.
 template <typename T, int E>
 __device__ __forceinline__ void offer_tile(Best& best, float (&v)[E], float vm, int base, int n,
                                            int lane) {

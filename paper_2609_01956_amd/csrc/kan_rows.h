@@ -189,15 +189,18 @@ __device__ __forceinline__ void load_params(const TP* p, int col, int n, float f
     }
 }
 
-// One lane's value moved by a DPP pattern (lanes without a source keep `old`).
+// Every lane's value from another lane of its row of 16, by a DPP pattern.
 template <int CTRL>
-__device__ __forceinline__ uint32_t dpp(uint32_t old, uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, 0xf, 0xf, false);
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
 }
 template <int CTRL>
 __device__ __forceinline__ float dppf(float v) {
-    const uint32_t u = __float_as_uint(v);
-    return __uint_as_float(dpp<CTRL>(u, u));
+    return __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
+}
+// The previous lane's value (lane 0 keeps its own).
+__device__ __forceinline__ uint32_t dpp_shr(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x138, 0xf, 0xf, false);
 }
 constexpr int kDppFlip4 = 0x1B;        // quad_perm [3, 2, 1, 0]
 constexpr int kDppRor8 = 0x128;        // lane i of 16 <- (i + 8) % 16
@@ -205,7 +208,6 @@ constexpr int kDppXor1 = 0xB1;         // quad_perm [1, 0, 3, 2]
 constexpr int kDppXor2 = 0x4E;         // quad_perm [2, 3, 0, 1]
 constexpr int kDppHalfMirror = 0x141;  // lane i of 8 <-> 7 - i
 constexpr int kDppMirror = 0x140;      // lane i of 16 <-> 15 - i
-constexpr int kDppWaveShr1 = 0x138;    // lane i <- lane i - 1
 
 // op over the `lanes` (a power of two) neighbouring lanes of each group; every lane
 // gets the same bits (each step adds the same two values in either order).  All lanes

@@ -5,14 +5,17 @@
 // Bound by HBM: every gradient is read once for the norm and, when it is clipped (or goes to
 // other tensors), read again and written.  Squares and their sums are binary64, which costs
 // nothing beside the reads and neither overflows nor drops small gradients: every fp32
-// gradient's square is exact.  Each workgroup sums its own chunks into one partial; a
-// one-workgroup launch adds the partials in a fixed order and leaves N and c; the third
-// launch scales, each product rounded once.  In place with c = 1 it returns without touching the gradients.
+// gradient's square is exact.  Each workgroup sums its own chunks into one partial, and each
+// workgroup of the second launch adds all partials in the same fixed order (at most
+// kClipGroups and one per launch: 2 us from the caches, less than a launch between them) before
+// it scales, each product rounded once.  It goes through the chunks from the last to the
+// first, as the last ones read are still in the Infinity Cache.  In place with c = 1 it
+// returns without touching the gradients.
 //
-// The tensors go by value, kClipTensors per launch (a kernel's arguments hold 4 KB): no
-// table is copied to the device or kept.  A tensor is cut into chunks of kClipChunk
-// elements, numbered over the launch's tensors; a workgroup takes every gridDim-th chunk
-// and finds its tensor by bisection.
+// The tensors go by value, as many per launch as a kernel's 4 KB of arguments hold: no table
+// is copied to the device or kept.  A tensor is cut into chunks of kClipChunk elements,
+// numbered over the launch's tensors; a workgroup takes every gridDim-th chunk and finds its
+// tensor by bisection.
 #include "kan_internal.h"
 #include "kan_rows.h"
 
@@ -20,155 +23,189 @@ namespace kan {
 
 namespace {
 
-// The chunk's tensor: the last one whose first chunk is not past it.
-__device__ __forceinline__ int tensor_of(const ClipArgs& a, int chunk) {
+// A chunk's tensor (the last one whose first chunk is not past it) and place in it.
+struct Chunk {
+    int tensor, n;
+    int64_t at;
+    bool bf16;
+};
+template <int N>
+__device__ __forceinline__ Chunk chunk_of(const ClipArgs<N>& a, int chunk) {
     int lo = 0, hi = a.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (a.first[mid] <= chunk) lo = mid;
         else hi = mid - 1;
     }
-    return lo;
+    Chunk c;
+    c.tensor = lo;
+    c.at = (int64_t)(chunk - a.first[lo]) * kClipChunk;
+    c.n = chunk + 1 == a.first[lo + 1] ? (a.tail[lo] >> 1) + 1 : kClipChunk;
+    c.bf16 = a.tail[lo] & 1;
+    return c;
 }
 
-__device__ __forceinline__ double sum_of_waves(double v, double* red) {
+// Sum over the workgroup, every lane gets it.
+__device__ __forceinline__ double group_total(double v) {
+    __shared__ double red[4];
     for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
-    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    if ((threadIdx.x & 63) == 0) red[wave] = v;
     __syncthreads();
-    v = 0.0;
-    for (int w = 0; w < waves; ++w) v += red[w];
-    return v;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// f(units of a chunk at p, column of the first, elements left) for the 256 lanes' units, four
+// in flight.
+template <typename T, typename F>
+__device__ __forceinline__ void for_units(const T* p, int n, F&& f) {
+    constexpr int V = kVec<T>, U = 4;
+    for (int i = threadIdx.x * V; i < n; i += 256 * V * U) {
+        u32x4 raw[U];
+        issue_units<0, true>(p, i, 256 * V, n, 0u, raw);
+        settle_units<0, true, T>(i, 256 * V, n, 0u, raw);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[V];
+            widen(raw[u], v);
+            f(i + u * 256 * V, v);
+        }
+    }
 }
 
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const T* p, int n) {
     constexpr int V = kVec<T>;
-    double s = 0.0;
-    for (int i = threadIdx.x * V; i < n; i += 256 * V) {
-        float v[V];
-        load_unit(p, i, n, 0u, v);
+    double s0 = 0.0, s1 = 0.0;
+    for_units(p, n, [&](int, const float(&v)[V]) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) s = __builtin_fma((double)v[k], (double)v[k], s);
-    }
-    return s;
+        for (int k = 0; k < V; k += 2) {
+            s0 = __builtin_fma((double)v[k], (double)v[k], s0);
+            s1 = __builtin_fma((double)v[k + 1], (double)v[k + 1], s1);
+        }
+    });
+    return s0 + s1;
 }
 
-__global__ void __launch_bounds__(256) clip_norm_kernel(ClipArgs a, double* part) {
-    __shared__ double red[4];
+__global__ void __launch_bounds__(256) clip_norm_kernel(ClipArgs<kClipTensors> a, double* part) {
     double s = 0.0;
-    for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-        const int t = tensor_of(a, c);
-        const int64_t at = (int64_t)(c - a.first[t]) * kClipChunk;
-        const int64_t left = (a.size[t] >> 1) - at;
-        const int n = (int)(left < kClipChunk ? left : kClipChunk);
-        s += (a.size[t] & 1) ? chunk_squares(static_cast<const uint16_t*>(a.in[t]) + at, n)
-                             : chunk_squares(static_cast<const float*>(a.in[t]) + at, n);
+    for (int i = blockIdx.x; i < a.chunks; i += gridDim.x) {
+        const Chunk c = chunk_of(a, i);
+        s += c.bf16 ? chunk_squares(static_cast<const uint16_t*>(a.in[c.tensor]) + c.at, c.n)
+                    : chunk_squares(static_cast<const float*>(a.in[c.tensor]) + c.at, c.n);
     }
-    s = sum_of_waves(s, red);
+    s = group_total(s);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-// The norm, and the factor after it.
-__global__ void __launch_bounds__(256) clip_join_kernel(const double* part, int parts,
-                                                        float max_norm, float eps, float* norm,
-                                                        double* factor) {
-    __shared__ double red[4];
+__device__ __forceinline__ double norm_of(const double* part, int parts) {
     double s = 0.0;
     for (int i = threadIdx.x; i < parts; i += 256) s += part[i];
-    s = sum_of_waves(s, red);
-    if (threadIdx.x != 0) return;
-    const double n = __builtin_sqrt(s);
-    *norm = (float)n;
-    if (factor != nullptr) {
-        // (gradients that are all 0 stay as they are; a NaN among them reaches all)
-        const double c = n == 0.0 ? 1.0 : (double)max_norm / (n + (double)eps);
-        *factor = c >= 1.0 ? 1.0 : c;
-    }
+    return __builtin_sqrt(group_total(s));
+}
+
+__global__ void __launch_bounds__(256) clip_join_kernel(const double* part, int parts,
+                                                        float* norm) {
+    const double n = norm_of(part, parts);
+    if (threadIdx.x == 0) *norm = (float)n;
 }
 
 template <typename T>
 __device__ __forceinline__ void chunk_scale(const T* p, T* q, int n, double c) {
     constexpr int V = kVec<T>;
-    for (int i = threadIdx.x * V; i < n; i += 256 * V) {
-        float v[V];
-        load_unit(p, i, n, 0u, v);
+    for_units(p, n, [&](int i, float(&v)[V]) {
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = (float)((double)v[k] * c);
         store_unit<false>(q, i, n, v);
-    }
+    });
 }
 
-__global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs a, ClipOuts o,
-                                                         const double* factor) {
-    const double f = *factor;
-    for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-        const int t = tensor_of(a, c);
-        if (f == 1.0 && a.in[t] == o.out[t]) continue;
-        const int64_t at = (int64_t)(c - a.first[t]) * kClipChunk;
-        const int64_t left = (a.size[t] >> 1) - at;
-        const int n = (int)(left < kClipChunk ? left : kClipChunk);
-        if (a.size[t] & 1)
-            chunk_scale(static_cast<const uint16_t*>(a.in[t]) + at,
-                        static_cast<uint16_t*>(o.out[t]) + at, n, f);
+// OUT: the tensors' outputs stand after the N tensors' arguments (else in place).
+template <int N, bool OUT>
+__global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs<N> a, ClipOuts<OUT ? N : 1> o,
+                                                         const double* part, int parts,
+                                                         ClipBound b) {
+    const double n = norm_of(part, parts);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *b.norm = (float)n;
+    // (gradients that are all 0 stay as they are; a NaN among them reaches all)
+    const double ratio = n == 0.0 ? 1.0 : (double)b.max_norm / (n + (double)b.eps);
+    const double f = ratio >= 1.0 ? 1.0 : ratio;
+    for (int i = a.chunks - 1 - (int)blockIdx.x; i >= 0; i -= gridDim.x) {
+        const Chunk c = chunk_of(a, i);
+        void* out = OUT ? o.out[c.tensor] : const_cast<void*>(a.in[c.tensor]);
+        if (f == 1.0 && a.in[c.tensor] == out) continue;
+        if (c.bf16)
+            chunk_scale(static_cast<const uint16_t*>(a.in[c.tensor]) + c.at,
+                        static_cast<uint16_t*>(out) + c.at, c.n, f);
         else
-            chunk_scale(static_cast<const float*>(a.in[t]) + at,
-                        static_cast<float*>(o.out[t]) + at, n, f);
+            chunk_scale(static_cast<const float*>(a.in[c.tensor]) + c.at,
+                        static_cast<float*>(out) + c.at, c.n, f);
     }
 }
 
-constexpr int kClipGroups = 2048;
-
-// The next launch's tensors from *t on.
-bool next_args(const ClipList& l, int64_t* t, ClipArgs* a, ClipOuts* o) {
+// The next launch's tensors from *t on (tensors of no elements are left out).
+template <int N>
+bool next_args(const ClipList& l, int64_t* t, ClipArgs<N>* a, void** out) {
     a->count = 0;
     a->chunks = 0;
-    for (; *t < l.count && a->count < kClipTensors; ++*t) {
-        const int64_t n = l.sizes[*t], chunks = (n + kClipChunk - 1) / kClipChunk;
+    for (; *t < l.count && a->count < N; ++*t) {
+        const int64_t n = l.sizes[*t];
         if (n == 0) continue;
         a->in[a->count] = l.in[*t];
-        a->size[a->count] = n << 1 | (l.bf16(*t) ? 1 : 0);
         a->first[a->count] = a->chunks;
-        if (l.out != nullptr) o->out[a->count] = l.out[*t];
-        a->chunks += (int)chunks;
+        a->tail[a->count] = (uint16_t)(((n - 1) % kClipChunk) << 1 | (l.bf16(*t) ? 1 : 0));
+        if (out != nullptr) out[a->count] = l.out[*t];
+        a->chunks += (int)((n + kClipChunk - 1) / kClipChunk);
         ++a->count;
     }
+    a->first[a->count] = a->chunks;
     return a->count > 0;
 }
 
-int clip_groups(const ClipArgs& a) { return a.chunks < kClipGroups ? a.chunks : kClipGroups; }
+template <int N, bool OUT>
+hipError_t scale(const ClipList& l, const double* part, int parts, ClipBound b, hipStream_t s) {
+    ClipArgs<N> a;
+    ClipOuts<OUT ? N : 1> o;
+    bool first = true;
+    for (int64_t t = 0; next_args(l, &t, &a, OUT ? o.out : nullptr) || first; first = false) {
+        // (one workgroup at least, for the norm)
+        const int groups = a.chunks < 1 ? 1 : a.chunks < kClipGroups ? a.chunks : kClipGroups;
+        clip_scale_kernel<N, OUT><<<groups, 256, 0, s>>>(a, o, part, parts, b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+int64_t clip_launches(int64_t count) { return (count + kClipTensors - 1) / kClipTensors; }
 
 }  // namespace
 
 size_t clip_workspace(int64_t count) {
-    // (tensors of no elements take no place in a launch: this many launches at most)
-    const int64_t launches = (count + kClipTensors - 1) / kClipTensors;
-    return 16 + sizeof(double) * kClipGroups * (size_t)launches;
+    return sizeof(double) * (kClipGroups + (size_t)clip_launches(count));
 }
 
-hipError_t launch_clip(const ClipList& l, float max_norm, float eps, float* norm, void* ws,
-                       hipStream_t s) {
-    double* factor = static_cast<double*>(ws);
-    double* part = reinterpret_cast<double*>(static_cast<char*>(ws) + 16);
-    ClipArgs a;
-    ClipOuts o;
+hipError_t launch_clip(const ClipList& l, const ClipBound& b, void* ws, hipStream_t s) {
+    double* part = static_cast<double*>(ws);
+    const int64_t launches = clip_launches(l.count);
+    const int most = launches > 0 ? kClipGroups / (int)launches + 1 : 1;
     int parts = 0;
-    for (int64_t t = 0; next_args(l, &t, &a, &o);) {
-        const int groups = clip_groups(a);
+    ClipArgs<kClipTensors> a;
+    for (int64_t t = 0; next_args(l, &t, &a, nullptr);) {
+        const int groups = a.chunks < most ? a.chunks : most;
         clip_norm_kernel<<<groups, 256, 0, s>>>(a, part + parts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         parts += groups;
     }
-    clip_join_kernel<<<1, 256, 0, s>>>(part, parts, max_norm, eps, norm,
-                                       l.out != nullptr ? factor : nullptr);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || l.out == nullptr) return e;
-    for (int64_t t = 0; next_args(l, &t, &a, &o);) {
-        clip_scale_kernel<<<clip_groups(a), 256, 0, s>>>(a, o, factor);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (l.out == nullptr) {
+        clip_join_kernel<<<1, 256, 0, s>>>(part, parts, b.norm);
+        return hipGetLastError();
     }
-    return hipSuccess;
+    bool in_place = true;
+    for (int64_t t = 0; t < l.count; ++t) in_place &= l.out[t] == l.in[t] || l.sizes[t] == 0;
+    return in_place ? scale<kClipTensors, false>(l, part, parts, b, s)
+                    : scale<kClipTensorsOut, true>(l, part, parts, b, s);
 }
 
 }  // namespace kan

@@ -449,20 +449,29 @@ hipError_t launch_logprob_grad(bool bf16, LogprobGradArgs a, hipStream_t s);
 
 // ---------------------------------------------------------------- gradient clipping
 
-// Tensors of one launch, by value: 20 bytes each and 8 for the outputs, within the 4 KB of a
-// kernel's arguments.
-constexpr int kClipTensors = 128;
+// Tensors of one launch, by value: 14 bytes each and 8 for an output elsewhere, within the
+// 4 KB of a kernel's arguments.
+constexpr int kClipTensors = 272, kClipTensorsOut = 176;
 constexpr int kClipChunk = 1 << 14;  // elements
+constexpr int kClipGroups = 2048;    // workgroups of a launch, and partial sums in all
+template <int N>
 struct ClipArgs {
-    const void* in[kClipTensors];
-    int64_t size[kClipTensors];  // elements, times 2, plus 1 for bf16
-    int first[kClipTensors];     // a tensor's first chunk
+    const void* in[N];
+    int first[N + 1];  // a tensor's first chunk; after the last tensor: all chunks
+    uint16_t tail[N];  // elements of the last chunk less 1, times 2, plus 1 for bf16
     int count, chunks;
 };
+template <int N>
 struct ClipOuts {
-    void* out[kClipTensors];
+    void* out[N];
 };
-static_assert(sizeof(ClipArgs) + sizeof(ClipOuts) + 64 <= 4096, "kernel arguments");
+struct ClipBound {
+    float max_norm, eps;
+    float* norm;
+};
+static_assert(sizeof(ClipArgs<kClipTensors>) + 64 <= 4096, "kernel arguments");
+static_assert(sizeof(ClipArgs<kClipTensorsOut>) + sizeof(ClipOuts<kClipTensorsOut>) + 64 <= 4096,
+              "kernel arguments");
 struct ClipList {
     int64_t count;
     const void* const* in;
@@ -476,7 +485,6 @@ struct ClipList {
 constexpr int kClipMaxTensors = 1 << 14;
 constexpr int64_t kClipMaxElements = INT64_C(1) << 40;
 size_t clip_workspace(int64_t count);
-hipError_t launch_clip(const ClipList& l, float max_norm, float eps, float* norm, void* ws,
-                       hipStream_t s);
+hipError_t launch_clip(const ClipList& l, const ClipBound& b, void* ws, hipStream_t s);
 
 }  // namespace kan

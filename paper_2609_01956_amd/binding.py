@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import operator
 import os
 import threading
 from typing import Iterable, Optional, Sequence, Tuple
@@ -448,9 +449,15 @@ def check(status: int) -> None:
 
 # ------------------------------------------------------------ torch marshalling
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t) -> int:
@@ -486,10 +493,11 @@ def _stream(device) -> int:
 def _call(device, fn, *args) -> int:
     """fn(*args) with `device` current; a small layer's call is bound by the host, so
     the device is switched only where it is another one."""
-    cuda = _torch().cuda
-    if cuda.current_device() == device.index:
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getDevice", None)
+    if (torch.cuda.current_device() if raw is None else raw()) == device.index:
         return fn(*args)
-    with cuda.device(device):
+    with torch.cuda.device(device):
         return fn(*args)
 
 
@@ -752,22 +760,26 @@ def _same(what: str, like, *ts) -> None:
                              "contiguous")
 
 
-def _norm_params(x, *ts) -> int:
+def _norm_params(x, n: int, first, second=None) -> int:
     """Checks a norm's parameters (or None) against x [..., n]: their dtype code."""
-    given = [t for t in ts if t is not None]
-    if not given:
+    like = second if first is None else first
+    if like is None:
         return _dtype_code(x)
-    _require_device(x, *given)
-    for t in given:
-        if tuple(t.shape) != (x.shape[-1],) or t.dtype != given[0].dtype:
+    for t in (first, second):
+        if t is None:
+            continue
+        if t.device != x.device or not t.is_contiguous():
+            raise ValueError("the norm's parameters must be contiguous, on the rows' device")
+        if t.dim() != 1 or t.shape[0] != n or t.dtype != like.dtype:
             raise ValueError("the norm's parameters must be [n] of one dtype for rows of n")
-    return _dtype_code(given[0])
+    return _dtype_code(like)
 
 
 def _rows(x) -> Tuple[int, int]:
-    if x.dim() < 1 or x.shape[-1] < 1:
+    shape = x.shape
+    if len(shape) < 1 or shape[-1] < 1:
         raise ValueError("expected rows [..., n] with n >= 1")
-    return x.numel() // x.shape[-1], x.shape[-1]
+    return x.numel() // shape[-1], shape[-1]
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None,
@@ -780,8 +792,9 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None,
     torch = _torch()
     _require_device(x)
     rows, n = _rows(x)
-    pdt = _norm_params(x, weight, bias)
-    _same("x and residual", x, residual)
+    pdt = _norm_params(x, n, weight, bias)
+    if residual is not None:
+        _same("x and residual", x, residual)
     if out is None:
         y = torch.empty_like(x)
         h = None if residual is None else torch.empty_like(x)
@@ -790,13 +803,14 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None,
         if (h is None) != (residual is None) or y is None:
             raise ValueError("out is (y, h), h with a residual only")
         _same("x and out", x, y, h)
+    device = x.device
     mean = rstd = None
     if need_stats:
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
         rstd = torch.empty_like(mean)
-    check(_call(x.device, _library().kan_layer_norm, _dtype_code(x), pdt, rows, n, x.data_ptr(),
+    check(_call(device, _library().kan_layer_norm, _dtype_code(x), pdt, rows, n, x.data_ptr(),
                 _ptr(residual), _ptr(weight), _ptr(bias), eps, _ptr(h), y.data_ptr(), _ptr(mean),
-                _ptr(rstd), _stream(x.device)))
+                _ptr(rstd), _stream(device)))
     return y, x if residual is None else h, mean, rstd
 
 
@@ -811,12 +825,12 @@ def layer_norm_backward(h, mean, rstd, weight, dy, dh=None, need_dx: bool = True
     torch = _torch()
     _require_device(h, dy)
     rows, n = _rows(h)
-    pdt = _norm_params(h, weight)
+    pdt = _norm_params(h, n, weight)
     _same("h, dy and dh", h, dy, dh)
-    _require_device(h, mean, rstd)
+    device, f32, lead = h.device, torch.float32, h.shape[:-1]
     for t in (mean, rstd):
-        if t.dtype != torch.float32 or t.shape != h.shape[:-1]:
-            raise ValueError("mean and rstd are fp32, one value per row")
+        if t.dtype != f32 or t.shape != lead or t.device != device or not t.is_contiguous():
+            raise ValueError("mean and rstd are fp32, one value per row, on the rows' device")
     if not (need_dx or need_dw):
         raise ValueError("nothing to compute")
     dw_dtype = h.dtype if weight is None else weight.dtype
@@ -827,11 +841,11 @@ def layer_norm_backward(h, mean, rstd, weight, dy, dh=None, need_dx: bool = True
         _same("h and dx", h, dx)
         for t in (dw, db):
             if t is not None and (tuple(t.shape) != (n,) or t.dtype != dw_dtype or
-                                  t.device != h.device or not t.is_contiguous()):
+                                  t.device != device or not t.is_contiguous()):
                 raise ValueError("dweight and dbias must be [n] with the weight's dtype")
     else:
         dx = torch.empty_like(h) if need_dx else None
-        dw = torch.empty((n,), dtype=dw_dtype, device=h.device) if need_dw else None
+        dw = torch.empty((n,), dtype=dw_dtype, device=device) if need_dw else None
         db = torch.empty_like(dw) if need_dw else None
     lib, dt = _library(), _dtype_code(h)
     ws, nbytes = None, 0
@@ -839,11 +853,11 @@ def layer_norm_backward(h, mean, rstd, weight, dy, dh=None, need_dx: bool = True
         size = ctypes.c_size_t(0)
         check(lib.kan_layer_norm_backward_workspace_bytes(dt, rows, n, ctypes.byref(size)))
         nbytes, ws = size.value, workspace
-        if ws is None or ws.numel() < nbytes or ws.device != h.device:
-            ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=h.device)
-    check(_call(h.device, lib.kan_layer_norm_backward, dt, pdt, rows, n, h.data_ptr(),
+        if ws is None or ws.numel() < nbytes or ws.device != device:
+            ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+    check(_call(device, lib.kan_layer_norm_backward, dt, pdt, rows, n, h.data_ptr(),
                 mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dy.data_ptr(), _ptr(dh), _ptr(dx),
-                _ptr(dw), _ptr(db), _ptr(ws), nbytes, _stream(h.device)))
+                _ptr(dw), _ptr(db), _ptr(ws), nbytes, _stream(device)))
     return dx, dw, db
 
 
@@ -931,21 +945,24 @@ def token_logprobs_backward(logits, targets, stats, dlogp, entropy=None, dentrop
     return out
 
 
+_dtype_of = operator.attrgetter("dtype")
+
+
 def _many(grads):
     """Checks a list of tensors: host arrays of their addresses, sizes and dtypes."""
-    torch = _torch()
-    devices = set(map(torch.Tensor.get_device, grads))
+    Tensor = _torch().Tensor
+    devices = set(map(Tensor.get_device, grads))
     if len(devices) > 1 or -1 in devices:
         raise ValueError("tensors must live on one GPU")
-    if not all(map(torch.Tensor.is_contiguous, grads)):
+    if not all(map(Tensor.is_contiguous, grads)):
         raise ValueError("tensors must be contiguous")
-    codes = {torch.float32: KAN_F32, torch.bfloat16: KAN_BF16}
-    try:
-        dtypes = array.array("i", [codes[g.dtype] for g in grads])
-    except KeyError as e:
-        raise NotImplementedError(f"dtype {e.args[0]} is not supported (float32 or bfloat16)")
-    return (array.array("Q", map(torch.Tensor.data_ptr, grads)),
-            array.array("q", map(torch.Tensor.numel, grads)), dtypes)
+    dtypes = list(map(_dtype_of, grads))
+    if dtypes.count(dtypes[0]) == len(dtypes):
+        codes = array.array("i", (_dtype_code(grads[0]),)) * len(dtypes)
+    else:
+        codes = array.array("i", map(_dtype_code, grads))
+    return (array.array("Q", map(Tensor.data_ptr, grads)),
+            array.array("q", map(Tensor.numel, grads)), codes)
 
 
 def _norm_buffers(count: int, device, workspace):

@@ -111,12 +111,12 @@ __global__ void __launch_bounds__(256) clip_join_kernel(const double* part, int 
 }
 
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const T* p, T* q, int n, double c) {
+__device__ __forceinline__ void chunk_scale(const T* p, T* q, int n, double c, bool past) {
     constexpr int V = kVec<T>;
     for_units(p, n, [&](int i, float(&v)[V]) {
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = (float)((double)v[k] * c);
-        store_unit<false>(q, i, n, v);
+        store_unit<false>(q, i, n, v, past);
     });
 }
 
@@ -136,10 +136,10 @@ __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs<N> a, ClipOuts
         if (f == 1.0 && a.in[c.tensor] == out) continue;
         if (c.bf16)
             chunk_scale(static_cast<const uint16_t*>(a.in[c.tensor]) + c.at,
-                        static_cast<uint16_t*>(out) + c.at, c.n, f);
+                        static_cast<uint16_t*>(out) + c.at, c.n, f, b.past);
         else
             chunk_scale(static_cast<const float*>(a.in[c.tensor]) + c.at,
-                        static_cast<float*>(out) + c.at, c.n, f);
+                        static_cast<float*>(out) + c.at, c.n, f, b.past);
     }
 }
 
@@ -185,7 +185,7 @@ size_t clip_workspace(int64_t count) {
     return sizeof(double) * (kClipGroups + (size_t)clip_launches(count));
 }
 
-hipError_t launch_clip(const ClipList& l, const ClipBound& b, void* ws, hipStream_t s) {
+hipError_t launch_clip(const ClipList& l, ClipBound b, void* ws, hipStream_t s) {
     double* part = static_cast<double*>(ws);
     const int64_t launches = clip_launches(l.count);
     const int most = launches > 0 ? kClipGroups / (int)launches + 1 : 1;
@@ -203,7 +203,12 @@ hipError_t launch_clip(const ClipList& l, const ClipBound& b, void* ws, hipStrea
         return hipGetLastError();
     }
     bool in_place = true;
-    for (int64_t t = 0; t < l.count; ++t) in_place &= l.out[t] == l.in[t] || l.sizes[t] == 0;
+    int64_t bytes = 0;
+    for (int64_t t = 0; t < l.count; ++t) {
+        in_place &= l.out[t] == l.in[t] || l.sizes[t] == 0;
+        bytes += l.sizes[t] * (l.bf16(t) ? 2 : 4);
+    }
+    b.past = bytes >= kPastCaches;
     return in_place ? scale<kClipTensors, false>(l, part, parts, b, s)
                     : scale<kClipTensorsOut, true>(l, part, parts, b, s);
 }

@@ -387,7 +387,8 @@ struct NormGradArgs {
     const void *h, *w, *dy, *dh;  // w, dh may be null
     const float *mean, *rstd;
     void* dx;     // may be null
-    float* part;  // [2][parts][n] partial weight gradients; null: none wanted
+    float* part;  // [2][parts][n] partial weight gradients; null: none, or one part:
+    void *dw, *db;  // then the gradients themselves; may be null
     int64_t rows;
     int n;
     int shift, waves;
@@ -407,7 +408,7 @@ struct NormPlan {
 NormPlan norm_plan(int64_t rows, int32_t n, int es, bool grad);
 hipError_t launch_norm(bool bf16, bool bf16_params, const NormPlan& p, NormArgs a, hipStream_t s);
 hipError_t launch_norm_grad(bool bf16, bool bf16_params, const NormPlan& p, NormGradArgs a,
-                            void* dw, void* db, hipStream_t s);
+                            hipStream_t s);
 
 // ---------------------------------------------------------------- log probabilities
 
@@ -435,6 +436,7 @@ struct LogprobGradArgs {
     int shift;       // short rows
     uint32_t items;  // (row, tile)
     uint32_t tiles;  // per row
+    bool past;       // store past the caches
 };
 constexpr int kMaxTop = 64;
 struct LogprobPlan {
@@ -468,6 +470,7 @@ struct ClipOuts {
 struct ClipBound {
     float max_norm, eps;
     float* norm;
+    bool past;  // store past the caches
 };
 static_assert(sizeof(ClipArgs<kClipTensors>) + 64 <= 4096, "kernel arguments");
 static_assert(sizeof(ClipArgs<kClipTensorsOut>) + sizeof(ClipOuts<kClipTensorsOut>) + 64 <= 4096,
@@ -485,6 +488,6 @@ struct ClipList {
 constexpr int kClipMaxTensors = 1 << 14;
 constexpr int64_t kClipMaxElements = INT64_C(1) << 40;
 size_t clip_workspace(int64_t count);
-hipError_t launch_clip(const ClipList& l, const ClipBound& b, void* ws, hipStream_t s);
+hipError_t launch_clip(const ClipList& l, ClipBound b, void* ws, hipStream_t s);
 
 }  // namespace kan

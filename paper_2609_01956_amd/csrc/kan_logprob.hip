@@ -525,8 +525,8 @@ __global__ void __launch_bounds__(256) logprob_grad_kernel(LogprobGradArgs a) {
 #pragma unroll
         for (int i = 0; i < V; ++i) d[i] = v[u * V + i];
         unit_grad(g, col, d);
-        if (base + Tile<T, E>::kElems <= n) store_unit<true>(dz, col, n, d);
-        else store_unit<false>(dz, col, n, d);
+        if (base + Tile<T, E>::kElems <= n) store_unit<true>(dz, col, n, d, a.past);
+        else store_unit<false>(dz, col, n, d, a.past);
     }
 }
 
@@ -605,6 +605,7 @@ hipError_t run_logprob_grad(LogprobGradArgs a, hipStream_t s) {
         return hipGetLastError();
     }
     const int elems = tile_elems(a.classes);
+    a.past = a.rows * a.classes * (int64_t)sizeof(T) >= kPastCaches;
     a.tiles = (a.classes + 64 * elems - 1) / (64 * elems);
     // (items are counted in 32 bits: rows in pieces, one but for 2^30 and more tiles)
     const int64_t most = (1 << 30) / a.tiles;

@@ -330,26 +330,39 @@ __global__ void __launch_bounds__(kThreads<M>) norm_grad_kernel(NormGradArgs a) 
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    if (a.part == nullptr) return;
-    // This workgroup's sums, [2][workgroups][n]: over the rows of a wave by lanes, over the
-    // rows of the workgroup through LDS, [rows][columns of the lanes].
+    if (a.dw == nullptr && a.db == nullptr) return;
+    // This workgroup's sums, [2][workgroups][n] (or, of a single one, the gradients): over the
+    // rows of a wave by lanes, over the rows of the workgroup through LDS, [rows][columns of
+    // the lanes].
     const int rows = M == kGroup ? p.rows : 4, mine = M == kGroup ? p.sub : p.wave;
     const int span = C * step;
     for (int k = 0; k < 2; ++k) {
         float(&acc)[C][V] = k == 0 ? dw : db;
-        float* out = a.part + ((int64_t)k * gridDim.x + blockIdx.x) * n;
+        float* part = a.part + ((int64_t)k * gridDim.x + blockIdx.x) * n;
+        TP* grad = static_cast<TP*>(k == 0 ? a.dw : a.db);
+        const bool direct = a.part == nullptr;
+        if (direct && grad == nullptr) continue;
         if (M == kShared)
             for (int o = p.lanes; o < 64; o *= 2)
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[0][i] += __shfl_xor(acc[0][i], o);
-        if (rows == 1) {
+        if (rows == 1 && !direct) {
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int i = 0; i < V; i += 4) {
                     const float u[4] = {acc[c][i], acc[c][i + 1], acc[c][i + 2], acc[c][i + 3]};
-                    store_unit<false>(out, col0 + c * step + i, n, u);
+                    store_unit<false>(part, col0 + c * step + i, n, u);
                 }
+            continue;
+        }
+        if (rows == 1) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (col0 + c * step + i < n)
+                        Storage<TP>::store(grad + col0 + c * step + i, acc[c][i]);
             continue;
         }
         if (k == 1) __syncthreads();
@@ -365,7 +378,8 @@ __global__ void __launch_bounds__(kThreads<M>) norm_grad_kernel(NormGradArgs a) 
         for (int j = threadIdx.x; j < n; j += blockDim.x) {
             float t = join[j];
             for (int r = 1; r < rows; ++r) t += join[r * span + j];
-            out[j] = t;
+            if (direct) Storage<TP>::store(grad + j, t);
+            else part[j] = t;
         }
     }
 }
@@ -406,7 +420,7 @@ __global__ void __launch_bounds__(512) norm_grad_long_kernel(NormGradArgs a) {
 
 // Partial weight gradients of the same rows: a lane per column, the rows split over
 // gridDim.y.
-template <typename T>
+template <typename T, typename TP>
 __global__ void __launch_bounds__(256) norm_grad_columns_kernel(NormGradArgs a) {
     const int col = blockIdx.x * 256 + threadIdx.x;
     if (col >= a.n) return;
@@ -418,6 +432,11 @@ __global__ void __launch_bounds__(256) norm_grad_columns_kernel(NormGradArgs a) 
             a.rstd[row];
         dw = __builtin_fmaf(dy, xh, dw);
         db += dy;
+    }
+    if (a.part == nullptr) {
+        if (a.dw != nullptr) Storage<TP>::store(static_cast<TP*>(a.dw) + col, dw);
+        if (a.db != nullptr) Storage<TP>::store(static_cast<TP*>(a.db) + col, db);
+        return;
     }
     a.part[(int64_t)blockIdx.y * a.n + col] = dw;
     a.part[((int64_t)gridDim.y + blockIdx.y) * a.n + col] = db;
@@ -485,6 +504,9 @@ NormPlan norm_plan(int64_t rows, int32_t n, int es, bool grad) {
     if (grad && per > 1 && p.waves > 0)
         p.lds = sizeof(float) * p.units * V *
                 (p.waves > 1 ? p.threads : p.units > 1 ? 256 : 4 << p.shift);
+    // (few rows: one workgroup, whose sums are the gradients: an iteration takes about 2 us,
+    // the launch that joins workgroups 5)
+    if (grad && rows <= 3 * per && p.waves > 0) most = 1;
     const int64_t need = (rows + per - 1) / per;
     p.blocks = (int)(need < most ? need : most);
     p.parts = p.waves == 0 ? (int)(rows < kLongParts ? rows : kLongParts) : p.blocks;
@@ -532,25 +554,26 @@ hipError_t norm_forward(const NormPlan& p, const NormArgs& a, hipStream_t s) {
 }
 
 template <typename T, typename TP>
-hipError_t norm_backward(const NormPlan& p, const NormGradArgs& a, void* dw, void* db,
-                         hipStream_t s) {
+hipError_t norm_backward(const NormPlan& p, const NormGradArgs& a, hipStream_t s) {
     hipError_t e = hipSuccess;
+    const bool params = a.dw != nullptr || a.db != nullptr;
     if (a.rows > 0 && p.waves == 0) {
         if (a.dx != nullptr) {
             norm_grad_long_kernel<T, TP><<<p.blocks, 512, 0, s>>>(a);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-        if (a.part != nullptr)
-            norm_grad_columns_kernel<T><<<dim3((a.n + 255) / 256, p.parts), 256, 0, s>>>(a);
+        if (params)
+            norm_grad_columns_kernel<T, TP><<<dim3((a.n + 255) / 256, p.parts), 256, 0, s>>>(a);
     } else if (a.rows > 0) {
         norm_dispatch<T>(p, [&](auto m, auto c, auto fc) {
             norm_grad_kernel<T, TP, decltype(m)::value, decltype(c)::value, decltype(fc)::value>
                 <<<p.blocks, p.threads, p.lds, s>>>(a);
         });
     }
-    if ((e = hipGetLastError()) != hipSuccess || (dw == nullptr && db == nullptr)) return e;
+    if ((e = hipGetLastError()) != hipSuccess || !params || p.parts == 1) return e;
+    // (without rows there are no parts: 0)
     norm_params_kernel<TP><<<dim3((a.n + 15) / 16, 2), 1024, 0, s>>>(
-        a.part, p.parts, a.n, static_cast<TP*>(dw), static_cast<TP*>(db));
+        a.part, p.parts, a.n, static_cast<TP*>(a.dw), static_cast<TP*>(a.db));
     return hipGetLastError();
 }
 
@@ -565,12 +588,12 @@ hipError_t launch_norm(bool bf16, bool bf16_params, const NormPlan& p, NormArgs 
 }
 
 hipError_t launch_norm_grad(bool bf16, bool bf16_params, const NormPlan& p, NormGradArgs a,
-                            void* dw, void* db, hipStream_t s) {
+                            hipStream_t s) {
     a.shift = p.shift;
     a.waves = p.waves;
-    if (!bf16) return norm_backward<float, float>(p, a, dw, db, s);
-    if (bf16_params) return norm_backward<uint16_t, uint16_t>(p, a, dw, db, s);
-    return norm_backward<uint16_t, float>(p, a, dw, db, s);
+    if (!bf16) return norm_backward<float, float>(p, a, s);
+    if (bf16_params) return norm_backward<uint16_t, uint16_t>(p, a, s);
+    return norm_backward<uint16_t, float>(p, a, s);
 }
 
 }  // namespace kan

@@ -195,9 +195,11 @@ kan_status kan_layer_norm_backward(kan_dtype dtype, kan_dtype param_dtype, int64
         return KAN_ERR_INVALID_ARG;
     if (rows == 0 && !params) return KAN_OK;
     const kan::NormGradArgs a = {h, weight, dy, dh, mean, rstd, dx,
-                                 need > 0 ? static_cast<float*>(workspace) : nullptr, rows, n, 0, 0};
+                                 // (one part is written as the gradients themselves)
+                                 p.parts > 1 ? static_cast<float*>(workspace) : nullptr,
+                                 dweight, dbias, rows, n, 0, 0};
     return device_status(kan::launch_norm_grad(dtype == KAN_BF16, param_dtype == KAN_BF16, p, a,
-                                               dweight, dbias, static_cast<hipStream_t>(stream)));
+                                               static_cast<hipStream_t>(stream)));
 }
 
 kan_status kan_token_logprobs_workspace_bytes(kan_dtype dtype, int64_t rows, int32_t classes,
@@ -299,7 +301,7 @@ kan_status kan_grad_norm(int32_t count, const void* const* grads, const int64_t*
     const kan_status st = check_clip(l, workspace, workspace_bytes, norm);
     if (st != KAN_OK) return st;
     return device_status(
-        kan::launch_clip(l, {0.0f, 0.0f, norm}, workspace, static_cast<hipStream_t>(stream)));
+        kan::launch_clip(l, {0.0f, 0.0f, norm, false}, workspace, static_cast<hipStream_t>(stream)));
 }
 
 kan_status kan_clip_grad_norm(int32_t count, const void* const* grads, const int64_t* sizes,
@@ -313,7 +315,7 @@ kan_status kan_clip_grad_norm(int32_t count, const void* const* grads, const int
     const kan_status st = check_clip(l, workspace, workspace_bytes, norm);
     if (st != KAN_OK) return st;
     if (clip_outputs_clash(l)) return KAN_ERR_INVALID_ARG;
-    return device_status(kan::launch_clip(l, {max_norm, eps, norm}, workspace,
+    return device_status(kan::launch_clip(l, {max_norm, eps, norm, false}, workspace,
                                           static_cast<hipStream_t>(stream)));
 }
 

@@ -15,7 +15,7 @@
 // The tensors go by value, as many per launch as a kernel's 4 KB of arguments hold: no table
 // is copied to the device or kept.  A tensor is cut into chunks of kClipChunk elements,
 // numbered over the launch's tensors; a workgroup takes every gridDim-th chunk and finds its
-// tensor by bisection.
+// tensor by a count over its lanes.
 #include "kan_internal.h"
 #include "kan_rows.h"
 
@@ -23,27 +23,38 @@ namespace kan {
 
 namespace {
 
-// A chunk's tensor (the last one whose first chunk is not past it) and place in it.
+// A chunk's tensor and place in it.
 struct Chunk {
     int tensor, n;
     int64_t at;
     bool bf16;
 };
+
+// Finds chunks: each lane holds the first chunks of every 64th tensor, so that a search is a
+// comparison and a count, without a load.
 template <int N>
-__device__ __forceinline__ Chunk chunk_of(const ClipArgs<N>& a, int chunk) {
-    int lo = 0, hi = a.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.first[mid] <= chunk) lo = mid;
-        else hi = mid - 1;
+struct Finder {
+    static constexpr int R = (N + 63) / 64;
+    int first[R];
+    __device__ __forceinline__ explicit Finder(const ClipArgs<N>& a) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int t = r * 64 + lane;
+            first[r] = t < a.count ? a.first[t] : 0x7fffffff;
+        }
     }
-    Chunk c;
-    c.tensor = lo;
-    c.at = (int64_t)(chunk - a.first[lo]) * kClipChunk;
-    c.n = chunk + 1 == a.first[lo + 1] ? (a.tail[lo] >> 1) + 1 : kClipChunk;
-    c.bf16 = a.tail[lo] & 1;
-    return c;
-}
+    __device__ __forceinline__ Chunk find(const ClipArgs<N>& a, int chunk) const {
+        Chunk c;
+        c.tensor = -1;  // (the last tensor whose first chunk is not past it)
+#pragma unroll
+        for (int r = 0; r < R; ++r) c.tensor += __popcll(__ballot(first[r] <= chunk));
+        c.at = (int64_t)(chunk - a.first[c.tensor]) * kClipChunk;
+        c.n = chunk + 1 == a.first[c.tensor + 1] ? (a.tail[c.tensor] >> 1) + 1 : kClipChunk;
+        c.bf16 = a.tail[c.tensor] & 1;
+        return c;
+    }
+};
 
 // Sum over the workgroup, every lane gets it.
 __device__ __forceinline__ double group_total(double v) {
@@ -88,9 +99,10 @@ __device__ __forceinline__ double chunk_squares(const T* p, int n) {
 }
 
 __global__ void __launch_bounds__(256) clip_norm_kernel(ClipArgs<kClipTensors> a, double* part) {
+    const Finder<kClipTensors> finder(a);
     double s = 0.0;
     for (int i = blockIdx.x; i < a.chunks; i += gridDim.x) {
-        const Chunk c = chunk_of(a, i);
+        const Chunk c = finder.find(a, i);
         s += c.bf16 ? chunk_squares(static_cast<const uint16_t*>(a.in[c.tensor]) + c.at, c.n)
                     : chunk_squares(static_cast<const float*>(a.in[c.tensor]) + c.at, c.n);
     }
@@ -110,36 +122,38 @@ __global__ void __launch_bounds__(256) clip_join_kernel(const double* part, int 
     if (threadIdx.x == 0) *norm = (float)n;
 }
 
-template <typename T>
-__device__ __forceinline__ void chunk_scale(const T* p, T* q, int n, double c, bool past) {
+template <bool PAST, typename T>
+__device__ __forceinline__ void chunk_scale(const T* p, T* q, int n, double c) {
     constexpr int V = kVec<T>;
     for_units(p, n, [&](int i, float(&v)[V]) {
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = (float)((double)v[k] * c);
-        store_unit<false>(q, i, n, v, past);
+        store_unit<false, PAST>(q, i, n, v);
     });
 }
 
-// OUT: the tensors' outputs stand after the N tensors' arguments (else in place).
-template <int N, bool OUT>
+// OUT: the tensors' outputs stand after the N tensors' arguments (else in place).  PAST: they are
+// stored past the caches.
+template <int N, bool OUT, bool PAST>
 __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs<N> a, ClipOuts<OUT ? N : 1> o,
                                                          const double* part, int parts,
                                                          ClipBound b) {
+    const Finder<N> finder(a);
     const double n = norm_of(part, parts);
     if (blockIdx.x == 0 && threadIdx.x == 0) *b.norm = (float)n;
     // (gradients that are all 0 stay as they are; a NaN among them reaches all)
     const double ratio = n == 0.0 ? 1.0 : (double)b.max_norm / (n + (double)b.eps);
     const double f = ratio >= 1.0 ? 1.0 : ratio;
     for (int i = a.chunks - 1 - (int)blockIdx.x; i >= 0; i -= gridDim.x) {
-        const Chunk c = chunk_of(a, i);
+        const Chunk c = finder.find(a, i);
         void* out = OUT ? o.out[c.tensor] : const_cast<void*>(a.in[c.tensor]);
         if (f == 1.0 && a.in[c.tensor] == out) continue;
         if (c.bf16)
-            chunk_scale(static_cast<const uint16_t*>(a.in[c.tensor]) + c.at,
-                        static_cast<uint16_t*>(out) + c.at, c.n, f, b.past);
+            chunk_scale<PAST>(static_cast<const uint16_t*>(a.in[c.tensor]) + c.at,
+                        static_cast<uint16_t*>(out) + c.at, c.n, f);
         else
-            chunk_scale(static_cast<const float*>(a.in[c.tensor]) + c.at,
-                        static_cast<float*>(out) + c.at, c.n, f, b.past);
+            chunk_scale<PAST>(static_cast<const float*>(a.in[c.tensor]) + c.at,
+                        static_cast<float*>(out) + c.at, c.n, f);
     }
 }
 
@@ -163,14 +177,16 @@ bool next_args(const ClipList& l, int64_t* t, ClipArgs<N>* a, void** out) {
 }
 
 template <int N, bool OUT>
-hipError_t scale(const ClipList& l, const double* part, int parts, ClipBound b, hipStream_t s) {
+hipError_t scale(const ClipList& l, const double* part, int parts, ClipBound b, bool past,
+                 hipStream_t s) {
     ClipArgs<N> a;
     ClipOuts<OUT ? N : 1> o;
     bool first = true;
     for (int64_t t = 0; next_args(l, &t, &a, OUT ? o.out : nullptr) || first; first = false) {
         // (one workgroup at least, for the norm)
         const int groups = a.chunks < 1 ? 1 : a.chunks < kClipGroups ? a.chunks : kClipGroups;
-        clip_scale_kernel<N, OUT><<<groups, 256, 0, s>>>(a, o, part, parts, b);
+        if (past) clip_scale_kernel<N, OUT, true><<<groups, 256, 0, s>>>(a, o, part, parts, b);
+        else clip_scale_kernel<N, OUT, false><<<groups, 256, 0, s>>>(a, o, part, parts, b);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -185,7 +201,7 @@ size_t clip_workspace(int64_t count) {
     return sizeof(double) * (kClipGroups + (size_t)clip_launches(count));
 }
 
-hipError_t launch_clip(const ClipList& l, ClipBound b, void* ws, hipStream_t s) {
+hipError_t launch_clip(const ClipList& l, const ClipBound& b, void* ws, hipStream_t s) {
     double* part = static_cast<double*>(ws);
     const int64_t launches = clip_launches(l.count);
     const int most = launches > 0 ? kClipGroups / (int)launches + 1 : 1;
@@ -208,9 +224,9 @@ hipError_t launch_clip(const ClipList& l, ClipBound b, void* ws, hipStream_t s) 
         in_place &= l.out[t] == l.in[t] || l.sizes[t] == 0;
         bytes += l.sizes[t] * (l.bf16(t) ? 2 : 4);
     }
-    b.past = bytes >= kPastCaches;
-    return in_place ? scale<kClipTensors, false>(l, part, parts, b, s)
-                    : scale<kClipTensorsOut, true>(l, part, parts, b, s);
+    const bool past = bytes >= kPastCaches;
+    return in_place ? scale<kClipTensors, false>(l, part, parts, b, past, s)
+                    : scale<kClipTensorsOut, true>(l, part, parts, b, past, s);
 }
 
 }  // namespace kan

@@ -436,7 +436,6 @@ struct LogprobGradArgs {
     int shift;       // short rows
     uint32_t items;  // (row, tile)
     uint32_t tiles;  // per row
-    bool past;       // store past the caches
 };
 constexpr int kMaxTop = 64;
 struct LogprobPlan {
@@ -470,7 +469,6 @@ struct ClipOuts {
 struct ClipBound {
     float max_norm, eps;
     float* norm;
-    bool past;  // store past the caches
 };
 static_assert(sizeof(ClipArgs<kClipTensors>) + 64 <= 4096, "kernel arguments");
 static_assert(sizeof(ClipArgs<kClipTensorsOut>) + sizeof(ClipOuts<kClipTensorsOut>) + 64 <= 4096,
@@ -488,6 +486,6 @@ struct ClipList {
 constexpr int kClipMaxTensors = 1 << 14;
 constexpr int64_t kClipMaxElements = INT64_C(1) << 40;
 size_t clip_workspace(int64_t count);
-hipError_t launch_clip(const ClipList& l, ClipBound b, void* ws, hipStream_t s);
+hipError_t launch_clip(const ClipList& l, const ClipBound& b, void* ws, hipStream_t s);
 
 }  // namespace kan

@@ -502,8 +502,8 @@ __global__ void __launch_bounds__(256) logprob_grad_short_kernel(LogprobGradArgs
     }
 }
 
-// One wave per (row, tile).
-template <typename T, int E>
+// One wave per (row, tile).  PAST: the gradient is stored past the caches.
+template <typename T, int E, bool PAST>
 __global__ void __launch_bounds__(256) logprob_grad_kernel(LogprobGradArgs a) {
     constexpr int V = kVec<T>;
     const int lane = threadIdx.x & 63, n = a.classes;
@@ -525,8 +525,8 @@ __global__ void __launch_bounds__(256) logprob_grad_kernel(LogprobGradArgs a) {
 #pragma unroll
         for (int i = 0; i < V; ++i) d[i] = v[u * V + i];
         unit_grad(g, col, d);
-        if (base + Tile<T, E>::kElems <= n) store_unit<true>(dz, col, n, d, a.past);
-        else store_unit<false>(dz, col, n, d, a.past);
+        if (base + Tile<T, E>::kElems <= n) store_unit<true, PAST>(dz, col, n, d);
+        else store_unit<false, PAST>(dz, col, n, d);
     }
 }
 
@@ -605,7 +605,7 @@ hipError_t run_logprob_grad(LogprobGradArgs a, hipStream_t s) {
         return hipGetLastError();
     }
     const int elems = tile_elems(a.classes);
-    a.past = a.rows * a.classes * (int64_t)sizeof(T) >= kPastCaches;
+    const bool past = a.rows * a.classes * (int64_t)sizeof(T) >= kPastCaches;
     a.tiles = (a.classes + 64 * elems - 1) / (64 * elems);
     // (items are counted in 32 bits: rows in pieces, one but for 2^30 and more tiles)
     const int64_t most = (1 << 30) / a.tiles;
@@ -613,9 +613,14 @@ hipError_t run_logprob_grad(LogprobGradArgs a, hipStream_t s) {
         const int64_t now = rows < most ? rows : most;
         a.items = (uint32_t)(now * a.tiles);
         const int grid = (int)((a.items + 3) / 4);
-        if (elems == 8) logprob_grad_kernel<T, 8><<<grid, 256, 0, s>>>(a);
-        else if (elems == 16) logprob_grad_kernel<T, 16><<<grid, 256, 0, s>>>(a);
-        else logprob_grad_kernel<T, 32><<<grid, 256, 0, s>>>(a);
+        auto go = [&](auto e) {
+            constexpr int E = decltype(e)::value;
+            if (past) logprob_grad_kernel<T, E, true><<<grid, 256, 0, s>>>(a);
+            else logprob_grad_kernel<T, E, false><<<grid, 256, 0, s>>>(a);
+        };
+        if (elems == 8) go(std::integral_constant<int, 8>{});
+        else if (elems == 16) go(std::integral_constant<int, 16>{});
+        else go(std::integral_constant<int, 32>{});
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         a.z = static_cast<const T*>(a.z) + now * a.stride;

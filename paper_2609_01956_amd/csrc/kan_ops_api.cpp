@@ -301,7 +301,7 @@ kan_status kan_grad_norm(int32_t count, const void* const* grads, const int64_t*
     const kan_status st = check_clip(l, workspace, workspace_bytes, norm);
     if (st != KAN_OK) return st;
     return device_status(
-        kan::launch_clip(l, {0.0f, 0.0f, norm, false}, workspace, static_cast<hipStream_t>(stream)));
+        kan::launch_clip(l, {0.0f, 0.0f, norm}, workspace, static_cast<hipStream_t>(stream)));
 }
 
 kan_status kan_clip_grad_norm(int32_t count, const void* const* grads, const int64_t* sizes,
@@ -315,7 +315,7 @@ kan_status kan_clip_grad_norm(int32_t count, const void* const* grads, const int
     const kan_status st = check_clip(l, workspace, workspace_bytes, norm);
     if (st != KAN_OK) return st;
     if (clip_outputs_clash(l)) return KAN_ERR_INVALID_ARG;
-    return device_status(kan::launch_clip(l, {max_norm, eps, norm, false}, workspace,
+    return device_status(kan::launch_clip(l, {max_norm, eps, norm}, workspace,
                                           static_cast<hipStream_t>(stream)));
 }
 

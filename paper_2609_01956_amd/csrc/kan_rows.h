@@ -146,16 +146,15 @@ __device__ __forceinline__ void load_unit(const T* row, int col, int n, uint32_t
 template <typename T> constexpr uint32_t kNegInfBits = sizeof(T) == 2 ? 0xff80u : 0xff800000u;
 
 // One unit of a row of n elements, those within the row: the last unit's n % V elements as
-// 8, 4 and 2 bytes.  past: whole units go past the caches (outputs that do not fit there).
-template <bool FULL, typename T, int V>
-__device__ __forceinline__ void store_unit(T* row, int col, int n, const float (&v)[V],
-                                           bool past = false) {
+// 8, 4 and 2 bytes.  PAST: whole units go past the caches (outputs that do not fit there).
+template <bool FULL, bool PAST = false, typename T, int V>
+__device__ __forceinline__ void store_unit(T* row, int col, int n, const float (&v)[V]) {
     static_assert(V == kVec<T>, "one unit");
     typedef uint32_t u32_any __attribute__((aligned(2)));
     typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
     const u32x4 r = narrow(v);
     if (FULL || col + V <= n) {
-        if (past) __builtin_nontemporal_store(r, unit_at(row, col));
+        if constexpr (PAST) __builtin_nontemporal_store(r, unit_at(row, col));
         else *unit_at(row, col) = r;
         return;
     }

@@ -6,11 +6,11 @@ exposes the same entry points to Python and marshals torch tensors into them;
 importing this package does not load the library, the first call does, and
 it raises if the library is missing.
 """
-__all__ = ["binding", "workloads"]
+__all__ = ["binding", "train", "workloads"]
 
 
 def __getattr__(name):
-    if name in ("binding", "workloads"):
+    if name in ("binding", "train", "workloads"):
         import importlib
         return importlib.import_module(f"{__name__}.{name}")
     raise AttributeError(name)

@@ -47,7 +47,7 @@ def test_gradients_against_autograd(sizes):
     params = [[p.double().requires_grad_() for p in layer] for layer in model.params]
     want, loss = model64(params, x.double(), t, model.grid, 0.3)
     loss.backward()
-    assert abs(float(logp) - float(want)) < 1e-5
+    assert abs(float(logp) - float(want.detach())) < 1e-5
     flat = [p for layer in params for p in layer]
     assert len(grads) == len(flat)
     for a, p in zip(grads, flat):

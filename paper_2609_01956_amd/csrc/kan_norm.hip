@@ -30,8 +30,8 @@ constexpr int kMaxWaves = 8;
 
 // How a workgroup takes rows.
 enum Mode {
-    kShared,  // four waves, 64 >> shift rows in each, one unit per lane (32 lanes a row at most)
-    kWave,    // four waves, a row each (33 units or more)
+    kShared,  // 64 >> shift rows in each wave, one unit per lane (32 lanes a row at most)
+    kWave,    // a row in each wave (33 units or more)
     kGroup,   // a.waves waves a row, as many rows as eight waves take
 };
 
@@ -53,7 +53,7 @@ struct Place {
             rows = (int)(blockDim.x >> 6) / waves;
             sub = wave / waves;
         } else {
-            rows = M == kShared ? 256 >> shift : 4;
+            rows = M == kShared ? (int)blockDim.x >> shift : (int)blockDim.x >> 6;
             sub = M == kShared ? (int)threadIdx.x >> shift : wave;
         }
         first = M == kGroup ? sub * waves : 0;
@@ -103,6 +103,7 @@ __device__ __forceinline__ void clear_units(u32x4 (&raw)[N]) {
 }
 
 template <int M> constexpr int kThreads = M == kGroup ? 64 * kMaxWaves : 256;
+constexpr int kGradThreads = 64 * kMaxWaves;
 
 // C units per lane, of which the first FC are full in every lane.
 template <typename T, typename TP, int M, int C, int FC>
@@ -259,7 +260,7 @@ struct GradRow {
 };
 
 template <typename T, typename TP, int M, int C, int FC>
-__global__ void __launch_bounds__(kThreads<M>) norm_grad_kernel(NormGradArgs a) {
+__global__ void __launch_bounds__(kGradThreads) norm_grad_kernel(NormGradArgs a) {
     constexpr int V = kVec<T>;
     constexpr bool kSub = M == kShared;
     __shared__ float red[2][kMaxWaves][2];
@@ -334,7 +335,7 @@ __global__ void __launch_bounds__(kThreads<M>) norm_grad_kernel(NormGradArgs a) 
     // This workgroup's sums, [2][workgroups][n] (or, of a single one, the gradients): over the
     // rows of a wave by lanes, over the rows of the workgroup through LDS, [rows][columns of
     // the lanes].
-    const int rows = M == kGroup ? p.rows : 4, mine = M == kGroup ? p.sub : p.wave;
+    const int rows = M == kGroup ? p.rows : kMaxWaves, mine = M == kGroup ? p.sub : p.wave;
     const int span = C * step;
     for (int k = 0; k < 2; ++k) {
         float(&acc)[C][V] = k == 0 ? dw : db;
@@ -484,9 +485,9 @@ NormPlan norm_plan(int64_t rows, int32_t n, int es, bool grad) {
         p.waves = 0;
     } else if (n <= 1024) {
         p.waves = 1;
-        p.threads = 256;
+        p.threads = grad ? kGradThreads : 256;
         while (V << p.shift < n && p.shift < 6) ++p.shift;
-        per = 256 >> p.shift;
+        per = p.threads >> p.shift;
         p.units = p.shift < 6 || n <= 64 * V ? 1 : (n <= 512 ? 8 : 16) / V;
     } else {
         // 16 elements per lane, 32 where eight waves need them
@@ -496,16 +497,16 @@ NormPlan norm_plan(int64_t rows, int32_t n, int es, bool grad) {
         p.threads = (int)(64 * p.waves * per);
     }
     // Workgroups of the gradient: each leaves a row of partial sums, so no more than keep the
-    // memory busy (16384 x 1024 fp32: 512 43 us, 768 45, 1024 47; one unit per lane, 65536 x
-    // 300 bf16: 512 50 us, 768 41, 1024 38).
-    if (grad) most = p.units == 1 ? 1024 : n <= 8192 ? 512 : 256;
+    // memory busy, of eight waves (with the joining launch: 16384 x 256 fp32 512 workgroups
+    // 15.5 us, 768 17.6, 1024 of four waves 17.3; 16384 x 1024 fp32 256 42.7 us, 384 45.0, 512 45.6).
+    if (grad) most = p.units == 1 ? 512 : p.waves == 1 ? 256 : n <= 8192 ? 512 : 256;
     // (the weight gradients' join: the columns of all lanes of the workgroup's waves that take
     // different rows)
     if (grad && per > 1 && p.waves > 0)
         p.lds = sizeof(float) * p.units * V *
-                (p.waves > 1 ? p.threads : p.units > 1 ? 256 : 4 << p.shift);
-    // (few rows: one workgroup, whose sums are the gradients: an iteration takes about 2 us,
-    // the launch that joins workgroups 5)
+                (p.waves > 1 || p.units > 1 ? p.threads : kMaxWaves << p.shift);
+    // (few rows: one workgroup, whose sums are the gradients: 16 x 784 bf16 11.0 us against
+    // 15.4 with the joining launch)
     if (grad && rows <= 3 * per && p.waves > 0) most = 1;
     const int64_t need = (rows + per - 1) / per;
     p.blocks = (int)(need < most ? need : most);

@@ -422,7 +422,7 @@ struct LogprobArgs {
     float* top_logp;
     int64_t* top_index;
     int shift;      // short rows: log2 of the lanes of a row
-    int parts;      // workgroups (of one wave) that share a row
+    int parts;      // waves that share a row
     float4* part;   // [rows][parts] sums of the parts
     uint64_t* keys; // [rows][parts][k] their best classes
 };
@@ -439,8 +439,7 @@ struct LogprobGradArgs {
 };
 constexpr int kMaxTop = 64;
 struct LogprobPlan {
-    int waves;  // per (row, part), 0: rows that share a wave
-    int elems;  // of a tile, per lane
+    int elems;  // of a tile, per lane; 0: rows that share a wave
     int shift, parts;
     size_t bytes;  // workspace
 };

@@ -14,9 +14,9 @@
 // 0.  Everything is fp32; a masked class is -infinity (or so low that its weight is 0).
 //
 // Rows of at most one 16-byte unit per lane of half a wave share a wave.  Longer rows are
-// taken in tiles of up to 32 elements per lane, the next tile's loads in flight, by one wave,
-// or four where rows are long and many, or by several workgroups where rows are few (each
-// leaves its sums and its best k in the workspace and a second launch joins them).
+// taken in tiles of up to 32 elements per lane, the next tile's loads in flight, by a wave
+// each, or by several where rows are few (each leaves its sums and its best k in the
+// workspace and a second launch joins them).
 //
 // The best k of a wave stand sorted across its lanes, one 64-bit key per lane (the value's
 // bits in order, then the complement of the index, so that keys are distinct and ties go
@@ -24,7 +24,6 @@
 // reaches the k-th best so far.  Then every such lane offers its largest: many at once (the
 // first tile) are sorted across the lanes and merged, few are inserted one after the
 // other; those lanes' next largest are compared again, until none reaches the k-th best.
-// The waves of a row share the k-th best that any of them has.
 #include "kan_internal.h"
 #include "kan_rows.h"
 
@@ -342,35 +341,25 @@ __device__ __forceinline__ void offer_nan(Best& best, const T* z, int n, int lan
     }
 }
 
-// W waves per (row, part): W = 1, four of them per workgroup, or W = 4.
-template <typename T, int W, int E, bool ENT, bool TOP>
+// A wave per (row, part), four per workgroup.
+template <typename T, int E, bool ENT, bool TOP>
 __global__ void __launch_bounds__(256) logprob_kernel(LogprobArgs a) {
-    __shared__ Sums part[W];
-    __shared__ uint64_t keys[W][64];
-    __shared__ unsigned long long bar;  // the highest k-th best of the waves of a row
     constexpr int kTile = Tile<T, E>::kElems;
     const int lane = threadIdx.x & 63, n = a.classes;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t items = a.rows * a.parts;
-    if (W > 1 && TOP) {
-        bar = 0;
-        __syncthreads();
-    }
-    for (int64_t i0 = (int64_t)blockIdx.x * (4 / W); i0 < items;
-         i0 += (int64_t)gridDim.x * (4 / W)) {
-        const int64_t item = i0 + (W == 1 ? wave : 0);
-        if (item >= items) break;  // (W = 1)
+    for (int64_t item = (int64_t)blockIdx.x * 4 + wave; item < items;
+         item += (int64_t)gridDim.x * 4) {
         const int64_t row = a.parts == 1 ? item : item / a.parts;
-        const int p = (int)(item - row * a.parts);
         const T* z = static_cast<const T*>(a.z) + row * a.stride;
         Sums r = {kNegInf, 0.0f, 0.0f};
         Best best(TOP ? a.k : 1);
-        int base = (W == 1 ? p : p * W + wave) * kTile;
-        const int step = a.parts * W * kTile;
+        int base = (int)(item - row * a.parts) * kTile;
+        const int step = a.parts * kTile;
         Tile<T, E> next;
         next.issue(z, base, n, lane);
         const Target target = target_of<T>(a, row);
-        // (kMaxClasses and a step stay below 2^31)
+        // (classes and a step stay below 2^31)
         for (; base < n; base += step) {
             Tile<T, E> tile = next;
             if (base + step < n) next.issue(z, base + step, n, lane);
@@ -378,35 +367,9 @@ __global__ void __launch_bounds__(256) logprob_kernel(LogprobArgs a) {
             tile.values(base, n, lane, v);
             const float vm = max_of(v);
             add_values<ENT>(r, v, vm);
-            if (TOP) {
-                if (W > 1)
-                    best.raise(__hip_atomic_load(&bar, __ATOMIC_RELAXED,
-                                                 __HIP_MEMORY_SCOPE_WORKGROUP));
-                const uint64_t had = best.bar;
-                offer_tile<T>(best, v, vm, base, n, lane);
-                if (W > 1 && best.bar > had && lane == 0)
-                    __hip_atomic_fetch_max(&bar, best.bar, __ATOMIC_RELAXED,
-                                           __HIP_MEMORY_SCOPE_WORKGROUP);
-            }
+            if (TOP) offer_tile<T>(best, v, vm, base, n, lane);
         }
         join_wave(r);
-        if (W > 1) {
-            if (lane == 0) part[wave] = r;
-            if (TOP) keys[wave][lane] = best.mine;
-            __syncthreads();
-            if (wave == 0) {
-                r = lane < W ? part[lane] : Sums{kNegInf, 0.0f, 0.0f};
-                join_wave(r);
-                if (TOP) {
-                    best.bar = 0;
-                    for (int w = 1; w < W; ++w) best.merge(keys[w][lane], lane);
-                }
-            } else if (TOP) {
-                bar = 0;
-            }
-            __syncthreads();
-            if (wave != 0) continue;
-        }
         if (a.parts > 1) {
             if (lane == 0) a.part[item] = make_float4(r.m, r.s, r.q, 0.0f);
             if (TOP && lane < a.k) a.keys[item * a.k + lane] = best.mine;
@@ -538,7 +501,7 @@ int grid_of(int64_t n, int64_t most) { return (int)(n < most ? n : most); }
 }  // namespace
 
 LogprobPlan logprob_plan(int64_t rows, int32_t classes, int es, int k) {
-    LogprobPlan p = {0, 0, 0, 1, 0};
+    LogprobPlan p = {0, 0, 1, 0};
     const int V = 16 / es;
     if (classes <= 32 * V) {
         while (V << p.shift < classes) ++p.shift;
@@ -546,10 +509,11 @@ LogprobPlan logprob_plan(int64_t rows, int32_t classes, int es, int k) {
     }
     p.elems = tile_elems(classes);
     const int64_t tiles = (classes + 64 * p.elems - 1) / (64 * p.elems);
-    // four waves a row where rows alone fill the GPU with such workgroups and are long
-    // enough that each wave gets a tile; below that, parts of rows to 16 waves per CU
-    p.waves = rows >= 1024 && tiles >= 4 ? 4 : 1;
-    if (p.waves == 1 && rows < 4096) {
+    // a wave a row where rows alone give every SIMD one, else parts of rows to four (1000 x
+    // 131072 bf16: 52 us in 5 parts; 2001 x 50001 39 us whole, 45 in 3 parts; four waves a row
+    // take 41, and with 5 alternatives 20000 x 9000 172 us against 105, since each wave
+    // begins a list of its own)
+    if (rows < 1024) {
         int64_t parts = rows > 0 ? (4096 + rows - 1) / rows : 1;
         if (parts > 64) parts = 64;
         if (parts > tiles) parts = tiles;
@@ -563,31 +527,29 @@ namespace {
 
 template <typename T>
 hipError_t run_logprob(const LogprobPlan& p, const LogprobArgs& a, hipStream_t s) {
-    if (p.waves == 0) {
+    if (p.elems == 0) {
         const int64_t per = 256 >> p.shift;
         logprob_short_kernel<T><<<grid_of((a.rows + per - 1) / per, 8192), 256, 0, s>>>(a);
         return hipGetLastError();
     }
-    const int64_t items = a.rows * p.parts, per = 4 / p.waves;
-    const int grid = grid_of((items + per - 1) / per, 1 << 30);
+    const int grid = grid_of((a.rows * p.parts + 3) / 4, 1 << 30);
     const bool ent = a.entropy != nullptr, top = a.k > 0;
     using std::false_type;
     using std::integral_constant;
     using std::true_type;
-    auto go = [&](auto w, auto e, auto ent_, auto top_) {
-        logprob_kernel<T, decltype(w)::value, decltype(e)::value, decltype(ent_)::value,
-                       decltype(top_)::value><<<grid, 256, 0, s>>>(a);
+    auto go = [&](auto e, auto ent_, auto top_) {
+        logprob_kernel<T, decltype(e)::value, decltype(ent_)::value, decltype(top_)::value>
+            <<<grid, 256, 0, s>>>(a);
     };
-    auto pick = [&](auto w, auto e) {
-        if (ent && top) go(w, e, true_type{}, true_type{});
-        else if (ent) go(w, e, true_type{}, false_type{});
-        else if (top) go(w, e, false_type{}, true_type{});
-        else go(w, e, false_type{}, false_type{});
+    auto pick = [&](auto e) {
+        if (ent && top) go(e, true_type{}, true_type{});
+        else if (ent) go(e, true_type{}, false_type{});
+        else if (top) go(e, false_type{}, true_type{});
+        else go(e, false_type{}, false_type{});
     };
-    if (p.waves == 4) pick(integral_constant<int, 4>{}, integral_constant<int, 32>{});
-    else if (p.elems == 8) pick(integral_constant<int, 1>{}, integral_constant<int, 8>{});
-    else if (p.elems == 16) pick(integral_constant<int, 1>{}, integral_constant<int, 16>{});
-    else pick(integral_constant<int, 1>{}, integral_constant<int, 32>{});
+    if (p.elems == 8) pick(integral_constant<int, 8>{});
+    else if (p.elems == 16) pick(integral_constant<int, 16>{});
+    else pick(integral_constant<int, 32>{});
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
     logprob_join_kernel<T><<<(int)a.rows, 64, 0, s>>>(a);

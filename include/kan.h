@@ -13,8 +13,8 @@
  *
  * Conventions shared by every entry point
  * ---------------------------------------
- *  * Pointers named x, phi, coef, base_w, packed, y are DEVICE pointers owned
- *    by the caller.  No entry point allocates device or host memory; where a
+ *  * Pointers to data are DEVICE pointers owned by the caller (the host arrays
+ *    of kan_grad_norm and kan_clip_grad_norm are named as such).  No entry point allocates device or host memory; where a
  *    call needs scratch memory the caller passes it (a workspace pointer with
  *    a size query).  The library keeps no global state; calls are reentrant
  *    and thread-safe.
@@ -22,7 +22,8 @@
  *    null stream) and returns before it finishes.  Results are visible after the
  *    caller synchronises that stream.  A device fault inside a kernel surfaces at
  *    that synchronisation, not in the return code.
- *  * Tensors are dense and row-major.  `dtype` applies to every tensor of a call:
+ *  * Tensors are dense and row-major, where a call takes no stride.  `dtype` applies
+ *    to every tensor of a call that names no type of its own:
  *    KAN_F32 is IEEE binary32 throughout; KAN_BF16 is bfloat16 storage with
  *    binary32 basis evaluation and accumulation, rounded to nearest-even on
  *    store.

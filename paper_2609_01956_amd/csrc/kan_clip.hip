@@ -16,6 +16,10 @@
 // is copied to the device or kept.  A tensor is cut into chunks of kClipChunk elements,
 // numbered over the launch's tensors; a workgroup takes every gridDim-th chunk and finds its
 // tensor by a count over its lanes.
+//
+// Measured on MI355X: 235 M bf16 gradients in 64 tensors into other tensors 243-251 us (the two
+// reads and the write at 5.6-5.8 TB/s), the norm of 224 M bf16 in place and within the bound
+// 87 us (5.2 TB/s), 64 x 2^20 fp32 135 us.
 #include "kan_internal.h"
 #include "kan_rows.h"
 

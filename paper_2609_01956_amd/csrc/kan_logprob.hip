@@ -24,6 +24,11 @@
 // reaches the k-th best so far.  Then every such lane offers its largest: many at once (the
 // first tile) are sorted across the lanes and merged, few are inserted one after the
 // other; those lanes' next largest are compared again, until none reaches the k-th best.
+//
+// Measured on MI355X: 2001 x 50001 bf16 with entropy 39 us (5.1 TB/s), with 5 alternatives too
+// 51-56 us (bound by the vector ALUs: 10.5 operations per element counting the exponential
+// as four, and the lists); 4096 x 131072 bf16 190 us (5.7 TB/s); 1 x 131072 bf16 with 20
+// alternatives 7.4 us and 4 us for the join; gradient of 4096 x 131072 bf16 363 us (5.9 TB/s).
 #include "kan_internal.h"
 #include "kan_rows.h"
 

@@ -20,7 +20,7 @@
 // Measured on MI355X: 235 M bf16 gradients in 64 tensors into other tensors 243-251 us (the two
 // reads and the write at 5.6-5.8 TB/s), the norm of 224 M bf16 in place and within the bound
 // 87 us (5.2 TB/s), 64 x 2^20 fp32 135 us.
-#include "kan_internal.h"
+#include "kan_ops.h"
 #include "kan_rows.h"
 
 namespace kan {

@@ -29,7 +29,7 @@
 // 51-56 us (bound by the vector ALUs: 10.5 operations per element counting the exponential
 // as four, and the lists); 4096 x 131072 bf16 190 us (5.7 TB/s); 1 x 131072 bf16 with 20
 // alternatives 7.4 us and 4 us for the join; gradient of 4096 x 131072 bf16 363 us (5.9 TB/s).
-#include "kan_internal.h"
+#include "kan_ops.h"
 #include "kan_rows.h"
 
 namespace kan {

@@ -26,7 +26,7 @@
 // bf16 with dh 51.5 us (4.7 TB/s), 16384 x 256 fp32 15.5 us (3.2 TB/s, both launches).  Loads
 // of the next row ahead of time did not help (58.9 us against 52.3 for 30001 x 1001): the other
 // waves hide them, and the registers cost some of those.
-#include "kan_internal.h"
+#include "kan_ops.h"
 #include "kan_rows.h"
 
 namespace kan {

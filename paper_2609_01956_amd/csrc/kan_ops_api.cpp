@@ -8,7 +8,7 @@
 #include <cstdint>
 #include <initializer_list>
 
-#include "kan_internal.h"
+#include "kan_ops.h"
 
 namespace {
 

@@ -162,3 +162,17 @@ def test_refusals():
         kb.grad_norm([g[0].half()])
     with pytest.raises(NotImplementedError):
         kb.grad_norm([g[0].double()])
+
+
+def test_offsets_past_32_bits():
+    """A tensor of more than 2^31 elements, 0 but for its ends."""
+    n = (1 << 31) + 12345
+    g = torch.zeros(n, dtype=BF16, device=device())
+    g[:3] = 2.0
+    g[-7:] = 3.0
+    total = math.sqrt(3 * 4 + 7 * 9)
+    say("clip_grad_norm offsets past 2^31")
+    got = float(kb.clip_grad_norm([g], total / 2, eps=0.0))
+    assert abs(got - total) <= 2.0 ** -22 * total
+    assert bool((g[:3] == 1.0).all()) and bool((g[-7:] == 1.5).all())
+    assert int((g != 0).sum()) == 10

@@ -276,3 +276,45 @@ def test_refusals():
         kb.token_logprobs(wide, tw, top_k=65)
     with pytest.raises(NotImplementedError):
         kb.token_logprobs(z.half(), t)
+
+
+@pytest.mark.parametrize("rows,classes", [(100, 10), (2, 60000), (1100, 3000)])
+def test_in_a_graph(rows, classes):
+    """Captured with its gradient, and replayed with other inputs between eager calls."""
+    z, t = make(rows, classes, 0, BF16, 1)
+    z = z.clone()
+    d = torch.randn(rows, device=device())
+    run = lambda: kb.token_logprobs(z, t, top_k=7, entropy=True)
+    back = lambda o: kb.token_logprobs_backward(z, t, o[1], d, entropy=o[2], dentropy=d)
+    back(run())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o = run()
+        g = back(o)
+    for turn in range(3):
+        z.copy_(make(rows, classes, 0, BF16, 50 + turn)[0])
+        torch.cuda.synchronize()
+        say(f"token_logprobs graph rows={rows} classes={classes} replay {turn}")
+        graph.replay()
+        torch.cuda.synchronize()
+        o2 = run()
+        assert all(torch.equal(a, b) for a, b in zip(o, o2))
+        assert torch.equal(g, back(o2))
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_fewer_numbers_than_alternatives(dt):
+    """Rows that are NaN or masked but for a few classes: numbers first, then the masked, then
+    NaN, each by rising index, in one tile, several, and parts of a row."""
+    for rows, classes in [(2, 12), (3, 200), (2, 700), (2, 9000), (1030, 5000)]:
+        z = torch.full((rows, classes), float("nan"), dtype=dt, device=device())
+        t = torch.zeros(rows, dtype=torch.int64, device=device())
+        z[:, classes - 1] = 1.0
+        z[:, 5] = 1.0
+        z[:, 7] = 2.0
+        z[:, 9] = -math.inf
+        say(f"token_logprobs few numbers {dt} rows={rows} classes={classes}")
+        _, _, _, top, idx = kb.token_logprobs(z, t, top_k=8)
+        want = [7, 5, classes - 1, 9] + [i for i in range(classes) if i not in (5, 7, 9)][:4]
+        assert idx.tolist() == [want] * rows and bool(torch.isnan(top).all())

@@ -251,3 +251,51 @@ def test_refusals():
     for f in (lambda: kb.layer_norm(x.half()), lambda: kb.layer_norm(x, w.to(BF16), b.to(BF16))):
         with pytest.raises(NotImplementedError):
             f()
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 elements: the last rows as in a call of their own, forward and backward,
+    and the weight gradients of rows that are 0 but for those."""
+    rows, n = 140000, 16000
+    small = make(5, n, BF16, F32, 3)
+    say("layer_norm offsets past 2^31")
+    x = torch.zeros(rows, n, dtype=BF16, device=device())
+    x[-5:] = small["x"]
+    y, _, mean, rstd = kb.layer_norm(x, small["w"], small["b"])
+    y5, _, m5, r5 = kb.layer_norm(small["x"], small["w"], small["b"])
+    assert torch.equal(y[-5:], y5) and torch.equal(mean[-5:], m5) and torch.equal(rstd[-5:], r5)
+    del y
+    dy = torch.zeros_like(x)
+    dy[-5:] = small["dy"]
+    dx, dw, db = kb.layer_norm_backward(x, mean, rstd, small["w"], dy)
+    dx5, dw5, db5 = kb.layer_norm_backward(small["x"], m5, r5, small["w"], small["dy"])
+    assert torch.equal(dx[-5:], dx5) and not bool(dx[: rows - 5].any())
+    close(dw, dw5.double(), 1e-5, (small["dy"].double().abs() * 5).amax(0) + 1e-3)
+    close(db, db5.double(), 1e-5, small["dy"].double().abs().sum(0) + 1e-3)
+
+
+@pytest.mark.parametrize("rows,n", [(3, 300), (700, 784), (40, 5000)])
+def test_in_a_graph(rows, n):
+    """Captured with its gradient, and replayed with other inputs between eager calls."""
+    d = make(rows, n, BF16, F32, 11)
+    x, dy = d["x"].clone(), d["dy"].clone()
+    run = lambda: kb.layer_norm(x, d["w"], d["b"], residual=d["res"])
+    back = lambda o: kb.layer_norm_backward(o[1], o[2], o[3], d["w"], dy, dh=d["dh"])
+    back(run())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o = run()
+        g = back(o)
+    for turn in range(3):
+        e = make(rows, n, BF16, F32, 20 + turn)
+        x.copy_(e["x"])
+        dy.copy_(e["dy"])
+        torch.cuda.synchronize()
+        say(f"layer_norm graph rows={rows} n={n} replay {turn}")
+        graph.replay()
+        torch.cuda.synchronize()
+        o2 = run()
+        g2 = back(o2)
+        assert all(torch.equal(a, b) for a, b in zip(o, o2))
+        assert all(torch.equal(a, b) for a, b in zip(g, g2))

@@ -806,7 +806,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None,
     device = x.device
     mean = rstd = None
     if need_stats:
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
+        mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
         rstd = torch.empty_like(mean)
     check(_call(device, _library().kan_layer_norm, _dtype_code(x), pdt, rows, n, x.data_ptr(),
                 _ptr(residual), _ptr(weight), _ptr(bias), eps, _ptr(h), y.data_ptr(), _ptr(mean),
@@ -845,7 +845,7 @@ def layer_norm_backward(h, mean, rstd, weight, dy, dh=None, need_dx: bool = True
                 raise ValueError("dweight and dbias must be [n] with the weight's dtype")
     else:
         dx = torch.empty_like(h) if need_dx else None
-        dw = torch.empty((n,), dtype=dw_dtype, device=device) if need_dw else None
+        dw = h.new_empty((n,), dtype=dw_dtype) if need_dw else None
         db = torch.empty_like(dw) if need_dw else None
     lib, dt = _library(), _dtype_code(h)
     ws, nbytes = None, 0
@@ -854,7 +854,7 @@ def layer_norm_backward(h, mean, rstd, weight, dy, dh=None, need_dx: bool = True
         check(lib.kan_layer_norm_backward_workspace_bytes(dt, rows, n, ctypes.byref(size)))
         nbytes, ws = size.value, workspace
         if ws is None or ws.numel() < nbytes or ws.device != device:
-            ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+            ws = h.new_empty((max(nbytes, 1),), dtype=torch.uint8)
     check(_call(device, lib.kan_layer_norm_backward, dt, pdt, rows, n, h.data_ptr(),
                 mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dy.data_ptr(), _ptr(dh), _ptr(dx),
                 _ptr(dw), _ptr(db), _ptr(ws), nbytes, _stream(device)))
@@ -865,11 +865,14 @@ def _logits(z) -> Tuple[int, int, int]:
     """Checks logits [rows, classes]: (rows, classes, elements from row to row)."""
     if not z.is_cuda:
         raise ValueError("tensors must live on the GPU")
-    if z.dim() != 2 or z.shape[1] < 1:
+    shape = z.shape
+    if len(shape) != 2 or shape[1] < 1:
         raise ValueError("logits must be [rows, classes]")
-    rows, classes = z.shape
-    stride = z.stride(0) if rows > 1 else classes
-    if (classes > 1 and z.stride(1) != 1) or stride < classes:
+    rows, classes = shape
+    stride, inner = z.stride()
+    if rows <= 1:
+        stride = classes
+    if (classes > 1 and inner != 1) or stride < classes:
         raise ValueError("a row of logits must be contiguous, and rows must not overlap")
     return rows, classes, stride
 
@@ -877,14 +880,15 @@ def _logits(z) -> Tuple[int, int, int]:
 def _row_values(what: str, z, *ts) -> None:
     """fp32 values (or None), one per row of the logits."""
     torch = _torch()
+    rows, device, f32 = z.shape[0], z.device, torch.float32
     for t in ts:
-        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (z.shape[0],) or
-                              t.device != z.device or not t.is_contiguous()):
+        if t is not None and (t.dtype != f32 or t.dim() != 1 or t.shape[0] != rows or
+                              t.device != device or not t.is_contiguous()):
             raise ValueError(f"{what} must be fp32 [rows], contiguous, on the logits' device")
 
 
-def _check_targets(z, targets) -> None:
-    if targets.dtype != _torch().int64 or tuple(targets.shape) != (z.shape[0],) or \
+def _check_targets(z, rows: int, targets) -> None:
+    if targets.dtype != _torch().int64 or targets.dim() != 1 or targets.shape[0] != rows or \
             targets.device != z.device or not targets.is_contiguous():
         raise ValueError("targets must be int64 [rows], contiguous, on the logits' device")
 
@@ -898,20 +902,20 @@ def token_logprobs(logits, targets, top_k: int = 0, entropy: bool = False,
     when large enough, else a fresh one is taken."""
     torch = _torch()
     rows, classes, stride = _logits(logits)
-    _check_targets(logits, targets)
+    _check_targets(logits, rows, targets)
     dt, k, dev, lib = _dtype_code(logits), int(top_k), logits.device, _library()
     size = ctypes.c_size_t(0)
     check(lib.kan_token_logprobs_workspace_bytes(dt, rows, classes, k, ctypes.byref(size)))
-    logp = torch.empty((rows,), dtype=torch.float32, device=dev)
-    stats = torch.empty((rows, 2), dtype=torch.float32, device=dev)
+    logp = logits.new_empty((rows,), dtype=torch.float32)
+    stats = logp.new_empty((rows, 2))
     ent = torch.empty_like(logp) if entropy else None
-    top = torch.empty((rows, k), dtype=torch.float32, device=dev) if k else None
-    idx = torch.empty((rows, k), dtype=torch.int64, device=dev) if k else None
+    top = logp.new_empty((rows, k)) if k else None
+    idx = targets.new_empty((rows, k)) if k else None
     ws = None
     if size.value:
         ws = workspace
         if ws is None or ws.numel() < size.value or ws.device != dev:
-            ws = torch.empty(size.value, dtype=torch.uint8, device=dev)
+            ws = logits.new_empty((size.value,), dtype=torch.uint8)
     check(_call(dev, lib.kan_token_logprobs, dt, rows, classes, logits.data_ptr(), stride,
                 targets.data_ptr(), int(ignore_index), k, logp.data_ptr(), stats.data_ptr(),
                 _ptr(ent), _ptr(top), _ptr(idx), _ptr(ws), size.value, _stream(dev)))
@@ -926,22 +930,24 @@ def token_logprobs_backward(logits, targets, stats, dlogp, entropy=None, dentrop
     logits themselves: in place) receives the gradient instead of a fresh tensor."""
     torch = _torch()
     rows, classes, stride = _logits(logits)
-    _check_targets(logits, targets)
-    if stats.dtype != torch.float32 or tuple(stats.shape) != (rows, 2) or \
+    _check_targets(logits, rows, targets)
+    if stats.dtype != torch.float32 or stats.shape != (rows, 2) or \
             stats.device != logits.device or not stats.is_contiguous():
         raise ValueError("stats must be fp32 [rows, 2], contiguous, on the logits' device")
     _row_values("dlogp, entropy and dentropy", logits, dlogp, entropy, dentropy)
     if dlogp is None or (entropy is None) != (dentropy is None):
         raise ValueError("dlogp is needed, and entropy and dentropy go together")
     if out is None:
-        out = torch.empty((rows, classes), dtype=logits.dtype, device=logits.device)
-    _, _, ostride = _logits(out)
-    if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device:
-        raise ValueError("out must match the logits in shape, dtype and device")
-    check(_call(logits.device, _library().kan_token_logprobs_backward, _dtype_code(logits), rows,
+        out, ostride = logits.new_empty((rows, classes)), classes
+    else:
+        if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device:
+            raise ValueError("out must match the logits in shape, dtype and device")
+        _, _, ostride = _logits(out)
+    device = logits.device
+    check(_call(device, _library().kan_token_logprobs_backward, _dtype_code(logits), rows,
                 classes, logits.data_ptr(), stride, targets.data_ptr(), int(ignore_index),
                 stats.data_ptr(), dlogp.data_ptr(), _ptr(entropy), _ptr(dentropy), out.data_ptr(),
-                ostride, _stream(logits.device)))
+                ostride, _stream(device)))
     return out
 
 

@@ -95,9 +95,10 @@ struct Place {
 };
 
 // The variance from the mean square q around a rounded mean that is e off: q - e^2, which
-// takes away next to nothing (and never all but rounding: e is a rounding of the mean).
+// takes away next to nothing (and never all but rounding: e is a rounding of the mean).  A q
+// past fp32 stays infinite: rstd is 0.
 __device__ __forceinline__ float spread(float q, float e) {
-    return q - __builtin_fminf(e * e, q);
+    return q == __builtin_huge_valf() ? q : q - __builtin_fminf(e * e, q);
 }
 
 // (the instruction is good to one unit in the last place)
@@ -115,6 +116,7 @@ constexpr int kGradThreads = 64 * kMaxWaves;
 // C units per lane, of which the first FC are full in every lane.
 template <typename T, typename TP, int M, int C, int FC>
 __global__ void __launch_bounds__(kThreads<M>) norm_kernel(NormArgs a) {
+#pragma clang fp contract(off)  // (differences are from the rounded mean: exact near it)
     constexpr int V = kVec<T>;
     constexpr bool kSub = M == kShared;
     __shared__ float red[2][kMaxWaves][2];
@@ -177,8 +179,10 @@ __global__ void __launch_bounds__(kThreads<M>) norm_kernel(NormArgs a) {
             }
         });
         p.sum(q, e, red[1]);
-        // what the rounding of the sum left out of the mean
-        e *= inv_n;
+        // what the rounding of the sum left out of the mean (e / n, its rounding taken back once:
+        // it is all that y keeps of a constant row)
+        const float e0 = e * inv_n;
+        e = __builtin_fmaf(__builtin_fmaf(-e0, (float)n, e), inv_n, e0);
         const float rstd = inverse_root(spread(q * inv_n, e) + a.eps);
         if (a.mean != nullptr && live && p.slot == 0) {
             a.mean[row] = mu + e;
@@ -198,6 +202,7 @@ __global__ void __launch_bounds__(kThreads<M>) norm_kernel(NormArgs a) {
 // Rows that do not fit in registers: one workgroup per row, read three times.
 template <typename T, typename TP>
 __global__ void __launch_bounds__(512) norm_long_kernel(NormArgs a) {
+#pragma clang fp contract(off)
     __shared__ float red[2][kMaxWaves][2];
     const Place<kGroup> p(0, 8);
     const int n = a.n;

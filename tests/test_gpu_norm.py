@@ -299,3 +299,22 @@ def test_in_a_graph(rows, n):
         g2 = back(o2)
         assert all(torch.equal(a, b) for a, b in zip(o, o2))
         assert all(torch.equal(a, b) for a, b in zip(g, g2))
+
+
+@pytest.mark.parametrize("n", [10, 300, 900, 2050, 9000, 16500])
+def test_squares_past_fp32(n):
+    """Differences whose squares overflow: rstd 0 and y the bias, in that row alone; a constant
+    row of large values keeps the variance 0."""
+    d = make(3, n, F32, F32, n)
+    x = d["x"].clone()
+    x[1] *= 2.0 ** 100
+    x[2] = 3.0e6
+    say(f"layer_norm squares past fp32 n={n}")
+    y, _, mean, rstd = kb.layer_norm(x, d["w"], d["b"], 1e-5)
+    assert float(rstd[1]) == 0 and torch.equal(y[1], d["b"])
+    want, _, r64 = forward64(x.double(), d["w"].double(), d["b"].double(), 1e-5)
+    close(y[0], want[0], 1e-5)
+    close(y[2], d["b"].double(), 1e-5, 1.0)
+    # (the mean of equal values is off by a rounding at most, 0.25 here, squared and taken back
+    # to 2^-22 of it)
+    assert abs(float(rstd[2]) ** -2 - 1e-5) <= 2.0 ** -22 * 0.25 ** 2 + 1e-9

@@ -21,9 +21,9 @@
 // All sums and statistics are fp32; y, h and dx are rounded once, when stored (y from the
 // sum x + r before its rounding to h).
 //
-// Measured on MI355X: forward 65536 x 784 bf16 43.6 us (4.7 TB/s), 16384 x 8192 bf16 with the
+// Measured on MI355X: forward 65536 x 784 bf16 43.7 us (4.7 TB/s), 16384 x 8192 bf16 with the
 // residual 198 us (5.4 TB/s); gradient 16384 x 8192 bf16 with dh 216 us (5.0 TB/s), 30001 x 1001
-// bf16 with dh 51.5 us (4.7 TB/s), 16384 x 256 fp32 15.5 us (3.2 TB/s, both launches).  Loads
+// bf16 with dh 50.8 us (4.7 TB/s), 16384 x 256 fp32 15.5 us (3.2 TB/s, both launches).  Loads
 // of the next row ahead of time did not help (58.9 us against 52.3 for 30001 x 1001): the other
 // waves hide them, and the registers cost some of those.
 #include "kan_ops.h"

@@ -595,8 +595,9 @@ kan_status kan_token_logprobs_workspace_bytes(kan_dtype dtype, int64_t rows, int
  *                      themselves (same address and stride): in place.
  *
  * Masked classes (-infinity) get 0, and so does a row with no class left; a target outside
- * the classes that is not ignore_index makes its row's gradient NaN.  Otherwise overlap and
- * return codes as in kan_token_logprobs.
+ * the classes that is not ignore_index makes its row's gradient NaN, whatever the row holds, and
+ * so do a NaN or +infinity among the logits.  Otherwise overlap and return codes as in
+ * kan_token_logprobs.
  */
 kan_status kan_token_logprobs_backward(kan_dtype dtype, int64_t rows, int32_t classes,
                                        const void* logits, int64_t row_stride,

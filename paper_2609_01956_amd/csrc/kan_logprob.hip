@@ -433,7 +433,9 @@ __device__ __forceinline__ RowGrad row_grad(const LogprobGradArgs& a, int64_t ro
     const bool in = target >= 0 && target < a.classes;
     g.m = a.stats[2 * row];
     g.logs = a.stats[2 * row + 1];
-    g.empty = g.m == kNegInf;  // no class left: no gradient
+    // No class left (log s is -infinity too: the maximum passes over NaN, which log s shows): no
+    // gradient, but for an invalid target, whose NaN shows in any row.
+    g.empty = g.m == kNegInf && g.logs == kNegInf && (in || target == a.ignore);
     g.target = target != a.ignore && in && !g.empty ? (int)target : -1;
     g.d = target == a.ignore ? 0.0f : in ? a.dlogp[row] : __builtin_nanf("");
     g.dh = a.dentropy != nullptr ? a.dentropy[row] : 0.0f;

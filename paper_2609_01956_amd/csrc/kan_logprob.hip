@@ -539,7 +539,7 @@ hipError_t run_logprob(const LogprobPlan& p, const LogprobArgs& a, hipStream_t s
         logprob_short_kernel<T><<<grid_of((a.rows + per - 1) / per, 8192), 256, 0, s>>>(a);
         return hipGetLastError();
     }
-    const int grid = grid_of((a.rows * p.parts + 3) / 4, 1 << 30);
+    const int grid = logprob_groups(a.rows * p.parts);
     const bool ent = a.entropy != nullptr, top = a.k > 0;
     using std::false_type;
     using std::integral_constant;
@@ -576,33 +576,17 @@ hipError_t run_logprob_grad(LogprobGradArgs a, hipStream_t s) {
     const int elems = tile_elems(a.classes);
     const bool past = a.rows * a.classes * (int64_t)sizeof(T) >= kPastCaches;
     a.tiles = (a.classes + 64 * elems - 1) / (64 * elems);
-    // (items are counted in 32 bits: rows in pieces, one but for 2^30 and more tiles)
-    const int64_t most = (1 << 30) / a.tiles;
-    for (int64_t rows = a.rows; rows > 0; rows -= most) {
-        const int64_t now = rows < most ? rows : most;
-        a.items = (uint32_t)(now * a.tiles);
-        const int grid = (int)((a.items + 3) / 4);
+    return logprob_grad_pieces(a, sizeof(T), [&](const LogprobGradArgs& piece, int grid) {
         auto go = [&](auto e) {
             constexpr int E = decltype(e)::value;
-            if (past) logprob_grad_kernel<T, E, true><<<grid, 256, 0, s>>>(a);
-            else logprob_grad_kernel<T, E, false><<<grid, 256, 0, s>>>(a);
+            if (past) logprob_grad_kernel<T, E, true><<<grid, 256, 0, s>>>(piece);
+            else logprob_grad_kernel<T, E, false><<<grid, 256, 0, s>>>(piece);
         };
         if (elems == 8) go(std::integral_constant<int, 8>{});
         else if (elems == 16) go(std::integral_constant<int, 16>{});
         else go(std::integral_constant<int, 32>{});
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        a.z = static_cast<const T*>(a.z) + now * a.stride;
-        a.dz = static_cast<T*>(a.dz) + now * a.dstride;
-        a.targets += now;
-        a.stats += 2 * now;
-        a.dlogp += now;
-        if (a.dentropy != nullptr) {
-            a.entropy += now;
-            a.dentropy += now;
-        }
-    }
-    return hipSuccess;
+        return hipGetLastError();
+    });
 }
 
 }  // namespace

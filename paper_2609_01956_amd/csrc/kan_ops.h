@@ -8,6 +8,9 @@
 
 namespace kan {
 
+// Most workgroups of 256 lanes in a launch: a grid holds fewer than 2^32 work-items.
+constexpr int64_t kMaxGroups = (INT64_C(1) << 24) - 1;
+
 // ---------------------------------------------------------------- layer norm
 
 struct NormArgs {
@@ -74,6 +77,34 @@ struct LogprobGradArgs {
     uint32_t items;  // (row, tile)
     uint32_t tiles;  // per row
 };
+// Workgroups of the tiled forward: four items each at a time, as many turns as it takes.
+inline int logprob_groups(int64_t items) {
+    const int64_t groups = (items + 3) / 4;
+    return (int)(groups < kMaxGroups ? groups : kMaxGroups);
+}
+// The tiled gradient's rows in pieces of one launch each, four tiles per workgroup: launch(args
+// of a piece, its workgroups) until one fails.  es: bytes per logit.
+template <typename F>
+hipError_t logprob_grad_pieces(LogprobGradArgs a, size_t es, F&& launch) {
+    const int64_t all = a.rows, most = 4 * kMaxGroups / a.tiles;
+    for (int64_t done = 0; done < all;) {
+        a.rows = all - done < most ? all - done : most;
+        a.items = (uint32_t)(a.rows * a.tiles);
+        const hipError_t e = launch(static_cast<const LogprobGradArgs&>(a), (int)((a.items + 3) / 4));
+        if (e != hipSuccess) return e;
+        a.z = static_cast<const char*>(a.z) + a.rows * a.stride * (int64_t)es;
+        a.dz = static_cast<char*>(a.dz) + a.rows * a.dstride * (int64_t)es;
+        a.targets += a.rows;
+        a.stats += 2 * a.rows;
+        a.dlogp += a.rows;
+        if (a.dentropy != nullptr) {
+            a.entropy += a.rows;
+            a.dentropy += a.rows;
+        }
+        done += a.rows;
+    }
+    return hipSuccess;
+}
 constexpr int kMaxTop = 64;
 struct LogprobPlan {
     int elems;  // of a tile, per lane; 0: rows that share a wave

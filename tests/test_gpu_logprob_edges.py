@@ -1,4 +1,5 @@
-"""Log probabilities and their gradient at the edges of what a row can hold."""
+"""Log probabilities and their gradient at the edges of what a row can hold, and of how many rows
+there are."""
 import math
 
 import pytest
@@ -42,3 +43,27 @@ def test_gradient_of_rows_without_numbers_or_classes(dt, classes, rows):
         for r in (2, 4):
             assert not bool(dz[r].any()), r
         assert bool(torch.isfinite(dz[6:]).all()) and bool(dz[6].any())
+
+
+def test_more_rows_than_a_launch():
+    """2^26 rows and some: 257 classes of bf16; the last 1000, on both sides of a launch's
+    4 (2^24 - 1) tiles, as in a call of their own, forward and (in place) backward."""
+    rows, classes = (1 << 26) + 301, 257
+    g = torch.Generator(device=device())
+    g.manual_seed(1)
+    small = torch.randn(1000, classes, device=device(), generator=g).to(BF16)
+    ts = torch.randint(0, classes, (1000,), device=device(), generator=g)
+    say("token_logprobs more rows than a launch")
+    z = torch.zeros(rows, classes, dtype=BF16, device=device())
+    z[-1000:] = small
+    t = torch.zeros(rows, dtype=torch.int64, device=device())
+    t[-1000:] = ts
+    logp, stats, ent, _, _ = kb.token_logprobs(z, t, entropy=True)
+    want = kb.token_logprobs(small, ts, entropy=True)
+    assert torch.equal(logp[-1000:], want[0]) and torch.equal(stats[-1000:], want[1])
+    assert torch.equal(ent[-1000:], want[2]) and bool((logp[:-1000] == logp[0]).all())
+    d = torch.linspace(-1, 1, rows, device=device())
+    kb.token_logprobs_backward(z, t, stats, d, entropy=ent, dentropy=d, out=z)
+    dz = kb.token_logprobs_backward(small, ts, want[1], d[-1000:].clone(), entropy=want[2],
+                                    dentropy=d[-1000:].clone())
+    assert torch.equal(z[-1000:], dz)

@@ -487,8 +487,10 @@ kan_status kan_layer_forward_noalloc(const kan_grid* grid, kan_dtype dtype, int6
  *
  * Statistics and arithmetic are binary32: the mean corrected by the mean difference from
  * it, the variance from squared differences; in bf16 y comes from the sum before its
- * rounding to h.  A NaN or infinity in a row gives NaN in that row's y alone.  With eps = 0
- * a constant row gives NaN; a row whose squared differences leave binary32 has rstd 0.
+ * rounding to h.  A NaN or infinity in a row gives NaN in that row's y alone, and so does a
+ * sum of a row that leaves binary32.  With eps = 0 a row whose squared differences are all
+ * below 2^-150 has rstd infinite and no finite y (NaN where it is constant; below 2^-126 the
+ * squares lose bits); a row whose squared differences leave binary32 has rstd 0.
  *
  * Outputs must not overlap each other or an input.  Returns KAN_OK, KAN_ERR_INVALID_ARG
  * (rows < 0, n < 1, n > 2^24, rows * n > 2^48, eps negative or not finite, NULL,

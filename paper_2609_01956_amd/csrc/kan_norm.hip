@@ -101,8 +101,9 @@ __device__ __forceinline__ float spread(float q, float e) {
     return q == __builtin_huge_valf() ? q : q - __builtin_fminf(e * e, q);
 }
 
-// (the instruction is good to one unit in the last place)
-__device__ __forceinline__ float inverse_root(float v) { return __builtin_amdgcn_rsqf(v); }
+// (one unit in the last place; the bare instruction takes a subnormal v, as rows of little
+// spread have without eps, for 0)
+__device__ __forceinline__ float inverse_root(float v) { return rsqrtf(v); }
 
 template <int N>
 __device__ __forceinline__ void clear_units(u32x4 (&raw)[N]) {

@@ -631,7 +631,8 @@ kan_status kan_token_logprobs_backward(kan_dtype dtype, int64_t rows, int32_t cl
  * The host arrays are read before the call returns and not kept.  Squares are summed in
  * binary64 in a fixed order (deterministic; no overflow, no underflow).  With c = 1 a tensor
  * scaled in place is not written.  A NaN gradient makes norm and every scaled gradient NaN;
- * an infinite one makes norm infinite, c 0 and its own product NaN: test norm first.
+ * an infinite one makes norm infinite, c 0 and its own product NaN: test norm first (with
+ * max_norm infinite c is 1 then too).
  *
  * Returns KAN_OK, KAN_ERR_INVALID_ARG, KAN_ERR_UNSUPPORTED (unknown dtype) or
  * KAN_ERR_DEVICE.

@@ -145,9 +145,10 @@ __global__ void __launch_bounds__(256) clip_scale_kernel(ClipArgs<N> a, ClipOuts
     const Finder<N> finder(a);
     const double n = norm_of(part, parts);
     if (blockIdx.x == 0 && threadIdx.x == 0) *b.norm = (float)n;
-    // (gradients that are all 0 stay as they are; a NaN among them reaches all)
-    const double ratio = n == 0.0 ? 1.0 : (double)b.max_norm / (n + (double)b.eps);
-    const double f = ratio >= 1.0 ? 1.0 : ratio;
+    // (gradients that are all 0 stay as they are, and all do without a bound, whose ratio to an
+    // infinite norm is NaN; a NaN among them reaches all)
+    const double bound = b.max_norm, above = n + (double)b.eps;
+    const double f = n == 0.0 || bound >= above ? 1.0 : bound / above;
     for (int i = a.chunks - 1 - (int)blockIdx.x; i >= 0; i -= gridDim.x) {
         const Chunk c = finder.find(a, i);
         void* out = OUT ? o.out[c.tensor] : const_cast<void*>(a.in[c.tensor]);

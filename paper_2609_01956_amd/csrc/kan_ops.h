@@ -148,7 +148,7 @@ struct ClipList {
     const int32_t* dtypes;  // kan_dtype
     bool bf16(int64_t t) const { return dtypes[t] == 1; }
 };
-// Most tensors and elements of a call (the check for overlaps sorts on the stack, chunks
+// Most tensors and elements of a call (the check for overlaps numbers tensors in 16 bits, chunks
 // are counted in 32 bits).
 constexpr int kClipMaxTensors = 1 << 14;
 constexpr int64_t kClipMaxElements = INT64_C(1) << 40;

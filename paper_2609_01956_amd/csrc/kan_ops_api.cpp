@@ -3,11 +3,11 @@
 // only, before any HIP call), launch planning and dispatch onto the caller's stream.
 #include "kan.h"
 
-#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <initializer_list>
 
+#include "kan_clip_lists.h"
 #include "kan_ops.h"
 
 namespace {
@@ -103,35 +103,6 @@ kan_status check_clip(const kan::ClipList& l, const void* workspace, size_t work
             return KAN_ERR_INVALID_ARG;
     }
     return KAN_OK;
-}
-
-// Does any output overlap another output, or an input that is not its own in place?
-bool clip_outputs_clash(const kan::ClipList& l) {
-    // Item 2 t: output t (also its input, in place); 2 t + 1: input t, where it is another.
-    static_assert(kan::kClipMaxTensors <= 1 << 14, "128 KB of stack");
-    uint32_t items[2 * kan::kClipMaxTensors];
-    size_t count = 0;
-    auto start = [&](uint32_t i) {
-        return reinterpret_cast<uintptr_t>(i & 1 ? l.in[i >> 1] : l.out[i >> 1]);
-    };
-    auto end = [&](uint32_t i) {
-        return start(i) + (size_t)l.sizes[i >> 1] * (l.bf16(i >> 1) ? 2 : 4);
-    };
-    for (int64_t t = 0; t < l.count; ++t) {
-        if (l.sizes[t] == 0) continue;
-        items[count++] = (uint32_t)(2 * t);
-        if (l.in[t] != l.out[t]) items[count++] = (uint32_t)(2 * t + 1);
-    }
-    auto before = [&](uint32_t a, uint32_t b) { return start(a) < start(b); };
-    if (!std::is_sorted(items, items + count, before)) std::sort(items, items + count, before);
-    uintptr_t outs = 0, all = 0;  // ends of what starts earlier: outputs, anything
-    for (size_t k = 0; k < count; ++k) {
-        const uint32_t i = items[k];
-        if (start(i) < (i & 1 ? outs : all)) return true;
-        all = std::max(all, end(i));
-        if (!(i & 1)) outs = std::max(outs, end(i));
-    }
-    return false;
 }
 
 size_t norm_part_bytes(const kan::NormPlan& p, int32_t n) {
@@ -314,7 +285,7 @@ kan_status kan_clip_grad_norm(int32_t count, const void* const* grads, const int
     const kan::ClipList l = {count, grads, count > 0 ? out : &none, sizes, dtypes};
     const kan_status st = check_clip(l, workspace, workspace_bytes, norm);
     if (st != KAN_OK) return st;
-    if (clip_outputs_clash(l)) return KAN_ERR_INVALID_ARG;
+    if (kan::clip_outputs_clash(l)) return KAN_ERR_INVALID_ARG;
     return device_status(kan::launch_clip(l, {max_norm, eps, norm}, workspace,
                                           static_cast<hipStream_t>(stream)));
 }

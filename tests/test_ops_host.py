@@ -2,6 +2,7 @@
 import os
 import shutil
 import subprocess
+import sys
 
 import pytest
 
@@ -70,3 +71,102 @@ def test_rows_past_one_launch(tmp_path):
             done += n
             launches += 1
         assert done == rows and launches == -(-rows // (most // tiles))
+
+
+CLASH = r"""
+#include "kan_clip_lists.h"
+#include <cstdio>
+#include <random>
+#include <vector>
+int main() {
+    std::mt19937 rng(7);
+    auto draw = [&](int n) { return (int)(rng() %% n); };
+    int yes = 0, no = 0;
+    for (int round = 0; round < 3000; ++round) {
+        const int count = round %% 100 == 0 ? 900 + draw(1400) : 1 + draw(40);
+        std::vector<const void*> in(count);
+        std::vector<void*> out(count);
+        std::vector<int64_t> sizes(count);
+        std::vector<int32_t> dtypes(count);
+        // pieces of one buffer, side by side, in any order
+        std::vector<uintptr_t> at(2 * count);
+        uintptr_t p = 4096;
+        std::vector<int> order(count);
+        for (int t = 0; t < count; ++t) {
+            order[t] = t;
+            sizes[t] = draw(8) == 0 ? 0 : 1 + draw(60);
+            dtypes[t] = draw(2);
+        }
+        if (round %% 3) std::shuffle(order.begin(), order.end(), rng);
+        for (int k = 0; k < count; ++k) {
+            const int t = order[k];
+            const uintptr_t n = sizes[t] * (dtypes[t] ? 2 : 4);
+            in[t] = (const void*)p;
+            p += n;
+            out[t] = draw(3) ? (void*)in[t] : (void*)p;
+            if (out[t] != in[t]) p += n;
+        }
+        // sometimes a clash: an output or an input moved by a few bytes, or onto another
+        const int t = draw(count), u = draw(count);
+        switch (draw(6)) {
+            case 0: out[t] = (char*)out[t] + 4 * (1 + draw(3)); break;
+            case 1: out[t] = out[u]; break;
+            case 2: out[t] = (void*)in[u]; break;
+            case 3: in[t] = in[u]; break;
+            default: break;
+        }
+        const kan::ClipList l = {count, in.data(), out.data(), sizes.data(), dtypes.data()};
+        bool want = false;
+        for (int a = 0; a < count && !want; ++a)
+            for (int b = 0; b < count && !want; ++b) {
+                const int64_t na = sizes[a] * (dtypes[a] ? 2 : 4), nb = sizes[b] * (dtypes[b] ? 2 : 4);
+                if (na == 0 || nb == 0) continue;
+                auto over = [&](const void* x, const void* y) {
+                    return (uintptr_t)x < (uintptr_t)y + nb && (uintptr_t)y < (uintptr_t)x + na;
+                };
+                if (a != b && over(out[a], out[b])) want = true;
+                if (over(out[a], in[b]) && !(a == b && in[a] == out[a])) want = true;
+            }
+        if (kan::clip_outputs_clash(l) != want || kan::clip_outputs_clash<16>(l) != want ||
+            kan::clip_outputs_clash<500>(l) != want) {
+            printf("wrong: round %%d count %%d want %%d\n", round, count, (int)want);
+            return 0;
+        }
+        (want ? yes : no) += 1;
+    }
+    printf("%%d %%d\n", yes, no);
+}
+"""
+
+
+def test_overlaps_of_tensor_lists(tmp_path):
+    """Lists of up to 2300 tensors, in order and shuffled, with and without a clash of each kind
+    (outputs with outputs, outputs with other tensors' inputs, a partial one with its own),
+    in one block of outputs and in several, against a comparison of all pairs."""
+    line, = run_host(tmp_path, CLASH % ())
+    yes, no = map(int, line.split())
+    assert yes > 500 and no > 500
+
+
+STACK = r"""
+import sys, threading
+from paper_2609_01956_amd import binding as kb
+kb.load_library()
+count, got = int(sys.argv[1]), []
+need = kb.kan_grad_norm_workspace_bytes(count)[1]
+g = [(1 << 36) + 64 * (i * 1237 % count) for i in range(count)]
+o = [a + (1 << 36) for a in g]
+o[-1] = o[0] + 4
+args = (g, [16] * count, [kb.KAN_F32] * count, 1.0, 1e-6, o, 1 << 40, need, 1 << 41)
+threading.stack_size(128 << 10)
+t = threading.Thread(target=lambda: got.append(kb.kan_clip_grad_norm(*args)))
+t.start()
+t.join()
+assert got == [kb.KAN_ERR_INVALID_ARG], got
+"""
+
+
+@pytest.mark.parametrize("count", [2, 12, 16384])
+def test_a_small_stack_is_enough(count):
+    """A call from a thread of 128 KB (refused on the host for an overlap, the last check)."""
+    subprocess.run([sys.executable, "-c", STACK, str(count)], check=True, cwd=ROOT)

@@ -45,6 +45,22 @@ def test_gradient_of_rows_without_numbers_or_classes(dt, classes, rows):
         assert bool(torch.isfinite(dz[6:]).all()) and bool(dz[6].any())
 
 
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("classes", [20, 900, 5000])
+def test_gradient_of_improbable_classes(dt, classes):
+    """p = exp(z - m - log s) down to exp(-85): with m = log s = 0 the exponent is exact, so what
+    is left is the exponential: an instruction good to a unit in the last place (2^-23), its
+    argument's rounding taken back, and one rounding more: 2^-22 (bf16: the result's rounding)."""
+    z = (-85 * torch.rand(3, classes, device=device())).to(dt)
+    t = torch.zeros(3, dtype=torch.int64, device=device())
+    stats = torch.zeros(3, 2, device=device())
+    d = torch.full((3,), -1.0, device=device())
+    say(f"token_logprobs_backward improbable classes {dt} classes={classes}")
+    dz = kb.token_logprobs_backward(z, t, stats, d)[:, 1:].double()
+    want = torch.exp(z.double())[:, 1:]
+    assert bool(((dz - want).abs() <= (2.0 ** -22 if dt == F32 else 2.0 ** -8) * want).all())
+
+
 def test_more_rows_than_a_launch():
     """2^26 rows and some: 257 classes of bf16; the last 1000, on both sides of a launch's
     4 (2^24 - 1) tiles, as in a call of their own, forward and (in place) backward."""

@@ -596,10 +596,10 @@ kan_status kan_token_logprobs_workspace_bytes(kan_dtype dtype, int64_t rows, int
  *                      apart (what lies between is not written).  May be the logits
  *                      themselves (same address and stride): in place.
  *
- * Masked classes (-infinity) get 0, and so does a row with no class left; a target outside
- * the classes that is not ignore_index makes its row's gradient NaN, whatever the row holds, and
- * so do a NaN or +infinity among the logits.  Otherwise overlap and return codes as in
- * kan_token_logprobs.
+ * Masked classes (-infinity) get 0 (a masked target, whose logp is -infinity, its dlogp, as the
+ * formula says), and so does a row with no class left.  A target outside the classes that is not
+ * ignore_index makes its row's gradient NaN, whatever the row holds, and so do a NaN or +infinity
+ * among the logits.  Otherwise overlap and return codes as in kan_token_logprobs.
  */
 kan_status kan_token_logprobs_backward(kan_dtype dtype, int64_t rows, int32_t classes,
                                        const void* logits, int64_t row_stride,

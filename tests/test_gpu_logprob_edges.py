@@ -83,3 +83,28 @@ def test_more_rows_than_a_launch():
     dz = kb.token_logprobs_backward(small, ts, want[1], d[-1000:].clone(), entropy=want[2],
                                     dentropy=d[-1000:].clone())
     assert torch.equal(z[-1000:], dz)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("classes", [10, 300, 5000])
+def test_gradient_of_a_masked_target(dt, classes):
+    """Masked classes have no gradient but the target itself, which keeps the formula's dlogp
+    ([v = target] - 0); the others share -dlogp p.  Sums over them to 1e-5, as elsewhere (bf16: a
+    rounding of each, 2^-8 of the total at most)."""
+    g = torch.Generator(device=device())
+    g.manual_seed(classes)
+    z = torch.randn(4, classes, device=device(), generator=g).to(dt)
+    t = torch.full((4,), classes // 2, device=device())
+    z[:, ::2] = -math.inf
+    z[:, classes // 2] = -math.inf
+    say(f"token_logprobs_backward masked target {dt} classes={classes}")
+    logp, stats, _, _, _ = kb.token_logprobs(z, t)
+    d = torch.tensor([1.0, -0.5, 2.0, -1.0], device=device())
+    dz = kb.token_logprobs_backward(z, t, stats, d).double()
+    assert bool((logp == -math.inf).all())
+    assert torch.equal(dz[:, classes // 2], d.double())
+    masked = torch.isinf(z)
+    masked[:, classes // 2] = False
+    assert not bool(dz[masked].any())
+    rest = dz.sum(1) - d.double()
+    assert bool(((rest + d.double()).abs() <= (1e-5 if dt == F32 else 2.0 ** -8) * d.abs()).all())

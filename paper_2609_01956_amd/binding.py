@@ -505,6 +505,13 @@ def _library() -> ctypes.CDLL:
     return _lib if _lib is not None else load_library()
 
 
+def _fits(workspace, nbytes: int, device) -> bool:
+    """Can a caller's workspace (or None) be used: nbytes side by side on the device (an expanded
+    or strided tensor counts elements that it does not hold)."""
+    return workspace is not None and workspace.device == device and \
+        workspace.numel() >= nbytes and workspace.is_contiguous()
+
+
 def _query(fn, grid, *args) -> int:
     """A size query's bytes."""
     n = ctypes.c_size_t(0)
@@ -623,7 +630,7 @@ def layer_forward_packed(x, packed: PackedLayer, out=None, shape=None, workspace
             need = _query(lib.kan_layer_forward_packed_workspace_bytes, g, dt, B, packed.n_in,
                           packed.n_out, shape)
         if need > 0:
-            if workspace is None or workspace.numel() < need or workspace.device != x.device:
+            if not _fits(workspace, need, x.device):
                 workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
             ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
     check(_call(x.device, lib.kan_layer_forward_packed, ctypes.byref(g), dt, B, packed.n_in,
@@ -699,7 +706,7 @@ def layer_backward(x, coef, base_w, dy, grid_size: int, grid_lo: float = -1.0,
     g = make_grid(grid_size, grid_lo, grid_hi)
     lib = _library()
     nbytes = _query(lib.kan_layer_backward_workspace_bytes, g, dt, B, n_in, n_out)
-    if workspace is None or workspace.numel() < nbytes or workspace.device != x.device:
+    if not _fits(workspace, nbytes, x.device):
         workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=x.device)
     if out is not None:
         dx, dC, dW = out
@@ -735,7 +742,7 @@ def layer_forward_span(x, coef, base_w, grid_size: int, grid_lo: float = -1.0,
     g = make_grid(grid_size, grid_lo, grid_hi, spline_order)
     lib = _library()
     nbytes = _query(lib.kan_layer_forward_span_workspace_bytes, g, dt, B, n_in, n_out)
-    if workspace is None or workspace.numel() < nbytes or workspace.device != x.device:
+    if not _fits(workspace, nbytes, x.device):
         workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=x.device)
     if out is None:
         out = torch.empty((B, n_out), dtype=x.dtype, device=x.device)
@@ -853,7 +860,7 @@ def layer_norm_backward(h, mean, rstd, weight, dy, dh=None, need_dx: bool = True
         size = ctypes.c_size_t(0)
         check(lib.kan_layer_norm_backward_workspace_bytes(dt, rows, n, ctypes.byref(size)))
         nbytes, ws = size.value, workspace
-        if ws is None or ws.numel() < nbytes or ws.device != device:
+        if not _fits(ws, nbytes, device):
             ws = h.new_empty((max(nbytes, 1),), dtype=torch.uint8)
     check(_call(device, lib.kan_layer_norm_backward, dt, pdt, rows, n, h.data_ptr(),
                 mean.data_ptr(), rstd.data_ptr(), _ptr(weight), dy.data_ptr(), _ptr(dh), _ptr(dx),
@@ -914,7 +921,7 @@ def token_logprobs(logits, targets, top_k: int = 0, entropy: bool = False,
     ws = None
     if size.value:
         ws = workspace
-        if ws is None or ws.numel() < size.value or ws.device != dev:
+        if not _fits(ws, size.value, dev):
             ws = logits.new_empty((size.value,), dtype=torch.uint8)
     check(_call(dev, lib.kan_token_logprobs, dt, rows, classes, logits.data_ptr(), stride,
                 targets.data_ptr(), int(ignore_index), k, logp.data_ptr(), stats.data_ptr(),
@@ -975,7 +982,7 @@ def _norm_buffers(count: int, device, workspace):
     torch = _torch()
     size = ctypes.c_size_t(0)
     check(_library().kan_grad_norm_workspace_bytes(count, ctypes.byref(size)))
-    if workspace is None or workspace.numel() < size.value or workspace.device != device:
+    if not _fits(workspace, size.value, device):
         workspace = torch.empty(size.value, dtype=torch.uint8, device=device)
     return torch.empty((), dtype=torch.float32, device=device), workspace
 

@@ -746,6 +746,9 @@ def layer_forward_span(x, coef, base_w, grid_size: int, grid_lo: float = -1.0,
         workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=x.device)
     if out is None:
         out = torch.empty((B, n_out), dtype=x.dtype, device=x.device)
+    elif out.dtype != x.dtype or tuple(out.shape) != (B, n_out):
+        raise ValueError("out must be [B, out] with x's dtype")
+    _require_device(x, coef, out)
     check(_call(x.device, lib.kan_layer_forward_span, ctypes.byref(g), dt, B, n_in, n_out,
                 x.data_ptr(), coef.data_ptr(), base_w.data_ptr(), workspace.data_ptr(),
                 workspace.numel(), out.data_ptr(), _stream(x.device)))

@@ -35,3 +35,14 @@ def test_expanded_workspaces_are_left_alone():
         for a, b in zip(call(), call(workspace=ws)):
             assert torch.equal(a, b), name
         assert bool((buf == 77).all()), name
+
+
+def test_span_forward_refuses_outputs_that_do_not_fit():
+    x, coef, base = (torch.zeros(*s, device=device()) for s in ((40, 24), (12, 24, 8), (12, 24)))
+    out = torch.zeros(40, 12, device=device())
+    say("layer_forward_span outputs")
+    assert kb.layer_forward_span(x, coef, base, 5, out=out) is out
+    for bad in (out[:20], out.t(), out.to(torch.bfloat16), out.cpu(),
+                torch.zeros(80, 12, device=device())[::2]):
+        with pytest.raises(ValueError):
+            kb.layer_forward_span(x, coef, base, 5, out=bad)

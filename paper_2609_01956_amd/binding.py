@@ -839,7 +839,8 @@ def layer_norm_backward(h, mean, rstd, weight, dy, dh=None, need_dx: bool = True
     _same("h, dy and dh", h, dy, dh)
     device, f32, lead = h.device, torch.float32, h.shape[:-1]
     for t in (mean, rstd):
-        if t.dtype != f32 or t.shape != lead or t.device != device or not t.is_contiguous():
+        if t is None or t.dtype != f32 or t.shape != lead or t.device != device or \
+                not t.is_contiguous():
             raise ValueError("mean and rstd are fp32, one value per row, on the rows' device")
     if not (need_dx or need_dw):
         raise ValueError("nothing to compute")
@@ -941,7 +942,7 @@ def token_logprobs_backward(logits, targets, stats, dlogp, entropy=None, dentrop
     torch = _torch()
     rows, classes, stride = _logits(logits)
     _check_targets(logits, rows, targets)
-    if stats.dtype != torch.float32 or stats.shape != (rows, 2) or \
+    if stats is None or stats.dtype != torch.float32 or stats.shape != (rows, 2) or \
             stats.device != logits.device or not stats.is_contiguous():
         raise ValueError("stats must be fp32 [rows, 2], contiguous, on the logits' device")
     _row_values("dlogp, entropy and dentropy", logits, dlogp, entropy, dentropy)

@@ -46,3 +46,16 @@ def test_span_forward_refuses_outputs_that_do_not_fit():
                 torch.zeros(80, 12, device=device())[::2]):
         with pytest.raises(ValueError):
             kb.layer_forward_span(x, coef, base, 5, out=bad)
+
+
+def test_gradients_refuse_missing_statistics():
+    """A forward without statistics (need_stats=False) returns None for them."""
+    x = torch.randn(4, 16, device=device())
+    _, _, mean, rstd = kb.layer_norm(x)
+    t = torch.zeros(4, dtype=torch.int64, device=device())
+    for f in (lambda: kb.layer_norm_backward(x, None, None, None, x),
+              lambda: kb.layer_norm_backward(x, mean, None, None, x),
+              lambda: kb.layer_norm_backward(x, None, rstd, None, x),
+              lambda: kb.token_logprobs_backward(x, t, None, mean)):
+        with pytest.raises(ValueError):
+            f()

@@ -50,8 +50,9 @@ constexpr float kNegInf = -__builtin_huge_valf();
 __device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
 
 // The gradient's, whose every p is an output: to 2^-22 of the value (t above -1e5).  What the
-// rounding of t log2 e and of the constant left out, t - h ln 2, is taken back as a factor; hidden
-// behind the memory (4096 x 131072 bf16 363 -> 349 us, 65536 x 1000 bf16 49.4 -> 51.4).
+// rounding of t log2 e and of the constant left out, t - h ln 2, is taken back as a factor; mostly
+// hidden behind the memory (against the short form, bf16: 4096 x 131072 361 us both, 20000 x 4000
+// 60.0 -> 60.8, and where the gradient stays in the caches 65536 x 1000 49.2 -> 50.3).
 __device__ __forceinline__ float exp_exact(float t) {
     const float h = t * kLog2e, e = __builtin_amdgcn_exp2f(h);
     return __builtin_fmaf(e, __builtin_fmaf(-h, kLn2Low, __builtin_fmaf(-h, kLn2, t)), e);
@@ -440,20 +441,20 @@ __global__ void __launch_bounds__(64) logprob_join_kernel(LogprobArgs a) {
 struct RowGrad {
     float m, logs, d, dh, h;
     int target;  // -1: none
-    bool empty;
 };
 
 __device__ __forceinline__ RowGrad row_grad(const LogprobGradArgs& a, int64_t row) {
-    RowGrad g;
     const int64_t target = a.targets[row];
-    const bool in = target >= 0 && target < a.classes;
+    const bool in = target >= 0 && target < a.classes, ignored = target == a.ignore;
+    RowGrad g;
     g.m = a.stats[2 * row];
     g.logs = a.stats[2 * row + 1];
     // No class left (log s is -infinity too: the maximum passes over NaN, which log s shows): no
-    // gradient, but for an invalid target, whose NaN shows in any row.
-    g.empty = g.m == kNegInf && g.logs == kNegInf && (in || target == a.ignore);
-    g.target = target != a.ignore && in && !g.empty ? (int)target : -1;
-    g.d = target == a.ignore ? 0.0f : in ? a.dlogp[row] : __builtin_nanf("");
+    // gradient, but for an invalid target, whose NaN shows in any row.  Its logits are -infinity,
+    // so p and all it is multiplied by are 0.
+    if (g.m == kNegInf && g.logs == kNegInf && (in || ignored)) return {0, 0, 0, 0, 0, -1};
+    g.target = in && !ignored ? (int)target : -1;
+    g.d = ignored ? 0.0f : in ? a.dlogp[row] : __builtin_nanf("");
     g.dh = a.dentropy != nullptr ? a.dentropy[row] : 0.0f;
     g.h = a.dentropy != nullptr ? a.entropy[row] : 0.0f;
     return g;
@@ -467,9 +468,8 @@ __device__ __forceinline__ void unit_grad(const RowGrad& g, int col, float (&v)[
         const float at = v[i] - g.m - g.logs;
         // (below -1e4 the weight is 0, and the entropy's term with it; NaN stays)
         const float lp = at < -1e4f ? -1e4f : at;
-        const float p = g.empty ? 0.0f : exp_exact(lp);
         const float slope = __builtin_fmaf(g.dh, lp + g.h, g.d);
-        v[i] = (g.target == col + i ? g.d : 0.0f) - (g.empty ? 0.0f : p * slope);
+        v[i] = (g.target == col + i ? g.d : 0.0f) - exp_exact(lp) * slope;
     }
 }
 

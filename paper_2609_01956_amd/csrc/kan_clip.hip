@@ -8,9 +8,9 @@
 // gradient's square is exact.  Each workgroup sums its own chunks into one partial, and each
 // workgroup of the second launch adds all partials in the same fixed order (at most
 // kClipGroups and one per launch: 2 us from the caches, less than a launch between them) before
-// it scales, each product rounded once.  It goes through the chunks from the last to the
-// first, as the last ones read are still in the Infinity Cache.  In place with c = 1 it
-// returns without touching the gradients.
+// it scales, each product rounded to fp32 (and from there to bf16).  It goes through the chunks
+// from the last to the first, as the last ones read are still in the Infinity Cache.  In place
+// with c = 1 it returns without touching the gradients.
 //
 // The tensors go by value, as many per launch as a kernel's 4 KB of arguments hold: no table
 // is copied to the device or kept.  A tensor is cut into chunks of kClipChunk elements,
@@ -18,8 +18,8 @@
 // tensor by a count over its lanes.
 //
 // Measured on MI355X: 235 M bf16 gradients in 64 tensors into other tensors 243-251 us (the two
-// reads and the write at 5.6-5.8 TB/s), the norm of 224 M bf16 in place and within the bound
-// 87 us (5.2 TB/s), 64 x 2^20 fp32 135 us.
+// reads and the write at 5.6-5.8 TB/s) and 254 in place, within the bound 95 us (4.9 TB/s); 64 x
+// 2^20 fp32 into other tensors 135 us, in place 160, within the bound 57.
 #include "kan_ops.h"
 #include "kan_rows.h"
 

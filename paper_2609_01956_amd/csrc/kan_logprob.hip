@@ -26,10 +26,13 @@
 // first tile) are sorted across the lanes and merged, few are inserted one after the
 // other; those lanes' next largest are compared again, until none reaches the k-th best.
 //
-// Measured on MI355X: 2001 x 50001 bf16 with entropy 39 us (5.1 TB/s), with 5 alternatives too
-// 51-56 us (bound by the vector ALUs: 10.5 operations per element counting the exponential
+// Measured on MI355X: 2001 x 50001 bf16 with entropy 37-39 us (5.1-5.4 TB/s), with 5 alternatives
+// 51-54 us (bound by the vector ALUs: 10.5 operations per element counting the exponential
 // as four, and the lists); 4096 x 131072 bf16 190 us (5.7 TB/s); 1 x 131072 bf16 with 20
-// alternatives 7.4 us and 4 us for the join; gradient of 4096 x 131072 bf16 363 us (5.9 TB/s).
+// alternatives 7.3 us and 4 us for the join; gradient of 4096 x 131072 bf16 361 us (5.9 TB/s).
+// fp32: 2001 x 50001 with entropy 70 us (5.8 TB/s), with 5 alternatives 73; rows that share a wave,
+// 65536 x 10 with 3 or 10 alternatives 14 us (12 without; host bound), 65536 x 100 bf16 with 20
+// 61 us, a search over the row's lanes for each.
 #include "kan_ops.h"
 #include "kan_rows.h"
 

@@ -23,9 +23,14 @@
 //
 // Measured on MI355X: forward 65536 x 784 bf16 43.7 us (4.7 TB/s), 16384 x 8192 bf16 with the
 // residual 198 us (5.4 TB/s); gradient 16384 x 8192 bf16 with dh 216 us (5.0 TB/s), 30001 x 1001
-// bf16 with dh 50.8 us (4.7 TB/s), 16384 x 256 fp32 15.5 us (3.2 TB/s, both launches).  Loads
-// of the next row ahead of time did not help (58.9 us against 52.3 for 30001 x 1001): the other
-// waves hide them, and the registers cost some of those.
+// bf16 with dh 50.9 us (4.7 TB/s), 16384 x 256 fp32 15.5-16.4 us (3.1-3.3 TB/s, both launches,
+// outputs at hand).  fp32: forward 65536 x 784 80 us, 16384 x 12288 321 us (5.1 and 5.0 TB/s),
+// gradient 16384 x 8192 307 us (5.3 TB/s), but 16384 x 12288 661 us (3.7 TB/s): above 8192 columns
+// its 32 elements per lane spill 74 registers.  Rows that are read again: 16384 x 20000 forward
+// 1326 us in fp32 and 1109 in bf16 (2.0 and 1.2 TB/s of the bytes that have to move), 8192 x 20000
+// fp32 gradient 1376 us (1.4 TB/s): they load one element per lane.  Loads of the next row ahead
+// of time did not help where they were tried, at two units per lane (30001 x 1001: 58.9 us against
+// 52.3): the other waves hide them, and the registers cost some of those.
 #include "kan_ops.h"
 #include "kan_rows.h"
 
@@ -511,14 +516,14 @@ NormPlan norm_plan(int64_t rows, int32_t n, int es, bool grad) {
     }
     // Workgroups of the gradient: each leaves a row of partial sums, so no more than keep the
     // memory busy, of eight waves (with the joining launch: 16384 x 256 fp32 512 workgroups
-    // 15.5 us, 768 17.6, 1024 of four waves 17.3; 16384 x 1024 fp32 256 42.7 us, 384 45.0, 512 45.6).
+    // 15.9 us, 768 17.4; 16384 x 1024 fp32 256 42.6 us, 384 44.8, 512 45.4).
     if (grad) most = p.units == 1 ? 512 : p.waves == 1 ? 256 : n <= 8192 ? 512 : 256;
     // (the weight gradients' join: the columns of all lanes of the workgroup's waves that take
     // different rows)
     if (grad && per > 1 && p.waves > 0)
         p.lds = sizeof(float) * p.units * V *
                 (p.waves > 1 || p.units > 1 ? p.threads : kMaxWaves << p.shift);
-    // (few rows: one workgroup, whose sums are the gradients: 16 x 784 bf16 11.0 us against
+    // (few rows: one workgroup, whose sums are the gradients: 16 x 784 bf16 11-12 us against
     // 15.4 with the joining launch)
     if (grad && rows <= 3 * per && p.waves > 0) most = 1;
     const int64_t need = (rows + per - 1) / per;

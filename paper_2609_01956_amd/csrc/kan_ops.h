@@ -90,7 +90,8 @@ hipError_t logprob_grad_pieces(LogprobGradArgs a, size_t es, F&& launch) {
     for (int64_t done = 0; done < all;) {
         a.rows = all - done < most ? all - done : most;
         a.items = (uint32_t)(a.rows * a.tiles);
-        const hipError_t e = launch(static_cast<const LogprobGradArgs&>(a), (int)((a.items + 3) / 4));
+        const LogprobGradArgs& piece = a;
+        const hipError_t e = launch(piece, (int)((a.items + 3) / 4));
         if (e != hipSuccess) return e;
         a.z = static_cast<const char*>(a.z) + a.rows * a.stride * (int64_t)es;
         a.dz = static_cast<char*>(a.dz) + a.rows * a.dstride * (int64_t)es;

@@ -9,7 +9,9 @@
  * layer stand the operators of a training or serving step around it: layer norm, which
  * holds a layer's inputs on its grid, and the log probabilities of given
  * classes (tokens) under the logits that the last layer gives, with their gradient,
- * and the clipping of all gradients by their global norm.
+ * and the clipping of all gradients by their global norm; and the two ends of a token model:
+ * the embedding of tokens, and log probabilities under a linear head over a long vocabulary,
+ * whose logits are not kept, both with their gradients.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -647,6 +649,139 @@ kan_status kan_clip_grad_norm(int32_t count, const void* const* grads, const int
 
 /* Size in bytes of the workspace of kan_grad_norm and kan_clip_grad_norm. */
 kan_status kan_grad_norm_workspace_bytes(int32_t count, size_t* bytes);
+
+/*
+ * kan_embedding -- rows of a table for tokens, scaled:
+ *
+ *   y[b, :] = scale table[tokens[b], :]
+ *
+ *   dtype         of y;  table_dtype of the table: KAN_F32, or dtype
+ *   tokens        [rows] int64; ignore_index gives a row of 0, another value outside
+ *                 [0, classes) a row of NaN
+ *   table         [classes, n], rows table_stride >= n elements apart (what lies between is not
+ *                 read)
+ *   scale         finite
+ *   y             [rows, n]
+ *
+ * The product is binary32, rounded once.  y must not overlap an input.  Returns KAN_OK,
+ * KAN_ERR_INVALID_ARG (rows < 0 or > 2^30, classes < 1 or > 2^30, n < 1 or > 2^24, rows * n or
+ * classes * table_stride > 2^48, NULL, misaligned or overlapping pointers with rows > 0),
+ * KAN_ERR_UNSUPPORTED (unknown dtype, a bf16 table for fp32 rows) or KAN_ERR_DEVICE.
+ */
+kan_status kan_embedding(kan_dtype dtype, kan_dtype table_dtype, int64_t rows, int32_t classes,
+                         int32_t n, const int64_t* tokens, int64_t ignore_index, const void* table,
+                         int64_t table_stride, float scale, void* y, void* stream);
+
+/*
+ * kan_embedding_backward -- the gradient of kan_embedding's table for dy = dL/dy:
+ *
+ *   dtable[v, :] = base[v, :] + scale sum over the b with tokens[b] = v of dy[b, :]
+ *
+ *   dtype        of dy;  table_dtype of base and dtable: KAN_F32, or dtype
+ *   tokens       [rows] int64, as in the forward: ignore_index and values outside [0, classes)
+ *                contribute nothing
+ *   dy           [rows, n], rows dy_stride >= n elements apart
+ *   base         [classes, n] a gradient that the table has already (as the weights of a linear
+ *                head); NULL: 0.  May be dtable itself: then rows of tokens that do not occur
+ *                are neither read nor written.
+ *   dtable       [classes, n], fully overwritten (with rows == 0: base, or 0)
+ *   workspace    caller-owned, workspace_bytes >= kan_embedding_backward_workspace_bytes(...),
+ *                16-byte aligned, overlapping no other argument; overwritten
+ *
+ * Tokens are sorted; each row's sum is binary32, in an order that depends on the tokens alone
+ * (deterministic), and rounded once with the base.  Returns as kan_embedding.
+ */
+kan_status kan_embedding_backward(kan_dtype dtype, kan_dtype table_dtype, int64_t rows,
+                                  int32_t classes, int32_t n, const int64_t* tokens,
+                                  int64_t ignore_index, const void* dy, int64_t dy_stride,
+                                  float scale, const void* base, void* dtable, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* Size in bytes of kan_embedding_backward's workspace. */
+kan_status kan_embedding_backward_workspace_bytes(int64_t rows, int32_t classes, int32_t n,
+                                                  size_t* bytes);
+
+/*
+ * kan_linear_logprobs -- log probabilities of given classes (tokens) under the softmax of a linear
+ * head, whose logits are never in memory:
+ *
+ *   z[b, v] = scale sum_i x[b, i] weight[v, i]
+ *   m[b] = max_v z[b, v],  logs[b] = log sum_v exp(z[b, v] - m[b])
+ *   logp[b] = z[b, targets[b]] - m[b] - logs[b]
+ *   best[b] = the lowest v with z[b, v] = m[b]
+ *
+ *   x            [rows, n], rows x_stride >= n elements apart (what lies between is not read)
+ *   weight       [classes, n], rows weight_stride >= n elements apart
+ *   scale        finite
+ *   targets      [rows] int64; ignore_index gives logp 0, another value outside [0, classes)
+ *                gives NaN
+ *   logp         [rows] fp32
+ *   stats        [rows, 2] fp32: m and logs, for the backward
+ *   best         [rows] int64, or NULL
+ *   workspace    caller-owned, workspace_bytes >= kan_linear_logprobs_workspace_bytes(...),
+ *                16-byte aligned, overlapping no other argument; overwritten
+ *
+ * x and weight are of dtype; products and sums are binary32.  Rows of 16-byte aligned x and weight
+ * of whole 16-byte units are read as they stand; others are copied to the workspace (weights in
+ * pieces), except in calls of at most 64 rows.  A NaN or +infinity among a row's logits makes its
+ * logp and logs NaN (best then ranks NaN after every number); a row whose logits are all -infinity
+ * has logp -infinity.  Results of a row do not depend on what other rows hold.
+ *
+ * Outputs must not overlap each other or an input.  Returns KAN_OK, KAN_ERR_INVALID_ARG (rows < 0
+ * or > 2^20, classes < 1 or > 2^30, n < 1 or > 2^20, a stride below n, rows * x_stride or classes *
+ * weight_stride > 2^48, a scale that is not finite, NULL, misaligned or overlapping pointers or a
+ * short workspace with rows > 0), KAN_ERR_UNSUPPORTED (unknown dtype) or KAN_ERR_DEVICE.
+ */
+kan_status kan_linear_logprobs(kan_dtype dtype, int64_t rows, int32_t classes, int32_t n,
+                               const void* x, int64_t x_stride, const void* weight,
+                               int64_t weight_stride, float scale, const int64_t* targets,
+                               int64_t ignore_index, float* logp, float* stats, int64_t* best,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Size in bytes of kan_linear_logprobs's workspace; of x and weight only the alignment counts. */
+kan_status kan_linear_logprobs_workspace_bytes(kan_dtype dtype, int64_t rows, int32_t classes,
+                                               int32_t n, const void* x, int64_t x_stride,
+                                               const void* weight, int64_t weight_stride,
+                                               size_t* bytes);
+
+/*
+ * kan_linear_logprobs_backward -- gradients of kan_linear_logprobs for dlogp = dL/dlogp:
+ *
+ *   dz[b, v]      = dlogp[b] ([v = targets[b]] - p[b, v]),  p = exp(z - m - logs)
+ *   dx[b, i]      = scale sum_v dz[b, v] weight[v, i]
+ *   dweight[v, i] = scale sum_b dz[b, v] x[b, i]
+ *
+ *   x, x_stride, weight, weight_stride, scale, targets, ignore_index, stats  as in the forward
+ *   dlogp        [rows] fp32; that of an ignored row counts as 0
+ *   dx           [rows, n], or NULL to skip it
+ *   dweight      [classes, n], or NULL to skip it; with rows == 0 it is written as 0
+ *   workspace    caller-owned, workspace_bytes >= kan_linear_logprobs_backward_workspace_bytes
+ *                (...), 16-byte aligned, overlapping no other argument; overwritten.  May be NULL
+ *                with rows == 0.
+ *
+ * The logits are formed again, a piece of the vocabulary at a time.  dz is rounded to dtype between
+ * the products (at most 2^-8 of it in bf16, the precision of the products' operands), everything else is
+ * binary32, summed in a fixed order (deterministic).  An ignored row gives 0 to dx and nothing to
+ * dweight, whatever x holds there.  A target that is neither a class nor ignore_index makes its
+ * row of dx and all of dweight NaN, and so does a row whose logp is NaN.  Infinite weights and
+ * inputs give NaN where 0 multiplies them.
+ *
+ * Outputs must not overlap each other or an input.  Returns as kan_linear_logprobs;
+ * KAN_ERR_INVALID_ARG also without any output.
+ */
+kan_status kan_linear_logprobs_backward(kan_dtype dtype, int64_t rows, int32_t classes, int32_t n,
+                                        const void* x, int64_t x_stride, const void* weight,
+                                        int64_t weight_stride, float scale, const int64_t* targets,
+                                        int64_t ignore_index, const float* stats,
+                                        const float* dlogp, void* dx, void* dweight,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Size in bytes of kan_linear_logprobs_backward's workspace for both gradients; of x and weight
+ * only the alignment counts. */
+kan_status kan_linear_logprobs_backward_workspace_bytes(kan_dtype dtype, int64_t rows,
+                                                        int32_t classes, int32_t n, const void* x,
+                                                        int64_t x_stride, const void* weight,
+                                                        int64_t weight_stride, size_t* bytes);
 
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char* kan_status_string(kan_status status);

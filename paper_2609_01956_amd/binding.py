@@ -41,7 +41,10 @@ EXPORTED_SYMBOLS = ("kan_basis_eval", "kan_basis_eval_cdb", "kan_layer_forward",
                     "kan_layer_norm_backward", "kan_layer_norm_backward_workspace_bytes",
                     "kan_token_logprobs", "kan_token_logprobs_workspace_bytes",
                     "kan_token_logprobs_backward", "kan_grad_norm", "kan_clip_grad_norm",
-                    "kan_grad_norm_workspace_bytes", "kan_status_string",
+                    "kan_grad_norm_workspace_bytes", "kan_embedding", "kan_embedding_backward",
+                    "kan_embedding_backward_workspace_bytes", "kan_linear_logprobs",
+                    "kan_linear_logprobs_workspace_bytes", "kan_linear_logprobs_backward",
+                    "kan_linear_logprobs_backward_workspace_bytes", "kan_status_string",
                     "kan_abi_version")
 
 _VP = ctypes.c_void_p
@@ -155,6 +158,27 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
             lib.kan_grad_norm_workspace_bytes.argtypes = [ctypes.c_int32,
                                                           ctypes.POINTER(ctypes.c_size_t)]
             lib.kan_grad_norm_workspace_bytes.restype = ctypes.c_int
+            c_int, i32, i64, f32 = ctypes.c_int, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+            size, sizep = ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+            lib.kan_embedding.argtypes = [c_int, c_int, i64, i32, i32, _VP, i64, _VP, i64, f32, _VP,
+                                          _VP]
+            lib.kan_embedding.restype = c_int
+            lib.kan_embedding_backward.argtypes = [c_int, c_int, i64, i32, i32, _VP, i64, _VP, i64,
+                                                   f32, _VP, _VP, _VP, size, _VP]
+            lib.kan_embedding_backward.restype = c_int
+            lib.kan_embedding_backward_workspace_bytes.argtypes = [i64, i32, i32, sizep]
+            lib.kan_embedding_backward_workspace_bytes.restype = c_int
+            lib.kan_linear_logprobs.argtypes = [c_int, i64, i32, i32, _VP, i64, _VP, i64, f32, _VP,
+                                                i64, _VP, _VP, _VP, _VP, size, _VP]
+            lib.kan_linear_logprobs.restype = c_int
+            lib.kan_linear_logprobs_backward.argtypes = [c_int, i64, i32, i32, _VP, i64, _VP, i64,
+                                                         f32, _VP, i64, _VP, _VP, _VP, _VP, _VP,
+                                                         size, _VP]
+            lib.kan_linear_logprobs_backward.restype = c_int
+            for fn in (lib.kan_linear_logprobs_workspace_bytes,
+                       lib.kan_linear_logprobs_backward_workspace_bytes):
+                fn.argtypes = [c_int, i64, i32, i32, _VP, i64, _VP, i64, sizep]
+                fn.restype = c_int
             lib.kan_status_string.argtypes = [ctypes.c_int]
             lib.kan_status_string.restype = ctypes.c_char_p
             lib.kan_abi_version.argtypes = []
@@ -432,6 +456,78 @@ def kan_grad_norm_workspace_bytes(count: int) -> Tuple[int, int]:
     """Raw call: returns (kan_status, bytes)."""
     size = ctypes.c_size_t(0)
     st = int(load_library().kan_grad_norm_workspace_bytes(int(count), ctypes.byref(size)))
+    return st, int(size.value)
+
+
+def kan_embedding(dtype: int, table_dtype: int, rows: int, classes: int, n: int, tokens: int,
+                  ignore_index: int, table: int, table_stride: int, scale: float, y: int,
+                  stream: int = 0) -> int:
+    """Raw call: device addresses as integers; returns the kan_status code."""
+    return int(load_library().kan_embedding(
+        int(dtype), int(table_dtype), int(rows), int(classes), int(n), _VP(tokens),
+        int(ignore_index), _VP(table), int(table_stride), float(scale), _VP(y), _VP(stream)))
+
+
+def kan_embedding_backward(dtype: int, table_dtype: int, rows: int, classes: int, n: int,
+                           tokens: int, ignore_index: int, dy: int, dy_stride: int, scale: float,
+                           base: int, dtable: int, workspace: int, workspace_bytes: int,
+                           stream: int = 0) -> int:
+    """Raw call: device addresses as integers (0 for NULL); returns the kan_status code."""
+    return int(load_library().kan_embedding_backward(
+        int(dtype), int(table_dtype), int(rows), int(classes), int(n), _VP(tokens),
+        int(ignore_index), _VP(dy), int(dy_stride), float(scale), _VP(base), _VP(dtable),
+        _VP(workspace), ctypes.c_size_t(workspace_bytes), _VP(stream)))
+
+
+def kan_embedding_backward_workspace_bytes(rows: int, classes: int, n: int) -> Tuple[int, int]:
+    """Raw call: returns (kan_status, bytes)."""
+    size = ctypes.c_size_t(0)
+    st = int(load_library().kan_embedding_backward_workspace_bytes(
+        int(rows), int(classes), int(n), ctypes.byref(size)))
+    return st, int(size.value)
+
+
+def kan_linear_logprobs(dtype: int, rows: int, classes: int, n: int, x: int, x_stride: int,
+                        weight: int, weight_stride: int, scale: float, targets: int,
+                        ignore_index: int, logp: int, stats: int, best: int, workspace: int,
+                        workspace_bytes: int, stream: int = 0) -> int:
+    """Raw call: device addresses as integers (0 for NULL); returns the kan_status code."""
+    return int(load_library().kan_linear_logprobs(
+        int(dtype), int(rows), int(classes), int(n), _VP(x), int(x_stride), _VP(weight),
+        int(weight_stride), float(scale), _VP(targets), int(ignore_index), _VP(logp), _VP(stats),
+        _VP(best), _VP(workspace), ctypes.c_size_t(workspace_bytes), _VP(stream)))
+
+
+def kan_linear_logprobs_workspace_bytes(dtype: int, rows: int, classes: int, n: int, x: int,
+                                        x_stride: int, weight: int,
+                                        weight_stride: int) -> Tuple[int, int]:
+    """Raw call: returns (kan_status, bytes)."""
+    size = ctypes.c_size_t(0)
+    st = int(load_library().kan_linear_logprobs_workspace_bytes(
+        int(dtype), int(rows), int(classes), int(n), _VP(x), int(x_stride), _VP(weight),
+        int(weight_stride), ctypes.byref(size)))
+    return st, int(size.value)
+
+
+def kan_linear_logprobs_backward(dtype: int, rows: int, classes: int, n: int, x: int, x_stride: int,
+                                 weight: int, weight_stride: int, scale: float, targets: int,
+                                 ignore_index: int, stats: int, dlogp: int, dx: int, dweight: int,
+                                 workspace: int, workspace_bytes: int, stream: int = 0) -> int:
+    """Raw call: device addresses as integers (0 for NULL); returns the kan_status code."""
+    return int(load_library().kan_linear_logprobs_backward(
+        int(dtype), int(rows), int(classes), int(n), _VP(x), int(x_stride), _VP(weight),
+        int(weight_stride), float(scale), _VP(targets), int(ignore_index), _VP(stats), _VP(dlogp),
+        _VP(dx), _VP(dweight), _VP(workspace), ctypes.c_size_t(workspace_bytes), _VP(stream)))
+
+
+def kan_linear_logprobs_backward_workspace_bytes(dtype: int, rows: int, classes: int, n: int,
+                                                 x: int, x_stride: int, weight: int,
+                                                 weight_stride: int) -> Tuple[int, int]:
+    """Raw call: returns (kan_status, bytes)."""
+    size = ctypes.c_size_t(0)
+    st = int(load_library().kan_linear_logprobs_backward_workspace_bytes(
+        int(dtype), int(rows), int(classes), int(n), _VP(x), int(x_stride), _VP(weight),
+        int(weight_stride), ctypes.byref(size)))
     return st, int(size.value)
 
 
@@ -1027,3 +1123,162 @@ def clip_grad_norm(grads: Iterable, max_norm: float, eps: float = 1e-6, out=None
                 sizes.buffer_info()[0], dtypes.buffer_info()[0], float(max_norm), float(eps),
                 optrs.buffer_info()[0], ws.data_ptr(), ws.numel(), norm.data_ptr(), _stream(dev)))
     return norm
+
+
+# ------------------------------------------------- the two ends of a token model
+
+def _tokens(tokens) -> int:
+    if not tokens.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    if tokens.dtype != _torch().int64 or not tokens.is_contiguous():
+        raise ValueError("tokens must be int64 and contiguous")
+    return tokens.numel()
+
+
+def _matrix(what: str, t, device) -> Tuple[int, int, int]:
+    """Checks rows [rows, n] on `device`: (rows, n, elements from row to row)."""
+    if t.device != device:
+        raise ValueError("tensors must live on one device")
+    shape = t.shape
+    if len(shape) != 2 or shape[1] < 1:
+        raise ValueError(f"{what} must be [rows, n] with n >= 1")
+    rows, n = shape
+    stride, inner = t.stride()
+    if rows <= 1:
+        stride = n
+    if (n > 1 and inner != 1) or stride < n:
+        raise ValueError(f"a row of {what} must be contiguous, and rows must not overlap")
+    return rows, n, stride
+
+
+def embedding(tokens, table, scale: float = 1.0, ignore_index: int = -100, dtype=None, out=None):
+    """kan_embedding: tokens [...] int64, table [classes, n] (its rows may be padded) -> y [..., n]
+    of `dtype` (the table's own by default; a float32 table also gives bfloat16 rows).  `out`
+    receives the rows instead of a fresh tensor."""
+    torch = _torch()
+    rows = _tokens(tokens)
+    device = tokens.device
+    classes, n, stride = _matrix("the table", table, device)
+    shape = tokens.shape + (n,)
+    if out is None:
+        out = table.new_empty(shape, dtype=table.dtype if dtype is None else dtype)
+    elif out.shape != shape or out.device != device or not out.is_contiguous() or \
+            out.dtype != (table.dtype if dtype is None else dtype):
+        raise ValueError("out must be [..., n] of the rows' dtype, contiguous, on the tokens' device")
+    check(_call(device, _library().kan_embedding, _dtype_code(out), _dtype_code(table), rows, classes,
+                n, tokens.data_ptr(), int(ignore_index), table.data_ptr(), stride, scale,
+                out.data_ptr(), _stream(device)))
+    return out
+
+
+def embedding_backward(tokens, dy, classes: int, scale: float = 1.0, ignore_index: int = -100,
+                       dtype=None, base=None, out=None, workspace=None):
+    """The gradient of embedding's table (kan_embedding_backward): tokens [...] int64, dy [..., n]
+    -> [classes, n] of `dtype` (base's, out's or dy's by default; float32 goes with any dy), `base`
+    [classes, n] (None: 0) added: a gradient that the table has already, as a head's weights.
+    `out` receives it instead of a fresh tensor, and may be `base` itself.  `workspace` (a uint8
+    device tensor) is used when large enough, else a fresh one is taken."""
+    torch = _torch()
+    rows, device, classes = _tokens(tokens), tokens.device, int(classes)
+    if dy.shape[:-1] != tokens.shape or dy.dim() != tokens.dim() + 1:
+        raise ValueError("dy must be [..., n] for tokens [...]")
+    if dy.dim() != 2:
+        if not dy.is_contiguous():
+            raise ValueError("dy must be contiguous, or [rows, n]")
+        dy = dy.view(rows, dy.shape[-1]) if dy.shape[-1] else dy.reshape(rows, 0)
+    _, n, stride = _matrix("dy", dy, device)
+    for t in (base, out):
+        if dtype is None and t is not None:
+            dtype = t.dtype
+    dtype = dy.dtype if dtype is None else dtype
+    for t in (base, out):
+        if t is not None and (t.shape != (classes, n) or t.dtype != dtype or t.device != device or
+                              not t.is_contiguous()):
+            raise ValueError("base and out must be [classes, n] of one dtype, contiguous, on the "
+                             "tokens' device")
+    lib, size = _library(), ctypes.c_size_t(0)
+    check(lib.kan_embedding_backward_workspace_bytes(rows, classes, n, ctypes.byref(size)))
+    if out is None:
+        out = dy.new_empty((classes, n), dtype=dtype)
+    if not _fits(workspace, size.value, device):
+        workspace = dy.new_empty((size.value,), dtype=torch.uint8)
+    check(_call(device, lib.kan_embedding_backward, _dtype_code(dy), _dtype_code(out), rows, classes, n,
+                tokens.data_ptr(), int(ignore_index), dy.data_ptr(), stride, scale, _ptr(base),
+                out.data_ptr(), workspace.data_ptr(), size.value, _stream(device)))
+    return out
+
+
+def _head(x, weight, targets):
+    """Checks a head's tensors: the arguments that describe them."""
+    if not x.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    rows, n, stride = _matrix("x", x, x.device)
+    classes, width, wstride = _matrix("the weight", weight, x.device)
+    if width != n or weight.dtype != x.dtype:
+        raise ValueError("weight must be [classes, n] of x's dtype for x [rows, n]")
+    _check_targets(x, rows, targets)
+    return (_dtype_code(x), rows, classes, n, x.data_ptr(), stride, weight.data_ptr(), wstride)
+
+
+def _head_workspace(fn, args, device, workspace):
+    torch, size = _torch(), ctypes.c_size_t(0)
+    check(fn(*args, ctypes.byref(size)))
+    if not _fits(workspace, size.value, device):
+        workspace = torch.empty((size.value,), dtype=torch.uint8, device=device)
+    return workspace, size.value
+
+
+def linear_logprobs(x, weight, targets, scale: float = 1.0, best: bool = False,
+                    ignore_index: int = -100, workspace=None):
+    """kan_linear_logprobs: log probabilities of targets [rows] int64 under the softmax of scale x
+    weight^T, for x [rows, n] and weight [classes, n] (rows of both may be padded) -> (logp [rows],
+    stats [rows, 2], best [rows] int64 or None: the most probable class), logp and stats fp32.
+    stats goes to linear_logprobs_backward.  `workspace` (a uint8 device tensor) is used when large
+    enough, else a fresh one is taken."""
+    torch = _torch()
+    args = _head(x, weight, targets)
+    device, rows, lib = x.device, x.shape[0], _library()
+    ws, nbytes = _head_workspace(lib.kan_linear_logprobs_workspace_bytes, args, device, workspace)
+    logp = x.new_empty((rows,), dtype=torch.float32)
+    stats = logp.new_empty((rows, 2))
+    at = torch.empty_like(targets) if best else None
+    check(_call(device, lib.kan_linear_logprobs, *args, scale, targets.data_ptr(), int(ignore_index),
+                logp.data_ptr(), stats.data_ptr(), _ptr(at), ws.data_ptr(), nbytes,
+                _stream(device)))
+    return logp, stats, at
+
+
+def linear_logprobs_backward(x, weight, targets, stats, dlogp, scale: float = 1.0,
+                             ignore_index: int = -100, need_dx: bool = True, need_dw: bool = True,
+                             workspace=None, out=None):
+    """Gradients of linear_logprobs (kan_linear_logprobs_backward) for dlogp [rows] fp32; stats as
+    linear_logprobs returned them -> (dx [rows, n] or None, dweight [classes, n] or None).  `out`, a
+    (dx, dweight) tuple of contiguous tensors, receives the gradients instead of fresh ones.
+    `workspace` (a uint8 device tensor) is used when large enough, else a fresh one is taken."""
+    torch = _torch()
+    args = _head(x, weight, targets)
+    device, rows, lib = x.device, x.shape[0], _library()
+    if stats is None or stats.dtype != torch.float32 or stats.shape != (rows, 2) or \
+            stats.device != device or not stats.is_contiguous():
+        raise ValueError("stats must be fp32 [rows, 2], contiguous, on x's device")
+    if dlogp is None:
+        raise ValueError("dlogp is needed")
+    _row_values("dlogp", x, dlogp)
+    if not (need_dx or need_dw):
+        raise ValueError("nothing to compute")
+    if out is not None:
+        dx, dw = out
+        for t, like in ((dx, x), (dw, weight)):
+            if t is not None and (t.shape != like.shape or t.dtype != like.dtype or
+                                  t.device != device or not t.is_contiguous()):
+                raise ValueError("out tensors must match x and weight and be contiguous")
+        dx, dw = dx if need_dx else None, dw if need_dw else None
+    else:
+        dx = x.new_empty(x.shape) if need_dx else None
+        dw = weight.new_empty(weight.shape) if need_dw else None
+    ws, nbytes = _head_workspace(lib.kan_linear_logprobs_backward_workspace_bytes, args, device,
+                                 workspace)
+    check(_call(device, lib.kan_linear_logprobs_backward, *args, scale, targets.data_ptr(),
+                int(ignore_index), stats.data_ptr(), dlogp.data_ptr(), _ptr(dx), _ptr(dw),
+                ws.data_ptr(), nbytes, _stream(device)))
+    return dx, dw

@@ -21,7 +21,8 @@ SOURCES = ["kan_api.cpp", "kan_basis.hip", "kan_layer.hip", "kan_layer_bf16.hip"
            "kan_layer_f32.hip", "kan_window_f32.hip", "kan_window_bf16.hip",
            "kan_narrow.hip", "kan_backward.hip", "kan_bwd_dw.hip", "kan_bwd_dx.hip",
            "kan_span.hip", "kan_ops_api.cpp", "kan_norm.hip",
-           "kan_logprob.hip", "kan_clip.hip"]
+           "kan_logprob.hip", "kan_clip.hip", "kan_tokens_api.cpp", "kan_embed.hip",
+           "kan_head.hip"]
 ARCH = "gfx950"
 
 

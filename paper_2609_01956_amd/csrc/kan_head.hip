@@ -1,0 +1,871 @@
+// kan_head.hip -- log probabilities of given tokens under a linear head over a long vocabulary,
+// without its logits in memory, and their gradient.
+//
+//   z_bv = scale x_b . w_v,  m = max_v z_bv,  s = sum_v exp(z_bv - m)
+//   logp_b = z_bt - m - log s,  best_b = the lowest v with z_bv = m
+//   dz_bv = dlogp_b ([v = t_b] - p_bv),  p = exp(z - m - log s)
+//   dx = scale dz W,  dW = scale dz^T X
+#include "kan_head.h"
+
+#include <algorithm>
+
+#include "kan_ops.h"
+#include "kan_rows.h"
+#include "kan_tile.h"
+
+namespace kan {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f, kLn2Low = -1.904654299957768e-9f;  // their sum
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr int kNoIndex = 0x7fffffff;
+
+// exp(t) with the roundings of t log2 e and of the constant: off by at most 1e-7 + 7.3e-8 |t|.
+__device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
+// To 2^-22 of the value (t above -1e5): what the argument's rounding left out as a factor.
+__device__ __forceinline__ float exp_exact(float t) {
+    const float h = t * kLog2e, e = __builtin_amdgcn_exp2f(h);
+    return __builtin_fmaf(e, __builtin_fmaf(-h, kLn2Low, __builtin_fmaf(-h, kLn2, t)), e);
+}
+// What a maximum is subtracted as: rows (so far) without any class stay at 0.
+__device__ __forceinline__ float anchor(float m) { return m == kNegInf ? 0.0f : m; }
+
+// A row's running maximum, sum of exp(z - m), and the lowest class at the maximum.
+struct Best {
+    float m, s;
+    int at;
+};
+__device__ __forceinline__ Best join(const Best& a, const Best& b) {
+    Best c;
+    c.m = __builtin_fmaxf(a.m, b.m);
+    const float o = anchor(c.m);
+    c.s = a.s * exp_of(__builtin_fmaxf(a.m - o, -200.0f)) +
+          b.s * exp_of(__builtin_fmaxf(b.m - o, -200.0f));
+    c.at = a.m > b.m ? a.at : b.m > a.m ? b.at : min(a.at, b.at);
+    return c;
+}
+__device__ __forceinline__ Best from_lane(const Best& a, int mask) {
+    return Best{__shfl_xor(a.m, mask), __shfl_xor(a.s, mask), __shfl_xor(a.at, mask)};
+}
+
+// Where a launch leaves a row's parts.
+struct Parts {
+    float2* sums;  // [parts][rows] m and s
+    int* best;     // [parts][rows], or null
+    float* target; // [rows] the target's logit
+};
+__device__ __forceinline__ void leave(const Parts& o, int64_t part, int64_t rows, int64_t row,
+                                      const Best& b) {
+    o.sums[part * rows + row] = float2{b.m, b.s};
+    if (o.best != nullptr) o.best[part * rows + row] = b.at;
+}
+
+struct HeadTileArgs {
+    const void *x, *w;
+    int64_t rows, xstride, wstride;  // bytes from row to row
+    int classes;                     // of this launch, from class `first` on
+    int first;
+    int k_bytes;
+    int tp, tq;
+    float scale;
+    const int64_t* targets;
+    Parts out;
+    int64_t part;  // of the first tile
+};
+
+template <typename T, typename Tl, bool BEST>
+__global__ void __launch_bounds__(Tl::THREADS) head_tile_kernel(HeadTileArgs a) {
+    __shared__ __attribute__((aligned(128))) char lds[Tl::BYTES];
+    int tp, tq;
+    tile_of(blockIdx.x, a.tp, a.tq, &tp, &tq);
+    const int64_t q0 = (int64_t)tq * Tl::BQ;
+    const int p0 = tp * Tl::BP;
+    Tl t;
+    t.run((char KAN_LDS*)lds, tile_rows(a.w, p0, a.classes, Tl::BP, a.wstride, a.k_bytes),
+          tile_rows(a.x, q0, a.rows, Tl::BQ, a.xstride, a.k_bytes), 0, a.k_bytes);
+    Best* const red = reinterpret_cast<Best*>(lds);  // [WP][BQ]
+    const int lane = threadIdx.x & 63, wp = (threadIdx.x >> 6) % Tl::WP;
+#pragma unroll
+    for (int j = 0; j < Tl::RQ; ++j) {
+        const int64_t row = q0 + Tl::q_of(j);
+        const int64_t target = row < a.rows ? a.targets[row] - a.first : -1;
+        Best b = {kNegInf, 0.0f, kNoIndex};
+#pragma unroll
+        for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int p = p0 + Tl::p_of(i, e >> 2) + (e & 3);
+                const float z = p < a.classes ? t.acc[i][j][e] * a.scale : kNegInf;
+                if (p == target && p < a.classes) a.out.target[row] = z;
+                if (BEST) b.at = z > b.m ? p : b.at;
+                b.m = __builtin_fmaxf(b.m, z);
+                t.acc[i][j][e] = z;
+            }
+        if (BEST && b.at == kNoIndex) {  // (nothing above -infinity: its first class there)
+#pragma unroll
+            for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int p = p0 + Tl::p_of(i, e >> 2) + (e & 3);
+                    if (p < a.classes && t.acc[i][j][e] == kNegInf) b.at = min(b.at, p);
+                }
+        }
+        const float o = anchor(b.m);
+#pragma unroll
+        for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) b.s += exp_of(t.acc[i][j][e] - o);
+        if (BEST && b.at != kNoIndex) b.at += a.first;
+        b = join(b, from_lane(b, 32));
+        if (lane < 32) red[wp * Tl::BQ + Tl::q_of(j)] = b;
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < Tl::BQ; q += Tl::THREADS) {
+        if (q0 + q >= a.rows) break;
+        Best b = red[q];
+#pragma unroll
+        for (int i = 1; i < Tl::WP; ++i) b = join(b, red[i * Tl::BQ + q]);
+        leave(a.out, a.part + tp, a.rows, q0 + q, b);
+    }
+}
+
+// ------------------------------------------------------------ few rows
+
+// Elements [k, k + 16 bytes) of a row of n, 0 past its end.
+template <typename T>
+__device__ __forceinline__ u32x4 chunk_of(const T* row, int k, int n) {
+    constexpr int V = kVec<T>;
+    if (k + V <= n) return *unit_at(row, k);
+    u32x4 r = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if (k + i >= n) continue;
+        if constexpr (sizeof(T) == 2) r[i / 2] |= (uint32_t)row[k + i] << (16 * (i % 2));
+        else r[i] = __float_as_uint(row[k + i]);
+    }
+    return r;
+}
+
+struct HeadThinArgs {
+    const void *x, *w;
+    int rows;
+    int64_t xstride, wstride;  // elements
+    int classes, n;
+    float scale;
+    const int64_t* targets;
+    Parts out;
+};
+constexpr int kThinWaves = 8;
+constexpr int kThinLds = 64 << 10;  // bytes of x in LDS at a time
+
+// NT: groups of 16 rows.
+template <typename T, int NT, bool BEST>
+__global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs a) {
+    constexpr int V = kVec<T>, ROWS = 16 * NT;
+    constexpr int SLICE = kThinLds / ROWS / 16;  // chunks of a row in LDS at a time
+    extern __shared__ __attribute__((aligned(128))) char lds[];
+    __shared__ Best red[kThinWaves][ROWS];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r16 = lane & 15, quad = lane >> 4;
+    const T* const x = static_cast<const T*>(a.x);
+    const T* const w = static_cast<const T*>(a.w);
+    const int chunks = (a.n + V - 1) / V;
+    const int width = min((chunks + 7) & ~7, SLICE);  // chunks per row in LDS, a multiple of 8
+    const auto fill = [&](int c0) {
+        for (int i = threadIdx.x; i < ROWS * width; i += 64 * kThinWaves) {
+            const int row = i / width, c = i - row * width;
+            u32x4 v = {0, 0, 0, 0};
+            if (row < a.rows && (c0 + c) < chunks)
+                v = chunk_of(x + row * a.xstride, (c0 + c) * V, a.n);
+            *reinterpret_cast<u32x4*>(lds + ((size_t)row * width + (c ^ (row & 7))) * 16) = v;
+        }
+    };
+    Best best[NT];
+    int64_t target[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        best[t] = Best{kNegInf, 0.0f, kNoIndex};
+        target[t] = t * 16 + r16 < a.rows ? a.targets[t * 16 + r16] : -1;
+    }
+    const bool once = chunks <= width;
+    if (once) {
+        fill(0);
+        __syncthreads();
+    }
+    const int groups = (a.classes + 15) >> 4;
+    // (all waves of a workgroup take the same turns: x comes in slices between barriers)
+    for (int g0 = blockIdx.x * kThinWaves; g0 < groups; g0 += gridDim.x * kThinWaves) {
+        const int p0 = (g0 + wave) * 16;
+        const T* const row = w + (int64_t)min(p0 + r16, a.classes - 1) * a.wstride;
+        floatx4 acc[NT] = {};
+        for (int c0 = 0; c0 < chunks; c0 += width) {
+            if (!once) {
+                __syncthreads();
+                fill(c0);
+                __syncthreads();
+            }
+            const int here = min(width, chunks - c0);
+            const auto product = [&](int c, u32x4 wv) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const int r = t * 16 + r16;
+                    const u32x4 xv = *reinterpret_cast<const u32x4*>(
+                        lds + ((size_t)r * width + ((c + quad) ^ (r & 7))) * 16);
+                    if constexpr (sizeof(T) == 2) {
+                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8, wv), __builtin_bit_cast(bf16x8, xv), acc[t],
+                            0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                                __uint_as_float(wv[i]), __uint_as_float(xv[i]), acc[t], 0, 0, 0);
+                    }
+                }
+            };
+            // whole chunks in all four quarters of the wave
+            const int full = min(here, a.n / V - c0) & ~3;
+            constexpr int U = 8;
+            int c = 0;
+            for (; c + 4 * U <= full; c += 4 * U) {
+                u32x4 wv[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) wv[u] = *unit_at(row, (c0 + c + 4 * u + quad) * V);
+#pragma unroll
+                for (int u = 0; u < U; ++u) product(c + 4 * u, wv[u]);
+            }
+            for (; c < full; c += 4) product(c, *unit_at(row, (c0 + c + quad) * V));
+            for (; c < here; c += 4) {
+                const int k = c0 + c + quad;
+                product(c, k < chunks ? chunk_of(row, k * V, a.n) : u32x4{0, 0, 0, 0});
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float m = best[t].m;
+            int at = best[t].at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int p = p0 + quad * 4 + i;
+                const float z = p < a.classes ? acc[t][i] * a.scale : kNegInf;
+                if (p == target[t] && p < a.classes) a.out.target[t * 16 + r16] = z;
+                if (BEST && (z > m || (z == kNegInf && at == kNoIndex && p < a.classes))) at = p;
+                m = __builtin_fmaxf(m, z);
+                acc[t][i] = z;
+            }
+            const float o = anchor(m);
+            float s = best[t].s * exp_of(__builtin_fmaxf(best[t].m - o, -200.0f));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s += exp_of(acc[t][i] - o);
+            best[t] = Best{m, s, at};
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        best[t] = join(best[t], from_lane(best[t], 16));
+        best[t] = join(best[t], from_lane(best[t], 32));
+        if (quad == 0) red[wave][t * 16 + r16] = best[t];
+    }
+    __syncthreads();
+    const int row = threadIdx.x;
+    if (row < a.rows) {
+        Best b = red[0][row];
+        for (int i = 1; i < kThinWaves; ++i) b = join(b, red[i][row]);
+        leave(a.out, blockIdx.x, a.rows, row, b);
+    }
+}
+
+// ------------------------------------------------------------ parts into rows
+
+struct HeadJoinArgs {
+    Parts in;
+    int64_t rows;
+    int parts, classes, lanes;  // lanes (a power of two, at most 64) neighbouring rows
+    const int64_t* targets;
+    int64_t ignore;
+    float *logp, *stats;
+    int64_t* best;
+};
+__global__ void __launch_bounds__(256) head_join_kernel(HeadJoinArgs a) {
+    __shared__ Best red[256];
+    const int r = threadIdx.x & (a.lanes - 1), strand = threadIdx.x / a.lanes, strands = 256 / a.lanes;
+    const int64_t row = (int64_t)blockIdx.x * a.lanes + r;
+    Best b = {kNegInf, 0.0f, kNoIndex};
+    if (row < a.rows) {
+        for (int i = strand; i < a.parts; i += strands) {
+            const float2 v = a.in.sums[(int64_t)i * a.rows + row];
+            b = join(b, Best{v.x, v.y,
+                             a.in.best != nullptr ? a.in.best[(int64_t)i * a.rows + row] : kNoIndex});
+        }
+    }
+    red[threadIdx.x] = b;
+    for (int n = 128; n >= a.lanes; n >>= 1) {
+        __syncthreads();
+        if ((int)threadIdx.x < n) red[threadIdx.x] = join(red[threadIdx.x], red[threadIdx.x + n]);
+    }
+    if (strand != 0 || row >= a.rows) return;
+    b = red[r];
+    const float logs = logf(b.s);
+    const int64_t t = a.targets[row];
+    float lp = 0.0f;
+    if (t != a.ignore) {
+        lp = __builtin_nanf("");
+        if (t >= 0 && t < a.classes)
+            lp = b.m == kNegInf && b.s == 0.0f ? kNegInf : a.in.target[row] - b.m - logs;
+    }
+    a.logp[row] = lp;
+    a.stats[2 * row] = b.m;
+    a.stats[2 * row + 1] = logs;
+    if (a.best != nullptr) a.best[row] = b.at == kNoIndex ? 0 : b.at;
+}
+
+// ------------------------------------------------------------ gradient
+
+template <typename T>
+__device__ __forceinline__ T rounded(float v) {
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(uint16_t, (__bf16)v);
+    else return v;
+}
+
+// Four neighbours, `left` of them within the row.
+template <typename T>
+__device__ __forceinline__ void store_four(T* at, int64_t left, const T (&v)[4]) {
+    typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    if (left >= 4) {
+        *reinterpret_cast<four*>(at) = four{v[0], v[1], v[2], v[3]};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (i < left) at[i] = v[i];
+}
+
+struct HeadGradTileArgs {
+    HeadTileArgs z;  // (its `out` and `part` are not used)
+    const float *stats, *dlogp;
+    int64_t ignore;
+    int all;    // classes
+    void* dz;   // [rows][zstride], or null; 0 past the classes
+    void* dzt;  // [classes][tstride], or null; 0 past the rows
+    int64_t zstride, tstride;  // elements
+};
+
+// dz of a tile, and its transpose, in T: the products that follow take it as their operand.
+template <typename T, typename Tl>
+__global__ void __launch_bounds__(Tl::THREADS) head_grad_kernel(HeadGradTileArgs g) {
+    __shared__ __attribute__((aligned(128))) char lds[Tl::BYTES];
+    const HeadTileArgs& a = g.z;
+    int tp, tq;
+    tile_of(blockIdx.x, a.tp, a.tq, &tp, &tq);
+    const int64_t q0 = (int64_t)tq * Tl::BQ;
+    const int p0 = tp * Tl::BP;
+    Tl t;
+    t.run((char KAN_LDS*)lds, tile_rows(a.w, p0, a.classes, Tl::BP, a.wstride, a.k_bytes),
+          tile_rows(a.x, q0, a.rows, Tl::BQ, a.xstride, a.k_bytes), 0, a.k_bytes);
+    T* const dz = static_cast<T*>(g.dz);
+    T* const dzt = static_cast<T*>(g.dzt);
+#pragma unroll
+    for (int j = 0; j < Tl::RQ; ++j) {
+        const int64_t row = q0 + Tl::q_of(j);
+        // (rows that have no gradient: p = 0, whatever their logits are)
+        float m = __builtin_huge_valf(), logs = 0.0f, d = 0.0f;
+        int64_t target = -1;
+        if (row < a.rows) {
+            const int64_t c = a.targets[row];
+            const float rm = g.stats[2 * row], rl = g.stats[2 * row + 1];
+            if (c != g.ignore) {
+                // (a target that is no class, NaN and infinite logits show in the row's gradient)
+                d = c < 0 || c >= g.all || rm != rm || rl != rl ? __builtin_nanf("") : g.dlogp[row];
+                if (rm == kNegInf && rl == kNegInf && d == d) d = 0.0f;
+                else m = rm, logs = rl, target = c - a.first;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int p = p0 + Tl::p_of(i, v);
+                T o[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float z = t.acc[i][j][4 * v + e] * a.scale;
+                    const float pr = exp_exact(__builtin_fmaxf(z - m - logs, -1e4f));
+                    const float y = p + e == target ? d - d * pr : -d * pr;
+                    o[e] = rounded<T>(p + e < a.classes ? y : 0.0f);
+                }
+                if (dz != nullptr && row < a.rows && p < g.zstride)
+                    store_four(dz + row * g.zstride + p, 4, o);
+                if (dzt != nullptr && row < g.tstride) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (p + e < a.classes) dzt[(int64_t)(p + e) * g.tstride + row] = o[e];
+                }
+            }
+    }
+}
+
+struct ProductArgs {
+    const void *p, *q;          // [np] and [nq] rows of k_bytes
+    int64_t pstride, qstride;   // bytes
+    int64_t np, nq;
+    int64_t k_bytes, k_split;   // bytes of k in all, and of a split
+    int tp, tq;
+    float* acc;  // [splits][nq][np], or null
+    bool add;    // to what acc holds
+    void* out;   // [nq][np], or null
+    float scale;
+};
+
+// out = scale (sum over k + acc), or acc (+)= the sum over a split's k.
+template <typename T, typename Tl>
+__global__ void __launch_bounds__(Tl::THREADS) head_product_kernel(ProductArgs a) {
+    __shared__ __attribute__((aligned(128))) char lds[Tl::BYTES];
+    const int tiles = a.tp * a.tq, split = blockIdx.x / tiles;
+    int tp, tq;
+    tile_of(blockIdx.x - split * tiles, a.tp, a.tq, &tp, &tq);
+    const int64_t q0 = (int64_t)tq * Tl::BQ, p0 = (int64_t)tp * Tl::BP;
+    const int64_t k0 = split * a.k_split;
+    if (k0 >= a.k_bytes) return;  // (a last piece that is shorter: nothing to add)
+    Tl t;
+    t.run((char KAN_LDS*)lds, tile_rows(a.p, p0, a.np, Tl::BP, a.pstride, a.k_bytes),
+          tile_rows(a.q, q0, a.nq, Tl::BQ, a.qstride, a.k_bytes), k0,
+          a.k_bytes - k0 < a.k_split ? a.k_bytes - k0 : a.k_split);
+#pragma unroll
+    for (int j = 0; j < Tl::RQ; ++j) {
+        const int64_t q = q0 + Tl::q_of(j);
+        if (q >= a.nq) continue;
+        float* const acc = a.acc == nullptr ? nullptr : a.acc + (split * a.nq + q) * a.np;
+#pragma unroll
+        for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int64_t p = p0 + Tl::p_of(i, v), left = a.np - p;
+                if (left <= 0) continue;
+                float o[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    o[e] = t.acc[i][j][4 * v + e];
+                    if (a.add && e < left) o[e] += acc[p + e];
+                }
+                if (a.out == nullptr) {
+                    store_four(acc + p, left, o);
+                    continue;
+                }
+                T r[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = rounded<T>(o[e] * a.scale);
+                store_four(static_cast<T*>(a.out) + q * a.np + p, left, r);
+            }
+    }
+}
+
+// out = scale times the sum of the splits, in their order.
+template <typename T>
+__global__ void __launch_bounds__(256) head_sum_kernel(const float* acc, int splits, int64_t n,
+                                                       float scale, T* out) {
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n;
+         i += (int64_t)gridDim.x * 1024) {
+        typedef float four __attribute__((ext_vector_type(4), aligned(4)));
+        const int64_t left = n - i;
+        float s[4] = {};
+        for (int k = 0; k < splits; ++k) {
+            const float* const at = acc + k * n + i;
+            if (left >= 4) {
+                const four v = *reinterpret_cast<const four*>(at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] += v[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < left) s[e] += at[e];
+            }
+        }
+        T r[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = rounded<T>(s[e] * scale);
+        store_four(out + i, left, r);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) head_zero_kernel(T* out, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+        out[i] = T(0);
+}
+
+// ------------------------------------------------------------ rows laid out for the tiles
+
+// Rows of n elements copied to rows of `to` elements (a multiple of 16 bytes), 0 past n.
+template <typename T>
+__global__ void __launch_bounds__(256) head_pack_kernel(const T* x, int64_t stride, int64_t rows,
+                                                        int n, T* out, int to) {
+    constexpr int V = kVec<T>;
+    const int units = to / V;
+    const int64_t all = rows * units;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / units;
+        const int c = (int)(i - row * units) * V;
+        *reinterpret_cast<u32x4*>(out + row * to + c) = chunk_of(x + row * stride, c, n);
+    }
+}
+
+// out[c][r] = x[r][c], 0 from `rows` to `to`; 0 also for rows whose target is `ignore` (targets
+// null: none).  64 x 64 elements a workgroup.
+template <typename T>
+__global__ void __launch_bounds__(256) head_turn_kernel(const T* x, int64_t stride, int64_t rows,
+                                                        int n, T* out, int64_t to,
+                                                        const int64_t* targets, int64_t ignore,
+                                                        int across) {
+    constexpr int V = kVec<T>, U = 64 / V;
+    __shared__ T tile[64][64 + 4 / sizeof(T)];
+    const int64_t r0 = (int64_t)(blockIdx.x / across) * 64;
+    const int c0 = (blockIdx.x % across) * 64;
+    for (int i = threadIdx.x; i < 64 * U; i += 256) {
+        const int64_t row = r0 + i / U;
+        const int c = c0 + (i % U) * V;
+        u32x4 v = {0, 0, 0, 0};
+        if (row < rows && c < n && (targets == nullptr || targets[row] != ignore))
+            v = chunk_of(x + row * stride, c, n);
+        T e[V];
+        __builtin_memcpy(e, &v, 16);
+#pragma unroll
+        for (int k = 0; k < V; ++k) tile[i / U][(i % U) * V + k] = e[k];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64 * U; i += 256) {
+        const int c = i / U, r = (i % U) * V;
+        if (c0 + c >= n || r0 + r >= to) continue;
+        T e[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) e[k] = tile[r + k][c];
+        u32x4 v;
+        __builtin_memcpy(&v, e, 16);
+        *reinterpret_cast<u32x4*>(out + (int64_t)(c0 + c) * to + r0 + r) = v;
+    }
+}
+
+// ------------------------------------------------------------ plans
+
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+int64_t div_up(int64_t v, int64_t by) { return (v + by - 1) / by; }
+
+// Device memory handed out piece by piece (from null: sizes alone).
+struct Arena {
+    char* base;
+    size_t at = 0;
+    template <typename T = char>
+    T* take(int64_t bytes) {
+        char* p = base == nullptr ? nullptr : base + at;
+        at += (size_t)up(bytes, 256);
+        return reinterpret_cast<T*>(p);
+    }
+};
+
+template <typename T> using Big = Tile<T, 2, 4, 4, 2>;    // 256 x 256
+template <typename T> using Small = Tile<T, 2, 2, 2, 2>;  // 128 x 128
+constexpr int kBig = 256, kSmall = 128;
+constexpr int kThinRows = 64;
+// Bytes of a piece's intermediate tensors.
+constexpr int64_t kPieceBytes = INT64_C(256) << 20;
+constexpr int64_t kPieceClasses = 1 << 20, kPieceTiles = 1 << 20;
+constexpr int kFillTiles = 256;  // tiles that occupy the GPU
+
+struct HeadPlan {
+    bool thin, big;
+    int groups;         // thin: workgroups
+    int64_t parts;
+    int64_t piece;      // classes
+    int to;             // elements of a packed row
+    Parts out;
+    void *xp, *wp;      // packed rows, or null
+    size_t bytes;
+};
+
+HeadPlan head_plan(const HeadShape& s, void* ws) {
+    HeadPlan p = {};
+    Arena arena = {static_cast<char*>(ws)};
+    p.to = (int)up(s.n, 16 / s.es);
+    p.thin = s.rows <= kThinRows;
+    if (p.thin) {
+        p.groups = (int)std::min<int64_t>(div_up(div_up(s.classes, 16), kThinWaves), 512);
+        p.parts = p.groups;
+    } else {
+        p.big = div_up(s.rows, kBig) * div_up(s.classes, kBig) >= kFillTiles;
+        const int b = p.big ? kBig : kSmall;
+        p.parts = div_up(s.classes, b);
+        p.piece = kPieceTiles / div_up(s.rows, b);
+        if (!s.ws) p.piece = std::min(p.piece, std::max<int64_t>(1, kPieceBytes / p.to / s.es / b));
+        p.piece = std::min<int64_t>(p.piece * b, up(s.classes, b));
+        if (!s.xs) p.xp = arena.take(s.rows * p.to * s.es);
+        if (!s.ws) p.wp = arena.take(p.piece * p.to * s.es);
+    }
+    p.out.sums = arena.take<float2>(p.parts * s.rows * 8);
+    p.out.best = arena.take<int>(p.parts * s.rows * 4);
+    p.out.target = arena.take<float>(s.rows * 4);
+    p.bytes = arena.at;
+    return p;
+}
+
+int grid_of(int64_t items, int per) { return (int)std::min<int64_t>(div_up(items, per), 1 << 16); }
+
+template <typename T>
+hipError_t pack(const void* x, int64_t stride, int64_t rows, int n, void* out, int to,
+                hipStream_t st) {
+    head_pack_kernel<T><<<grid_of(rows * (to / kVec<T>), 256), 256, 0, st>>>(
+        static_cast<const T*>(x), stride, rows, n, static_cast<T*>(out), to);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t turn(const void* x, int64_t stride, int64_t rows, int n, void* out, int64_t to,
+                const int64_t* targets, int64_t ignore, hipStream_t st) {
+    const int across = (int)div_up(n, 64);
+    head_turn_kernel<T><<<(int)(div_up(to, 64) * across), 256, 0, st>>>(
+        static_cast<const T*>(x), stride, rows, n, static_cast<T*>(out), to, targets, ignore,
+        across);
+    return hipGetLastError();
+}
+
+#define KAN_TRY(...)                          \
+    do {                                      \
+        const hipError_t e_ = (__VA_ARGS__);  \
+        if (e_ != hipSuccess) return e_;      \
+    } while (0)
+
+template <typename T, int NT>
+hipError_t thin(const HeadPlan& p, const HeadThinArgs& a, bool best, hipStream_t st) {
+    const int chunks = (int)div_up(a.n, kVec<T>), slice = kThinLds / (16 * NT) / 16;
+    const size_t lds = (size_t)16 * NT * std::min((chunks + 7) & ~7, slice) * 16;
+    if (best) head_thin_kernel<T, NT, true><<<p.groups, 64 * kThinWaves, lds, st>>>(a);
+    else head_thin_kernel<T, NT, false><<<p.groups, 64 * kThinWaves, lds, st>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, typename Tl>
+hipError_t tiles(const HeadTileArgs& a, bool best, hipStream_t st) {
+    if (best) head_tile_kernel<T, Tl, true><<<a.tp * a.tq, Tl::THREADS, 0, st>>>(a);
+    else head_tile_kernel<T, Tl, false><<<a.tp * a.tq, Tl::THREADS, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st) {
+    HeadPlan p = head_plan(s, ws);
+    if (a.best == nullptr) p.out.best = nullptr;
+    if (p.thin) {
+        HeadThinArgs t = {};
+        t.x = a.x;
+        t.w = a.w;
+        t.rows = (int)s.rows;
+        t.xstride = s.xstride;
+        t.wstride = s.wstride;
+        t.classes = s.classes;
+        t.n = s.n;
+        t.scale = a.scale;
+        t.targets = a.targets;
+        t.out = p.out;
+        const bool best = a.best != nullptr;
+        KAN_TRY(s.rows <= 16 ? thin<T, 1>(p, t, best, st)
+                             : s.rows <= 32 ? thin<T, 2>(p, t, best, st) : thin<T, 4>(p, t, best, st));
+    } else {
+        HeadTileArgs t = {};
+        t.x = p.xp != nullptr ? p.xp : a.x;
+        t.xstride = (p.xp != nullptr ? p.to : s.xstride) * s.es;
+        t.wstride = (p.wp != nullptr ? p.to : s.wstride) * s.es;
+        t.rows = s.rows;
+        t.k_bytes = p.to * s.es;
+        t.scale = a.scale;
+        t.targets = a.targets;
+        t.out = p.out;
+        const int b = p.big ? kBig : kSmall;
+        t.tq = (int)div_up(s.rows, b);
+        if (p.xp != nullptr) KAN_TRY(pack<T>(a.x, s.xstride, s.rows, s.n, p.xp, p.to, st));
+        for (int64_t first = 0; first < s.classes; first += p.piece) {
+            t.first = (int)first;
+            t.classes = (int)std::min<int64_t>(s.classes - first, p.piece);
+            t.tp = (int)div_up(t.classes, b);
+            t.part = first / b;
+            t.w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
+            if (p.wp != nullptr) {
+                KAN_TRY(pack<T>(t.w, s.wstride, t.classes, s.n, p.wp, p.to, st));
+                t.w = p.wp;
+            }
+            KAN_TRY(p.big ? tiles<T, Big<T>>(t, a.best != nullptr, st)
+                          : tiles<T, Small<T>>(t, a.best != nullptr, st));
+        }
+    }
+    HeadJoinArgs j = {p.out, s.rows, (int)p.parts, s.classes, 1, a.targets, a.ignore, a.logp, a.stats,
+                      a.best};
+    while (j.lanes < 64 && j.lanes < s.rows && j.lanes * p.parts < 4096) j.lanes *= 2;
+    head_join_kernel<<<(int)div_up(s.rows, j.lanes), 256, 0, st>>>(j);
+    return hipGetLastError();
+}
+
+// A product out[nq][np] over k: its tiles, and how k is split where they are few.
+struct ProductPlan {
+    bool big;
+    int tp, tq, splits;
+    int64_t k_split;  // bytes
+};
+ProductPlan product_plan(int64_t np, int64_t nq, int64_t k_bytes) {
+    ProductPlan p;
+    p.big = div_up(np, kBig) * div_up(nq, kBig) >= kFillTiles;
+    const int b = p.big ? kBig : kSmall;
+    p.tp = (int)div_up(np, b);
+    p.tq = (int)div_up(nq, b);
+    // (a split takes at least eight steps)
+    const int64_t most = std::max<int64_t>(1, k_bytes / 1024);
+    const int64_t want = p.big ? 1 : 2 * kFillTiles / ((int64_t)p.tp * p.tq);
+    p.splits = (int)std::max<int64_t>(1, std::min(want, most));
+    p.k_split = up(div_up(k_bytes, p.splits), 128);
+    p.splits = (int)div_up(k_bytes, p.k_split);
+    return p;
+}
+
+struct HeadGradPlan {
+    int64_t piece, zstride, tstride;  // classes; elements
+    int to;
+    void *xp, *wp;   // packed rows, or null
+    void *xt, *wt;   // turned, or null
+    void *dz, *dzt;  // or null
+    float *dx, *dw;  // sums over k in parts, or null
+    ProductPlan px, pw;
+    size_t bytes;
+};
+
+HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
+    HeadGradPlan p = {};
+    Arena arena = {static_cast<char*>(ws)};
+    p.to = (int)up(s.n, 16 / s.es);
+    p.tstride = up(s.rows, 64);
+    const int64_t row = s.es * ((dx ? p.tstride + s.n : 0) + (dw ? p.tstride : 0) + (s.ws ? 0 : p.to));
+    p.piece = std::min(kPieceClasses, kPieceTiles / div_up(s.rows, kSmall) * kSmall);
+    p.piece = std::min(p.piece, std::max<int64_t>(kPieceBytes / row / kBig * kBig, kBig));
+    p.piece = std::min(p.piece, up(s.classes, kBig));
+    p.zstride = std::min(p.piece, up(s.classes, 64));
+    if (!s.xs) p.xp = arena.take(s.rows * p.to * s.es);
+    if (!s.ws) p.wp = arena.take(p.piece * p.to * s.es);
+    if (dx) {
+        p.wt = arena.take(s.n * p.zstride * s.es);
+        p.dz = arena.take(s.rows * p.zstride * s.es);
+        p.px = product_plan(s.n, s.rows, p.zstride * s.es);
+        if (p.px.splits > 1 || p.piece < s.classes)
+            p.dx = arena.take<float>((int64_t)p.px.splits * s.rows * s.n * 4);
+    }
+    if (dw) {
+        p.xt = arena.take(s.n * p.tstride * s.es);
+        p.dzt = arena.take(std::min<int64_t>(p.piece, s.classes) * p.tstride * s.es);
+        p.pw = product_plan(s.n, std::min<int64_t>(p.piece, s.classes), p.tstride * s.es);
+        if (p.pw.splits > 1)
+            p.dw = arena.take<float>((int64_t)p.pw.splits * std::min<int64_t>(p.piece, s.classes) *
+                                     s.n * 4);
+    }
+    p.bytes = arena.at;
+    return p;
+}
+
+template <typename T>
+hipError_t product(const ProductPlan& p, const ProductArgs& a, hipStream_t st) {
+    const int groups = p.tp * p.tq * p.splits;
+    if (p.big) head_product_kernel<T, Big<T>><<<groups, Big<T>::THREADS, 0, st>>>(a);
+    else head_product_kernel<T, Small<T>><<<groups, Small<T>::THREADS, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t sum(const float* acc, int splits, int64_t n, float scale, void* out, hipStream_t st) {
+    head_sum_kernel<T><<<grid_of(n, 1024), 256, 0, st>>>(acc, splits, n, scale,
+                                                         static_cast<T*>(out));
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStream_t st) {
+    if (s.rows == 0) {
+        if (a.dw == nullptr) return hipSuccess;
+        const int64_t n = (int64_t)s.classes * s.n;
+        head_zero_kernel<T><<<grid_of(n, 256), 256, 0, st>>>(static_cast<T*>(a.dw), n);
+        return hipGetLastError();
+    }
+    const HeadGradPlan p = head_grad_plan(s, a.dx != nullptr, a.dw != nullptr, ws);
+    HeadGradTileArgs g = {};
+    g.z.x = p.xp != nullptr ? p.xp : a.x;
+    g.z.xstride = (p.xp != nullptr ? p.to : s.xstride) * s.es;
+    g.z.wstride = (p.wp != nullptr ? p.to : s.wstride) * s.es;
+    g.z.rows = s.rows;
+    g.z.k_bytes = p.to * s.es;
+    g.z.scale = a.scale;
+    g.z.targets = a.targets;
+    g.stats = a.stats;
+    g.dlogp = a.dlogp;
+    g.ignore = a.ignore;
+    g.all = s.classes;
+    g.dz = p.dz;
+    g.dzt = p.dzt;
+    g.zstride = p.zstride;
+    g.tstride = p.tstride;
+    if (p.xp != nullptr) KAN_TRY(pack<T>(a.x, s.xstride, s.rows, s.n, p.xp, p.to, st));
+    if (p.xt != nullptr)
+        KAN_TRY(turn<T>(a.x, s.xstride, s.rows, s.n, p.xt, p.tstride, a.targets, a.ignore, st));
+    for (int64_t first = 0; first < s.classes; first += p.piece) {
+        const int64_t here = std::min<int64_t>(s.classes - first, p.piece);
+        const char* const w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
+        g.z.first = (int)first;
+        g.z.classes = (int)here;
+        g.z.w = w;
+        if (p.wp != nullptr) {
+            KAN_TRY(pack<T>(w, s.wstride, here, s.n, p.wp, p.to, st));
+            g.z.w = p.wp;
+        }
+        const bool big = div_up(s.rows, kBig) * div_up(here, kBig) >= kFillTiles;
+        const int b = big ? kBig : kSmall;
+        g.z.tp = (int)div_up(here, b);
+        g.z.tq = (int)div_up(s.rows, b);
+        if (big) head_grad_kernel<T, Big<T>><<<g.z.tp * g.z.tq, Big<T>::THREADS, 0, st>>>(g);
+        else head_grad_kernel<T, Small<T>><<<g.z.tp * g.z.tq, Small<T>::THREADS, 0, st>>>(g);
+        KAN_TRY(hipGetLastError());
+        if (a.dx != nullptr) {
+            // (the last piece's k ends with its classes: the rows of dz past them are not read)
+            const int64_t k = std::min(up(here, 64), p.zstride) * s.es;
+            const bool last = first + p.piece >= s.classes, whole = p.px.splits == 1 && last;
+            KAN_TRY(turn<T>(w, s.wstride, here, s.n, p.wt, p.zstride, nullptr, 0, st));
+            ProductArgs r = {p.wt, p.dz, p.zstride * s.es, p.zstride * s.es, s.n, s.rows, k,
+                             p.px.k_split, p.px.tp, p.px.tq, p.dx, first > 0,
+                             whole ? a.dx : nullptr, a.scale};
+            ProductPlan px = p.px;
+            KAN_TRY(product<T>(px, r, st));
+            if (last && !whole)
+                KAN_TRY(sum<T>(p.dx, p.px.splits, s.rows * s.n, a.scale, a.dx, st));
+        }
+        if (a.dw != nullptr) {
+            char* const out = static_cast<char*>(a.dw) + first * s.n * s.es;
+            ProductPlan pw = p.pw;
+            pw.tq = (int)div_up(here, pw.big ? kBig : kSmall);
+            ProductArgs r = {p.xt, p.dzt, p.tstride * s.es, p.tstride * s.es, s.n, here,
+                             p.tstride * s.es, pw.k_split, pw.tp, pw.tq, p.dw, false,
+                             pw.splits == 1 ? out : nullptr, a.scale};
+            KAN_TRY(product<T>(pw, r, st));
+            if (pw.splits > 1) KAN_TRY(sum<T>(p.dw, pw.splits, here * s.n, a.scale, out, st));
+        }
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t head_workspace(const HeadShape& s) {
+    return s.rows == 0 ? 0 : head_plan(s, nullptr).bytes;
+}
+size_t head_grad_workspace(const HeadShape& s, bool dx, bool dw) {
+    return s.rows == 0 ? 0 : head_grad_plan(s, dx, dw, nullptr).bytes;
+}
+hipError_t launch_head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st) {
+    return s.es == 2 ? head<uint16_t>(s, a, ws, st) : head<float>(s, a, ws, st);
+}
+hipError_t launch_head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStream_t st) {
+    return s.es == 2 ? head_grad<uint16_t>(s, a, ws, st) : head_grad<float>(s, a, ws, st);
+}
+
+}  // namespace kan

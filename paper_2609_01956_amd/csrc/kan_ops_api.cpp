@@ -5,51 +5,22 @@
 
 #include <cmath>
 #include <cstdint>
-#include <initializer_list>
 
+#include "kan_checks.h"
 #include "kan_clip_lists.h"
 #include "kan_ops.h"
 
 namespace {
 
-size_t dtype_size(kan_dtype dt) { return dt == KAN_BF16 ? 2 : 4; }
-bool known(kan_dtype dt) { return dt == KAN_F32 || dt == KAN_BF16; }
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-kan_status device_status(hipError_t e) { return e == hipSuccess ? KAN_OK : KAN_ERR_DEVICE; }
-
-// `n` bytes at p (p NULL: not given), of elements of `a` bytes.
-struct Buf {
-    const void* p;
-    size_t n;
-    size_t a;
-};
-
-bool overlap(const Buf& x, const Buf& y) {
-    if (x.p == nullptr || y.p == nullptr || x.n == 0 || y.n == 0) return false;
-    const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
-    return a < b + y.n && b < a + x.n;
-}
-
-// Every buffer aligned to its elements, no output over another output or an input.
-bool placed(std::initializer_list<Buf> ins, std::initializer_list<Buf> outs) {
-    for (const Buf& i : ins)
-        if (!aligned(i.p, i.a)) return false;
-    for (const Buf* o = outs.begin(); o != outs.end(); ++o) {
-        if (!aligned(o->p, o->a)) return false;
-        for (const Buf& i : ins)
-            if (overlap(*o, i)) return false;
-        for (const Buf* q = outs.begin(); q != o; ++q)
-            if (overlap(*o, *q)) return false;
-    }
-    return true;
-}
-
-// Rows of n elements: sizes that the kernels' indexes hold.
-kan_status check_rows(int64_t rows, int32_t n, int32_t most) {
-    if (rows < 0 || n < 1 || n > most) return KAN_ERR_INVALID_ARG;
-    if (rows > (INT64_C(1) << 48) / n) return KAN_ERR_INVALID_ARG;
-    return KAN_OK;
-}
+using kan::aligned;
+using kan::Buf;
+using kan::check_rows;
+using kan::device_status;
+using kan::dtype_size;
+using kan::known;
+using kan::logits_bytes;
+using kan::overlap;
+using kan::placed;
 
 constexpr int32_t kMaxNormRow = 1 << 24;
 
@@ -64,13 +35,6 @@ constexpr int32_t kMaxClasses = 1 << 30;
 kan_status check_logits(kan_dtype dtype, int64_t rows, int32_t classes) {
     if (!known(dtype)) return KAN_ERR_UNSUPPORTED;
     return check_rows(rows, classes, kMaxClasses);
-}
-
-// Bytes from the first to past the last logit of rows `stride` elements apart; 0 for
-// strides that rows of `classes` elements do not fit or that pass the indexes.
-size_t logits_bytes(int64_t rows, int32_t classes, int64_t stride, size_t es) {
-    if (stride < classes || rows > (INT64_C(1) << 48) / stride) return 0;
-    return ((size_t)(rows - 1) * stride + classes) * es;
 }
 
 // Shared validation of the calls on many tensors.

@@ -76,7 +76,7 @@ struct HeadTileArgs {
 };
 
 template <typename T, typename Tl, bool BEST>
-__global__ void __launch_bounds__(Tl::THREADS) head_tile_kernel(HeadTileArgs a) {
+__global__ void __launch_bounds__(Tl::THREADS, 2) head_tile_kernel(HeadTileArgs a) {
     __shared__ __attribute__((aligned(128))) char lds[Tl::BYTES];
     int tp, tq;
     tile_of(blockIdx.x, a.tp, a.tq, &tp, &tq);
@@ -86,17 +86,17 @@ __global__ void __launch_bounds__(Tl::THREADS) head_tile_kernel(HeadTileArgs a) 
     t.run((char KAN_LDS*)lds, tile_rows(a.w, p0, a.classes, Tl::BP, a.wstride, a.k_bytes),
           tile_rows(a.x, q0, a.rows, Tl::BQ, a.xstride, a.k_bytes), 0, a.k_bytes);
     Best* const red = reinterpret_cast<Best*>(lds);  // [WP][BQ]
-    const int lane = threadIdx.x & 63, wp = (threadIdx.x >> 6) % Tl::WP;
+    const int tid = Tl::thread(), lane = tid & 63, wp = (tid >> 6) % Tl::WP;
 #pragma unroll
     for (int j = 0; j < Tl::RQ; ++j) {
-        const int64_t row = q0 + Tl::q_of(j);
+        const int64_t row = q0 + Tl::q_of(tid, j);
         const int64_t target = row < a.rows ? a.targets[row] - a.first : -1;
         Best b = {kNegInf, 0.0f, kNoIndex};
 #pragma unroll
         for (int i = 0; i < Tl::RP; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int p = p0 + Tl::p_of(i, e >> 2) + (e & 3);
+                const int p = p0 + Tl::p_of(tid, i, e >> 2) + (e & 3);
                 const float z = p < a.classes ? t.acc[i][j][e] * a.scale : kNegInf;
                 if (p == target && p < a.classes) a.out.target[row] = z;
                 if (BEST) b.at = z > b.m ? p : b.at;
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(Tl::THREADS) head_tile_kernel(HeadTileArgs a) 
             for (int i = 0; i < Tl::RP; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int p = p0 + Tl::p_of(i, e >> 2) + (e & 3);
+                    const int p = p0 + Tl::p_of(tid, i, e >> 2) + (e & 3);
                     if (p < a.classes && t.acc[i][j][e] == kNegInf) b.at = min(b.at, p);
                 }
         }
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(Tl::THREADS) head_tile_kernel(HeadTileArgs a) 
             for (int e = 0; e < 16; ++e) b.s += exp_of(t.acc[i][j][e] - o);
         if (BEST && b.at != kNoIndex) b.at += a.first;
         b = join(b, from_lane(b, 32));
-        if (lane < 32) red[wp * Tl::BQ + Tl::q_of(j)] = b;
+        if (lane < 32) red[wp * Tl::BQ + Tl::q_of(tid, j)] = b;
     }
     __syncthreads();
     for (int q = threadIdx.x; q < Tl::BQ; q += Tl::THREADS) {
@@ -353,7 +353,7 @@ struct HeadGradTileArgs {
 
 // dz of a tile, and its transpose, in T: the products that follow take it as their operand.
 template <typename T, typename Tl>
-__global__ void __launch_bounds__(Tl::THREADS) head_grad_kernel(HeadGradTileArgs g) {
+__global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileArgs g) {
     __shared__ __attribute__((aligned(128))) char lds[Tl::BYTES];
     const HeadTileArgs& a = g.z;
     int tp, tq;
@@ -363,14 +363,15 @@ __global__ void __launch_bounds__(Tl::THREADS) head_grad_kernel(HeadGradTileArgs
     Tl t;
     t.run((char KAN_LDS*)lds, tile_rows(a.w, p0, a.classes, Tl::BP, a.wstride, a.k_bytes),
           tile_rows(a.x, q0, a.rows, Tl::BQ, a.xstride, a.k_bytes), 0, a.k_bytes);
-    T* const dz = static_cast<T*>(g.dz);
-    T* const dzt = static_cast<T*>(g.dzt);
+    const int tid = Tl::thread();
+    constexpr int V = kVec<T>, U = Tl::BP / V;
+    constexpr int PITCH = Tl::template PITCH<T>;
 #pragma unroll
     for (int j = 0; j < Tl::RQ; ++j) {
-        const int64_t row = q0 + Tl::q_of(j);
+        const int64_t row = q0 + Tl::q_of(tid, j);
         // (rows that have no gradient: p = 0, whatever their logits are)
         float m = __builtin_huge_valf(), logs = 0.0f, d = 0.0f;
-        int64_t target = -1;
+        int target = -1;
         if (row < a.rows) {
             const int64_t c = a.targets[row];
             const float rm = g.stats[2 * row], rl = g.stats[2 * row + 1];
@@ -378,30 +379,43 @@ __global__ void __launch_bounds__(Tl::THREADS) head_grad_kernel(HeadGradTileArgs
                 // (a target that is no class, NaN and infinite logits show in the row's gradient)
                 d = c < 0 || c >= g.all || rm != rm || rl != rl ? __builtin_nanf("") : g.dlogp[row];
                 if (rm == kNegInf && rl == kNegInf && d == d) d = 0.0f;
-                else m = rm, logs = rl, target = c - a.first;
+                else m = rm, logs = rl, target = (int)c - a.first;
             }
         }
-#pragma unroll
-        for (int i = 0; i < Tl::RP; ++i)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int p = p0 + Tl::p_of(i, v);
-                T o[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float z = t.acc[i][j][4 * v + e] * a.scale;
-                    const float pr = exp_exact(__builtin_fmaxf(z - m - logs, -1e4f));
-                    const float y = p + e == target ? d - d * pr : -d * pr;
-                    o[e] = rounded<T>(p + e < a.classes ? y : 0.0f);
-                }
-                if (dz != nullptr && row < a.rows && p < g.zstride)
-                    store_four(dz + row * g.zstride + p, 4, o);
-                if (dzt != nullptr && row < g.tstride) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (p + e < a.classes) dzt[(int64_t)(p + e) * g.tstride + row] = o[e];
-                }
+        const int p1 = p0 + Tl::p_of(tid, 0, 0), classes = a.classes - p1;
+        target -= p1;
+        t.template put<T>(lds, tid, j, [&](int i, int e, float z) {
+            const int p = i * 32 + 8 * (e >> 2) + (e & 3);
+            const float pr = exp_exact(__builtin_fmaxf(z * a.scale - m - logs, -1e4f));
+            return rounded<T>(p >= classes ? 0.0f : p == target ? d - d * pr : -d * pr);
+        });
+        __syncthreads();
+        if (g.dz != nullptr) {
+            for (int u = tid; u < Tl::ROWS * U; u += Tl::THREADS) {
+                const int r = u / U, p = (u % U) * V;
+                const int64_t q = q0 + Tl::q_of_row(r, j);
+                if (q < a.rows && p0 + p < g.zstride)
+                    *reinterpret_cast<u32x4*>(static_cast<T*>(g.dz) + q * g.zstride + p0 + p) =
+                        *reinterpret_cast<const u32x4*>(lds + r * PITCH + p * (int)sizeof(T));
             }
+        }
+        if (g.dzt != nullptr) {
+            constexpr int UQ = Tl::ROWS / V;
+            for (int u = tid; u < Tl::BP * UQ; u += Tl::THREADS) {
+                const int p = u / UQ, r = (u % UQ) * V;
+                const int64_t q = q0 + Tl::q_of_row(r, j);
+                if (p0 + p >= a.classes || q >= g.tstride) continue;
+                T v[V];
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    v[k] = *reinterpret_cast<const T*>(lds + (r + k) * PITCH + p * (int)sizeof(T));
+                u32x4 w;
+                __builtin_memcpy(&w, v, 16);
+                *reinterpret_cast<u32x4*>(static_cast<T*>(g.dzt) + (int64_t)(p0 + p) * g.tstride + q) =
+                    w;
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -419,7 +433,7 @@ struct ProductArgs {
 
 // out = scale (sum over k + acc), or acc (+)= the sum over a split's k.
 template <typename T, typename Tl>
-__global__ void __launch_bounds__(Tl::THREADS) head_product_kernel(ProductArgs a) {
+__global__ void __launch_bounds__(Tl::THREADS, 2) head_product_kernel(ProductArgs a) {
     __shared__ __attribute__((aligned(128))) char lds[Tl::BYTES];
     const int tiles = a.tp * a.tq, split = blockIdx.x / tiles;
     int tp, tq;
@@ -431,32 +445,41 @@ __global__ void __launch_bounds__(Tl::THREADS) head_product_kernel(ProductArgs a
     t.run((char KAN_LDS*)lds, tile_rows(a.p, p0, a.np, Tl::BP, a.pstride, a.k_bytes),
           tile_rows(a.q, q0, a.nq, Tl::BQ, a.qstride, a.k_bytes), k0,
           a.k_bytes - k0 < a.k_split ? a.k_bytes - k0 : a.k_split);
+    const int tid = Tl::thread();
+    constexpr int U = Tl::BP / 4, PITCH = Tl::template PITCH<float>;
 #pragma unroll
     for (int j = 0; j < Tl::RQ; ++j) {
-        const int64_t q = q0 + Tl::q_of(j);
-        if (q >= a.nq) continue;
-        float* const acc = a.acc == nullptr ? nullptr : a.acc + (split * a.nq + q) * a.np;
+        t.template put<float>(lds, tid, j, [](int, int, float v) { return v; });
+        __syncthreads();
+        for (int u = tid; u < Tl::ROWS * U; u += Tl::THREADS) {
+            const int r = u / U, c = (u % U) * 4;
+            const int64_t q = q0 + Tl::q_of_row(r, j), left = a.np - p0 - c;
+            if (q >= a.nq || left <= 0) continue;
+            const floatx4 v = *reinterpret_cast<const floatx4*>(lds + r * PITCH + c * 4);
+            float o[4] = {v[0], v[1], v[2], v[3]};
+            float* const acc = a.acc + (split * a.nq + q) * a.np + p0 + c;
+            if (a.add) {
+                if (left >= 4) {
+                    typedef float four __attribute__((ext_vector_type(4), aligned(4)));
+                    const four w = *reinterpret_cast<const four*>(acc);
 #pragma unroll
-        for (int i = 0; i < Tl::RP; ++i)
+                    for (int e = 0; e < 4; ++e) o[e] += w[e];
+                } else {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int64_t p = p0 + Tl::p_of(i, v), left = a.np - p;
-                if (left <= 0) continue;
-                float o[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    o[e] = t.acc[i][j][4 * v + e];
-                    if (a.add && e < left) o[e] += acc[p + e];
+                    for (int e = 0; e < 3; ++e)
+                        if (e < left) o[e] += acc[e];
                 }
-                if (a.out == nullptr) {
-                    store_four(acc + p, left, o);
-                    continue;
-                }
-                T r[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) r[e] = rounded<T>(o[e] * a.scale);
-                store_four(static_cast<T*>(a.out) + q * a.np + p, left, r);
             }
+            if (a.out == nullptr) {
+                store_four(acc, left, o);
+                continue;
+            }
+            T w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = rounded<T>(o[e] * a.scale);
+            store_four(static_cast<T*>(a.out) + q * a.np + p0 + c, left, w);
+        }
+        __syncthreads();
     }
 }
 

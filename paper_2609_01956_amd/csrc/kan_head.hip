@@ -62,73 +62,138 @@ __device__ __forceinline__ void leave(const Parts& o, int64_t part, int64_t rows
     if (o.best != nullptr) o.best[part * rows + row] = b.at;
 }
 
-struct HeadTileArgs {
+template <typename T> using BigLogits = Tile<T, 2, 4, 4, 2, kByRows, kByRows>;  // 256 x 256
+template <typename T> using SmallLogits = Tile<T, 2, 2, 2, 2, kByRows, kByRows>;  // 128 x 128
+
+// The tiles of rows x classes logits.
+struct LogitArgs {
     const void *x, *w;
     int64_t rows, xstride, wstride;  // bytes from row to row
     int classes;                     // of this launch, from class `first` on
     int first;
-    int k_bytes;
+    int k;                           // elements of a row, with its padding
     int tp, tq;
     float scale;
     const int64_t* targets;
+};
+
+// Each workgroup's tiles, one after the other: ready(tile, p, q) with the products of tile (p, q),
+// after ahead() there has begun the next one's loads, which from then on own the first Tl::STEP bytes
+// of lds.
+template <typename T, typename Tl, typename F>
+__device__ __forceinline__ void for_tiles(const LogitArgs& a, char* lds, F&& ready) {
+    char KAN_LDS* const to = (char KAN_LDS*)lds;
+    const int tiles = a.tp * a.tq;
+    int tp, tq;
+    Operand p, q;
+    const auto find = [&](int id) {
+        tile_of(id, a.tp, a.tq, &tp, &tq);
+        p = operand<T, kByRows>(a.w, (int64_t)tp * Tl::BP, a.classes, Tl::BP, a.wstride);
+        q = operand<T, kByRows>(a.x, (int64_t)tq * Tl::BQ, a.rows, Tl::BQ, a.xstride);
+    };
+    Tl t;
+    find(blockIdx.x);
+    t.start(to, p, q, 0, a.k);
+    for (int id = blockIdx.x; id < tiles; id += gridDim.x) {
+        t.run(to, p, q, 0, a.k);
+        const int here_p = tp, here_q = tq;
+        ready(t, here_p, here_q, [&] {
+            if (id + (int)gridDim.x >= tiles) return;
+            find(id + gridDim.x);
+            t.start(to, p, q, 0, a.k);
+        });
+    }
+}
+
+// Makes acc the logits over c, with c > 0 returned, and those of classes past the end `none`.
+template <typename Tl>
+__device__ __forceinline__ float settle(Tl& t, const LogitArgs& a, int p0, int tid, float none) {
+    if (a.scale > 0.0f && p0 + Tl::BP <= a.classes) return a.scale;
+    const int classes = a.classes - p0 - Tl::p_of(tid);
+#pragma unroll
+    for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+        for (int j = 0; j < Tl::RQ; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                t.acc[i][j][e] = Tl::p_step(i, e) < classes ? t.acc[i][j][e] * a.scale : none;
+    return 1.0f;
+}
+
+struct HeadTileArgs {
+    LogitArgs z;
     Parts out;
     int64_t part;  // of the first tile
 };
 
+// Bound by the matrix cores; what the logits cost after the products is four operations and an
+// exponential each, while the next tile's first loads are on their way.
 template <typename T, typename Tl, bool BEST>
-__global__ void __launch_bounds__(Tl::THREADS, 2) head_tile_kernel(HeadTileArgs a) {
+__global__ void __launch_bounds__(Tl::THREADS, 2) head_tile_kernel(HeadTileArgs h) {
     __shared__ __attribute__((aligned(128))) char lds[Tl::BYTES];
-    int tp, tq;
-    tile_of(blockIdx.x, a.tp, a.tq, &tp, &tq);
-    const int64_t q0 = (int64_t)tq * Tl::BQ;
-    const int p0 = tp * Tl::BP;
-    Tl t;
-    t.run((char KAN_LDS*)lds, tile_rows(a.w, p0, a.classes, Tl::BP, a.wstride, a.k_bytes),
-          tile_rows(a.x, q0, a.rows, Tl::BQ, a.xstride, a.k_bytes), 0, a.k_bytes);
-    Best* const red = reinterpret_cast<Best*>(lds);  // [WP][BQ]
-    const int tid = Tl::thread(), lane = tid & 63, wp = (tid >> 6) % Tl::WP;
+    const LogitArgs& a = h.z;
+    Best* const red = reinterpret_cast<Best*>(lds + Tl::STEP);  // [WP][BQ]
+    static_assert(Tl::STEP + Tl::WP * Tl::BQ * (int)sizeof(Best) <= Tl::BYTES, "LDS");
+    for_tiles<T, Tl>(a, lds, [&](Tl& t, int tp, int tq, auto&& ahead) {
+        const int tid = Tl::thread(), p0 = tp * Tl::BP, p1 = p0 + Tl::p_of(tid);
+        const int64_t q0 = (int64_t)tq * Tl::BQ;
+        int64_t target[Tl::RQ];
 #pragma unroll
-    for (int j = 0; j < Tl::RQ; ++j) {
-        const int64_t row = q0 + Tl::q_of(tid, j);
-        const int64_t target = row < a.rows ? a.targets[row] - a.first : -1;
-        Best b = {kNegInf, 0.0f, kNoIndex};
+        for (int j = 0; j < Tl::RQ; ++j) {
+            const int64_t row = q0 + Tl::q_of(tid, j);
+            target[j] = row < a.rows ? a.targets[row] - a.first : -1;
+        }
+        ahead();
+        const float scale = settle(t, a, p0, tid, kNegInf);
 #pragma unroll
-        for (int i = 0; i < Tl::RP; ++i)
+        for (int j = 0; j < Tl::RQ; ++j) {
+            const int64_t row = q0 + Tl::q_of(tid, j);
+            if (target[j] >= p0 && target[j] < p0 + Tl::BP && target[j] < a.classes) {
+                const int p = (int)target[j] - p1;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int p = p0 + Tl::p_of(tid, i, e >> 2) + (e & 3);
-                const float z = p < a.classes ? t.acc[i][j][e] * a.scale : kNegInf;
-                if (p == target && p < a.classes) a.out.target[row] = z;
-                if (BEST) b.at = z > b.m ? p : b.at;
-                b.m = __builtin_fmaxf(b.m, z);
-                t.acc[i][j][e] = z;
+                for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (p == Tl::p_step(i, e)) h.out.target[row] = t.acc[i][j][e] * scale;
             }
-        if (BEST && b.at == kNoIndex) {  // (nothing above -infinity: its first class there)
+            Best b = {kNegInf, 0.0f, kNoIndex};
 #pragma unroll
             for (int i = 0; i < Tl::RP; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int p = p0 + Tl::p_of(tid, i, e >> 2) + (e & 3);
-                    if (p < a.classes && t.acc[i][j][e] == kNegInf) b.at = min(b.at, p);
+                    if (BEST) b.at = t.acc[i][j][e] > b.m ? Tl::p_step(i, e) : b.at;
+                    b.m = __builtin_fmaxf(b.m, t.acc[i][j][e]);
                 }
+            if (BEST && b.at == kNoIndex) {  // (nothing above -infinity: its first class there)
+#pragma unroll
+                for (int i = Tl::RP - 1; i >= 0; --i)
+#pragma unroll
+                    for (int e = 15; e >= 0; --e)
+                        if (t.acc[i][j][e] == kNegInf && p1 + Tl::p_step(i, e) < a.classes)
+                            b.at = Tl::p_step(i, e);
+            }
+            if (BEST && b.at != kNoIndex) b.at += p1 + a.first;
+            b.m *= scale;
+            // (a logit less m with one rounding)
+            const float o = -anchor(b.m);
+#pragma unroll
+            for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    b.s += exp_of(__builtin_fmaf(t.acc[i][j][e], scale, o));
+            b = join(b, from_lane(b, 32));
+            if ((tid & 63) < 32) red[((tid >> 6) % Tl::WP) * Tl::BQ + Tl::q_of(tid, j)] = b;
         }
-        const float o = anchor(b.m);
+        Tl::meet();
+        for (int q = tid; q < Tl::BQ; q += Tl::THREADS) {
+            if (q0 + q >= a.rows) break;
+            Best b = red[q];
 #pragma unroll
-        for (int i = 0; i < Tl::RP; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) b.s += exp_of(t.acc[i][j][e] - o);
-        if (BEST && b.at != kNoIndex) b.at += a.first;
-        b = join(b, from_lane(b, 32));
-        if (lane < 32) red[wp * Tl::BQ + Tl::q_of(tid, j)] = b;
-    }
-    __syncthreads();
-    for (int q = threadIdx.x; q < Tl::BQ; q += Tl::THREADS) {
-        if (q0 + q >= a.rows) break;
-        Best b = red[q];
-#pragma unroll
-        for (int i = 1; i < Tl::WP; ++i) b = join(b, red[i * Tl::BQ + q]);
-        leave(a.out, a.part + tp, a.rows, q0 + q, b);
-    }
+            for (int i = 1; i < Tl::WP; ++i) b = join(b, red[i * Tl::BQ + q]);
+            leave(h.out, h.part + tp, a.rows, q0 + q, b);
+        }
+        Tl::meet();
+    });
 }
 
 // ------------------------------------------------------------ few rows
@@ -342,88 +407,102 @@ __device__ __forceinline__ void store_four(T* at, int64_t left, const T (&v)[4])
 }
 
 struct HeadGradTileArgs {
-    HeadTileArgs z;  // (its `out` and `part` are not used)
+    LogitArgs z;
     const float *stats, *dlogp;
     int64_t ignore;
-    int all;    // classes
-    void* dz;   // [rows][zstride], or null; 0 past the classes
-    void* dzt;  // [classes][tstride], or null; 0 past the rows
-    int64_t zstride, tstride;  // elements
+    int all;          // classes
+    void* dz;         // [rows][zstride], 0 past the classes
+    int64_t zstride;  // elements, a multiple of 16 bytes
 };
 
-// dz of a tile, and its transpose, in T: the products that follow take it as their operand.
+// dz of the tiles in T, the operand of the products that follow.  Its rows go through LDS, so that
+// they are stored by whole lines, while the next tile's first loads are on their way (bf16; fp32
+// rows take all of LDS).
 template <typename T, typename Tl>
 __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileArgs g) {
-    __shared__ __attribute__((aligned(128))) char lds[Tl::BYTES];
-    const HeadTileArgs& a = g.z;
-    int tp, tq;
-    tile_of(blockIdx.x, a.tp, a.tq, &tp, &tq);
-    const int64_t q0 = (int64_t)tq * Tl::BQ;
-    const int p0 = tp * Tl::BP;
-    Tl t;
-    t.run((char KAN_LDS*)lds, tile_rows(a.w, p0, a.classes, Tl::BP, a.wstride, a.k_bytes),
-          tile_rows(a.x, q0, a.rows, Tl::BQ, a.xstride, a.k_bytes), 0, a.k_bytes);
-    const int tid = Tl::thread();
-    constexpr int V = kVec<T>, U = Tl::BP / V;
-    constexpr int PITCH = Tl::template PITCH<T>;
-#pragma unroll
-    for (int j = 0; j < Tl::RQ; ++j) {
-        const int64_t row = q0 + Tl::q_of(tid, j);
+    constexpr bool AHEAD = sizeof(T) == 2;
+    constexpr int V = kVec<T>, U = Tl::BP / V, PITCH = Tl::template PITCH<T>;
+    constexpr int AT = AHEAD ? Tl::STEP : 0, NEED = AT + Tl::ROWS * PITCH;
+    __shared__ __attribute__((aligned(128))) char lds[NEED > Tl::BYTES ? NEED : Tl::BYTES];
+    const LogitArgs& a = g.z;
+    for_tiles<T, Tl>(a, lds, [&](Tl& t, int tp, int tq, auto&& ahead) {
+        const int tid = Tl::thread(), p0 = tp * Tl::BP, p1 = p0 + Tl::p_of(tid);
+        const int64_t q0 = (int64_t)tq * Tl::BQ;
         // (rows that have no gradient: p = 0, whatever their logits are)
-        float m = __builtin_huge_valf(), logs = 0.0f, d = 0.0f;
-        int target = -1;
-        if (row < a.rows) {
+        float m[Tl::RQ], logs[Tl::RQ], d[Tl::RQ];
+        int target[Tl::RQ];
+#pragma unroll
+        for (int j = 0; j < Tl::RQ; ++j) {
+            const int64_t row = q0 + Tl::q_of(tid, j);
+            m[j] = __builtin_huge_valf();
+            logs[j] = d[j] = 0.0f;
+            target[j] = -1;
+            if (row >= a.rows) continue;
             const int64_t c = a.targets[row];
-            const float rm = g.stats[2 * row], rl = g.stats[2 * row + 1];
-            if (c != g.ignore) {
-                // (a target that is no class, NaN and infinite logits show in the row's gradient)
-                d = c < 0 || c >= g.all || rm != rm || rl != rl ? __builtin_nanf("") : g.dlogp[row];
-                if (rm == kNegInf && rl == kNegInf && d == d) d = 0.0f;
-                else m = rm, logs = rl, target = (int)c - a.first;
+            const float rm = g.stats[2 * row], rl = g.stats[2 * row + 1], rd = g.dlogp[row];
+            if (c == g.ignore) continue;
+            // (a target that is no class, NaN and infinite logits show in the row's gradient)
+            d[j] = c < 0 || c >= g.all || rm != rm || rl != rl ? __builtin_nanf("") : rd;
+            if (rm == kNegInf && rl == kNegInf && d[j] == d[j]) {
+                d[j] = 0.0f;
+            } else {
+                m[j] = rm;
+                logs[j] = rl;
+                target[j] = (int)c - a.first;
             }
         }
-        const int p1 = p0 + Tl::p_of(tid, 0, 0), classes = a.classes - p1;
-        target -= p1;
-        t.template put<T>(lds, tid, j, [&](int i, int e, float z) {
-            const int p = i * 32 + 8 * (e >> 2) + (e & 3);
-            const float pr = exp_exact(__builtin_fmaxf(z * a.scale - m - logs, -1e4f));
-            return rounded<T>(p >= classes ? 0.0f : p == target ? d - d * pr : -d * pr);
-        });
-        __syncthreads();
-        if (g.dz != nullptr) {
+        if (AHEAD) ahead();
+        const float scale = settle(t, a, p0, tid, kNegInf);
+#pragma unroll
+        for (int j = 0; j < Tl::RQ; ++j) {
+            // (in bf16 p's own rounding hides that of the exponential's argument)
+            const float o = AHEAD ? m[j] + logs[j] : m[j];
+#pragma unroll
+            for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float z = __builtin_fmaf(t.acc[i][j][e], scale, -o);
+                    t.acc[i][j][e] = -d[j] * (AHEAD ? exp_of(__builtin_fmaxf(z, -1e4f))
+                                                    : exp_exact(__builtin_fmaxf(z - logs[j], -1e4f)));
+                }
+            if (target[j] >= p0 && target[j] < p0 + Tl::BP) {
+                const int p = target[j] - p1;
+#pragma unroll
+                for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        t.acc[i][j][e] += p == Tl::p_step(i, e) ? d[j] : 0.0f;
+            }
+            if (p0 + Tl::BP > a.classes) {
+                const int classes = a.classes - p1;
+#pragma unroll
+                for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (Tl::p_step(i, e) >= classes) t.acc[i][j][e] = 0.0f;
+            }
+            t.template put<T>(lds + AT, tid, j, [](float v) { return rounded<T>(v); });
+            Tl::meet();
             for (int u = tid; u < Tl::ROWS * U; u += Tl::THREADS) {
                 const int r = u / U, p = (u % U) * V;
                 const int64_t q = q0 + Tl::q_of_row(r, j);
                 if (q < a.rows && p0 + p < g.zstride)
                     *reinterpret_cast<u32x4*>(static_cast<T*>(g.dz) + q * g.zstride + p0 + p) =
-                        *reinterpret_cast<const u32x4*>(lds + r * PITCH + p * (int)sizeof(T));
+                        *reinterpret_cast<const u32x4*>(lds + AT + r * PITCH + p * (int)sizeof(T));
             }
+            Tl::meet();
         }
-        if (g.dzt != nullptr) {
-            constexpr int UQ = Tl::ROWS / V;
-            for (int u = tid; u < Tl::BP * UQ; u += Tl::THREADS) {
-                const int p = u / UQ, r = (u % UQ) * V;
-                const int64_t q = q0 + Tl::q_of_row(r, j);
-                if (p0 + p >= a.classes || q >= g.tstride) continue;
-                T v[V];
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-                    v[k] = *reinterpret_cast<const T*>(lds + (r + k) * PITCH + p * (int)sizeof(T));
-                u32x4 w;
-                __builtin_memcpy(&w, v, 16);
-                *reinterpret_cast<u32x4*>(static_cast<T*>(g.dzt) + (int64_t)(p0 + p) * g.tstride + q) =
-                    w;
-            }
-        }
-        __syncthreads();
-    }
+        if (!AHEAD) ahead();
+    });
 }
 
+// out[q][p] = scale (sum over k of P(p, k) Q(q, k) + acc), or acc (+)= the sum over a split's k.
 struct ProductArgs {
-    const void *p, *q;          // [np] and [nq] rows of k_bytes
-    int64_t pstride, qstride;   // bytes
-    int64_t np, nq;
-    int64_t k_bytes, k_split;   // bytes of k in all, and of a split
+    const void *p, *q;
+    int64_t pstride, qstride;  // bytes
+    int64_t np, nq, k;
+    int64_t pk, qk;            // rows of an operand that stands by k
+    int64_t k_split;           // k of a split
     int tp, tq;
     float* acc;  // [splits][nq][np], or null
     bool add;    // to what acc holds
@@ -431,33 +510,33 @@ struct ProductArgs {
     float scale;
 };
 
-// out = scale (sum over k + acc), or acc (+)= the sum over a split's k.
-template <typename T, typename Tl>
+template <typename T, typename Tl, int MP, int MQ>
 __global__ void __launch_bounds__(Tl::THREADS, 2) head_product_kernel(ProductArgs a) {
-    __shared__ __attribute__((aligned(128))) char lds[Tl::BYTES];
+    constexpr int U = Tl::BP / 4, PITCH = Tl::template PITCH<float>, NEED = Tl::ROWS * PITCH;
+    __shared__ __attribute__((aligned(128))) char lds[NEED > Tl::BYTES ? NEED : Tl::BYTES];
     const int tiles = a.tp * a.tq, split = blockIdx.x / tiles;
     int tp, tq;
     tile_of(blockIdx.x - split * tiles, a.tp, a.tq, &tp, &tq);
     const int64_t q0 = (int64_t)tq * Tl::BQ, p0 = (int64_t)tp * Tl::BP;
-    const int64_t k0 = split * a.k_split;
-    if (k0 >= a.k_bytes) return;  // (a last piece that is shorter: nothing to add)
+    const int64_t k0 = split * a.k_split, k1 = a.k - k0 < a.k_split ? a.k : k0 + a.k_split;
+    if (k0 >= a.k) return;  // (a last piece that is shorter: nothing to add)
+    const Operand p = operand<T, MP>(a.p, p0, a.np, Tl::BP, a.pstride, a.pk);
+    const Operand q = operand<T, MQ>(a.q, q0, a.nq, Tl::BQ, a.qstride, a.qk);
     Tl t;
-    t.run((char KAN_LDS*)lds, tile_rows(a.p, p0, a.np, Tl::BP, a.pstride, a.k_bytes),
-          tile_rows(a.q, q0, a.nq, Tl::BQ, a.qstride, a.k_bytes), k0,
-          a.k_bytes - k0 < a.k_split ? a.k_bytes - k0 : a.k_split);
+    t.start((char KAN_LDS*)lds, p, q, k0, k1);
+    t.run((char KAN_LDS*)lds, p, q, k0, k1);
     const int tid = Tl::thread();
-    constexpr int U = Tl::BP / 4, PITCH = Tl::template PITCH<float>;
 #pragma unroll
     for (int j = 0; j < Tl::RQ; ++j) {
-        t.template put<float>(lds, tid, j, [](int, int, float v) { return v; });
-        __syncthreads();
+        t.template put<float>(lds, tid, j, [](float v) { return v; });
+        Tl::meet();
         for (int u = tid; u < Tl::ROWS * U; u += Tl::THREADS) {
             const int r = u / U, c = (u % U) * 4;
-            const int64_t q = q0 + Tl::q_of_row(r, j), left = a.np - p0 - c;
-            if (q >= a.nq || left <= 0) continue;
+            const int64_t row = q0 + Tl::q_of_row(r, j), left = a.np - p0 - c;
+            if (row >= a.nq || left <= 0) continue;
             const floatx4 v = *reinterpret_cast<const floatx4*>(lds + r * PITCH + c * 4);
             float o[4] = {v[0], v[1], v[2], v[3]};
-            float* const acc = a.acc + (split * a.nq + q) * a.np + p0 + c;
+            float* const acc = a.acc + (split * a.nq + row) * a.np + p0 + c;
             if (a.add) {
                 if (left >= 4) {
                     typedef float four __attribute__((ext_vector_type(4), aligned(4)));
@@ -477,9 +556,9 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_product_kernel(ProductArg
             T w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = rounded<T>(o[e] * a.scale);
-            store_four(static_cast<T*>(a.out) + q * a.np + p0 + c, left, w);
+            store_four(static_cast<T*>(a.out) + row * a.np + p0 + c, left, w);
         }
-        __syncthreads();
+        Tl::meet();
     }
 }
 
@@ -519,10 +598,12 @@ __global__ void __launch_bounds__(256) head_zero_kernel(T* out, int64_t n) {
 
 // ------------------------------------------------------------ rows laid out for the tiles
 
-// Rows of n elements copied to rows of `to` elements (a multiple of 16 bytes), 0 past n.
+// Rows of n elements copied to rows of `to` elements (a multiple of 16 bytes), 0 past n; 0
+// throughout for rows whose target is `ignore` (targets null: none).
 template <typename T>
 __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, int64_t stride, int64_t rows,
-                                                        int n, T* out, int to) {
+                                                        int n, T* out, int to,
+                                                        const int64_t* targets, int64_t ignore) {
     constexpr int V = kVec<T>;
     const int units = to / V;
     const int64_t all = rows * units;
@@ -530,42 +611,9 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, int64_t stri
          i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / units;
         const int c = (int)(i - row * units) * V;
-        *reinterpret_cast<u32x4*>(out + row * to + c) = chunk_of(x + row * stride, c, n);
-    }
-}
-
-// out[c][r] = x[r][c], 0 from `rows` to `to`; 0 also for rows whose target is `ignore` (targets
-// null: none).  64 x 64 elements a workgroup.
-template <typename T>
-__global__ void __launch_bounds__(256) head_turn_kernel(const T* x, int64_t stride, int64_t rows,
-                                                        int n, T* out, int64_t to,
-                                                        const int64_t* targets, int64_t ignore,
-                                                        int across) {
-    constexpr int V = kVec<T>, U = 64 / V;
-    __shared__ T tile[64][64 + 4 / sizeof(T)];
-    const int64_t r0 = (int64_t)(blockIdx.x / across) * 64;
-    const int c0 = (blockIdx.x % across) * 64;
-    for (int i = threadIdx.x; i < 64 * U; i += 256) {
-        const int64_t row = r0 + i / U;
-        const int c = c0 + (i % U) * V;
         u32x4 v = {0, 0, 0, 0};
-        if (row < rows && c < n && (targets == nullptr || targets[row] != ignore))
-            v = chunk_of(x + row * stride, c, n);
-        T e[V];
-        __builtin_memcpy(e, &v, 16);
-#pragma unroll
-        for (int k = 0; k < V; ++k) tile[i / U][(i % U) * V + k] = e[k];
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 64 * U; i += 256) {
-        const int c = i / U, r = (i % U) * V;
-        if (c0 + c >= n || r0 + r >= to) continue;
-        T e[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) e[k] = tile[r + k][c];
-        u32x4 v;
-        __builtin_memcpy(&v, e, 16);
-        *reinterpret_cast<u32x4*>(out + (int64_t)(c0 + c) * to + r0 + r) = v;
+        if (targets == nullptr || targets[row] != ignore) v = chunk_of(x + row * stride, c, n);
+        *reinterpret_cast<u32x4*>(out + row * to + c) = v;
     }
 }
 
@@ -586,12 +634,10 @@ struct Arena {
     }
 };
 
-template <typename T> using Big = Tile<T, 2, 4, 4, 2>;    // 256 x 256
-template <typename T> using Small = Tile<T, 2, 2, 2, 2>;  // 128 x 128
-constexpr int kBig = 256, kSmall = 128;
+constexpr int kBig = 256, kSmall = 128;  // a tile's sides
 constexpr int kThinRows = 64;
 // Bytes of a piece's intermediate tensors.
-constexpr int64_t kPieceBytes = INT64_C(256) << 20;
+constexpr int64_t kPieceBytes = INT64_C(512) << 20;
 constexpr int64_t kPieceClasses = 1 << 20, kPieceTiles = 1 << 20;
 constexpr int kFillTiles = 256;  // tiles that occupy the GPU
 
@@ -635,19 +681,9 @@ int grid_of(int64_t items, int per) { return (int)std::min<int64_t>(div_up(items
 
 template <typename T>
 hipError_t pack(const void* x, int64_t stride, int64_t rows, int n, void* out, int to,
-                hipStream_t st) {
-    head_pack_kernel<T><<<grid_of(rows * (to / kVec<T>), 256), 256, 0, st>>>(
-        static_cast<const T*>(x), stride, rows, n, static_cast<T*>(out), to);
-    return hipGetLastError();
-}
-
-template <typename T>
-hipError_t turn(const void* x, int64_t stride, int64_t rows, int n, void* out, int64_t to,
                 const int64_t* targets, int64_t ignore, hipStream_t st) {
-    const int across = (int)div_up(n, 64);
-    head_turn_kernel<T><<<(int)(div_up(to, 64) * across), 256, 0, st>>>(
-        static_cast<const T*>(x), stride, rows, n, static_cast<T*>(out), to, targets, ignore,
-        across);
+    head_pack_kernel<T><<<grid_of(rows * (to / kVec<T>), 256), 256, 0, st>>>(
+        static_cast<const T*>(x), stride, rows, n, static_cast<T*>(out), to, targets, ignore);
     return hipGetLastError();
 }
 
@@ -666,10 +702,14 @@ hipError_t thin(const HeadPlan& p, const HeadThinArgs& a, bool best, hipStream_t
     return hipGetLastError();
 }
 
+// Workgroups that are resident together: one of a big tile on a CU, or two of a small one.
+int resident(int tiles, bool big) { return std::min(tiles, big ? kFillTiles : 2 * kFillTiles); }
+
 template <typename T, typename Tl>
-hipError_t tiles(const HeadTileArgs& a, bool best, hipStream_t st) {
-    if (best) head_tile_kernel<T, Tl, true><<<a.tp * a.tq, Tl::THREADS, 0, st>>>(a);
-    else head_tile_kernel<T, Tl, false><<<a.tp * a.tq, Tl::THREADS, 0, st>>>(a);
+hipError_t tiles(const HeadTileArgs& a, bool best, bool big, hipStream_t st) {
+    const int groups = resident(a.z.tp * a.z.tq, big);
+    if (best) head_tile_kernel<T, Tl, true><<<groups, Tl::THREADS, 0, st>>>(a);
+    else head_tile_kernel<T, Tl, false><<<groups, Tl::THREADS, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -694,29 +734,31 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
                              : s.rows <= 32 ? thin<T, 2>(p, t, best, st) : thin<T, 4>(p, t, best, st));
     } else {
         HeadTileArgs t = {};
-        t.x = p.xp != nullptr ? p.xp : a.x;
-        t.xstride = (p.xp != nullptr ? p.to : s.xstride) * s.es;
-        t.wstride = (p.wp != nullptr ? p.to : s.wstride) * s.es;
-        t.rows = s.rows;
-        t.k_bytes = p.to * s.es;
-        t.scale = a.scale;
-        t.targets = a.targets;
+        t.z.x = p.xp != nullptr ? p.xp : a.x;
+        t.z.xstride = (p.xp != nullptr ? p.to : s.xstride) * s.es;
+        t.z.wstride = (p.wp != nullptr ? p.to : s.wstride) * s.es;
+        t.z.rows = s.rows;
+        t.z.k = p.to;
+        t.z.scale = a.scale;
+        t.z.targets = a.targets;
         t.out = p.out;
         const int b = p.big ? kBig : kSmall;
-        t.tq = (int)div_up(s.rows, b);
-        if (p.xp != nullptr) KAN_TRY(pack<T>(a.x, s.xstride, s.rows, s.n, p.xp, p.to, st));
+        t.z.tq = (int)div_up(s.rows, b);
+        if (p.xp != nullptr)
+            KAN_TRY(pack<T>(a.x, s.xstride, s.rows, s.n, p.xp, p.to, nullptr, 0, st));
         for (int64_t first = 0; first < s.classes; first += p.piece) {
-            t.first = (int)first;
-            t.classes = (int)std::min<int64_t>(s.classes - first, p.piece);
-            t.tp = (int)div_up(t.classes, b);
+            t.z.first = (int)first;
+            t.z.classes = (int)std::min<int64_t>(s.classes - first, p.piece);
+            t.z.tp = (int)div_up(t.z.classes, b);
             t.part = first / b;
-            t.w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
+            t.z.w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
             if (p.wp != nullptr) {
-                KAN_TRY(pack<T>(t.w, s.wstride, t.classes, s.n, p.wp, p.to, st));
-                t.w = p.wp;
+                KAN_TRY(pack<T>(t.z.w, s.wstride, t.z.classes, s.n, p.wp, p.to, nullptr, 0, st));
+                t.z.w = p.wp;
             }
-            KAN_TRY(p.big ? tiles<T, Big<T>>(t, a.best != nullptr, st)
-                          : tiles<T, Small<T>>(t, a.best != nullptr, st));
+            const bool best = a.best != nullptr;
+            KAN_TRY(p.big ? tiles<T, BigLogits<T>>(t, best, true, st)
+                          : tiles<T, SmallLogits<T>>(t, best, false, st));
         }
     }
     HeadJoinArgs j = {p.out, s.rows, (int)p.parts, s.classes, 1, a.targets, a.ignore, a.logp, a.stats,
@@ -730,30 +772,30 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
 struct ProductPlan {
     bool big;
     int tp, tq, splits;
-    int64_t k_split;  // bytes
+    int64_t k_split;
 };
-ProductPlan product_plan(int64_t np, int64_t nq, int64_t k_bytes) {
+ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, int es) {
     ProductPlan p;
+    const int step = 128 / es;
     p.big = div_up(np, kBig) * div_up(nq, kBig) >= kFillTiles;
     const int b = p.big ? kBig : kSmall;
     p.tp = (int)div_up(np, b);
     p.tq = (int)div_up(nq, b);
     // (a split takes at least eight steps)
-    const int64_t most = std::max<int64_t>(1, k_bytes / 1024);
+    const int64_t most = std::max<int64_t>(1, k / (8 * step));
     const int64_t want = p.big ? 1 : 2 * kFillTiles / ((int64_t)p.tp * p.tq);
     p.splits = (int)std::max<int64_t>(1, std::min(want, most));
-    p.k_split = up(div_up(k_bytes, p.splits), 128);
-    p.splits = (int)div_up(k_bytes, p.k_split);
+    p.k_split = up(div_up(k, p.splits), step);
+    p.splits = (int)div_up(k, p.k_split);
     return p;
 }
 
 struct HeadGradPlan {
-    int64_t piece, zstride, tstride;  // classes; elements
+    int64_t piece, zstride;  // classes; elements
     int to;
-    void *xp, *wp;   // packed rows, or null
-    void *xt, *wt;   // turned, or null
-    void *dz, *dzt;  // or null
-    float *dx, *dw;  // sums over k in parts, or null
+    void *xp, *wp;           // packed rows, or null
+    void* dz;
+    float *dx, *dw;          // sums over k in parts, or null
     ProductPlan px, pw;
     size_t bytes;
 };
@@ -762,38 +804,37 @@ HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
     HeadGradPlan p = {};
     Arena arena = {static_cast<char*>(ws)};
     p.to = (int)up(s.n, 16 / s.es);
-    p.tstride = up(s.rows, 64);
-    const int64_t row = s.es * ((dx ? p.tstride + s.n : 0) + (dw ? p.tstride : 0) + (s.ws ? 0 : p.to));
-    p.piece = std::min(kPieceClasses, kPieceTiles / div_up(s.rows, kSmall) * kSmall);
-    p.piece = std::min(p.piece, std::max<int64_t>(kPieceBytes / row / kBig * kBig, kBig));
-    p.piece = std::min(p.piece, up(s.classes, kBig));
+    // as few pieces as their dz (and packed weights) and launches allow, of one size
+    const int64_t row = s.es * (s.rows + (s.ws ? 0 : p.to));
+    int64_t most = std::min(kPieceClasses, kPieceTiles / div_up(s.rows, kSmall) * kSmall);
+    most = std::min(most, std::max<int64_t>(kPieceBytes / row / kBig * kBig, kBig));
+    p.piece = up(div_up(s.classes, div_up(s.classes, most)), kBig);
     p.zstride = std::min(p.piece, up(s.classes, 64));
-    if (!s.xs) p.xp = arena.take(s.rows * p.to * s.es);
+    const int64_t here = std::min<int64_t>(p.piece, s.classes);
+    // (a copy without what ignored rows hold: 0 times it need not be 0)
+    if (!s.xs || dw) p.xp = arena.take(s.rows * p.to * s.es);
     if (!s.ws) p.wp = arena.take(p.piece * p.to * s.es);
+    p.dz = arena.take(s.rows * p.zstride * s.es);
     if (dx) {
-        p.wt = arena.take(s.n * p.zstride * s.es);
-        p.dz = arena.take(s.rows * p.zstride * s.es);
-        p.px = product_plan(s.n, s.rows, p.zstride * s.es);
+        p.px = product_plan(s.n, s.rows, p.zstride, s.es);
         if (p.px.splits > 1 || p.piece < s.classes)
             p.dx = arena.take<float>((int64_t)p.px.splits * s.rows * s.n * 4);
     }
     if (dw) {
-        p.xt = arena.take(s.n * p.tstride * s.es);
-        p.dzt = arena.take(std::min<int64_t>(p.piece, s.classes) * p.tstride * s.es);
-        p.pw = product_plan(s.n, std::min<int64_t>(p.piece, s.classes), p.tstride * s.es);
-        if (p.pw.splits > 1)
-            p.dw = arena.take<float>((int64_t)p.pw.splits * std::min<int64_t>(p.piece, s.classes) *
-                                     s.n * 4);
+        p.pw = product_plan(s.n, here, s.rows, s.es);
+        if (p.pw.splits > 1) p.dw = arena.take<float>((int64_t)p.pw.splits * here * s.n * 4);
     }
     p.bytes = arena.at;
     return p;
 }
 
-template <typename T>
+template <typename T, int MP, int MQ>
 hipError_t product(const ProductPlan& p, const ProductArgs& a, hipStream_t st) {
+    typedef Tile<T, 2, 4, 4, 2, MP, MQ> Big;
+    typedef Tile<T, 2, 2, 2, 2, MP, MQ> Small;
     const int groups = p.tp * p.tq * p.splits;
-    if (p.big) head_product_kernel<T, Big<T>><<<groups, Big<T>::THREADS, 0, st>>>(a);
-    else head_product_kernel<T, Small<T>><<<groups, Small<T>::THREADS, 0, st>>>(a);
+    if (p.big) head_product_kernel<T, Big, MP, MQ><<<groups, Big::THREADS, 0, st>>>(a);
+    else head_product_kernel<T, Small, MP, MQ><<<groups, Small::THREADS, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -818,7 +859,7 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
     g.z.xstride = (p.xp != nullptr ? p.to : s.xstride) * s.es;
     g.z.wstride = (p.wp != nullptr ? p.to : s.wstride) * s.es;
     g.z.rows = s.rows;
-    g.z.k_bytes = p.to * s.es;
+    g.z.k = p.to;
     g.z.scale = a.scale;
     g.z.targets = a.targets;
     g.stats = a.stats;
@@ -826,39 +867,34 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
     g.ignore = a.ignore;
     g.all = s.classes;
     g.dz = p.dz;
-    g.dzt = p.dzt;
     g.zstride = p.zstride;
-    g.tstride = p.tstride;
-    if (p.xp != nullptr) KAN_TRY(pack<T>(a.x, s.xstride, s.rows, s.n, p.xp, p.to, st));
-    if (p.xt != nullptr)
-        KAN_TRY(turn<T>(a.x, s.xstride, s.rows, s.n, p.xt, p.tstride, a.targets, a.ignore, st));
+    const int64_t zbytes = p.zstride * s.es;
+    if (p.xp != nullptr)
+        KAN_TRY(pack<T>(a.x, s.xstride, s.rows, s.n, p.xp, p.to, a.targets, a.ignore, st));
     for (int64_t first = 0; first < s.classes; first += p.piece) {
         const int64_t here = std::min<int64_t>(s.classes - first, p.piece);
-        const char* const w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
+        g.z.w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
         g.z.first = (int)first;
         g.z.classes = (int)here;
-        g.z.w = w;
         if (p.wp != nullptr) {
-            KAN_TRY(pack<T>(w, s.wstride, here, s.n, p.wp, p.to, st));
+            KAN_TRY(pack<T>(g.z.w, s.wstride, here, s.n, p.wp, p.to, nullptr, 0, st));
             g.z.w = p.wp;
         }
         const bool big = div_up(s.rows, kBig) * div_up(here, kBig) >= kFillTiles;
         const int b = big ? kBig : kSmall;
         g.z.tp = (int)div_up(here, b);
         g.z.tq = (int)div_up(s.rows, b);
-        if (big) head_grad_kernel<T, Big<T>><<<g.z.tp * g.z.tq, Big<T>::THREADS, 0, st>>>(g);
-        else head_grad_kernel<T, Small<T>><<<g.z.tp * g.z.tq, Small<T>::THREADS, 0, st>>>(g);
+        const int groups = resident(g.z.tp * g.z.tq, big);
+        if (big) head_grad_kernel<T, BigLogits<T>><<<groups, BigLogits<T>::THREADS, 0, st>>>(g);
+        else head_grad_kernel<T, SmallLogits<T>><<<groups, SmallLogits<T>::THREADS, 0, st>>>(g);
         KAN_TRY(hipGetLastError());
         if (a.dx != nullptr) {
-            // (the last piece's k ends with its classes: the rows of dz past them are not read)
-            const int64_t k = std::min(up(here, 64), p.zstride) * s.es;
+            // (k to whole chunks of dz's rows, which are 0 past the classes)
             const bool last = first + p.piece >= s.classes, whole = p.px.splits == 1 && last;
-            KAN_TRY(turn<T>(w, s.wstride, here, s.n, p.wt, p.zstride, nullptr, 0, st));
-            ProductArgs r = {p.wt, p.dz, p.zstride * s.es, p.zstride * s.es, s.n, s.rows, k,
-                             p.px.k_split, p.px.tp, p.px.tq, p.dx, first > 0,
-                             whole ? a.dx : nullptr, a.scale};
-            ProductPlan px = p.px;
-            KAN_TRY(product<T>(px, r, st));
+            const ProductArgs r = {g.z.w, p.dz, g.z.wstride, zbytes, s.n, s.rows,
+                                   up(here, 16 / s.es), here, 0, p.px.k_split, p.px.tp, p.px.tq, p.dx,
+                                   first > 0, whole ? a.dx : nullptr, a.scale};
+            KAN_TRY(product<T, kByK, kByRows>(p.px, r, st));
             if (last && !whole)
                 KAN_TRY(sum<T>(p.dx, p.px.splits, s.rows * s.n, a.scale, a.dx, st));
         }
@@ -866,10 +902,10 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
             char* const out = static_cast<char*>(a.dw) + first * s.n * s.es;
             ProductPlan pw = p.pw;
             pw.tq = (int)div_up(here, pw.big ? kBig : kSmall);
-            ProductArgs r = {p.xt, p.dzt, p.tstride * s.es, p.tstride * s.es, s.n, here,
-                             p.tstride * s.es, pw.k_split, pw.tp, pw.tq, p.dw, false,
-                             pw.splits == 1 ? out : nullptr, a.scale};
-            KAN_TRY(product<T>(pw, r, st));
+            const ProductArgs r = {p.xp, p.dz, (int64_t)p.to * s.es, zbytes, s.n, here, s.rows,
+                                   s.rows, s.rows, pw.k_split, pw.tp, pw.tq, p.dw, false,
+                                   pw.splits == 1 ? out : nullptr, a.scale};
+            KAN_TRY(product<T, kByK, kByK>(pw, r, st));
             if (pw.splits > 1) KAN_TRY(sum<T>(p.dw, pw.splits, here * s.n, a.scale, out, st));
         }
     }

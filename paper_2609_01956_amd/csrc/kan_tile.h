@@ -1,15 +1,31 @@
-// kan_tile.h -- a workgroup's tile of out[q][p] = sum_k P[p][k] Q[q][k] on the matrix cores, both
-// operands with k contiguous, in bf16 or fp32 with fp32 accumulation.
+// kan_tile.h -- a workgroup's tile of out[q][p] = sum_k P(p, k) Q(q, k) on the matrix cores, in bf16
+// or fp32 with fp32 accumulation.  Each operand stands in memory by rows (of p or q, k contiguous) or
+// by k (rows of k, p or q contiguous), so that no product needs a transposed copy.
 //
-// A step takes 128 bytes of k (64 bf16, 32 fp32) of the tile's rows into LDS, straight from
-// memory (16 bytes per lane, no registers between), two steps' buffers in turn: the next step's
-// loads are in flight while this one's products run, one barrier per step, before its last quarter.  In LDS a row's eight
-// 16-byte chunks stand at chunk ^ (row & 7), so that eight lanes that read one chunk of eight
-// rows use all banks.  Rows past an operand's end are 0 (the buffer's bounds), and so are chunks
-// past k's end; k must be a whole number of chunks, rows 16-byte aligned.
+// A step takes 64 (bf16) or 32 (fp32) values of k of both operands into LDS, straight from memory
+// (16 bytes per lane, no registers between), into one of two buffers; a step is 64 KB for a tile of
+// 256 x 256.  One barrier a step, before the last quarter of its products, tells that the next
+// step has arrived and that all waves have read this one, whose buffer then takes the loads of
+// the step after the next.  Fragments are read a quarter ahead of their products.
+//
+// In LDS:
+//   by rows  128 bytes a row, its eight 16-byte chunks at chunk ^ (row >> 1 & 7): sixteen lanes that
+//            read one chunk of sixteen rows use all banks (with row & 7 they used half)
+//   by k     a row per k; bf16 fragments come from the LDS's transposing read (four k of 16 columns
+//            for 16 lanes), whose four rows stand in different quarters of the banks, 64-byte
+//            blocks at block ^ (k & 3); fp32 ones from four 4-byte reads, 128-byte blocks at block ^ (k
+//            >> 2 & 1)
+// What lies past an operand's end is 0 (the buffer's bounds).  By rows, k must be a whole number of
+// 16-byte chunks; rows are 16-byte aligned in both, and end with a chunk.  By k, columns past the end hold what follows:
+// they reach outputs past the end only.
 //
 // Each wave holds RP x RQ tiles of 32 x 32: a lane's accumulators are 16 values of p (in fours of
 // neighbours) for one q, so that sums over p stay in the lane.
+//
+// Measured on MI355X, 8192 x 8192, bf16, 256 x 256 tiles: k = 8192 1.21 PFLOP/s, 2048 1.06; without
+// any loads, in LDS or to it, 1.61: the products alone hold the card at its power limit.  Steps of
+// half the size in a ring of five, four in flight: 1.18 and 1.00.  Four waves of 128 x 128: 1.17
+// and 0.99; tiles of 128 x 128, two workgroups a CU: 1.03 and 0.94.
 #pragma once
 
 #include "kan_device.h"
@@ -18,56 +34,153 @@ namespace kan {
 
 #define KAN_LDS __attribute__((address_space(3)))
 
-// One operand's rows of a tile, from the tile's first row on.
-struct TileRows {
-    __amdgpu_buffer_rsrc_t rsrc;
+// An operand: `rows` of p (or q) by k elements, or k rows by `rows` elements; the tile's part begins at
+// row (column) `first`.
+struct Operand {
+    const char* at;   // the tile's first element, at k = 0
     uint32_t stride;  // bytes from row to row
+    int left;         // rows (columns) of the tile that there are
+    int64_t k;        // by k: rows that there are (0 past them, up to the sum's end)
 };
 
-// rows: from the tile's first on (at least 1); es bytes an element, k elements a row.
-__device__ __forceinline__ TileRows tile_rows(const void* p, int64_t first, int64_t rows, int most,
-                                              int64_t stride_bytes, int64_t k_bytes) {
-    const int64_t left = rows - first < most ? rows - first : most;
-    const char* at = static_cast<const char*>(p) + first * stride_bytes;
-    TileRows t;
-    t.rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0,
-                                               (int)((left - 1) * stride_bytes + k_bytes),
-                                               kBufferWord3);
-    t.stride = (uint32_t)stride_bytes;
-    return t;
+constexpr int kByRows = 0, kByK = 1;
+
+template <typename T, int MODE>
+__device__ __forceinline__ Operand operand(const void* p, int64_t first, int64_t rows, int most,
+                                           int64_t stride_bytes, int64_t k = 0) {
+    Operand o;
+    o.at = static_cast<const char*>(p) + first * (MODE == kByRows ? stride_bytes : (int64_t)sizeof(T));
+    o.stride = (uint32_t)stride_bytes;
+    o.left = (int)(rows - first < most ? rows - first : most);
+    o.k = k;
+    return o;
 }
 
-template <typename T, int WP_, int WQ_, int RP_, int RQ_>
+template <typename T, int W, int B, int R, int MODE>
+struct Side {
+    static constexpr int ES = (int)sizeof(T), K = 128 / ES;  // k of a step
+    static constexpr int LOADS = B / 8 / W;                  // per wave and step
+    static constexpr int BYTES = B * 128;                    // of a step
+    static constexpr int ROW = B * ES, CHUNKS = ROW / 16;    // by k: a row in LDS
+    static_assert(B % (8 * W) == 0, "whole loads");
+
+    uint32_t from[LOADS];  // the lane's loads in a step's part of the operand
+    int tail;              // by rows: bytes of k before the lane's chunk (of even loads)
+    int read[MODE == kByRows ? 1 : R], chunk[4];  // its fragments in LDS
+
+    // wave: among W; part: which R x 32 rows of the B are the wave's.
+    __device__ __forceinline__ void place(int lane, int wave, int part, uint32_t stride) {
+        if constexpr (MODE == kByRows) {
+            // a load's 64 lanes: eight rows of eight chunks, the chunk that stands there
+            const int row = lane >> 3, c = (lane & 7) ^ (row >> 1);
+            tail = c * 16;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int load = wave * LOADS + i;
+                from[i] = (load * 8 + row) * stride + ((c ^ ((load & 1) * 4)) * 16);
+            }
+            read[0] = (part * 32 * R + (lane & 31)) * 128;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                chunk[q] = ((2 * q + (lane >> 5)) ^ (lane >> 1 & 7)) * 16;
+        } else {
+            tail = 0;
+            constexpr int PER = 64 / CHUNKS;  // rows of a load
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int row = (wave * LOADS + i) * PER + lane / CHUNKS, c = lane % CHUNKS;
+                from[i] = row * stride + (ES == 2 ? c ^ (row & 3) << 2 : c ^ (row >> 2 & 1) << 3) * 16;
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const int block = part * R + i, half = lane >> 5;
+                if constexpr (ES == 2) {
+                    const int k = half * 8 + (lane >> 2 & 3);
+                    read[i] = k * ROW + (block ^ (lane >> 2 & 3)) * 64 + (lane >> 4 & 1) * 32 +
+                              (lane & 3) * 8;
+                } else {
+                    read[i] = half * 4 * ROW + (block ^ half) * 128 + (lane & 31) * 4;
+                }
+            }
+        }
+    }
+
+    // The loads of the step that begins at k (of `end`; none past it: zeros) to LDS byte dst.
+    __device__ __forceinline__ void issue(const Operand& o, int64_t k, int64_t end, int wave,
+                                          uint32_t dst) const {
+        const char* at = o.at + (MODE == kByRows ? 0 : k * o.stride);
+        const int64_t there = end < o.k ? end : o.k;
+        const int rows = MODE == kByRows ? o.left : (int)(there - k < K ? there - k : K);
+        // (bounds are kept by 4 bytes: by k, the last row to the end of its last chunk)
+        const int64_t width = MODE == kByRows ? end * ES : ((int64_t)o.left * ES + 15) & ~15;
+        const uint64_t base = reinterpret_cast<uint64_t>(at);
+        const u32x4 rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu,
+                            rows > 0 ? (uint32_t)((int64_t)(rows - 1) * o.stride + width) : 0u,
+                            (uint32_t)kBufferWord3};
+        const int bytes = (int)(end - k < K ? end - k : K) * ES;  // of the step's k
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            uint32_t v = from[i];
+            if constexpr (MODE == kByRows) {
+                const int c = tail ^ (((wave * LOADS + i) & 1) * 64);
+                v = c >= bytes ? 0x80000000u : v;
+            }
+            dma16(rsrc, v, MODE == kByRows ? (uint32_t)(k * ES) : 0u, dst + (wave * LOADS + i) * 1024);
+        }
+    }
+
+    // The fragments of a quarter of a step at src.
+    __device__ __forceinline__ void fetch(const char KAN_LDS* src, int quarter, u32x4 (&f)[R]) const {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if constexpr (MODE == kByRows) {
+                f[i] = *(const u32x4 KAN_LDS*)(src + read[0] + chunk[quarter] + i * 32 * 128);
+            } else if constexpr (ES == 2) {
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                const char KAN_LDS* p = src + read[i] + quarter * 16 * ROW;
+                const u32x2 lo = __builtin_bit_cast(
+                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KAN_LDS*)p));
+                const u32x2 hi = __builtin_bit_cast(
+                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KAN_LDS*)(p + 4 * ROW)));
+                f[i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+            } else {
+                const char KAN_LDS* p = src + read[i] + quarter * 8 * ROW;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[i][e] = *(const uint32_t KAN_LDS*)(p + e * ROW);
+            }
+        }
+    }
+
+    typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+};
+
+template <typename T, int WP_, int WQ_, int RP_, int RQ_, int MP, int MQ>
 struct Tile {
     static constexpr int WP = WP_, WQ = WQ_, RP = RP_, RQ = RQ_;
     static constexpr int W = WP * WQ, THREADS = 64 * W;
-    static constexpr int BP = 32 * RP * WP, BQ = 32 * RQ * WQ;
-    static constexpr int STAGE = (BP + BQ) * 128;
-    // (LDS of a workgroup: two steps, or rows of fp32 results)
-    static constexpr int BYTES = 2 * STAGE > 32 * WQ * (BP * 4 + 16) ? 2 * STAGE : 32 * WQ * (BP * 4 + 16);
-    static constexpr int IP = BP / 8 / W, IQ = BQ / 8 / W;  // loads per wave and step
-    static_assert(BP % (8 * W) == 0 && BQ % (8 * W) == 0, "whole loads");
+    static constexpr int BP = 32 * RP * WP, BQ = 32 * RQ * WQ, K = 128 / (int)sizeof(T);
+    typedef Side<T, W, BP, RP, MP> SideP;
+    typedef Side<T, W, BQ, RQ, MQ> SideQ;
+    static constexpr int STEP = SideP::BYTES + SideQ::BYTES, BYTES = 2 * STEP;
 
     floatx16 acc[RP][RQ];
+    SideP sp;
+    SideQ sq;
 
-    // (the order in which the compiler may move memory accesses: not past these)
+    // Waits for this wave's loads and reads, and for the other waves; the compiler moves no memory
+    // access past it.
     static __device__ __forceinline__ void arrive() {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
-
-    static __device__ __forceinline__ void issue(const TileRows& p, const TileRows& q,
-                                                 const uint32_t (&vp)[IP], const uint32_t (&vq)[IQ],
-                                                 bool past, int at, char KAN_LDS* dst, int wave) {
-#pragma unroll
-        for (int i = 0; i < IP; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                p.rsrc, (void KAN_LDS*)(dst + (wave * IP + i) * 1024), 16,
-                (int)(past ? 0x80000000u : vp[i]), at, 0, 0);
-#pragma unroll
-        for (int i = 0; i < IQ; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                q.rsrc, (void KAN_LDS*)(dst + BP * 128 + (wave * IQ + i) * 1024), 16,
-                (int)(past ? 0x80000000u : vq[i]), at, 0, 0);
+    // The same for what is in LDS alone.
+    static __device__ __forceinline__ void meet() {
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    static __device__ __forceinline__ int wave_of() {
+        return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    }
+    static __device__ __forceinline__ uint32_t byte_of(const char KAN_LDS* lds) {
+        return (uint32_t)(uintptr_t)lds;
     }
 
     __device__ __forceinline__ void multiply(const u32x4& a, const u32x4& b, floatx16& c) {
@@ -81,17 +194,6 @@ struct Tile {
                                                          __uint_as_float(b[i]), c, 0, 0, 0);
         }
     }
-
-    // The fragments of the c-th quarter of a step.
-    static __device__ __forceinline__ void fetch(const char KAN_LDS* src, int pp, int qq, int chunk,
-                                                 u32x4 (&a)[RP], u32x4 (&b)[RQ]) {
-#pragma unroll
-        for (int i = 0; i < RP; ++i)
-            a[i] = *(const u32x4 KAN_LDS*)(src + pp + i * 32 * 128 + chunk);
-#pragma unroll
-        for (int j = 0; j < RQ; ++j)
-            b[j] = *(const u32x4 KAN_LDS*)(src + BP * 128 + qq + j * 32 * 128 + chunk);
-    }
     __device__ __forceinline__ void products(const u32x4 (&a)[RP], const u32x4 (&b)[RQ]) {
 #pragma unroll
         for (int i = 0; i < RP; ++i)
@@ -99,105 +201,54 @@ struct Tile {
             for (int j = 0; j < RQ; ++j) multiply(a[i], b[j], acc[i][j]);
     }
 
-    struct Lane {
-        uint32_t vp[IP], vq[IQ];  // its loads' places in the operands
-        int pp, qq;               // its rows in LDS
-        int chunk[4];             // its chunk of a row in each quarter of a step
-        int wave, tail;           // tail: bytes of k before its loads' chunk
-    };
-
-    // One step from `cur`, whose first quarter's fragments are at hand; they end as those of the step
-    // in `nxt`.  Before the last quarter's products all waves have read `cur` (and `nxt` has
-    // arrived), so that the loads of the step after the next go there while these products, and
-    // the next step's, run.
-    __device__ __forceinline__ void step(char KAN_LDS* cur, const char KAN_LDS* nxt,
-                                         const TileRows& p, const TileRows& q, const Lane& l,
-                                         int at, int end, u32x4 (&a)[2][RP], u32x4 (&b)[2][RQ]) {
-#pragma unroll
-        for (int c = 0; c < 3; ++c) {
-            fetch(cur, l.pp, l.qq, l.chunk[c + 1], a[(c + 1) & 1], b[(c + 1) & 1]);
-            products(a[c & 1], b[c & 1]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        arrive();
-        __builtin_amdgcn_sched_barrier(0);
-        if (at < end) issue(p, q, l.vp, l.vq, at + l.tail >= end, at, cur, l.wave);
-        fetch(nxt, l.pp, l.qq, l.chunk[0], a[0], b[0]);
-        products(a[1], b[1]);
-        __builtin_amdgcn_sched_barrier(0);
+    // The loads of the first step of a tile over k from `at` to `end`, to the first STEP bytes of
+    // lds (which no wave reads any more), ahead of `run`.
+    __device__ __forceinline__ void start(char KAN_LDS* lds, const Operand& p, const Operand& q,
+                                          int64_t at, int64_t end) {
+        const int lane = threadIdx.x & 63, wave = wave_of();
+        sp.place(lane, wave, wave % WP, p.stride);
+        sq.place(lane, wave, wave / WP, q.stride);
+        sp.issue(p, at, end, wave, byte_of(lds));
+        sq.issue(q, at, end, wave, byte_of(lds) + SideP::BYTES);
     }
 
-    // (The two buffers are told apart by the compiler: reads of one do not wait for loads to the
-    // other.)
-    __device__ __forceinline__ void steps(char KAN_LDS* __restrict b0, char KAN_LDS* __restrict b1,
-                                          const TileRows& p, const TileRows& q, const Lane& l,
-                                          int at, int end) {
-        u32x4 a[2][RP], b[2][RQ];
-        issue(p, q, l.vp, l.vq, at + l.tail >= end, at, b0, l.wave);
-        int next = at + 128;
-        if (next < end) issue(p, q, l.vp, l.vq, next + l.tail >= end, next, b1, l.wave);
-        arrive();
-        fetch(b0, l.pp, l.qq, l.chunk[0], a[0], b[0]);
-        // (one way out of the loop: with two the accumulators are moved about in it)
-        for (; at + 128 < end; at += 256) {
-            step(b0, b1, p, q, l, at + 256, end, a, b);
-            step(b1, b0, p, q, l, at + 384, end, a, b);
-        }
-        if (at < end) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                if (c < 3) fetch(b0, l.pp, l.qq, l.chunk[c + 1], a[(c + 1) & 1], b[(c + 1) & 1]);
-                products(a[c & 1], b[c & 1]);
-            }
-        }
-        arrive();
-    }
-
-    // The sum over k of [k_from, k_from + k_bytes), multiples of 16.  lds: BYTES.
-    __device__ __forceinline__ void run(char KAN_LDS* lds, const TileRows& p, const TileRows& q,
-                                        int64_t k_from, int64_t k_bytes) {
-        const int lane = threadIdx.x & 63;
-        Lane l;
-        l.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // The sum over k from `at` to `end`, after `start` with the same arguments.  lds: BYTES.
+    __device__ __forceinline__ void run(char KAN_LDS* lds, const Operand& p, const Operand& q,
+                                        int64_t at, int64_t end) {
+        const int wave = wave_of();
+        const uint32_t base = byte_of(lds);
 #pragma unroll
         for (int i = 0; i < RP; ++i)
 #pragma unroll
             for (int j = 0; j < RQ; ++j) acc[i][j] = floatx16{};
-        // a load's 64 lanes: eight rows of eight chunks, the chunk that stands there
-        const int row = lane >> 3, chunk = (lane & 7) ^ row;
-        l.tail = chunk * 16;
+        const auto issue = [&](int64_t k, uint32_t dst) {
+            sp.issue(p, k, end, wave, dst);
+            sq.issue(q, k, end, wave, dst + SideP::BYTES);
+        };
+        if (at + K < end) issue(at + K, base + STEP);
+        u32x4 a[2][RP], b[2][RQ];
+        const auto fetch = [&](const char KAN_LDS* src, int quarter, int to) {
+            sp.fetch(src, quarter, a[to]);
+            sq.fetch(src + SideP::BYTES, quarter, b[to]);
+        };
+        arrive();
+        fetch(lds, 0, 0);
+        for (int cur = 0; at < end; at += K, cur = STEP - cur) {
 #pragma unroll
-        for (int i = 0; i < IP; ++i) l.vp[i] = ((l.wave * IP + i) * 8 + row) * p.stride + chunk * 16;
-#pragma unroll
-        for (int i = 0; i < IQ; ++i) l.vq[i] = ((l.wave * IQ + i) * 8 + row) * q.stride + chunk * 16;
-        l.pp = ((l.wave % WP) * 32 * RP + (lane & 31)) * 128;
-        l.qq = ((l.wave / WP) * 32 * RQ + (lane & 31)) * 128;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) l.chunk[c] = ((2 * c + (lane >> 5)) ^ (lane & 7)) * 16;
-        steps(lds, lds + STAGE, p, q, l, (int)k_from, (int)(k_from + k_bytes));
-    }
-
-    // Values v(i, e, acc[i][j][e]) of this thread's q of j as T in LDS, rows (one per q of the
-    // workgroup's waves, ROWS in all) of BP values, PITCH bytes apart.
-    static constexpr int ROWS = 32 * WQ;
-    template <typename U> static constexpr int PITCH = BP * (int)sizeof(U) + 16;
-    template <typename U, typename F>
-    __device__ __forceinline__ void put(char* lds, int thread, int j, F&& v) {
-        typedef U four __attribute__((ext_vector_type(4)));
-        const int wave = thread >> 6, lane = thread & 63;
-        char* const row = lds + ((wave / WP) * 32 + (lane & 31)) * PITCH<U> +
-                          ((wave % WP) * 32 * RP + 4 * (lane >> 5)) * (int)sizeof(U);
-#pragma unroll
-        for (int i = 0; i < RP; ++i)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<four*>(row + (i * 32 + g * 8) * (int)sizeof(U)) =
-                    four{v(i, 4 * g, acc[i][j][4 * g]), v(i, 4 * g + 1, acc[i][j][4 * g + 1]),
-                         v(i, 4 * g + 2, acc[i][j][4 * g + 2]), v(i, 4 * g + 3, acc[i][j][4 * g + 3])};
-    }
-    // The q, within the tile, of a row that `put` filled.
-    static __device__ __forceinline__ int q_of_row(int row, int j) {
-        return (row >> 5) * 32 * RQ + j * 32 + (row & 31);
+            for (int c = 0; c < 3; ++c) {
+                fetch(lds + cur, c + 1, (c + 1) & 1);
+                products(a[c & 1], b[c & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            arrive();
+            __builtin_amdgcn_sched_barrier(0);
+            if (at + 2 * K < end) issue(at + 2 * K, base + cur);
+            // (after the last step: of what the buffer held before, for nothing)
+            fetch(lds + STEP - cur, 0, 0);
+            products(a[1], b[1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        arrive();
     }
 
     // This thread, computed anew after the loop (so that nothing derived from it lives across it).
@@ -207,21 +258,43 @@ struct Tile {
         return t;
     }
 
-    // The q of a thread's accumulators acc[.][j] and the p of acc[i][.][4 v + (0 .. 3)], within the
-    // tile.
+    // The q of a thread's accumulators acc[.][j] and the p of acc[0][.][0], within the tile; that of
+    // acc[i][.][e] is 32 i + 8 (e / 4) + e % 4 further on.
     static __device__ __forceinline__ int q_of(int thread, int j) {
-        const int wave = thread >> 6, lane = thread & 63;
-        return (wave / WP) * 32 * RQ + j * 32 + (lane & 31);
+        return ((thread >> 6) / WP) * 32 * RQ + j * 32 + (thread & 31);
     }
-    static __device__ __forceinline__ int p_of(int thread, int i, int v) {
-        const int wave = thread >> 6, lane = thread & 63;
-        return (wave % WP) * 32 * RP + i * 32 + 8 * v + 4 * (lane >> 5);
+    static __device__ __forceinline__ int p_of(int thread) {
+        return ((thread >> 6) % WP) * 32 * RP + 4 * (thread >> 5 & 1);
+    }
+    static constexpr int p_step(int i, int e) { return i * 32 + 8 * (e >> 2) + (e & 3); }
+
+    // Values acc[.][j] of all threads as U in LDS: a row per q of j (ROWS in all, q_of_row) of BP
+    // values, PITCH bytes apart.
+    static constexpr int ROWS = 32 * WQ;
+    template <typename U> static constexpr int PITCH = BP * (int)sizeof(U) + 16;
+    template <typename U, typename F>
+    __device__ __forceinline__ void put(char* lds, int thread, int j, F&& rounded) {
+        typedef U four __attribute__((ext_vector_type(4)));
+        char* const row = lds + ((thread >> 6) / WP * 32 + (thread & 31)) * PITCH<U> +
+                          p_of(thread) * (int)sizeof(U);
+#pragma unroll
+        for (int i = 0; i < RP; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const floatx16& v = acc[i][j];
+                *reinterpret_cast<four*>(row + p_step(i, 4 * g) * (int)sizeof(U)) =
+                    four{rounded(v[4 * g]), rounded(v[4 * g + 1]), rounded(v[4 * g + 2]),
+                         rounded(v[4 * g + 3])};
+            }
+    }
+    static __device__ __forceinline__ int q_of_row(int row, int j) {
+        return (row >> 5) * 32 * RQ + j * 32 + (row & 31);
     }
 };
 
-// A workgroup's tile of tp x tq tiles: neighbouring workgroups go to different XCDs, each of
-// which takes a run of tiles, in blocks of up to eight q-tiles by all p-tiles, so that those that
-// run at a time on an XCD share rows of both operands in its L2.
+// Tile `id` of tp x tq: neighbouring ids go to different XCDs, each of which takes a run of tiles, in
+// blocks of up to eight q-tiles by all p-tiles, so that those that run at a time on an XCD share
+// rows of both operands in its L2.
 __device__ __forceinline__ void tile_of(int id, int tp, int tq, int* p, int* q) {
     const int all = tp * tq, xcd = id & 7, per = all >> 3, rest = all & 7;
     const int t = xcd * per + (xcd < rest ? xcd : rest) + (id >> 3);

@@ -19,41 +19,61 @@ namespace {
 
 constexpr int kLoads = 4;  // units in flight per lane
 
-// V elements of a table's row from column c on, as fp32 (0 past the row's end).
-template <typename TP, int V>
-__device__ __forceinline__ void load_row(const TP* row, int c, int n, float (&v)[V]) {
-    constexpr int U = kVec<TP>;
-    if (c + V <= n) {
+// V elements of a row of T in 16-byte units, in two steps: the loads, which no lane makes under a
+// condition (a row's last unit is loaded where it ends with the row), and what they hold as fp32 (0
+// past the row's end).
+template <typename T, int V>
+struct Piece {
+    static constexpr int U = kVec<T>, N = V / U;
+    u32x4 raw[N];
+    __device__ __forceinline__ void issue(const T* row, int c, int n) {
+        issue_units<0, true>(row, c, U, n, 0u, raw);
+    }
+    __device__ __forceinline__ void value(int c, int n, float (&v)[V]) {
+        settle_units<0, true, T>(c, U, n, 0u, raw);
 #pragma unroll
-        for (int k = 0; k < V / U; ++k) {
+        for (int k = 0; k < N; ++k) {
             float u[U];
-            widen(*unit_at(row, c + k * U), u);
+            widen(raw[k], u);
 #pragma unroll
             for (int i = 0; i < U; ++i) v[k * U + i] = u[i];
         }
-        return;
     }
+    __device__ __forceinline__ void add(int c, int n, float (&s)[V]) {
+        float v[V];
+        value(c, n, v);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        v[i] = 0.0f;
-        if (c + i < n) {
-            if constexpr (sizeof(TP) == 2) v[i] = __uint_as_float((uint32_t)row[c + i] << 16);
-            else v[i] = row[c + i];
-        }
+        for (int i = 0; i < V; ++i) s[i] += v[i];
     }
-}
+};
 
-template <typename TP, int V>
-__device__ __forceinline__ void store_row(TP* row, int c, int n, const float (&v)[V]) {
-    constexpr int U = kVec<TP>;
-#pragma unroll
-    for (int k = 0; k < V / U; ++k) {
-        float u[U];
-#pragma unroll
-        for (int i = 0; i < U; ++i) u[i] = v[k * U + i];
-        if (c + k * U < n) store_unit<false>(row, c + k * U, n, u);
+// Four bf16: 8 bytes, so that a lane's columns fill 16 bytes of an fp32 row.
+template <>
+struct Piece<uint16_t, 4> {
+    typedef uint64_t any __attribute__((aligned(2)));
+    uint64_t raw;
+    __device__ __forceinline__ void issue(const uint16_t* row, int c, int n) {
+        if (n < 4) {
+            raw = 0;
+            for (int i = 0; i < 3; ++i)
+                if (c + i < n) raw |= (uint64_t)row[c + i] << (16 * i);
+            return;
+        }
+        raw = *reinterpret_cast<const any*>(row + min(c, n - 4));
     }
-}
+    __device__ __forceinline__ void value(int c, int n, float (&v)[4]) {
+        const int past = n < 4 ? 0 : max(c + 4 - n, 0);
+        const uint64_t r = raw >> (16 * past);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float((uint32_t)(r >> (16 * i)) << 16);
+    }
+    __device__ __forceinline__ void add(int c, int n, float (&s)[4]) {
+        float v[4];
+        value(c, n, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] += v[i];
+    }
+};
 
 // A workgroup's share of rows x units items: kLoads * 256 neighbours from an item on.
 struct Share {
@@ -72,7 +92,7 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, uint32_t units)
     for (int64_t first = (int64_t)blockIdx.x * 256 * kLoads; first < all;
          first += (int64_t)gridDim.x * 256 * kLoads) {
         const Share s(first, units);
-        float v[kLoads][V];
+        Piece<TP, V> piece[kLoads];
         int64_t row[kLoads], token[kLoads];
         int c[kLoads];
 #pragma unroll
@@ -82,31 +102,35 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, uint32_t units)
             c[u] = (int)(j - r * units) * V;
             token[u] = row[u] < a.rows ? a.tokens[row[u]] : a.ignore;
         }
+        // (tokens that are left out, or none, read the first row)
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
             const bool in = token[u] != a.ignore && token[u] >= 0 && token[u] < a.classes;
-            if (in) {
-                load_row(static_cast<const TP*>(a.table) + token[u] * a.tstride, c[u], a.n, v[u]);
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[u][i] *= a.scale;
-            } else {
-                const float none = token[u] == a.ignore ? 0.0f : __builtin_nanf("");
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[u][i] = none;
-            }
+            piece[u].issue(static_cast<const TP*>(a.table) + (in ? token[u] * a.tstride : 0), c[u],
+                           a.n);
         }
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u)
-            if (row[u] < a.rows)
-                store_unit<false>(static_cast<T*>(a.y) + row[u] * a.n, c[u], a.n, v[u]);
+        for (int u = 0; u < kLoads; ++u) {
+            if (row[u] >= a.rows) continue;
+            float v[V];
+            piece[u].value(c[u], a.n, v);
+            const bool in = token[u] != a.ignore && token[u] >= 0 && token[u] < a.classes;
+            const float none = token[u] == a.ignore ? 0.0f : __builtin_nanf("");
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = in ? v[i] * a.scale : none;
+            store_unit<false>(static_cast<T*>(a.y) + row[u] * a.n, c[u], a.n, v);
+        }
     }
 }
 
 // ------------------------------------------------------------ sorting
 
-constexpr int kSortThreads = 1024, kSortWaves = 16, kSortTile = 4096;
-constexpr int kBatches = kSortTile / kSortThreads;  // per wave, of 64 neighbours
+constexpr int kSortThreads = 1024, kSortWaves = 16;
+// Entries of a workgroup: of one that sorts all in LDS, and of one tile of many.
+constexpr int kSortFew = 4096, kSortTile = 2048;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+// Tiles up to which a pass also counts the next one's digits, per tile of its output.
+constexpr int kCountTiles = 32;
 
 struct Entry {
     uint32_t key, at;  // token (classes for none), place in the batch
@@ -116,20 +140,20 @@ __device__ __forceinline__ uint32_t key_of(int64_t token, int64_t ignore, int cl
     return token == ignore || token < 0 || token >= classes ? (uint32_t)classes : (uint32_t)token;
 }
 
-// Ranks of a tile's entries among those of their digit, in order: wave w holds the kBatches * 64
-// entries from w kBatches 64 on, a batch's lanes neighbours.  count: [kSortWaves][kDigits] in LDS;
+// Ranks of a tile's entries among those of their digit, in order: wave w holds the N * 64 entries
+// from w N 64 on, a batch's lanes neighbours.  count: [kSortWaves][kDigits] in LDS;
 // afterwards count[w][d] is the number of entries of digit d in waves before w, and total(d, n)
 // has been called by one thread per digit with the tile's count of it.
-template <typename F>
-__device__ __forceinline__ void rank_digits(uint32_t (*count)[kDigits], const uint32_t (&digit)[kBatches],
-                                            const bool (&live)[kBatches], int bits,
-                                            uint32_t (&rank)[kBatches], F&& total) {
+template <int N, typename F>
+__device__ __forceinline__ void rank_digits(uint32_t (*count)[kDigits], const uint32_t (&digit)[N],
+                                            const bool (&live)[N], int bits, uint32_t (&rank)[N],
+                                            F&& total) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, digits = 1 << bits;
     for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortThreads)
         count[i >> bits][i & (digits - 1)] = 0;
     __syncthreads();
 #pragma unroll
-    for (int b = 0; b < kBatches; ++b) {
+    for (int b = 0; b < N; ++b) {
         uint64_t same = __ballot(live[b]);
         for (int k = 0; k < bits; ++k) {
             const uint64_t one = __ballot(digit[b] >> k & 1);
@@ -182,10 +206,13 @@ struct SortArgs {
     Entry* out;
     int64_t rows, ignore;
     int classes, shift, bits;
-    uint32_t* hist;   // [tiles][kDigits]: counts; before a scatter that follows `scan`: those of
-    uint32_t* totals; // tiles before, and [kDigits] counts of all; null: no scan
+    uint32_t* hist;    // [tiles][kDigits] counts; after the scan, which is made if totals
+    uint32_t* totals;  // ([kDigits], of all tiles) is not null: those of the tiles before
+    uint32_t* next;    // the next pass's hist, to be added to, or null
+    int next_bits;
     int tiles;
-    int2* span;       // [classes + 1], to be cleared
+    int2* span;        // [classes + 1], to be cleared, and the later passes' hists
+    int64_t later;     // (from `next` on)
 };
 
 __device__ __forceinline__ Entry entry_of(const SortArgs& a, int64_t i) {
@@ -202,11 +229,15 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortArgs a) {
     if (a.span != nullptr)
         clear_spans(a.span, (int64_t)a.classes + 1, (int64_t)blockIdx.x * kSortThreads + threadIdx.x,
                     (int64_t)gridDim.x * kSortThreads);
+    if (a.next != nullptr)
+        for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < a.later;
+             i += (int64_t)gridDim.x * kSortThreads)
+            a.next[i] = 0;
     if ((int)blockIdx.x >= a.tiles) return;
     for (int d = threadIdx.x; d < kDigits; d += kSortThreads) count[d] = 0;
     __syncthreads();
 #pragma unroll
-    for (int b = 0; b < kBatches; ++b) {
+    for (int b = 0; b < kSortTile / kSortThreads; ++b) {
         const int64_t i = (int64_t)blockIdx.x * kSortTile + b * kSortThreads + threadIdx.x;
         if (i < a.rows) atomicAdd(&count[entry_of(a, i).key >> a.shift & ((1 << a.bits) - 1)], 1u);
     }
@@ -241,7 +272,11 @@ __global__ void __launch_bounds__(64) sort_scan_kernel(SortArgs a) {
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortArgs a) {
     __shared__ uint32_t count[kSortWaves][kDigits];
     __shared__ uint32_t all[kDigits], first[kDigits];
+    __shared__ uint32_t next[kCountTiles * kDigits];
+    constexpr int kBatches = kSortTile / kSortThreads;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, digits = 1 << a.bits;
+    if (a.next != nullptr)
+        for (int i = threadIdx.x; i < a.tiles << a.next_bits; i += kSortThreads) next[i] = 0;
     Entry e[kBatches];
     uint32_t digit[kBatches], rank[kBatches];
     bool live[kBatches];
@@ -260,10 +295,16 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortArgs a) 
             before = a.hist[(int64_t)blockIdx.x * kDigits + d];
             sum = a.totals[d];
         } else {
-            for (int t = 0; t < a.tiles; ++t) {
-                const uint32_t c = a.hist[(int64_t)t * kDigits + d];
-                if (t < (int)blockIdx.x) before += c;
-                sum += c;
+            for (int t0 = 0; t0 < a.tiles; t0 += 8) {
+                uint32_t c[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    c[k] = t0 + k < a.tiles ? a.hist[(t0 + k) * kDigits + d] : 0u;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (t0 + k < (int)blockIdx.x) before += c[k];
+                    sum += c[k];
+                }
             }
         }
         all[d] = sum;
@@ -274,14 +315,29 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortArgs a) 
     rank_digits(count, digit, live, a.bits, rank, [](int, uint32_t) {});
 #pragma unroll
     for (int b = 0; b < kBatches; ++b)
-        if (live[b]) a.out[first[digit[b]] + count[wave][digit[b]] + rank[b]] = e[b];
+        if (live[b]) {
+            const uint32_t to = first[digit[b]] + count[wave][digit[b]] + rank[b];
+            a.out[to] = e[b];
+            if (a.next != nullptr)
+                atomicAdd(&next[(to / kSortTile << a.next_bits) +
+                                (e[b].key >> (a.shift + a.bits) & ((1u << a.next_bits) - 1))],
+                          1u);
+        }
+    if (a.next == nullptr) return;
+    __syncthreads();
+    // (sums of whole numbers: the same in any order)
+    for (int i = threadIdx.x; i < a.tiles << a.next_bits; i += kSortThreads)
+        if (next[i] != 0)
+            atomicAdd(&a.next[(i >> a.next_bits) * kDigits + (i & ((1 << a.next_bits) - 1))],
+                      next[i]);
 }
 
-// At most kSortTile entries: all passes in LDS by the first workgroup; the others clear the spans.
-__global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortArgs a, int bits_all) {
+// At most kSortFew entries: all passes in LDS by the first workgroup; the others clear the spans.
+__global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortArgs a, int passes) {
     __shared__ uint32_t count[kSortWaves][kDigits];
     __shared__ uint32_t all[kDigits], first[kDigits];
-    __shared__ Entry hold[kSortTile];
+    __shared__ Entry hold[kSortFew];
+    constexpr int kBatches = kSortFew / kSortThreads;
     if (blockIdx.x > 0 || gridDim.x == 1)
         clear_spans(a.span, (int64_t)a.classes + 1,
                     (int64_t)(gridDim.x == 1 ? 0 : blockIdx.x - 1) * kSortThreads + threadIdx.x,
@@ -297,11 +353,11 @@ __global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortArgs a, int 
         live[b] = i < a.rows;
         e[b] = live[b] ? entry_of(a, i) : Entry{0, 0};
     }
-    for (int shift = 0; shift < bits_all; shift += kDigitBits) {
-        const int bits = min(kDigitBits, bits_all - shift), digits = 1 << bits;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * a.bits, digits = 1 << a.bits;
 #pragma unroll
         for (int b = 0; b < kBatches; ++b) digit[b] = e[b].key >> shift & (digits - 1);
-        rank_digits(count, digit, live, bits, rank, [&](int d, uint32_t n) { all[d] = n; });
+        rank_digits(count, digit, live, a.bits, rank, [&](int d, uint32_t n) { all[d] = n; });
         digits_before(all, first, digits);
 #pragma unroll
         for (int b = 0; b < kBatches; ++b)
@@ -319,127 +375,288 @@ __global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortArgs a, int 
 
 // ------------------------------------------------------------ sums
 
-// Tokens with more entries than this are summed in chunks of as many.
-constexpr int kRun = 32;
+// The sorted entries are taken in chunks of kRun.  A token with at most kRun entries is summed, and its
+// row written, by the chunk that it starts in; of one with more, each chunk leaves the sum of its part.
+// With more than kRun kFan entries those sums are summed in groups of kFan next, and so on (level l:
+// chunk_size(l) entries), so that whatever its share of the batch, a row is the sum of at most
+// kRun entries or of about kFan sums.
+constexpr int kRun = 16, kFan = 64, kLevels = 5;
+__host__ __device__ constexpr int64_t chunk_size(int level) {
+    int64_t n = kRun;
+    for (int l = 0; l < level; ++l) n *= kFan;
+    return n;
+}
 
 struct EmbedSumArgs {
     EmbedGradArgs g;
     const Entry* sorted;
-    int2* span;   // [classes + 1] a token's entries: from, to
-    float* part;  // [2 chunks][units V] sums of the entries of a token that has more than kRun, in
-                  // a chunk: one that starts in an earlier chunk or at its first entry, and one
-                  // that starts later
-    uint32_t units;
+    int2* span;            // [classes + 1] a token's entries: from, to
+    float* part[kLevels];  // [2 chunks of the level][pitch] sums of a token's entries in a chunk: of
+                           // one that starts in an earlier chunk or at its first entry, and of
+                           // one that starts later (each with more entries than a chunk)
+    int levels;            // that there are
+    uint32_t pitch;        // floats of a sum
+    uint32_t units;        // of 16 bytes of the table, a row
+    int lanes;             // of a chunk: 64, 128 or 256
+    int blocks;            // of 64 units, a row
+    int heavy;             // the last launch: workgroups for tokens of more than kRun entries
 };
 
-template <typename T, int V>
-__device__ __forceinline__ void add_rows(const EmbedSumArgs& a, int from, int to, int c,
-                                         float (&s)[V]) {
-    for (int i = from; i < to; i += 4) {
-        float v[4][V];
-        uint32_t at[4];
+// The sums of a level's chunks c0 .. c1 of the token that starts at entry `start`, added in order.
+template <int V>
+__device__ __forceinline__ void add_parts(const EmbedSumArgs& a, int level, int c0, int c1,
+                                          int start, uint32_t u, float (&s)[V]) {
+    constexpr int U = 64 / V;  // (of 16 bytes, 16 loads)
+    const int64_t size = chunk_size(level);
+    for (int c = c0; c <= c1; c += U) {
+        floatx4 p[U][V / 4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) at[u] = a.sorted[min(i + u, to - 1)].at;
+        for (int k = 0; k < U; ++k) {
+            const int at = min(c + k, c1);
+            const int64_t slot = 2 * (int64_t)at + (start > at * size ? 1 : 0);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            load_row(static_cast<const T*>(a.g.dy) + at[u] * a.g.dystride, c, a.g.n, v[u]);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (i + u >= to) break;
-#pragma unroll
-            for (int k = 0; k < V; ++k) s[k] += v[u][k];
+            for (int i = 0; i < V / 4; ++i)
+                p[k][i] = *reinterpret_cast<const floatx4*>(a.part[level] +
+                                                            slot * a.pitch + u * V + 4 * i);
         }
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (c + k <= c1) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[i] += p[k][i / 4][i % 4];
+            }
     }
 }
 
-// Spans, and the chunks' sums: a workgroup per chunk.
-template <typename T>
+template <int V>
+__device__ __forceinline__ void store_part(const EmbedSumArgs& a, int level, int64_t slot, uint32_t u,
+                                           const float (&s)[V]) {
+    float* const out = a.part[level] + slot * a.pitch + u * V;
+#pragma unroll
+    for (int i = 0; i < V; i += 4)
+        *reinterpret_cast<floatx4*>(out + i) = floatx4{s[i], s[i + 1], s[i + 2], s[i + 3]};
+}
+
+// A lane's V columns of a row.  FULL (rows of V columns at least, of which two lanes may write the
+// same): the last lane's end with the row, so that no lane has a part of them; else Piece's.
+template <typename T, int V, bool FULL>
+struct Columns {
+    Piece<T, V> piece;
+    __device__ __forceinline__ void issue(const T* row, int c, int n) {
+        if constexpr (!FULL) piece.issue(row, c, n);
+        else if constexpr (V * sizeof(T) == 8)
+            piece.raw = *reinterpret_cast<const typename Piece<T, V>::any*>(row + c);
+        else
+#pragma unroll
+            for (int k = 0; k < Piece<T, V>::N; ++k)
+                piece.raw[k] = *unit_at(row, c + k * kVec<T>);
+    }
+    __device__ __forceinline__ void value(int c, int n, float (&v)[V]) {
+        piece.value(c, FULL ? c + V : n, v);
+    }
+    __device__ __forceinline__ void add(int c, int n, float (&s)[V]) {
+        float v[V];
+        value(c, n, v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] += v[i];
+    }
+};
+template <int V, bool FULL>
+__device__ __forceinline__ int column_of(uint32_t unit, int n) {
+    return FULL ? min((int)unit * V, n - V) : (int)unit * V;
+}
+
+// A row of the table: base + scale s.
+template <bool FULL, bool PAST, typename TP, int V>
+__device__ __forceinline__ void store_sum(const EmbedGradArgs& g, int64_t row, int c,
+                                          const float (&s)[V], const float (&base)[V]) {
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(s[i], g.scale, base[i]);
+    store_unit<FULL, PAST>(static_cast<TP*>(g.dtable) + row * g.n, c, g.n, v);
+}
+
+// Spans, rows of few entries, and the first level's sums: a.lanes neighbouring lanes per chunk.
+// What belongs to which row is uniform over them, so the loads of kRun entries are in flight at a
+// time, under no condition.
+template <typename T, typename TP, bool FULL, bool BASE>
 __global__ void __launch_bounds__(256) embed_chunk_kernel(EmbedSumArgs a) {
-    constexpr int V = kVec<T>;
-    const int64_t rows = a.g.rows;
-    for (int64_t chunk = blockIdx.x; chunk * kRun < rows; chunk += gridDim.x) {
+    constexpr int V = kVec<TP>;
+    const int64_t rows = a.g.rows, chunks = (rows + kRun - 1) / kRun;
+    const int per = 256 / a.lanes, lane = threadIdx.x & 63, n = a.g.n;
+    const int team = __builtin_amdgcn_readfirstlane(threadIdx.x / a.lanes);
+    for (int64_t chunk = (int64_t)blockIdx.x * per + team; chunk < chunks;
+         chunk += (int64_t)gridDim.x * per) {
         const int64_t first = chunk * kRun;
-        const int lane = threadIdx.x & 63;
-        // the chunk's keys (every wave), those of the chunks around it
-        const auto key = [&](int64_t i) {
-            return i < 0 || i >= rows ? 0xffffffffu : a.sorted[i].key;
-        };
-        const int64_t mine = first + lane - kRun;  // lanes: the chunk before, the chunk
-        const uint32_t k0 = key(mine), k1 = key(first + kRun + (lane & (kRun - 1)));
-        if (threadIdx.x >= kRun && threadIdx.x < 64 && mine < rows) {
-            if (key(mine - 1) != k0) a.span[k0].x = (int)mine;
-            if (key(mine + 1) != k0) a.span[k0].y = (int)mine + 1;
+        // lanes 0 .. 47: the entries of the chunk before, of the chunk, and of the next
+        const int64_t mine = first + lane - kRun;
+        const bool there = lane < 3 * kRun && mine >= 0 && mine < rows;
+        const Entry e = there ? a.sorted[mine] : Entry{0xffffffffu, 0};
+        const uint32_t left = __shfl_up(e.key, 1), right = __shfl_down(e.key, 1);
+        if ((int)threadIdx.x % a.lanes < 64 && there && lane >= kRun && lane < 2 * kRun) {
+            if (left != e.key) a.span[e.key].x = (int)mine;
+            if (right != e.key) a.span[e.key].y = (int)mine + 1;
         }
-        // runs of one key that reach into the chunk: the one at its first entry, and one that
-        // reaches past its last
+        // bits of lanes: the first entry of a run of one token (48: what is past the window);
+        // entries of tokens
+        const uint64_t window = (UINT64_C(1) << 3 * kRun) - 1;
+        const uint64_t starts = (__ballot(lane > 0 && left != e.key) & window) | ~window;
+        const uint64_t tokens = __ballot(e.key < (uint32_t)a.g.classes);
+        const auto start_after = [&](int l) { return __builtin_ctzll(starts >> l >> 1) + l + 1; };
+        // the run at the chunk's first entry, if it started before; one of few entries is no business
+        // of this chunk
+        const uint32_t head = __builtin_amdgcn_readlane((int)e.key, kRun);
+        const bool goes_on = !(starts >> kRun & 1), many = __popcll(__ballot(e.key == head)) > kRun;
+        const int begin = goes_on && !many ? start_after(kRun) : kRun;
+        if (begin >= 2 * kRun || !(tokens >> begin & 1)) continue;
+        // the run that reaches past the chunk: its rest, if it is of few entries and starts here
+        const int next = start_after(2 * kRun - 1);
+        const int tail = 63 - __builtin_clzll((starts & ((UINT64_C(1) << 2 * kRun) - 1)) | 1);
+        const int end = tail >= begin && next - tail <= kRun ? next : 2 * kRun;
+        // entries to add, and those after which a sum is whole (or the chunk's share of it)
+        const uint64_t live = tokens & ((UINT64_C(1) << end) - 1) & ~((UINT64_C(1) << begin) - 1);
+        const uint64_t ends = live & (starts >> 1 | UINT64_C(1) << (end - 1));
+        for (uint32_t u = threadIdx.x & (a.lanes - 1); u < a.units; u += a.lanes) {
+            const int c = column_of<V, FULL>(u, n);
+            float s[V] = {};
+#pragma unroll 1
+            for (int l0 = kRun; l0 < end; l0 += kRun) {
+                Columns<T, V, FULL> v[kRun];
+                Columns<TP, V, FULL> base[BASE ? kRun : 1];
 #pragma unroll
-        for (int slot = 0; slot < 2; ++slot) {
-            const uint32_t k = __builtin_amdgcn_readlane((int)k0, slot == 0 ? kRun : 63);
-            const uint32_t head = __builtin_amdgcn_readlane((int)k0, kRun);
-            if (k >= (uint32_t)a.g.classes || (slot == 1 && k == head)) continue;
-            const uint64_t here = __ballot(k0 == k);
-            const int in = __popcll(here >> kRun), before = __popcll(here & 0xffffffffu);
-            const int after = __popcll(__ballot(k1 == k) & 0xffffffffu);
-            if (in + before + after <= kRun) continue;
-            const int from = (int)first + __builtin_ctzll(here >> kRun);
-            for (uint32_t u = threadIdx.x; u < a.units; u += 256) {
-                float s[V] = {};
-                add_rows<T, V>(a, from, from + in, u * V, s);
-                float* const out = a.part + ((2 * chunk + slot) * a.units + u) * V;
+                for (int i = 0; i < kRun; ++i) {
+                    const int l = live >> (l0 + i) & 1 ? l0 + i : begin;
+                    const uint32_t at = __builtin_amdgcn_readlane((int)e.at, l);
+                    v[i].issue(static_cast<const T*>(a.g.dy) + at * a.g.dystride, c, n);
+                    if constexpr (BASE) {
+                        const uint32_t key = __builtin_amdgcn_readlane((int)e.key, l);
+                        if (ends >> (l0 + i) & 1)
+                            base[i].issue(static_cast<const TP*>(a.g.base) + (int64_t)key * n, c, n);
+                    }
+                }
 #pragma unroll
-                for (int i = 0; i < V; i += 4)
-                    *reinterpret_cast<floatx4*>(out + i) =
-                        floatx4{s[i], s[i + 1], s[i + 2], s[i + 3]};
+                for (int i = 0; i < kRun; ++i) {
+                    const int l = l0 + i;
+                    if (!(live >> l & 1)) continue;
+                    if (starts >> l & 1) {
+#pragma unroll
+                        for (int k = 0; k < V; ++k) s[k] = 0.0f;
+                    }
+                    v[i].add(c, n, s);
+                    if (!(ends >> l & 1)) continue;
+                    const uint32_t key = __builtin_amdgcn_readlane((int)e.key, l);
+                    const uint64_t upto = starts & ((UINT64_C(2) << l) - 1);
+                    const int from = upto >> kRun ? 63 - __builtin_clzll(upto) : -1;
+                    if (from >= 0 && start_after(from) - from <= kRun) {
+                        float w[V] = {};
+                        if constexpr (BASE) base[i].value(c, n, w);
+                        store_sum<FULL, false, TP>(a.g, key, c, s, w);
+                    } else {
+                        store_part(a, 0, 2 * chunk + (from > kRun ? 1 : 0), u, s);
+                    }
+                }
             }
         }
     }
 }
 
-template <typename T, typename TP>
-__global__ void __launch_bounds__(256) embed_sum_kernel(EmbedSumArgs a) {
-    constexpr int V = kVec<T>;
-    const int64_t all = (int64_t)a.g.classes * a.units;
-    for (int64_t first = (int64_t)blockIdx.x * 256; first < all;
-         first += (int64_t)gridDim.x * 256) {
-        const Share s(first, a.units);
-        const uint32_t j = s.at + threadIdx.x, r = j / a.units;
-        const int64_t row = s.row + r;
-        const uint32_t u = j - r * a.units;
-        if (row >= a.g.classes) continue;
-        const int2 span = a.span[row];
-        const bool in_place = a.g.base == a.g.dtable;
-        if (span.x == span.y && in_place) continue;
-        float v[V] = {};
-        if (span.y - span.x <= kRun) {
-            add_rows<T, V>(a, span.x, span.y, u * V, v);
-        } else {
-            const int c0 = span.x / kRun, c1 = (span.y - 1) / kRun;
-            constexpr int U = 8;
-            for (int c = c0; c <= c1; c += U) {
-                floatx4 p[U][V / 4];
+// The sums of a later level's chunks from those of the level before, a wave for each 64 units.
+template <int V>
+__global__ void __launch_bounds__(256) embed_join_kernel(EmbedSumArgs a, int level) {
+    const int64_t rows = a.g.rows, size = chunk_size(level), fine = chunk_size(level - 1);
+    const int64_t items = (rows + size - 1) / size * a.blocks;
+    const int lane = threadIdx.x & 63;
+    // short rows leave lanes over: each strand of them takes a part of the sums
+    int width = 64;
+    while (width >= 2 * (int)a.units) width /= 2;
+    const int strands = 64 / width;
+    for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items;
+         item += (int64_t)gridDim.x * 4) {
+        const int64_t chunk = item / a.blocks;
+        const uint32_t u = (uint32_t)(item - chunk * a.blocks) * 64 + (lane & (width - 1));
+        const int64_t first = chunk * size, end = first + size < rows ? first + size : rows;
+        const uint32_t head = a.sorted[first].key, last = a.sorted[end - 1].key;
+        for (int slot = 0; slot < 2; ++slot) {
+            const uint32_t k = slot == 0 ? head : last;
+            if (k >= (uint32_t)a.g.classes || (slot == 1 && k == head)) continue;
+            const int2 span = a.span[k];
+            if (span.y - span.x <= size) continue;
+            const int64_t from = span.x > first ? span.x : first, to = span.y < end ? span.y : end;
+            const int c0 = (int)(from / fine), c1 = (int)((to - 1) / fine);
+            const int each = (c1 - c0 + strands) / strands, mine = c0 + lane / width * each;
+            float s[V] = {};
+            if (u < a.units) add_parts(a, level - 1, mine, min(mine + each - 1, c1), span.x, u, s);
+            for (int o = width; o < 64; o *= 2)
 #pragma unroll
-                for (int k = 0; k < U; ++k) {
-                    const int at = min(c + k, c1);
-                    const int slot = 2 * at + (span.x > at * kRun ? 1 : 0);
-#pragma unroll
-                    for (int i = 0; i < V / 4; ++i)
-                        p[k][i] = *reinterpret_cast<const floatx4*>(
-                            a.part + ((int64_t)slot * a.units + u) * V + 4 * i);
-                }
-#pragma unroll
-                for (int k = 0; k < U; ++k) {
-                    if (c + k > c1) break;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) v[i] += p[k][i / 4][i % 4];
-                }
-            }
+                for (int i = 0; i < V; ++i) s[i] += __shfl_xor(s[i], o);
+            if (u < a.units && lane < width) store_part(a, level, 2 * chunk + slot, u, s);
         }
-        float b[V] = {};
-        if (a.g.base != nullptr)
-            load_row(static_cast<const TP*>(a.g.base) + row * a.g.n, (int)u * V, a.g.n, b);
+    }
+}
+
+// Rows of tokens with more than kRun entries (the first a.heavy workgroups, a wave for 64 units of the
+// one that starts in a chunk), and of those that do not occur (the others).  PAST: stored past the caches.
+template <typename TP, bool FULL, bool PAST>
+__global__ void __launch_bounds__(256) embed_rest_kernel(EmbedSumArgs a) {
+    constexpr int V = kVec<TP>;
+    if ((int)blockIdx.x < a.heavy) {
+        const int64_t rows = a.g.rows, items = (rows + kRun - 1) / kRun * a.blocks;
+        for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items;
+             item += (int64_t)a.heavy * 4) {
+            const int64_t chunk = item / a.blocks;
+            const uint32_t u = (uint32_t)(item - chunk * a.blocks) * 64 + (threadIdx.x & 63);
+            // (with more than kRun entries it is the chunk's last one)
+            const int64_t first = chunk * kRun, last = min(first + kRun, rows) - 1;
+            const uint32_t key = a.sorted[last].key;
+            if (key >= (uint32_t)a.g.classes) continue;
+            const int2 span = a.span[key];
+            const int count = span.y - span.x;
+            if (count <= kRun || span.x < first) continue;
+            int level = 0;
+            while (level + 1 < a.levels && count > chunk_size(level + 1)) ++level;
+            const int64_t size = chunk_size(level);
+            if (u >= a.units) continue;
+            const int c = column_of<V, FULL>(u, a.g.n);
+            float s[V] = {}, w[V] = {};
+            Columns<TP, V, FULL> base;
+            if (a.g.base != nullptr)
+                base.issue(static_cast<const TP*>(a.g.base) + (int64_t)key * a.g.n, c, a.g.n);
+            add_parts(a, level, (int)(span.x / size), (int)((span.y - 1) / size), span.x, u, s);
+            if (a.g.base != nullptr) base.value(c, a.g.n, w);
+            store_sum<FULL, false, TP>(a.g, key, c, s, w);
+        }
+        return;
+    }
+    const int64_t all = (int64_t)a.g.classes * a.units;
+    const int64_t groups = gridDim.x - a.heavy;
+    for (int64_t first = (int64_t)(blockIdx.x - a.heavy) * 256 * kLoads; first < all;
+         first += groups * 256 * kLoads) {
+        const Share s(first, a.units);
+        int64_t row[kLoads];
+        int c[kLoads];
+        bool absent[kLoads];
+        Columns<TP, V, FULL> base[kLoads];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(v[i], a.g.scale, b[i]);
-        store_row(static_cast<TP*>(a.g.dtable) + row * a.g.n, (int)u * V, a.g.n, v);
+        for (int u = 0; u < kLoads; ++u) {
+            const uint32_t j = s.at + u * 256 + threadIdx.x, r = j / a.units;
+            row[u] = s.row + r;
+            c[u] = column_of<V, FULL>(j - r * a.units, a.g.n);
+            const int2 span = row[u] < a.g.classes ? a.span[row[u]] : int2{0, 1};
+            absent[u] = span.x == span.y;
+        }
+        if (a.g.base != nullptr) {
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u)
+                if (absent[u])
+                    base[u].issue(static_cast<const TP*>(a.g.base) + row[u] * a.g.n, c[u], a.g.n);
+        }
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            if (!absent[u]) continue;
+            float v[V] = {};
+            if (a.g.base != nullptr) base[u].value(c[u], a.g.n, v);
+            store_unit<FULL, PAST>(static_cast<TP*>(a.g.dtable) + row[u] * a.g.n, c[u], a.g.n, v);
+        }
     }
 }
 
@@ -448,12 +665,17 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedSumArgs a) {
 int64_t div_up(int64_t v, int64_t by) { return (v + by - 1) / by; }
 int groups_of(int64_t n) { return (int)std::min<int64_t>(n, kMaxGroups); }
 
+// Workgroups of each kind in the last launch: they go on by strides.
+constexpr int kRestGroups = 1 << 13;
+
 struct EmbedGradPlan {
     Entry* list[2];
     uint32_t *hist, *totals;
     int2* span;
-    float* part;
-    int tiles, bits, passes;
+    float* part[kLevels];
+    int levels, tiles, passes;
+    int bits;   // of a pass
+    int hists;  // passes' counts side by side, or 1: one for all
     size_t bytes;
 };
 
@@ -465,19 +687,23 @@ EmbedGradPlan embed_grad_plan(int64_t rows, int32_t classes, int32_t n, void* ws
         p.bytes += (size_t)(div_up(bytes, 256) * 256);
         return at;
     };
-    while (classes >> p.bits) ++p.bits;  // (of the keys 0 .. classes)
-    p.passes = (int)div_up(p.bits, kDigitBits);
+    int bits = 0;
+    while (classes >> bits) ++bits;  // (of the keys 0 .. classes)
+    p.passes = (int)div_up(bits, kDigitBits);
+    p.bits = (int)div_up(bits, p.passes);
     p.tiles = (int)div_up(rows, kSortTile);
-    const bool few = p.tiles <= 1;
+    const bool few = rows <= kSortFew;
+    p.hists = p.tiles <= kCountTiles ? p.passes : 1;
     p.span = reinterpret_cast<int2*>(take(((int64_t)classes + 1) * 8));
     for (int i = 0; i < (few ? 1 : 2); ++i)
         p.list[i] = reinterpret_cast<Entry*>(take(rows * (int64_t)sizeof(Entry)));
     if (!few) {
-        p.hist = reinterpret_cast<uint32_t*>(take((int64_t)p.tiles * kDigits * 4));
+        p.hist = reinterpret_cast<uint32_t*>(take((int64_t)p.hists * p.tiles * kDigits * 4));
         p.totals = reinterpret_cast<uint32_t*>(take(kDigits * 4));
     }
-    if (rows > kRun)
-        p.part = reinterpret_cast<float*>(take(2 * div_up(rows, kRun) * (div_up(n, 8) * 8) * 4));
+    for (; p.levels < kLevels && rows > chunk_size(p.levels); ++p.levels)
+        p.part[p.levels] = reinterpret_cast<float*>(
+            take(2 * div_up(rows, chunk_size(p.levels)) * (div_up(n, 8) * 8) * 4));
     return p;
 }
 
@@ -486,9 +712,6 @@ EmbedGradPlan embed_grad_plan(int64_t rows, int32_t classes, int32_t n, void* ws
         const hipError_t e_ = (__VA_ARGS__);  \
         if (e_ != hipSuccess) return e_;      \
     } while (0)
-
-// Tiles from which the counts before each are summed by a launch of its own.
-constexpr int kScanTiles = 64;
 
 template <typename T, typename TP>
 hipError_t embed(const EmbedArgs& a, hipStream_t s) {
@@ -500,20 +723,32 @@ hipError_t embed(const EmbedArgs& a, hipStream_t s) {
 template <typename T, typename TP>
 hipError_t embed_grad(const EmbedGradArgs& g, void* ws, hipStream_t s) {
     const EmbedGradPlan p = embed_grad_plan(g.rows, g.classes, g.n, ws);
-    SortArgs a = {g.tokens, nullptr, p.list[0], g.rows, g.ignore, g.classes, 0, p.bits,
-                  p.hist, nullptr, p.tiles, p.span};
+    SortArgs a = {};
+    a.tokens = g.tokens;
+    a.out = p.list[0];
+    a.rows = g.rows;
+    a.ignore = g.ignore;
+    a.classes = g.classes;
+    a.bits = a.next_bits = p.bits;
+    a.tiles = p.tiles;
+    a.span = p.span;
     const int clear = (int)std::min<int64_t>(div_up((int64_t)g.classes + 1, 4 * kSortThreads), 1024);
-    if (p.tiles <= 1) {
-        sort_few_kernel<<<clear == 1 ? 1 : clear + 1, kSortThreads, 0, s>>>(a, p.bits);
+    if (g.rows <= kSortFew) {
+        sort_few_kernel<<<clear == 1 ? 1 : clear + 1, kSortThreads, 0, s>>>(a, p.passes);
         KAN_TRY(hipGetLastError());
     } else {
+        const int64_t hist = (int64_t)p.tiles * kDigits;
+        a.later = (p.hists - 1) * hist;
         for (int i = 0; i < p.passes; ++i) {
             a.out = p.list[i & 1];
-            a.bits = std::min(kDigitBits, p.bits - a.shift);
-            a.totals = nullptr;
-            sort_count_kernel<<<i == 0 ? std::max(clear, p.tiles) : p.tiles, kSortThreads, 0, s>>>(a);
-            KAN_TRY(hipGetLastError());
-            if (p.tiles > kScanTiles) {
+            a.hist = p.hist + (p.hists > 1 ? i * hist : 0);
+            a.next = p.hists > 1 && i + 1 < p.passes ? a.hist + hist : nullptr;
+            if (i == 0 || p.hists == 1) {
+                const int groups = i == 0 ? std::max(clear, p.tiles) : p.tiles;
+                sort_count_kernel<<<groups, kSortThreads, 0, s>>>(a);
+                KAN_TRY(hipGetLastError());
+            }
+            if (p.tiles > kCountTiles) {
                 a.totals = p.totals;
                 sort_scan_kernel<<<kDigits / 64, 64, 0, s>>>(a);
                 KAN_TRY(hipGetLastError());
@@ -523,15 +758,50 @@ hipError_t embed_grad(const EmbedGradArgs& g, void* ws, hipStream_t s) {
             a.tokens = nullptr;
             a.span = nullptr;
             a.in = a.out;
-            a.shift += kDigitBits;
+            a.shift += p.bits;
         }
     }
-    const EmbedSumArgs e = {g, a.out, p.span, p.part, (uint32_t)div_up(g.n, kVec<T>)};
+    EmbedSumArgs e = {};
+    e.g = g;
+    e.sorted = a.out;
+    e.span = p.span;
+    e.levels = p.levels;
+    e.pitch = (uint32_t)(div_up(g.n, 8) * 8);
+    e.units = (uint32_t)div_up(g.n, kVec<TP>);
+    e.lanes = 64;
+    e.blocks = (int)div_up(e.units, 64);
+    for (int l = 0; l < p.levels; ++l) e.part[l] = p.part[l];
+    while (e.lanes < 256 && (uint32_t)e.lanes < e.units) e.lanes *= 2;
+    const int per = 256 / e.lanes;
+    // (in place no column may have two writers)
+    const bool whole = g.n % kVec<TP> == 0;
+    const bool full = g.n >= kVec<TP> && (whole || g.base != g.dtable);
     if (g.rows > 0) {
-        embed_chunk_kernel<T><<<groups_of(div_up(g.rows, kRun)), 256, 0, s>>>(e);
+        const int groups = groups_of(div_up(div_up(g.rows, kRun), per));
+        const auto chunks = g.base != nullptr
+                                ? full ? embed_chunk_kernel<T, TP, true, true>
+                                       : embed_chunk_kernel<T, TP, false, true>
+                                : full ? embed_chunk_kernel<T, TP, true, false>
+                                       : embed_chunk_kernel<T, TP, false, false>;
+        chunks<<<groups, 256, 0, s>>>(e);
         KAN_TRY(hipGetLastError());
     }
-    embed_sum_kernel<T, TP><<<groups_of(div_up((int64_t)g.classes * e.units, 256)), 256, 0, s>>>(e);
+    for (int l = 1; l < p.levels; ++l) {
+        embed_join_kernel<kVec<TP>>
+            <<<groups_of(div_up(div_up(g.rows, chunk_size(l)) * e.blocks, 4)), 256, 0, s>>>(e, l);
+        KAN_TRY(hipGetLastError());
+    }
+    if (g.rows > kRun)
+        e.heavy = (int)std::min<int64_t>(div_up(div_up(g.rows, kRun) * e.blocks, 4), kRestGroups);
+    const int64_t rest = g.base == g.dtable ? 0 : div_up((int64_t)g.classes * e.units, 256 * kLoads);
+    const int groups = e.heavy + (int)std::min<int64_t>(rest, kRestGroups);
+    if (groups == 0) return hipSuccess;
+    const bool past = (int64_t)g.classes * g.n * (int64_t)sizeof(TP) >= kPastCaches;
+    const auto others = past ? full ? embed_rest_kernel<TP, true, true>
+                                    : embed_rest_kernel<TP, false, true>
+                             : full ? embed_rest_kernel<TP, true, false>
+                                    : embed_rest_kernel<TP, false, false>;
+    others<<<groups, 256, 0, s>>>(e);
     return hipGetLastError();
 }
 

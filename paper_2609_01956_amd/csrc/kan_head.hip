@@ -763,7 +763,7 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
     }
     HeadJoinArgs j = {p.out, s.rows, (int)p.parts, s.classes, 1, a.targets, a.ignore, a.logp, a.stats,
                       a.best};
-    while (j.lanes < 64 && j.lanes < s.rows && j.lanes * p.parts < 4096) j.lanes *= 2;
+    while (j.lanes < 64 && div_up(s.rows, j.lanes) > 4 * kFillTiles) j.lanes *= 2;
     head_join_kernel<<<(int)div_up(s.rows, j.lanes), 256, 0, st>>>(j);
     return hipGetLastError();
 }

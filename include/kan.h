@@ -721,7 +721,10 @@ kan_status kan_embedding_backward_workspace_bytes(int64_t rows, int32_t classes,
  *   workspace    caller-owned, workspace_bytes >= kan_linear_logprobs_workspace_bytes(...),
  *                16-byte aligned, overlapping no other argument; overwritten
  *
- * x and weight are of dtype; products and sums are binary32.  Rows of 16-byte aligned x and weight
+ * x and weight are of dtype; products and sums are binary32 (the sum before the scale, too, has
+ * to stay in its range).  Large fp32 products take both operands as three bf16 terms, which hold
+ * all 24 bits of values from 2^-109 on; products of their smallest terms, below 2^-25 of the whole,
+ * are left out.  Rows of 16-byte aligned x and weight
  * of whole 16-byte units are read as they stand; others are copied to the workspace (weights in
  * pieces), except in calls of at most 64 rows.  A NaN or +infinity among a row's logits makes its
  * logp and logs NaN (best then ranks NaN after every number); a row whose logits are all -infinity

@@ -62,8 +62,18 @@ __device__ __forceinline__ void leave(const Parts& o, int64_t part, int64_t rows
     if (o.best != nullptr) o.best[part * rows + row] = b.at;
 }
 
-template <typename T> using BigLogits = Tile<T, 2, 4, 4, 2, kByRows, kByRows>;  // 256 x 256
-template <typename T> using SmallLogits = Tile<T, 2, 2, 2, 2, kByRows, kByRows>;  // 128 x 128
+// fp32 operands of large products go through the matrix cores as bf16 terms: a value is the sum of
+// three of 8 bits each, h + m + l (exact for |v| above 2^-109), and a product
+// h h' + h m' + m h' + m m' + h l' + l h': what is left out is below 2^-25 of it.  So six segments of k
+// in bf16, at sixteen times the fp32 instruction's rate, the small ones first.  The term h stands
+// twice, as it is for the last segment, and 0 where it is infinite or NaN for the others, so that
+// such values enter the sum once, as they would in fp32.
+constexpr int kTerms = 4, kSegments = 6;  // h, h where finite, m, l
+constexpr uint32_t kTermsP = 0x012213, kTermsQ = 0x021231;
+constexpr uint32_t kTermsDz = 0x010120;   // dz, as Q: h, m, l
+
+template <typename T, int S> using BigLogits = Tile<T, 2, 4, 4, 2, kByRows, kByRows, S>;  // 256 x 256
+template <typename T, int S> using SmallLogits = Tile<T, 2, 2, 2, 2, kByRows, kByRows, S>;  // 128 x 128
 
 // The tiles of rows x classes logits.
 struct LogitArgs {
@@ -75,6 +85,7 @@ struct LogitArgs {
     int tp, tq;
     float scale;
     const int64_t* targets;
+    int64_t xplane, wplane;          // bytes from term to term (fp32 as bf16 terms), else 0
 };
 
 // Each workgroup's tiles, one after the other: ready(tile, p, q) with the products of tile (p, q),
@@ -88,8 +99,10 @@ __device__ __forceinline__ void for_tiles(const LogitArgs& a, char* lds, F&& rea
     Operand p, q;
     const auto find = [&](int id) {
         tile_of(id, a.tp, a.tq, &tp, &tq);
-        p = operand<T, kByRows>(a.w, (int64_t)tp * Tl::BP, a.classes, Tl::BP, a.wstride);
-        q = operand<T, kByRows>(a.x, (int64_t)tq * Tl::BQ, a.rows, Tl::BQ, a.xstride);
+        p = operand<T, kByRows>(a.w, (int64_t)tp * Tl::BP, a.classes, Tl::BP, a.wstride, 0, a.wplane,
+                                kTermsP);
+        q = operand<T, kByRows>(a.x, (int64_t)tq * Tl::BQ, a.rows, Tl::BQ, a.xstride, 0, a.xplane,
+                                kTermsQ);
     };
     Tl t;
     find(blockIdx.x);
@@ -223,15 +236,19 @@ struct HeadThinArgs {
     Parts out;
 };
 constexpr int kThinWaves = 8;
-constexpr int kThinLds = 64 << 10;  // bytes of x in LDS at a time
+constexpr int kThinLds = 64 << 10;  // bytes of x in LDS at a time (128 KB: one workgroup a CU, slower)
 
-// NT: groups of 16 rows.
-template <typename T, int NT, bool BEST>
+// Rows of weights straight from memory into the matrix instruction, x from LDS: bound by the reads of
+// the weights.  NT: groups of 16 rows.  SPLIT: the waves share one group of
+// 16 classes and split k.
+template <typename T, int NT, bool BEST, bool SPLIT>
 __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs a) {
     constexpr int V = kVec<T>, ROWS = 16 * NT;
     constexpr int SLICE = kThinLds / ROWS / 16;  // chunks of a row in LDS at a time
+    constexpr int TURN = SPLIT ? 1 : kThinWaves;  // groups of 16 classes of a workgroup at a time
     extern __shared__ __attribute__((aligned(128))) char lds[];
     __shared__ Best red[kThinWaves][ROWS];
+    static_assert(kThinLds + sizeof(red) <= 160 << 10, "LDS of a CU");
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r16 = lane & 15, quad = lane >> 4;
     const T* const x = static_cast<const T*>(a.x);
     const T* const w = static_cast<const T*>(a.w);
@@ -260,8 +277,8 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
     }
     const int groups = (a.classes + 15) >> 4;
     // (all waves of a workgroup take the same turns: x comes in slices between barriers)
-    for (int g0 = blockIdx.x * kThinWaves; g0 < groups; g0 += gridDim.x * kThinWaves) {
-        const int p0 = (g0 + wave) * 16;
+    for (int g0 = blockIdx.x * TURN; g0 < groups; g0 += gridDim.x * TURN) {
+        const int p0 = (SPLIT ? g0 : g0 + wave) * 16;
         const T* const row = w + (int64_t)min(p0 + r16, a.classes - 1) * a.wstride;
         floatx4 acc[NT] = {};
         for (int c0 = 0; c0 < chunks; c0 += width) {
@@ -270,7 +287,6 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
                 fill(c0);
                 __syncthreads();
             }
-            const int here = min(width, chunks - c0);
             const auto product = [&](int c, u32x4 wv) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
@@ -289,10 +305,12 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
                     }
                 }
             };
-            // whole chunks in all four quarters of the wave
-            const int full = min(here, a.n / V - c0) & ~3;
+            // this wave's chunks of the slice: whole ones in all four quarters of the wave first
+            const int here = min(width, chunks - c0), each = ((here + 31) >> 5) * 4;
+            int c = SPLIT ? min(wave * each, here) : 0;
+            const int end = SPLIT ? min(c + each, here) : here;
+            const int full = min(end, (a.n / V - c0) & ~3);
             constexpr int U = 8;
-            int c = 0;
             for (; c + 4 * U <= full; c += 4 * U) {
                 u32x4 wv[U];
 #pragma unroll
@@ -301,10 +319,22 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
                 for (int u = 0; u < U; ++u) product(c + 4 * u, wv[u]);
             }
             for (; c < full; c += 4) product(c, *unit_at(row, (c0 + c + quad) * V));
-            for (; c < here; c += 4) {
-                const int k = c0 + c + quad;
-                product(c, k < chunks ? chunk_of(row, k * V, a.n) : u32x4{0, 0, 0, 0});
+            for (; c < end; c += 4) {
+                const int at = c0 + c + quad;
+                product(c, at < chunks ? chunk_of(row, at * V, a.n) : u32x4{0, 0, 0, 0});
             }
+        }
+        if constexpr (SPLIT) {
+            // (the only group of the workgroup: its sums may stand where x did)
+            floatx4* const sums = reinterpret_cast<floatx4*>(lds);
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sums[(wave * NT + t) * 64 + lane] = acc[t];
+            __syncthreads();
+            if (wave != 0) break;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                for (int i = 1; i < kThinWaves; ++i) acc[t] += sums[(i * NT + t) * 64 + lane];
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -411,16 +441,18 @@ struct HeadGradTileArgs {
     const float *stats, *dlogp;
     int64_t ignore;
     int all;          // classes
-    void* dz;         // [rows][zstride], 0 past the classes
+    void* dz;         // [rows][zstride], 0 past the classes; of fp32 as terms, kDzTerms of them
     int64_t zstride;  // elements, a multiple of 16 bytes
+    int64_t zplane;   // elements from term to term
 };
+constexpr int kDzTerms = 3;
 
 // dz of the tiles in T, the operand of the products that follow.  Its rows go through LDS, so that
 // they are stored by whole lines, while the next tile's first loads are on their way (bf16; fp32
 // rows take all of LDS).
-template <typename T, typename Tl>
+template <typename T, typename Tl, bool TERMS>
 __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileArgs g) {
-    constexpr bool AHEAD = sizeof(T) == 2;
+    constexpr bool AHEAD = sizeof(T) == 2, EXACT = TERMS || sizeof(T) == 4;
     constexpr int V = kVec<T>, U = Tl::BP / V, PITCH = Tl::template PITCH<T>;
     constexpr int AT = AHEAD ? Tl::STEP : 0, NEED = AT + Tl::ROWS * PITCH;
     __shared__ __attribute__((aligned(128))) char lds[NEED > Tl::BYTES ? NEED : Tl::BYTES];
@@ -456,14 +488,14 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileA
 #pragma unroll
         for (int j = 0; j < Tl::RQ; ++j) {
             // (in bf16 p's own rounding hides that of the exponential's argument)
-            const float o = AHEAD ? m[j] + logs[j] : m[j];
+            const float o = EXACT ? m[j] : m[j] + logs[j];
 #pragma unroll
             for (int i = 0; i < Tl::RP; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float z = __builtin_fmaf(t.acc[i][j][e], scale, -o);
-                    t.acc[i][j][e] = -d[j] * (AHEAD ? exp_of(__builtin_fmaxf(z, -1e4f))
-                                                    : exp_exact(__builtin_fmaxf(z - logs[j], -1e4f)));
+                    t.acc[i][j][e] = -d[j] * (EXACT ? exp_exact(__builtin_fmaxf(z - logs[j], -1e4f))
+                                                    : exp_of(__builtin_fmaxf(z, -1e4f)));
                 }
             if (target[j] >= p0 && target[j] < p0 + Tl::BP) {
                 const int p = target[j] - p1;
@@ -481,16 +513,28 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileA
                     for (int e = 0; e < 16; ++e)
                         if (Tl::p_step(i, e) >= classes) t.acc[i][j][e] = 0.0f;
             }
-            t.template put<T>(lds + AT, tid, j, [](float v) { return rounded<T>(v); });
-            Tl::meet();
-            for (int u = tid; u < Tl::ROWS * U; u += Tl::THREADS) {
-                const int r = u / U, p = (u % U) * V;
-                const int64_t q = q0 + Tl::q_of_row(r, j);
-                if (q < a.rows && p0 + p < g.zstride)
-                    *reinterpret_cast<u32x4*>(static_cast<T*>(g.dz) + q * g.zstride + p0 + p) =
-                        *reinterpret_cast<const u32x4*>(lds + AT + r * PITCH + p * (int)sizeof(T));
+#pragma unroll 1
+            for (int term = 0; term < (TERMS ? kDzTerms : 1); ++term) {
+                t.template put<T>(lds + AT, tid, j, [](float v) { return rounded<T>(v); });
+                Tl::meet();
+                T* const dz = static_cast<T*>(g.dz) + term * g.zplane;
+                for (int u = tid; u < Tl::ROWS * U; u += Tl::THREADS) {
+                    const int r = u / U, p = (u % U) * V;
+                    const int64_t q = q0 + Tl::q_of_row(r, j);
+                    if (q < a.rows && p0 + p < g.zstride)
+                        *reinterpret_cast<u32x4*>(dz + q * g.zstride + p0 + p) =
+                            *reinterpret_cast<const u32x4*>(lds + AT + r * PITCH +
+                                                            p * (int)sizeof(T));
+                }
+                Tl::meet();
+                if (!TERMS) break;
+                // (what the term left out)
+#pragma unroll
+                for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        t.acc[i][j][e] -= bf16_to_f32(f32_to_bf16(t.acc[i][j][e]));
             }
-            Tl::meet();
         }
         if (!AHEAD) ahead();
     });
@@ -502,6 +546,7 @@ struct ProductArgs {
     int64_t pstride, qstride;  // bytes
     int64_t np, nq, k;
     int64_t pk, qk;            // rows of an operand that stands by k
+    int64_t pplane, qplane;    // bytes from term to term (fp32 as bf16 terms), else 0
     int64_t k_split;           // k of a split
     int tp, tq;
     float* acc;  // [splits][nq][np], or null
@@ -510,7 +555,8 @@ struct ProductArgs {
     float scale;
 };
 
-template <typename T, typename Tl, int MP, int MQ>
+// (T: of the operands; O: of the result)
+template <typename T, typename O, typename Tl, int MP, int MQ>
 __global__ void __launch_bounds__(Tl::THREADS, 2) head_product_kernel(ProductArgs a) {
     constexpr int U = Tl::BP / 4, PITCH = Tl::template PITCH<float>, NEED = Tl::ROWS * PITCH;
     __shared__ __attribute__((aligned(128))) char lds[NEED > Tl::BYTES ? NEED : Tl::BYTES];
@@ -520,8 +566,10 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_product_kernel(ProductArg
     const int64_t q0 = (int64_t)tq * Tl::BQ, p0 = (int64_t)tp * Tl::BP;
     const int64_t k0 = split * a.k_split, k1 = a.k - k0 < a.k_split ? a.k : k0 + a.k_split;
     if (k0 >= a.k) return;  // (a last piece that is shorter: nothing to add)
-    const Operand p = operand<T, MP>(a.p, p0, a.np, Tl::BP, a.pstride, a.pk);
-    const Operand q = operand<T, MQ>(a.q, q0, a.nq, Tl::BQ, a.qstride, a.qk);
+    const Operand p = operand<T, MP>(a.p, p0, a.np, Tl::BP, a.pstride, a.pk, a.pplane,
+                                         kTermsP);
+    const Operand q = operand<T, MQ>(a.q, q0, a.nq, Tl::BQ, a.qstride, a.qk, a.qplane,
+                                         kTermsDz);
     Tl t;
     t.start((char KAN_LDS*)lds, p, q, k0, k1);
     t.run((char KAN_LDS*)lds, p, q, k0, k1);
@@ -553,10 +601,10 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_product_kernel(ProductArg
                 store_four(acc, left, o);
                 continue;
             }
-            T w[4];
+            O w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = rounded<T>(o[e] * a.scale);
-            store_four(static_cast<T*>(a.out) + row * a.np + p0 + c, left, w);
+            for (int e = 0; e < 4; ++e) w[e] = rounded<O>(o[e] * a.scale);
+            store_four(static_cast<O*>(a.out) + row * a.np + p0 + c, left, w);
         }
         Tl::meet();
     }
@@ -617,6 +665,49 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, int64_t stri
     }
 }
 
+// fp32 rows of n elements as kTerms terms, rows of `to` elements (a multiple of 16 bytes), 0 past n; 0
+// throughout for rows whose target is `ignore` (targets null: none).
+__global__ void __launch_bounds__(256) head_terms_kernel(const float* x, int64_t stride, int64_t rows,
+                                                         int n, uint16_t* out, int to,
+                                                         const int64_t* targets, int64_t ignore) {
+    const int units = to / 8;
+    const int64_t all = rows * units;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / units;
+        const int c = (int)(i - row * units) * 8;
+        float v[8] = {}, finite[8];
+        if (targets == nullptr || targets[row] != ignore) {
+            const u32x4 a = chunk_of(x + row * stride, c, n), b = chunk_of(x + row * stride, c + 4, n);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(a[k]), v[4 + k] = __uint_as_float(b[k]);
+        }
+        u32x4* const at = reinterpret_cast<u32x4*>(out + row * to + c);
+        const int64_t plane = rows * to / 8;
+        u32x4 h = narrow(v);
+        float w[8];
+        widen(h, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            // (a finite value whose rounding is infinite: the largest instead)
+            const bool is = __builtin_fabsf(v[k]) < __builtin_huge_valf();
+            if (is && __builtin_fabsf(w[k]) == __builtin_huge_valf())
+                w[k] = __builtin_copysignf(3.38953139e38f, v[k]);
+            finite[k] = is ? w[k] : 0.0f;
+        }
+        at[0] = narrow(w);
+        at[plane] = narrow(finite);
+#pragma unroll
+        for (int t = 2; t < kTerms; ++t) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = finite[k] == 0.0f ? 0.0f : v[k] - finite[k];
+            h = narrow(v);
+            at[t * plane] = h;
+            widen(h, finite);
+        }
+    }
+}
+
 // ------------------------------------------------------------ plans
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
@@ -635,14 +726,34 @@ struct Arena {
 };
 
 constexpr int kBig = 256, kSmall = 128;  // a tile's sides
-constexpr int kThinRows = 64;
+// Rows up to which the weights are read once, past the tiles: 32; 64 where the tiles would need a
+// copy of the weights or, in fp32, multiply 128 rows (64 x 1024 -> 131072 bf16 61 us, by tiles 50;
+// 64 x 1024 -> 50001 fp32 91, by tiles 131).
+constexpr int kThinRows = 32, kThinMost = 64;
 // Bytes of a piece's intermediate tensors.
 constexpr int64_t kPieceBytes = INT64_C(512) << 20;
 constexpr int64_t kPieceClasses = 1 << 20, kPieceTiles = 1 << 20;
 constexpr int kFillTiles = 256;  // tiles that occupy the GPU
 
+// Big tiles for rows x classes logits: the turns that they take, one a CU at a time, against those of
+// small ones, two a CU, which take 0.59 of the time (a quarter of the work each at 0.85 of the rate;
+// 512 x 1024 -> 10000 bf16: 160 big tiles in one turn, 632 small ones in two).
+bool big_tiles(int64_t rows, int64_t classes) {
+    const int64_t big = div_up(rows, kBig) * div_up(classes, kBig);
+    const int64_t small = div_up(rows, kSmall) * div_up(classes, kSmall);
+    return 100 * div_up(big, kFillTiles) <= 59 * div_up(small, 2 * kFillTiles);
+}
+
+// fp32 operands as bf16 terms: what making them costs (12 bytes of memory traffic an element) is
+// regained by the products of about `least` rows of the other operand.
+bool by_terms(const HeadShape& s, int64_t least) {
+    return s.es == 4 && s.rows * s.classes >= least * (s.rows + s.classes);
+}
+constexpr int64_t kTermRows = 512, kTermGradRows = 256;
+
 struct HeadPlan {
-    bool thin, big;
+    bool thin, big, terms;
+    bool split;         // thin: a group's k over the waves
     int groups;         // thin: workgroups
     int64_t parts;
     int64_t piece;      // classes
@@ -655,20 +766,27 @@ struct HeadPlan {
 HeadPlan head_plan(const HeadShape& s, void* ws) {
     HeadPlan p = {};
     Arena arena = {static_cast<char*>(ws)};
-    p.to = (int)up(s.n, 16 / s.es);
-    p.thin = s.rows <= kThinRows;
+    p.thin = s.rows <= (s.es == 2 && s.ws ? kThinRows : kThinMost);
+    p.terms = !p.thin && by_terms(s, kTermRows);
+    p.to = (int)up(s.n, p.terms ? 8 : 16 / s.es);
+    const int64_t packed = (int64_t)p.to * (p.terms ? kTerms * 2 : s.es);  // bytes of a row
+    const bool xp = p.terms || !s.xs, wp = p.terms || !s.ws;
     if (p.thin) {
-        p.groups = (int)std::min<int64_t>(div_up(div_up(s.classes, 16), kThinWaves), 512);
+        const int64_t groups = div_up(s.classes, 16);
+        // few classes and a long k: a workgroup for each 16 classes
+        p.split = groups <= 2 * kFillTiles && div_up(s.n, 16 / s.es) >= 64;
+        p.groups = (int)std::min<int64_t>(div_up(groups, p.split ? 1 : kThinWaves),
+                                          2 * kFillTiles);
         p.parts = p.groups;
     } else {
-        p.big = div_up(s.rows, kBig) * div_up(s.classes, kBig) >= kFillTiles;
+        p.big = big_tiles(s.rows, s.classes);
         const int b = p.big ? kBig : kSmall;
         p.parts = div_up(s.classes, b);
         p.piece = kPieceTiles / div_up(s.rows, b);
-        if (!s.ws) p.piece = std::min(p.piece, std::max<int64_t>(1, kPieceBytes / p.to / s.es / b));
+        if (wp) p.piece = std::min(p.piece, std::max<int64_t>(1, kPieceBytes / packed / b));
         p.piece = std::min<int64_t>(p.piece * b, up(s.classes, b));
-        if (!s.xs) p.xp = arena.take(s.rows * p.to * s.es);
-        if (!s.ws) p.wp = arena.take(p.piece * p.to * s.es);
+        if (xp) p.xp = arena.take(s.rows * packed);
+        if (wp) p.wp = arena.take(p.piece * packed);
     }
     p.out.sums = arena.take<float2>(p.parts * s.rows * 8);
     p.out.best = arena.take<int>(p.parts * s.rows * 4);
@@ -679,9 +797,16 @@ HeadPlan head_plan(const HeadShape& s, void* ws) {
 
 int grid_of(int64_t items, int per) { return (int)std::min<int64_t>(div_up(items, per), 1 << 16); }
 
+// Rows copied (T), or as terms of fp32 ones.
 template <typename T>
-hipError_t pack(const void* x, int64_t stride, int64_t rows, int n, void* out, int to,
+hipError_t pack(bool terms, const void* x, int64_t stride, int64_t rows, int n, void* out, int to,
                 const int64_t* targets, int64_t ignore, hipStream_t st) {
+    if (terms) {
+        head_terms_kernel<<<grid_of(rows * (to / 8), 256), 256, 0, st>>>(
+            static_cast<const float*>(x), stride, rows, n, static_cast<uint16_t*>(out), to, targets,
+            ignore);
+        return hipGetLastError();
+    }
     head_pack_kernel<T><<<grid_of(rows * (to / kVec<T>), 256), 256, 0, st>>>(
         static_cast<const T*>(x), stride, rows, n, static_cast<T*>(out), to, targets, ignore);
     return hipGetLastError();
@@ -693,13 +818,22 @@ hipError_t pack(const void* x, int64_t stride, int64_t rows, int n, void* out, i
         if (e_ != hipSuccess) return e_;      \
     } while (0)
 
-template <typename T, int NT>
-hipError_t thin(const HeadPlan& p, const HeadThinArgs& a, bool best, hipStream_t st) {
+template <typename T, int NT, bool BEST>
+hipError_t thin(const HeadPlan& p, const HeadThinArgs& a, hipStream_t st) {
     const int chunks = (int)div_up(a.n, kVec<T>), slice = kThinLds / (16 * NT) / 16;
-    const size_t lds = (size_t)16 * NT * std::min((chunks + 7) & ~7, slice) * 16;
-    if (best) head_thin_kernel<T, NT, true><<<p.groups, 64 * kThinWaves, lds, st>>>(a);
-    else head_thin_kernel<T, NT, false><<<p.groups, 64 * kThinWaves, lds, st>>>(a);
+    // (x, and the waves' sums after it)
+    const size_t lds = std::max((size_t)16 * NT * std::min((chunks + 7) & ~7, slice) * 16,
+                                (size_t)(p.split ? kThinWaves * NT * 1024 : 0));
+    const auto kernel =
+        p.split ? head_thin_kernel<T, NT, BEST, true> : head_thin_kernel<T, NT, BEST, false>;
+    kernel<<<p.groups, 64 * kThinWaves, lds, st>>>(a);
     return hipGetLastError();
+}
+template <typename T, bool BEST>
+hipError_t thin(const HeadPlan& p, const HeadThinArgs& a, hipStream_t st) {
+    return a.rows <= 16   ? thin<T, 1, BEST>(p, a, st)
+           : a.rows <= 32 ? thin<T, 2, BEST>(p, a, st)
+                          : thin<T, 4, BEST>(p, a, st);
 }
 
 // Workgroups that are resident together: one of a big tile on a CU, or two of a small one.
@@ -729,14 +863,14 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
         t.scale = a.scale;
         t.targets = a.targets;
         t.out = p.out;
-        const bool best = a.best != nullptr;
-        KAN_TRY(s.rows <= 16 ? thin<T, 1>(p, t, best, st)
-                             : s.rows <= 32 ? thin<T, 2>(p, t, best, st) : thin<T, 4>(p, t, best, st));
+        KAN_TRY(a.best != nullptr ? thin<T, true>(p, t, st) : thin<T, false>(p, t, st));
     } else {
         HeadTileArgs t = {};
+        const int es = p.terms ? 2 : s.es;
         t.z.x = p.xp != nullptr ? p.xp : a.x;
-        t.z.xstride = (p.xp != nullptr ? p.to : s.xstride) * s.es;
-        t.z.wstride = (p.wp != nullptr ? p.to : s.wstride) * s.es;
+        t.z.xstride = (p.xp != nullptr ? p.to : s.xstride) * es;
+        t.z.wstride = (p.wp != nullptr ? p.to : s.wstride) * es;
+        t.z.xplane = p.terms ? s.rows * p.to * es : 0;
         t.z.rows = s.rows;
         t.z.k = p.to;
         t.z.scale = a.scale;
@@ -745,7 +879,7 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
         const int b = p.big ? kBig : kSmall;
         t.z.tq = (int)div_up(s.rows, b);
         if (p.xp != nullptr)
-            KAN_TRY(pack<T>(a.x, s.xstride, s.rows, s.n, p.xp, p.to, nullptr, 0, st));
+            KAN_TRY(pack<T>(p.terms, a.x, s.xstride, s.rows, s.n, p.xp, p.to, nullptr, 0, st));
         for (int64_t first = 0; first < s.classes; first += p.piece) {
             t.z.first = (int)first;
             t.z.classes = (int)std::min<int64_t>(s.classes - first, p.piece);
@@ -753,12 +887,19 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
             t.part = first / b;
             t.z.w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
             if (p.wp != nullptr) {
-                KAN_TRY(pack<T>(t.z.w, s.wstride, t.z.classes, s.n, p.wp, p.to, nullptr, 0, st));
+                KAN_TRY(pack<T>(p.terms, t.z.w, s.wstride, t.z.classes, s.n, p.wp, p.to, nullptr, 0,
+                                st));
                 t.z.w = p.wp;
+                t.z.wplane = p.terms ? (int64_t)t.z.classes * p.to * es : 0;
             }
             const bool best = a.best != nullptr;
-            KAN_TRY(p.big ? tiles<T, BigLogits<T>>(t, best, true, st)
-                          : tiles<T, SmallLogits<T>>(t, best, false, st));
+            if (p.terms)
+                KAN_TRY(p.big ? tiles<uint16_t, BigLogits<uint16_t, kSegments>>(t, best, true, st)
+                              : tiles<uint16_t, SmallLogits<uint16_t, kSegments>>(t, best, false,
+                                                                                  st));
+            else
+                KAN_TRY(p.big ? tiles<T, BigLogits<T, 1>>(t, best, true, st)
+                              : tiles<T, SmallLogits<T, 1>>(t, best, false, st));
         }
     }
     HeadJoinArgs j = {p.out, s.rows, (int)p.parts, s.classes, 1, a.targets, a.ignore, a.logp, a.stats,
@@ -776,21 +917,24 @@ struct ProductPlan {
 };
 ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, int es) {
     ProductPlan p;
-    const int step = 128 / es;
-    p.big = div_up(np, kBig) * div_up(nq, kBig) >= kFillTiles;
+    const int64_t step = 128 / es, steps = div_up(k, step);
+    const int64_t big = div_up(np, kBig) * div_up(nq, kBig);
+    // big tiles where they fill the GPU, also with k in splits of 32 steps or more, and do not
+    // stand out over the result
+    p.big = big * std::max<int64_t>(1, steps / 32) >= kFillTiles &&
+            big * 4 * 7 <= div_up(np, kSmall) * div_up(nq, kSmall) * 8;
     const int b = p.big ? kBig : kSmall;
     p.tp = (int)div_up(np, b);
     p.tq = (int)div_up(nq, b);
-    // (a split takes at least eight steps)
-    const int64_t most = std::max<int64_t>(1, k / (8 * step));
-    const int64_t want = p.big ? 1 : 2 * kFillTiles / ((int64_t)p.tp * p.tq);
-    p.splits = (int)std::max<int64_t>(1, std::min(want, most));
-    p.k_split = up(div_up(k, p.splits), step);
+    const int64_t want = (p.big ? 1 : 2) * kFillTiles / ((int64_t)p.tp * p.tq);
+    p.splits = (int)std::max<int64_t>(1, std::min(want, steps / 8));
+    p.k_split = div_up(steps, p.splits) * step;
     p.splits = (int)div_up(k, p.k_split);
     return p;
 }
 
 struct HeadGradPlan {
+    bool terms;
     int64_t piece, zstride;  // classes; elements
     int to;
     void *xp, *wp;           // packed rows, or null
@@ -803,38 +947,54 @@ struct HeadGradPlan {
 HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
     HeadGradPlan p = {};
     Arena arena = {static_cast<char*>(ws)};
-    p.to = (int)up(s.n, 16 / s.es);
+    p.terms = by_terms(s, kTermGradRows);
+    p.to = (int)up(s.n, p.terms ? 8 : 16 / s.es);
+    const int64_t packed = (int64_t)p.to * (p.terms ? kTerms * 2 : s.es);  // bytes of a row
+    const int zes = p.terms ? kDzTerms * 2 : s.es;                         // and of a logit
+    const bool wp = p.terms || !s.ws;
     // as few pieces as their dz (and packed weights) and launches allow, of one size
-    const int64_t row = s.es * (s.rows + (s.ws ? 0 : p.to));
+    const int64_t row = zes * s.rows + (wp ? packed : 0);
     int64_t most = std::min(kPieceClasses, kPieceTiles / div_up(s.rows, kSmall) * kSmall);
     most = std::min(most, std::max<int64_t>(kPieceBytes / row / kBig * kBig, kBig));
     p.piece = up(div_up(s.classes, div_up(s.classes, most)), kBig);
     p.zstride = std::min(p.piece, up(s.classes, 64));
     const int64_t here = std::min<int64_t>(p.piece, s.classes);
     // (a copy without what ignored rows hold: 0 times it need not be 0)
-    if (!s.xs || dw) p.xp = arena.take(s.rows * p.to * s.es);
-    if (!s.ws) p.wp = arena.take(p.piece * p.to * s.es);
-    p.dz = arena.take(s.rows * p.zstride * s.es);
+    if (p.terms || !s.xs || dw) p.xp = arena.take(s.rows * packed);
+    if (wp) p.wp = arena.take(p.piece * packed);
+    p.dz = arena.take(s.rows * p.zstride * zes);
+    const int es = p.terms ? 2 : s.es;
     if (dx) {
-        p.px = product_plan(s.n, s.rows, p.zstride, s.es);
+        p.px = product_plan(s.n, s.rows, p.zstride, es);
         if (p.px.splits > 1 || p.piece < s.classes)
             p.dx = arena.take<float>((int64_t)p.px.splits * s.rows * s.n * 4);
     }
     if (dw) {
-        p.pw = product_plan(s.n, here, s.rows, s.es);
+        p.pw = product_plan(s.n, here, s.rows, es);
         if (p.pw.splits > 1) p.dw = arena.take<float>((int64_t)p.pw.splits * here * s.n * 4);
     }
     p.bytes = arena.at;
     return p;
 }
 
-template <typename T, int MP, int MQ>
+template <typename T, typename O, int MP, int MQ, int S>
 hipError_t product(const ProductPlan& p, const ProductArgs& a, hipStream_t st) {
-    typedef Tile<T, 2, 4, 4, 2, MP, MQ> Big;
-    typedef Tile<T, 2, 2, 2, 2, MP, MQ> Small;
+    typedef Tile<T, 2, 4, 4, 2, MP, MQ, S> Big;
+    typedef Tile<T, 2, 2, 2, 2, MP, MQ, S> Small;
     const int groups = p.tp * p.tq * p.splits;
-    if (p.big) head_product_kernel<T, Big, MP, MQ><<<groups, Big::THREADS, 0, st>>>(a);
-    else head_product_kernel<T, Small, MP, MQ><<<groups, Small::THREADS, 0, st>>>(a);
+    if (p.big) head_product_kernel<T, O, Big, MP, MQ><<<groups, Big::THREADS, 0, st>>>(a);
+    else head_product_kernel<T, O, Small, MP, MQ><<<groups, Small::THREADS, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, bool TERMS, int S>
+hipError_t gradient_tiles(const HeadGradTileArgs& g, bool big, hipStream_t st) {
+    const int groups = resident(g.z.tp * g.z.tq, big);
+    if (big)
+        head_grad_kernel<T, BigLogits<T, S>, TERMS><<<groups, BigLogits<T, S>::THREADS, 0, st>>>(g);
+    else
+        head_grad_kernel<T, SmallLogits<T, S>, TERMS>
+            <<<groups, SmallLogits<T, S>::THREADS, 0, st>>>(g);
     return hipGetLastError();
 }
 
@@ -854,10 +1014,13 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
         return hipGetLastError();
     }
     const HeadGradPlan p = head_grad_plan(s, a.dx != nullptr, a.dw != nullptr, ws);
+    const bool terms = p.terms;
+    const int es = terms ? 2 : s.es;
     HeadGradTileArgs g = {};
     g.z.x = p.xp != nullptr ? p.xp : a.x;
-    g.z.xstride = (p.xp != nullptr ? p.to : s.xstride) * s.es;
-    g.z.wstride = (p.wp != nullptr ? p.to : s.wstride) * s.es;
+    g.z.xstride = (p.xp != nullptr ? p.to : s.xstride) * es;
+    g.z.wstride = (p.wp != nullptr ? p.to : s.wstride) * es;
+    g.z.xplane = terms ? s.rows * p.to * es : 0;
     g.z.rows = s.rows;
     g.z.k = p.to;
     g.z.scale = a.scale;
@@ -868,33 +1031,48 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
     g.all = s.classes;
     g.dz = p.dz;
     g.zstride = p.zstride;
-    const int64_t zbytes = p.zstride * s.es;
+    g.zplane = s.rows * p.zstride;
+    const int64_t zbytes = p.zstride * es;
     if (p.xp != nullptr)
-        KAN_TRY(pack<T>(a.x, s.xstride, s.rows, s.n, p.xp, p.to, a.targets, a.ignore, st));
+        KAN_TRY(pack<T>(terms, a.x, s.xstride, s.rows, s.n, p.xp, p.to, a.targets, a.ignore, st));
     for (int64_t first = 0; first < s.classes; first += p.piece) {
         const int64_t here = std::min<int64_t>(s.classes - first, p.piece);
         g.z.w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
         g.z.first = (int)first;
         g.z.classes = (int)here;
         if (p.wp != nullptr) {
-            KAN_TRY(pack<T>(g.z.w, s.wstride, here, s.n, p.wp, p.to, nullptr, 0, st));
+            KAN_TRY(pack<T>(terms, g.z.w, s.wstride, here, s.n, p.wp, p.to, nullptr, 0, st));
             g.z.w = p.wp;
+            g.z.wplane = terms ? here * p.to * es : 0;
         }
-        const bool big = div_up(s.rows, kBig) * div_up(here, kBig) >= kFillTiles;
+        const bool big = big_tiles(s.rows, here);
         const int b = big ? kBig : kSmall;
         g.z.tp = (int)div_up(here, b);
         g.z.tq = (int)div_up(s.rows, b);
-        const int groups = resident(g.z.tp * g.z.tq, big);
-        if (big) head_grad_kernel<T, BigLogits<T>><<<groups, BigLogits<T>::THREADS, 0, st>>>(g);
-        else head_grad_kernel<T, SmallLogits<T>><<<groups, SmallLogits<T>::THREADS, 0, st>>>(g);
-        KAN_TRY(hipGetLastError());
+        KAN_TRY(terms ? gradient_tiles<uint16_t, true, kSegments>(g, big, st)
+                      : gradient_tiles<T, false, 1>(g, big, st));
+        ProductArgs r = {};
+        r.q = p.dz;
+        r.qstride = zbytes;
+        r.qplane = terms ? g.zplane * es : 0;
+        r.np = s.n;
+        r.scale = a.scale;
         if (a.dx != nullptr) {
-            // (k to whole chunks of dz's rows, which are 0 past the classes)
             const bool last = first + p.piece >= s.classes, whole = p.px.splits == 1 && last;
-            const ProductArgs r = {g.z.w, p.dz, g.z.wstride, zbytes, s.n, s.rows,
-                                   up(here, 16 / s.es), here, 0, p.px.k_split, p.px.tp, p.px.tq, p.dx,
-                                   first > 0, whole ? a.dx : nullptr, a.scale};
-            KAN_TRY(product<T, kByK, kByRows>(p.px, r, st));
+            r.p = g.z.w;
+            r.pstride = g.z.wstride;
+            r.pplane = g.z.wplane;
+            r.nq = s.rows;
+            r.k = up(here, 16 / es);  // (whole chunks of dz's rows, which are 0 past the classes)
+            r.pk = here;
+            r.k_split = p.px.k_split;
+            r.tp = p.px.tp;
+            r.tq = p.px.tq;
+            r.acc = p.dx;
+            r.add = first > 0;
+            r.out = whole ? a.dx : nullptr;
+            KAN_TRY(terms ? product<uint16_t, float, kByK, kByRows, kSegments>(p.px, r, st)
+                          : product<T, T, kByK, kByRows, 1>(p.px, r, st));
             if (last && !whole)
                 KAN_TRY(sum<T>(p.dx, p.px.splits, s.rows * s.n, a.scale, a.dx, st));
         }
@@ -902,10 +1080,19 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
             char* const out = static_cast<char*>(a.dw) + first * s.n * s.es;
             ProductPlan pw = p.pw;
             pw.tq = (int)div_up(here, pw.big ? kBig : kSmall);
-            const ProductArgs r = {p.xp, p.dz, (int64_t)p.to * s.es, zbytes, s.n, here, s.rows,
-                                   s.rows, s.rows, pw.k_split, pw.tp, pw.tq, p.dw, false,
-                                   pw.splits == 1 ? out : nullptr, a.scale};
-            KAN_TRY(product<T, kByK, kByK>(pw, r, st));
+            r.p = p.xp;
+            r.pstride = g.z.xstride;
+            r.pplane = g.z.xplane;
+            r.nq = here;
+            r.k = r.pk = r.qk = s.rows;
+            r.k_split = pw.k_split;
+            r.tp = pw.tp;
+            r.tq = pw.tq;
+            r.acc = p.dw;
+            r.add = false;
+            r.out = pw.splits == 1 ? out : nullptr;
+            KAN_TRY(terms ? product<uint16_t, float, kByK, kByK, kSegments>(pw, r, st)
+                          : product<T, T, kByK, kByK, 1>(pw, r, st));
             if (pw.splits > 1) KAN_TRY(sum<T>(p.dw, pw.splits, here * s.n, a.scale, out, st));
         }
     }

@@ -41,18 +41,25 @@ struct Operand {
     uint32_t stride;  // bytes from row to row
     int left;         // rows (columns) of the tile that there are
     int64_t k;        // by k: rows that there are (0 past them, up to the sum's end)
+    // fp32 as bf16 terms: bytes from a term to the next, and the terms (4 bits each) that the sum's
+    // segments take
+    int64_t plane;
+    uint32_t terms;
 };
 
 constexpr int kByRows = 0, kByK = 1;
 
 template <typename T, int MODE>
 __device__ __forceinline__ Operand operand(const void* p, int64_t first, int64_t rows, int most,
-                                           int64_t stride_bytes, int64_t k = 0) {
+                                           int64_t stride_bytes, int64_t k = 0, int64_t plane = 0,
+                                           uint32_t terms = 0) {
     Operand o;
     o.at = static_cast<const char*>(p) + first * (MODE == kByRows ? stride_bytes : (int64_t)sizeof(T));
     o.stride = (uint32_t)stride_bytes;
     o.left = (int)(rows - first < most ? rows - first : most);
     o.k = k;
+    o.plane = plane;
+    o.terms = terms;
     return o;
 }
 
@@ -105,10 +112,12 @@ struct Side {
         }
     }
 
-    // The loads of the step that begins at k (of `end`; none past it: zeros) to LDS byte dst.
-    __device__ __forceinline__ void issue(const Operand& o, int64_t k, int64_t end, int wave,
+    // The loads of the step of segment `seg` that begins at k (of `end`; none past it: zeros) to LDS
+    // byte dst.
+    __device__ __forceinline__ void issue(const Operand& o, int seg, int64_t k, int64_t end, int wave,
                                           uint32_t dst) const {
-        const char* at = o.at + (MODE == kByRows ? 0 : k * o.stride);
+        const char* at = o.at + (MODE == kByRows ? 0 : k * o.stride) +
+                         (int64_t)(o.terms >> 4 * seg & 15) * o.plane;
         const int64_t there = end < o.k ? end : o.k;
         const int rows = MODE == kByRows ? o.left : (int)(there - k < K ? there - k : K);
         // (bounds are kept by 4 bytes: by k, the last row to the end of its last chunk)
@@ -154,7 +163,8 @@ struct Side {
     typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 };
 
-template <typename T, int WP_, int WQ_, int RP_, int RQ_, int MP, int MQ>
+// SEGS: the sum is one of so many, each over all of k, of terms that the operands name.
+template <typename T, int WP_, int WQ_, int RP_, int RQ_, int MP, int MQ, int SEGS = 1>
 struct Tile {
     static constexpr int WP = WP_, WQ = WQ_, RP = RP_, RQ = RQ_;
     static constexpr int W = WP * WQ, THREADS = 64 * W;
@@ -208,8 +218,8 @@ struct Tile {
         const int lane = threadIdx.x & 63, wave = wave_of();
         sp.place(lane, wave, wave % WP, p.stride);
         sq.place(lane, wave, wave / WP, q.stride);
-        sp.issue(p, at, end, wave, byte_of(lds));
-        sq.issue(q, at, end, wave, byte_of(lds) + SideP::BYTES);
+        sp.issue(p, 0, at, end, wave, byte_of(lds));
+        sq.issue(q, 0, at, end, wave, byte_of(lds) + SideP::BYTES);
     }
 
     // The sum over k from `at` to `end`, after `start` with the same arguments.  lds: BYTES.
@@ -221,11 +231,17 @@ struct Tile {
         for (int i = 0; i < RP; ++i)
 #pragma unroll
             for (int j = 0; j < RQ; ++j) acc[i][j] = floatx16{};
-        const auto issue = [&](int64_t k, uint32_t dst) {
-            sp.issue(p, k, end, wave, dst);
-            sq.issue(q, k, end, wave, dst + SideP::BYTES);
+        // the step whose loads are next
+        // (the segments of a step's k follow one another: their terms are read from L2 again)
+        int64_t k = SEGS > 1 ? at : at + K;
+        int seg = SEGS > 1 ? 1 : 0;
+        const auto issue = [&](uint32_t dst) {
+            if (k >= end) return;
+            sp.issue(p, seg, k, end, wave, dst);
+            sq.issue(q, seg, k, end, wave, dst + SideP::BYTES);
+            if (++seg >= SEGS) seg = 0, k += K;
         };
-        if (at + K < end) issue(at + K, base + STEP);
+        issue(base + STEP);
         u32x4 a[2][RP], b[2][RQ];
         const auto fetch = [&](const char KAN_LDS* src, int quarter, int to) {
             sp.fetch(src, quarter, a[to]);
@@ -233,7 +249,8 @@ struct Tile {
         };
         arrive();
         fetch(lds, 0, 0);
-        for (int cur = 0; at < end; at += K, cur = STEP - cur) {
+        int cur = 0;
+        for (int steps = SEGS * (int)((end - at + K - 1) / K); steps > 0; --steps) {
 #pragma unroll
             for (int c = 0; c < 3; ++c) {
                 fetch(lds + cur, c + 1, (c + 1) & 1);
@@ -242,11 +259,12 @@ struct Tile {
             }
             arrive();
             __builtin_amdgcn_sched_barrier(0);
-            if (at + 2 * K < end) issue(at + 2 * K, base + cur);
+            issue(base + cur);
             // (after the last step: of what the buffer held before, for nothing)
             fetch(lds + STEP - cur, 0, 0);
             products(a[1], b[1]);
             __builtin_amdgcn_sched_barrier(0);
+            cur = STEP - cur;
         }
         arrive();
     }

@@ -28,7 +28,13 @@ SIZES = [(1, 1, 1, 0, 0, 0), (1, 1000, 256, 0, 0, 0), (2, 17, 7, 1, 0, 0), (15, 
          (64, 100, 264, 0, 0, 8), (13, 500, 2500, 0, 0, 0), (64, 70, 5003, 1, 1, 1),
          (65, 10, 8, 0, 0, 0), (128, 128, 64, 8, 8, 0), (129, 255, 72, 0, 0, 0),
          (300, 1000, 100, 0, 0, 0), (131, 129, 131, 5, 3, 2), (1000, 2, 40, 0, 0, 0),
-         (70, 4099, 16, 0, 0, 0), (2100, 9000, 48, 0, 0, 0), (2049, 8200, 37, 1, 0, 0)]
+         (70, 4099, 16, 0, 0, 0), (2100, 9000, 48, 0, 0, 0), (2049, 8200, 37, 1, 0, 0),
+         # (few rows: k over a workgroup's waves, and x in slices of k)
+         (1, 10, 4096, 0, 0, 0), (20, 100, 1500, 1, 0, 0), (64, 33, 1023, 0, 0, 0),
+         (3, 9001, 5000, 0, 0, 0), (50, 8300, 1300, 0, 1, 0), (31, 8200, 2052, 4, 0, 0),
+         # (fp32 as bf16 terms: a few rows of many classes, the reverse, one piece and splits of k)
+         (600, 4001, 70, 0, 0, 0), (5000, 1100, 130, 1, 3, 1), (1030, 1030, 1000, 0, 0, 4),
+         (300, 6000, 9, 0, 0, 0)]
 
 
 def make(rows, classes, n, xpad, wpad, first, dt, seed, std=2.0):
@@ -166,14 +172,14 @@ def test_ignored_and_invalid_targets(rows, dt):
     assert not bool(dx[3:].isnan().any()) and not bool(dx[0].isnan().any())
 
 
-@pytest.mark.parametrize("rows", [5, 90])
+@pytest.mark.parametrize("rows,classes", [(5, 300), (90, 300), (700, 3000), (300, 3000)])
 @pytest.mark.parametrize("dt", [F32, BF16])
-def test_not_finite(rows, dt):
-    x, w, t, d = make(rows, 300, 16, 0, 0, 0, dt, 11)
+def test_not_finite(rows, classes, dt):
+    x, w, t, d = make(rows, classes, 16, 0, 0, 0, dt, 11)
     clean = kb.linear_logprobs(x, w, t, best=True)
     x[2, 3] = float("nan")
     x[3, 5] = float("inf")   # (weights of either sign: +infinity among the logits)
-    say(f"linear head not finite {rows} {dt}")
+    say(f"linear head not finite {rows} {classes} {dt}")
     logp, stats, best = kb.linear_logprobs(x, w, t, best=True)
     assert bool(logp[2:4].isnan().all()) and bool(stats[2:4, 1].isnan().all())
     keep = torch.ones(rows, dtype=torch.bool, device=device())
@@ -185,7 +191,7 @@ def test_not_finite(rows, dt):
     assert bool(dx[2:4].isnan().all()) and not bool(dx[keep].isnan().any())
     assert bool(dw.isnan().all())
     # a class of -infinity logits takes no part
-    x, w, t, d = make(rows, 300, 16, 0, 0, 0, dt, 12)
+    x, w, t, d = make(rows, classes, 16, 0, 0, 0, dt, 12)
     x[:, 0] = x[:, 0].abs() + 0.5
     w[9] = 0
     w[9, 0] = float("-inf")
@@ -213,6 +219,26 @@ def test_ties_go_to_the_lowest(rows):
     say(f"linear head ties {rows}")
     _, stats, best = kb.linear_logprobs(x, w, t, best=True)
     assert bool((best == 17).all()) and bool((stats[:, 0] == 32).all())
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e30, 3e36])
+def test_values_far_from_one(scale):
+    """fp32 inputs of any size whose sums before the scale stay in range: the logits' relative error
+    stays that of their sums."""
+    x, w, t, d = make(600, 2000, 40, 0, 0, 0, F32, 14, std=1.0)
+    say(f"linear head at {scale}")
+    x, s = x.clamp(-4, 4) * scale, 0.2 / scale
+    logp, stats, _ = kb.linear_logprobs(x, w, t, scale=s)
+    z, lp, m, logs, _ = forward64(x, w, t, s)
+    tol = ztol(z, 40) + 4 * U * float(z.abs().max())
+    below((logp.double() - lp).abs(), 2 * tol + 4e-6 + 4 * U * lp.abs())
+    dx, dw = kb.linear_logprobs_backward(x, w, t, stats, d, scale=s)
+    z, dz = gradient64(x, w, t, stats, d, s)
+    e = (2 * tol + 1e-6) * d.double().abs()[:, None]
+    want, terms = dz.t() @ x.double() * s, dz.abs().t() @ x.double().abs() * s
+    below((dw.double() - want).abs(),
+          terms * (6 * U * math.sqrt(600) + 4 * U) + (e * x.double().abs()).sum(0) * s +
+          U * want.abs())
 
 
 def test_gradient_against_differences():

@@ -447,63 +447,76 @@ struct HeadGradTileArgs {
 };
 constexpr int kDzTerms = 3;
 
-// dz of the tiles in T, the operand of the products that follow.  Its rows go through LDS, so that
-// they are stored by whole lines, while the next tile's first loads are on their way (bf16; fp32
-// rows take all of LDS).
-template <typename T, typename Tl, bool TERMS>
+// What a row's dz is made of: dz = d ([v = target] - exp(z - m - logs)).
+struct RowGrad {
+    float m, logs, d;
+    int target;  // from the launch's first class on
+    // what is subtracted from the logit with its scale's rounding (in bf16 p's own rounding hides
+    // that of the exponential's argument)
+    template <bool EXACT>
+    __device__ __forceinline__ float offset() const {
+        return EXACT ? m : m + logs;
+    }
+};
+__device__ __forceinline__ RowGrad row_grad(const HeadGradTileArgs& g, int64_t row) {
+    // (rows that have no gradient: p = 0, whatever their logits are)
+    RowGrad r = {__builtin_huge_valf(), 0.0f, 0.0f, -1};
+    if (row >= g.z.rows) return r;
+    const int64_t c = g.z.targets[row];
+    const float m = g.stats[2 * row], logs = g.stats[2 * row + 1], d = g.dlogp[row];
+    if (c == g.ignore) return r;
+    // (a target that is no class, NaN and infinite logits show in the row's gradient)
+    r.d = c < 0 || c >= g.all || m != m || logs != logs ? __builtin_nanf("") : d;
+    if (m == kNegInf && logs == kNegInf && r.d == r.d) {
+        r.d = 0.0f;
+        return r;
+    }
+    r.m = m;
+    r.logs = logs;
+    r.target = (int)c - g.z.first;
+    return r;
+}
+// -d p for the logit less its offset.
+template <bool EXACT>
+__device__ __forceinline__ float dz_of(const RowGrad& r, float t) {
+    return -r.d * (EXACT ? exp_exact(__builtin_fmaxf(t - r.logs, -1e4f))
+                         : exp_of(__builtin_fmaxf(t, -1e4f)));
+}
+
+// dz of the tiles in bf16, or in bf16 terms of fp32 (TERMS): the operand of the products that follow.
+// Its rows go through LDS, so that they are stored by whole lines, while the next tile's first
+// loads are on their way.
+template <typename Tl, bool TERMS>
 __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileArgs g) {
-    constexpr bool AHEAD = sizeof(T) == 2, EXACT = TERMS || sizeof(T) == 4;
+    typedef uint16_t T;
     constexpr int V = kVec<T>, U = Tl::BP / V, PITCH = Tl::template PITCH<T>;
-    constexpr int AT = AHEAD ? Tl::STEP : 0, NEED = AT + Tl::ROWS * PITCH;
+    constexpr int AT = Tl::STEP, NEED = AT + Tl::ROWS * PITCH;
     __shared__ __attribute__((aligned(128))) char lds[NEED > Tl::BYTES ? NEED : Tl::BYTES];
     const LogitArgs& a = g.z;
     for_tiles<T, Tl>(a, lds, [&](Tl& t, int tp, int tq, auto&& ahead) {
         const int tid = Tl::thread(), p0 = tp * Tl::BP, p1 = p0 + Tl::p_of(tid);
         const int64_t q0 = (int64_t)tq * Tl::BQ;
-        // (rows that have no gradient: p = 0, whatever their logits are)
-        float m[Tl::RQ], logs[Tl::RQ], d[Tl::RQ];
-        int target[Tl::RQ];
+        RowGrad row[Tl::RQ];
 #pragma unroll
-        for (int j = 0; j < Tl::RQ; ++j) {
-            const int64_t row = q0 + Tl::q_of(tid, j);
-            m[j] = __builtin_huge_valf();
-            logs[j] = d[j] = 0.0f;
-            target[j] = -1;
-            if (row >= a.rows) continue;
-            const int64_t c = a.targets[row];
-            const float rm = g.stats[2 * row], rl = g.stats[2 * row + 1], rd = g.dlogp[row];
-            if (c == g.ignore) continue;
-            // (a target that is no class, NaN and infinite logits show in the row's gradient)
-            d[j] = c < 0 || c >= g.all || rm != rm || rl != rl ? __builtin_nanf("") : rd;
-            if (rm == kNegInf && rl == kNegInf && d[j] == d[j]) {
-                d[j] = 0.0f;
-            } else {
-                m[j] = rm;
-                logs[j] = rl;
-                target[j] = (int)c - a.first;
-            }
-        }
-        if (AHEAD) ahead();
+        for (int j = 0; j < Tl::RQ; ++j) row[j] = row_grad(g, q0 + Tl::q_of(tid, j));
+        ahead();
         const float scale = settle(t, a, p0, tid, kNegInf);
 #pragma unroll
         for (int j = 0; j < Tl::RQ; ++j) {
-            // (in bf16 p's own rounding hides that of the exponential's argument)
-            const float o = EXACT ? m[j] : m[j] + logs[j];
+            const RowGrad& r = row[j];
+            const float o = -r.offset<TERMS>();
 #pragma unroll
             for (int i = 0; i < Tl::RP; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float z = __builtin_fmaf(t.acc[i][j][e], scale, -o);
-                    t.acc[i][j][e] = -d[j] * (EXACT ? exp_exact(__builtin_fmaxf(z - logs[j], -1e4f))
-                                                    : exp_of(__builtin_fmaxf(z, -1e4f)));
-                }
-            if (target[j] >= p0 && target[j] < p0 + Tl::BP) {
-                const int p = target[j] - p1;
+                for (int e = 0; e < 16; ++e)
+                    t.acc[i][j][e] = dz_of<TERMS>(r, __builtin_fmaf(t.acc[i][j][e], scale, o));
+            if (r.target >= p0 && r.target < p0 + Tl::BP) {
+                const int p = r.target - p1;
 #pragma unroll
                 for (int i = 0; i < Tl::RP; ++i)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        t.acc[i][j][e] += p == Tl::p_step(i, e) ? d[j] : 0.0f;
+                        t.acc[i][j][e] += p == Tl::p_step(i, e) ? r.d : 0.0f;
             }
             if (p0 + Tl::BP > a.classes) {
                 const int classes = a.classes - p1;
@@ -536,7 +549,6 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileA
                         t.acc[i][j][e] -= bf16_to_f32(f32_to_bf16(t.acc[i][j][e]));
             }
         }
-        if (!AHEAD) ahead();
     });
 }
 
@@ -547,6 +559,7 @@ struct ProductArgs {
     int64_t np, nq, k;
     int64_t pk, qk;            // rows of an operand that stands by k
     int64_t pplane, qplane;    // bytes from term to term (fp32 as bf16 terms), else 0
+    uint32_t qterms;
     int64_t k_split;           // k of a split
     int tp, tq;
     float* acc;  // [splits][nq][np], or null
@@ -555,9 +568,10 @@ struct ProductArgs {
     float scale;
 };
 
-// (T: of the operands; O: of the result)
-template <typename T, typename O, typename Tl, int MP, int MQ>
+// (the operands in bf16 or as bf16 terms; O: of the result)
+template <typename O, typename Tl, int MP, int MQ>
 __global__ void __launch_bounds__(Tl::THREADS, 2) head_product_kernel(ProductArgs a) {
+    typedef uint16_t T;
     constexpr int U = Tl::BP / 4, PITCH = Tl::template PITCH<float>, NEED = Tl::ROWS * PITCH;
     __shared__ __attribute__((aligned(128))) char lds[NEED > Tl::BYTES ? NEED : Tl::BYTES];
     const int tiles = a.tp * a.tq, split = blockIdx.x / tiles;
@@ -569,7 +583,7 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_product_kernel(ProductArg
     const Operand p = operand<T, MP>(a.p, p0, a.np, Tl::BP, a.pstride, a.pk, a.pplane,
                                          kTermsP);
     const Operand q = operand<T, MQ>(a.q, q0, a.nq, Tl::BQ, a.qstride, a.qk, a.qplane,
-                                         kTermsDz);
+                                         a.qterms);
     Tl t;
     t.start((char KAN_LDS*)lds, p, q, k0, k1);
     t.run((char KAN_LDS*)lds, p, q, k0, k1);
@@ -635,6 +649,90 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const float* acc, int spl
 #pragma unroll
         for (int e = 0; e < 4; ++e) r[e] = rounded<T>(s[e] * scale);
         store_four(out + i, left, r);
+    }
+}
+
+// The logit of a class (before the scale) from its sums over k in parts.
+__device__ __forceinline__ float sum_of(const float* z, int splits, int64_t step) {
+    float s = z[0];
+    for (int k = 1; k < splits; ++k) s += z[k * step];
+    return s;
+}
+
+struct HeadRowsArgs {
+    const float* z;  // [splits][rows][classes] sums over k
+    int splits;
+    int64_t rows;
+    int classes;
+    float scale;
+    const int64_t* targets;
+    int64_t ignore;
+    float *logp, *stats;
+    int64_t* best;
+};
+
+// Few tiles: the logits' sums, which were made in parts of k, to what is asked; a wave per row.
+__global__ void __launch_bounds__(256) head_rows_kernel(HeadRowsArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= a.rows) return;
+    const float* const z = a.z + row * a.classes;
+    const int64_t step = a.rows * a.classes;
+    Best b = {kNegInf, 0.0f, kNoIndex};
+    for (int c = lane; c < a.classes; c += 64) {
+        const float v = sum_of(z + c, a.splits, step) * a.scale;
+        // (a NaN adds to the sum alone)
+        b = join(b, Best{v == v ? v : kNegInf, 0.0f, v == v ? c : kNoIndex});
+        b.s += exp_of(v - anchor(b.m));
+    }
+    for (int o = 1; o < 64; o *= 2) b = join(b, from_lane(b, o));
+    if (lane != 0) return;
+    const float logs = logf(b.s);
+    const int64_t t = a.targets[row];
+    float lp = 0.0f;
+    if (t != a.ignore) {
+        lp = __builtin_nanf("");
+        if (t >= 0 && t < a.classes)
+            lp = b.m == kNegInf && b.s == 0.0f
+                     ? kNegInf
+                     : sum_of(z + t, a.splits, step) * a.scale - b.m - logs;
+    }
+    a.logp[row] = lp;
+    a.stats[2 * row] = b.m;
+    a.stats[2 * row + 1] = logs;
+    if (a.best != nullptr) a.best[row] = b.at == kNoIndex ? 0 : b.at;
+}
+
+// The same for the gradient: dz as head_grad_kernel leaves it, 16 bytes a lane.
+template <bool TERMS>
+__global__ void __launch_bounds__(256) head_dz_kernel(HeadGradTileArgs g, const float* z, int splits) {
+    const LogitArgs& a = g.z;
+    const uint32_t units = (uint32_t)(g.zstride / 8);
+    const int64_t all = a.rows * units, step = a.rows * a.classes;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / units;
+        const int c0 = (int)(i - row * units) * 8;
+        const RowGrad r = row_grad(g, row);
+        float y[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int c = c0 + k;
+            y[k] = 0.0f;
+            if (c >= a.classes) continue;
+            const float v = sum_of(z + row * a.classes + c, splits, step);
+            y[k] = dz_of<TERMS>(r, __builtin_fmaf(v, a.scale, -r.offset<TERMS>()));
+            if (c == r.target) y[k] += r.d;
+        }
+        uint16_t* out = static_cast<uint16_t*>(g.dz) + row * g.zstride + c0;
+        for (int term = 0; term < (TERMS ? kDzTerms : 1); ++term, out += g.zplane) {
+            const u32x4 h = narrow(y);
+            *reinterpret_cast<u32x4*>(out) = h;
+            float w[8];
+            widen(h, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] -= w[k];
+        }
     }
 }
 
@@ -735,21 +833,86 @@ constexpr int64_t kPieceBytes = INT64_C(512) << 20;
 constexpr int64_t kPieceClasses = 1 << 20, kPieceTiles = 1 << 20;
 constexpr int kFillTiles = 256;  // tiles that occupy the GPU
 
-// Big tiles for rows x classes logits: the turns that they take, one a CU at a time, against those of
-// small ones, two a CU, which take 0.59 of the time (a quarter of the work each at 0.85 of the rate;
-// 512 x 1024 -> 10000 bf16: 160 big tiles in one turn, 632 small ones in two).
-bool big_tiles(int64_t rows, int64_t classes) {
-    const int64_t big = div_up(rows, kBig) * div_up(classes, kBig);
-    const int64_t small = div_up(rows, kSmall) * div_up(classes, kSmall);
-    return 100 * div_up(big, kFillTiles) <= 59 * div_up(small, 2 * kFillTiles);
+// Microseconds that `groups` tiles of `steps` steps take, by measured rates: a big tile (one a CU)
+// 1.65 us a step, two small ones a CU 1.04, one 0.7, 4.2 times that on the fp32 instruction; what
+// comes before and after the steps 8 and 5.
+double tile_time(bool big, int64_t groups, int64_t steps, int es) {
+    const double step = (big ? 1.65 : groups > kFillTiles ? 1.04 : 0.7) * (es == 4 ? 4.2 : 1.0);
+    return (double)div_up(groups, big ? kFillTiles : 2 * kFillTiles) * (steps * step + (big ? 8 : 5));
+}
+int64_t tiles_of(int64_t a, int64_t b, bool big) {
+    const int side = big ? kBig : kSmall;
+    return div_up(a, side) * div_up(b, side);
+}
+// Steps of k in `segments` segments; es: bytes of the operands' elements.
+int64_t steps_of(int64_t k, int es, bool terms) {
+    return div_up(k, 128 / es) * (terms ? kSegments : 1);
+}
+bool big_tiles(int64_t rows, int64_t classes, int64_t k, int es, bool terms) {
+    const int64_t steps = steps_of(k, es, terms);
+    return tile_time(true, tiles_of(rows, classes, true), steps, es) <=
+           tile_time(false, tiles_of(rows, classes, false), steps, es);
 }
 
+constexpr int64_t kTermRows = 384;
 // fp32 operands as bf16 terms: what making them costs (12 bytes of memory traffic an element) is
-// regained by the products of about `least` rows of the other operand.
-bool by_terms(const HeadShape& s, int64_t least) {
-    return s.es == 4 && s.rows * s.classes >= least * (s.rows + s.classes);
+// regained by the product with about kTermRows rows of the other operand, and where a tile a CU or
+// less leaves the time to its steps of k.
+bool by_terms(const HeadShape& s) {
+    if (s.es != 4) return false;
+    return s.rows * s.classes >= kTermRows * (s.rows + s.classes) ||
+           (s.n >= 64 && tiles_of(s.rows, s.classes, false) <= kFillTiles);
 }
-constexpr int64_t kTermRows = 512, kTermGradRows = 256;
+
+// A product out[nq][np] over k: its tiles, and how k is split where they are few.
+struct ProductPlan {
+    bool big;
+    double time;
+    int tp, tq, splits;
+    int64_t k_split;
+};
+// The least of the time for the tiles and, with k in splits, for their sums (written and read at
+// about 4.5 TB/s, one more launch).
+ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, int es, bool terms) {
+    ProductPlan p;
+    const int64_t step = 128 / es, steps = div_up(k, step);
+    double least = 0.0;
+    for (const bool big : {true, false}) {
+        const int64_t tiles = tiles_of(np, nq, big);
+        for (int64_t splits = 1; splits == 1 || (splits <= 64 && splits <= steps / 4 &&
+                                                 tiles * splits <= 8 * kFillTiles);
+             ++splits) {
+            const double time =
+                tile_time(big, tiles * splits, steps_of(div_up(k, splits), es, terms), es) +
+                (splits > 1 ? 4.0 + 2.0 * splits * np * nq * 4 / 4.5e6 : 0.0);
+            if (least > 0.0 && time >= least) continue;
+            least = time;
+            p.big = big;
+            p.splits = (int)splits;
+        }
+    }
+    p.time = least;
+    const int b = p.big ? kBig : kSmall;
+    p.tp = (int)div_up(np, b);
+    p.tq = (int)div_up(nq, b);
+    p.k_split = div_up(steps, p.splits) * step;
+    p.splits = (int)div_up(k, p.k_split);
+    return p;
+}
+
+// Few tiles with a long k: the logits' sums over parts of k, in memory, rather than the tiles' own
+// logits (8 us: the launch that reads them).  0: no.
+constexpr int64_t kSumsBytes = INT64_C(64) << 20;
+ProductPlan sums_plan(int64_t rows, int64_t classes, int64_t k, int es, bool terms) {
+    ProductPlan p = {};
+    const int64_t steps = steps_of(k, es, terms);
+    if (es != 2 || tiles_of(rows, classes, true) > kFillTiles) return p;
+    const double own = std::min(tile_time(true, tiles_of(rows, classes, true), steps, es),
+                                tile_time(false, tiles_of(rows, classes, false), steps, es));
+    p = product_plan(classes, rows, k, es, terms);
+    if (p.time + 8.0 >= own || p.splits * rows * classes * 4 > kSumsBytes) p.splits = 0;
+    return p;
+}
 
 struct HeadPlan {
     bool thin, big, terms;
@@ -760,6 +923,8 @@ struct HeadPlan {
     int to;             // elements of a packed row
     Parts out;
     void *xp, *wp;      // packed rows, or null
+    ProductPlan pz;     // splits > 0: the logits' sums
+    float* z;
     size_t bytes;
 };
 
@@ -767,7 +932,7 @@ HeadPlan head_plan(const HeadShape& s, void* ws) {
     HeadPlan p = {};
     Arena arena = {static_cast<char*>(ws)};
     p.thin = s.rows <= (s.es == 2 && s.ws ? kThinRows : kThinMost);
-    p.terms = !p.thin && by_terms(s, kTermRows);
+    p.terms = !p.thin && by_terms(s);
     p.to = (int)up(s.n, p.terms ? 8 : 16 / s.es);
     const int64_t packed = (int64_t)p.to * (p.terms ? kTerms * 2 : s.es);  // bytes of a row
     const bool xp = p.terms || !s.xs, wp = p.terms || !s.ws;
@@ -779,7 +944,7 @@ HeadPlan head_plan(const HeadShape& s, void* ws) {
                                           2 * kFillTiles);
         p.parts = p.groups;
     } else {
-        p.big = big_tiles(s.rows, s.classes);
+        p.big = big_tiles(s.rows, s.classes, s.n, p.terms ? 2 : s.es, p.terms);
         const int b = p.big ? kBig : kSmall;
         p.parts = div_up(s.classes, b);
         p.piece = kPieceTiles / div_up(s.rows, b);
@@ -787,6 +952,13 @@ HeadPlan head_plan(const HeadShape& s, void* ws) {
         p.piece = std::min<int64_t>(p.piece * b, up(s.classes, b));
         if (xp) p.xp = arena.take(s.rows * packed);
         if (wp) p.wp = arena.take(p.piece * packed);
+        if (p.piece >= s.classes)
+            p.pz = sums_plan(s.rows, s.classes, s.n, p.terms ? 2 : s.es, p.terms);
+        if (p.pz.splits > 0) {
+            p.z = arena.take<float>((int64_t)p.pz.splits * s.rows * s.classes * 4);
+            p.bytes = arena.at;
+            return p;
+        }
     }
     p.out.sums = arena.take<float2>(p.parts * s.rows * 8);
     p.out.best = arena.take<int>(p.parts * s.rows * 4);
@@ -847,6 +1019,39 @@ hipError_t tiles(const HeadTileArgs& a, bool best, bool big, hipStream_t st) {
     return hipGetLastError();
 }
 
+// O: the type of the call (of its operands, in fp32 as bf16 terms, and its results).
+template <typename O, int MP, int MQ>
+hipError_t product(const ProductPlan& p, const ProductArgs& a, hipStream_t st) {
+    constexpr int S = sizeof(O) == 4 ? kSegments : 1;
+    typedef Tile<uint16_t, 2, 4, 4, 2, MP, MQ, S> Big;
+    typedef Tile<uint16_t, 2, 2, 2, 2, MP, MQ, S> Small;
+    const int groups = p.tp * p.tq * p.splits;
+    if (p.big) head_product_kernel<O, Big, MP, MQ><<<groups, Big::THREADS, 0, st>>>(a);
+    else head_product_kernel<O, Small, MP, MQ><<<groups, Small::THREADS, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+// The sums over k of a launch's logits, in parts: [splits][rows][classes].
+template <typename O>
+hipError_t sums(const ProductPlan& p, const LogitArgs& z, float* out, hipStream_t st) {
+    ProductArgs r = {};
+    r.p = z.w;
+    r.q = z.x;
+    r.pstride = z.wstride;
+    r.qstride = z.xstride;
+    r.pplane = z.wplane;
+    r.qplane = z.xplane;
+    r.qterms = kTermsQ;
+    r.np = z.classes;
+    r.nq = z.rows;
+    r.k = z.k;
+    r.k_split = p.k_split;
+    r.tp = p.tp;
+    r.tq = p.tq;
+    r.acc = out;
+    return product<O, kByRows, kByRows>(p, r, st);
+}
+
 template <typename T>
 hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st) {
     HeadPlan p = head_plan(s, ws);
@@ -892,6 +1097,13 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
                 t.z.w = p.wp;
                 t.z.wplane = p.terms ? (int64_t)t.z.classes * p.to * es : 0;
             }
+            if (p.pz.splits > 0) {
+                KAN_TRY(sums<T>(p.pz, t.z, p.z, st));
+                const HeadRowsArgs r = {p.z, p.pz.splits, s.rows, s.classes, a.scale, a.targets,
+                                        a.ignore, a.logp, a.stats, a.best};
+                head_rows_kernel<<<(int)div_up(s.rows, 4), 256, 0, st>>>(r);
+                return hipGetLastError();
+            }
             const bool best = a.best != nullptr;
             if (p.terms)
                 KAN_TRY(p.big ? tiles<uint16_t, BigLogits<uint16_t, kSegments>>(t, best, true, st)
@@ -909,45 +1121,21 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
     return hipGetLastError();
 }
 
-// A product out[nq][np] over k: its tiles, and how k is split where they are few.
-struct ProductPlan {
-    bool big;
-    int tp, tq, splits;
-    int64_t k_split;
-};
-ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, int es) {
-    ProductPlan p;
-    const int64_t step = 128 / es, steps = div_up(k, step);
-    const int64_t big = div_up(np, kBig) * div_up(nq, kBig);
-    // big tiles where they fill the GPU, also with k in splits of 32 steps or more, and do not
-    // stand out over the result
-    p.big = big * std::max<int64_t>(1, steps / 32) >= kFillTiles &&
-            big * 4 * 7 <= div_up(np, kSmall) * div_up(nq, kSmall) * 8;
-    const int b = p.big ? kBig : kSmall;
-    p.tp = (int)div_up(np, b);
-    p.tq = (int)div_up(nq, b);
-    const int64_t want = (p.big ? 1 : 2) * kFillTiles / ((int64_t)p.tp * p.tq);
-    p.splits = (int)std::max<int64_t>(1, std::min(want, steps / 8));
-    p.k_split = div_up(steps, p.splits) * step;
-    p.splits = (int)div_up(k, p.k_split);
-    return p;
-}
-
 struct HeadGradPlan {
     bool terms;
     int64_t piece, zstride;  // classes; elements
     int to;
     void *xp, *wp;           // packed rows, or null
     void* dz;
-    float *dx, *dw;          // sums over k in parts, or null
-    ProductPlan px, pw;
+    float *dx, *dw, *z;      // sums over k in parts, or null
+    ProductPlan px, pw, pz;  // (pz.splits > 0: the logits')
     size_t bytes;
 };
 
 HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
     HeadGradPlan p = {};
     Arena arena = {static_cast<char*>(ws)};
-    p.terms = by_terms(s, kTermGradRows);
+    p.terms = s.es == 4;  // (three products of each)
     p.to = (int)up(s.n, p.terms ? 8 : 16 / s.es);
     const int64_t packed = (int64_t)p.to * (p.terms ? kTerms * 2 : s.es);  // bytes of a row
     const int zes = p.terms ? kDzTerms * 2 : s.es;                         // and of a logit
@@ -964,37 +1152,29 @@ HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
     if (wp) p.wp = arena.take(p.piece * packed);
     p.dz = arena.take(s.rows * p.zstride * zes);
     const int es = p.terms ? 2 : s.es;
+    if (p.piece >= s.classes) p.pz = sums_plan(s.rows, s.classes, s.n, es, p.terms);
+    if (p.pz.splits > 0) p.z = arena.take<float>((int64_t)p.pz.splits * s.rows * s.classes * 4);
     if (dx) {
-        p.px = product_plan(s.n, s.rows, p.zstride, es);
+        p.px = product_plan(s.n, s.rows, p.zstride, es, p.terms);
         if (p.px.splits > 1 || p.piece < s.classes)
             p.dx = arena.take<float>((int64_t)p.px.splits * s.rows * s.n * 4);
     }
     if (dw) {
-        p.pw = product_plan(s.n, here, s.rows, es);
+        p.pw = product_plan(s.n, here, s.rows, es, p.terms);
         if (p.pw.splits > 1) p.dw = arena.take<float>((int64_t)p.pw.splits * here * s.n * 4);
     }
     p.bytes = arena.at;
     return p;
 }
 
-template <typename T, typename O, int MP, int MQ, int S>
-hipError_t product(const ProductPlan& p, const ProductArgs& a, hipStream_t st) {
-    typedef Tile<T, 2, 4, 4, 2, MP, MQ, S> Big;
-    typedef Tile<T, 2, 2, 2, 2, MP, MQ, S> Small;
-    const int groups = p.tp * p.tq * p.splits;
-    if (p.big) head_product_kernel<T, O, Big, MP, MQ><<<groups, Big::THREADS, 0, st>>>(a);
-    else head_product_kernel<T, O, Small, MP, MQ><<<groups, Small::THREADS, 0, st>>>(a);
-    return hipGetLastError();
-}
-
-template <typename T, bool TERMS, int S>
+template <typename O>
 hipError_t gradient_tiles(const HeadGradTileArgs& g, bool big, hipStream_t st) {
+    constexpr bool TERMS = sizeof(O) == 4;
+    typedef BigLogits<uint16_t, TERMS ? kSegments : 1> Big;
+    typedef SmallLogits<uint16_t, TERMS ? kSegments : 1> Small;
     const int groups = resident(g.z.tp * g.z.tq, big);
-    if (big)
-        head_grad_kernel<T, BigLogits<T, S>, TERMS><<<groups, BigLogits<T, S>::THREADS, 0, st>>>(g);
-    else
-        head_grad_kernel<T, SmallLogits<T, S>, TERMS>
-            <<<groups, SmallLogits<T, S>::THREADS, 0, st>>>(g);
+    if (big) head_grad_kernel<Big, TERMS><<<groups, Big::THREADS, 0, st>>>(g);
+    else head_grad_kernel<Small, TERMS><<<groups, Small::THREADS, 0, st>>>(g);
     return hipGetLastError();
 }
 
@@ -1045,16 +1225,23 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
             g.z.w = p.wp;
             g.z.wplane = terms ? here * p.to * es : 0;
         }
-        const bool big = big_tiles(s.rows, here);
+        const bool big = big_tiles(s.rows, here, s.n, es, terms);
         const int b = big ? kBig : kSmall;
         g.z.tp = (int)div_up(here, b);
         g.z.tq = (int)div_up(s.rows, b);
-        KAN_TRY(terms ? gradient_tiles<uint16_t, true, kSegments>(g, big, st)
-                      : gradient_tiles<T, false, 1>(g, big, st));
+        if (p.pz.splits > 0) {
+            KAN_TRY(sums<T>(p.pz, g.z, p.z, st));
+            head_dz_kernel<sizeof(T) == 4>
+                <<<grid_of(s.rows * (p.zstride / 8), 256), 256, 0, st>>>(g, p.z, p.pz.splits);
+            KAN_TRY(hipGetLastError());
+        } else {
+            KAN_TRY(gradient_tiles<T>(g, big, st));
+        }
         ProductArgs r = {};
         r.q = p.dz;
         r.qstride = zbytes;
         r.qplane = terms ? g.zplane * es : 0;
+        r.qterms = kTermsDz;
         r.np = s.n;
         r.scale = a.scale;
         if (a.dx != nullptr) {
@@ -1071,8 +1258,7 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
             r.acc = p.dx;
             r.add = first > 0;
             r.out = whole ? a.dx : nullptr;
-            KAN_TRY(terms ? product<uint16_t, float, kByK, kByRows, kSegments>(p.px, r, st)
-                          : product<T, T, kByK, kByRows, 1>(p.px, r, st));
+            KAN_TRY(product<T, kByK, kByRows>(p.px, r, st));
             if (last && !whole)
                 KAN_TRY(sum<T>(p.dx, p.px.splits, s.rows * s.n, a.scale, a.dx, st));
         }
@@ -1091,8 +1277,7 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
             r.acc = p.dw;
             r.add = false;
             r.out = pw.splits == 1 ? out : nullptr;
-            KAN_TRY(terms ? product<uint16_t, float, kByK, kByK, kSegments>(pw, r, st)
-                          : product<T, T, kByK, kByK, 1>(pw, r, st));
+            KAN_TRY(product<T, kByK, kByK>(pw, r, st));
             if (pw.splits > 1) KAN_TRY(sum<T>(p.dw, pw.splits, here * s.n, a.scale, out, st));
         }
     }

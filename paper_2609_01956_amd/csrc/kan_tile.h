@@ -11,10 +11,9 @@
 // In LDS:
 //   by rows  128 bytes a row, its eight 16-byte chunks at chunk ^ (row >> 1 & 7): sixteen lanes that
 //            read one chunk of sixteen rows use all banks (with row & 7 they used half)
-//   by k     a row per k; bf16 fragments come from the LDS's transposing read (four k of 16 columns
+//   by k     (bf16) a row per k; fragments come from the LDS's transposing read (four k of 16 columns
 //            for 16 lanes), whose four rows stand in different quarters of the banks, 64-byte
-//            blocks at block ^ (k & 3); fp32 ones from four 4-byte reads, 128-byte blocks at block ^ (k
-//            >> 2 & 1)
+//            blocks at block ^ (k & 3)
 // What lies past an operand's end is 0 (the buffer's bounds).  By rows, k must be a whole number of
 // 16-byte chunks; rows are 16-byte aligned in both, and end with a chunk.  By k, columns past the end hold what follows:
 // they reach outputs past the end only.
@@ -70,6 +69,7 @@ struct Side {
     static constexpr int BYTES = B * 128;                    // of a step
     static constexpr int ROW = B * ES, CHUNKS = ROW / 16;    // by k: a row in LDS
     static_assert(B % (8 * W) == 0, "whole loads");
+    static_assert(MODE == kByRows || ES == 2, "operands by k are bf16");
 
     uint32_t from[LOADS];  // the lane's loads in a step's part of the operand
     int tail;              // by rows: bytes of k before the lane's chunk (of even loads)
@@ -96,19 +96,14 @@ struct Side {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 const int row = (wave * LOADS + i) * PER + lane / CHUNKS, c = lane % CHUNKS;
-                from[i] = row * stride + (ES == 2 ? c ^ (row & 3) << 2 : c ^ (row >> 2 & 1) << 3) * 16;
+                from[i] = row * stride + (c ^ (row & 3) << 2) * 16;
             }
+            // (its quarter of the wave's four k, its 16 columns' 32 bytes and its 8 of them)
+            const int k = (lane >> 5) * 8 + (lane >> 2 & 3);
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const int block = part * R + i, half = lane >> 5;
-                if constexpr (ES == 2) {
-                    const int k = half * 8 + (lane >> 2 & 3);
-                    read[i] = k * ROW + (block ^ (lane >> 2 & 3)) * 64 + (lane >> 4 & 1) * 32 +
-                              (lane & 3) * 8;
-                } else {
-                    read[i] = half * 4 * ROW + (block ^ half) * 128 + (lane & 31) * 4;
-                }
-            }
+            for (int i = 0; i < R; ++i)
+                read[i] = k * ROW + ((part * R + i) ^ (k & 3)) * 64 + (lane >> 4 & 1) * 32 +
+                          (lane & 3) * 8;
         }
     }
 
@@ -144,7 +139,7 @@ struct Side {
         for (int i = 0; i < R; ++i) {
             if constexpr (MODE == kByRows) {
                 f[i] = *(const u32x4 KAN_LDS*)(src + read[0] + chunk[quarter] + i * 32 * 128);
-            } else if constexpr (ES == 2) {
+            } else {
                 typedef short s16x4 __attribute__((ext_vector_type(4)));
                 const char KAN_LDS* p = src + read[i] + quarter * 16 * ROW;
                 const u32x2 lo = __builtin_bit_cast(
@@ -152,10 +147,6 @@ struct Side {
                 const u32x2 hi = __builtin_bit_cast(
                     u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KAN_LDS*)(p + 4 * ROW)));
                 f[i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
-            } else {
-                const char KAN_LDS* p = src + read[i] + quarter * 8 * ROW;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[i][e] = *(const uint32_t KAN_LDS*)(p + e * ROW);
             }
         }
     }

@@ -627,35 +627,65 @@ __global__ void __launch_bounds__(256) embed_rest_kernel(EmbedSumArgs a) {
         }
         return;
     }
-    const int64_t all = (int64_t)a.g.classes * a.units;
-    const int64_t groups = gridDim.x - a.heavy;
-    for (int64_t first = (int64_t)(blockIdx.x - a.heavy) * 256 * kLoads; first < all;
+    // the table as one run of aligned 16-byte units, whatever its rows are: stores of odd rows at their
+    // own places take twice as long (109776 x 1153 fp32 in all 147 us, so 105)
+    TP* const table = static_cast<TP*>(a.g.dtable);
+    const int64_t total = (int64_t)a.g.classes * a.g.n;
+    const int head = (int)((reinterpret_cast<uintptr_t>(table) & 15) / sizeof(TP));
+    const int64_t units = (total + head + V - 1) / V, groups = gridDim.x - a.heavy;
+    for (int64_t first = (int64_t)(blockIdx.x - a.heavy) * 256 * kLoads; first < units;
          first += groups * 256 * kLoads) {
-        const Share s(first, a.units);
-        int64_t row[kLoads];
-        int c[kLoads];
-        bool absent[kLoads];
-        Columns<TP, V, FULL> base[kLoads];
+        // rows of the workgroup's elements, from that of the first one on
+        const int64_t e0 = first * V - head, origin = e0 < 0 ? 0 : e0;
+        const int64_t row0 = origin / a.g.n;
+        const uint32_t at0 = (uint32_t)(origin - row0 * a.g.n);
+        int64_t e[kLoads], row[kLoads];
+        int from[kLoads], to[kLoads], turn[kLoads];  // a unit's elements, and the next row's first
+        int2 one[kLoads], two[kLoads];               // spans of the first row and of the next
+        uint32_t absent[kLoads];                     // bits: elements of rows that do not occur
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
-            const uint32_t j = s.at + u * 256 + threadIdx.x, r = j / a.units;
-            row[u] = s.row + r;
-            c[u] = column_of<V, FULL>(j - r * a.units, a.g.n);
-            const int2 span = row[u] < a.g.classes ? a.span[row[u]] : int2{0, 1};
-            absent[u] = span.x == span.y;
+            e[u] = e0 + (int64_t)(u * 256 + (int)threadIdx.x) * V;
+            from[u] = e[u] < 0 ? (int)-e[u] : 0;
+            to[u] = (int)(total - e[u] < V ? total - e[u] : V);
+            const uint32_t j = at0 + (uint32_t)(e[u] + from[u] - origin), r = j / (uint32_t)a.g.n;
+            row[u] = row0 + r;
+            turn[u] = (int)min((uint32_t)from[u] + a.g.n - (j - r * a.g.n), (uint32_t)V);
+            one[u] = to[u] > from[u] ? a.span[row[u]] : int2{0, 1};
+            two[u] = to[u] > turn[u] ? a.span[row[u] + 1] : int2{0, 1};
         }
-        if (a.g.base != nullptr) {
+        const auto bits = [](int lo, int hi) { return hi > lo ? (1u << hi) - (1u << lo) : 0u; };
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u)
-                if (absent[u])
-                    base[u].issue(static_cast<const TP*>(a.g.base) + row[u] * a.g.n, c[u], a.g.n);
+        for (int u = 0; u < kLoads; ++u) {
+            absent[u] = (one[u].x == one[u].y ? bits(from[u], min(turn[u], to[u])) : 0u) |
+                        (two[u].x == two[u].y ? bits(turn[u], min(turn[u] + a.g.n, to[u])) : 0u);
+            // (rows shorter than a unit)
+            for (int at = turn[u] + a.g.n, k = 2; at < to[u]; at += a.g.n, ++k) {
+                const int2 span = a.span[row[u] + k];
+                if (span.x == span.y) absent[u] |= bits(at, min(at + a.g.n, to[u]));
+            }
+        }
+        constexpr uint32_t FULL_UNIT = (1u << V) - 1;
+        u32x4 base[kLoads];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            base[u] = u32x4{0, 0, 0, 0};
+            if (a.g.base != nullptr && absent[u] == FULL_UNIT)
+                base[u] = *unit_at(static_cast<const TP*>(a.g.base) + e[u], 0);
         }
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
-            if (!absent[u]) continue;
-            float v[V] = {};
-            if (a.g.base != nullptr) base[u].value(c[u], a.g.n, v);
-            store_unit<FULL, PAST>(static_cast<TP*>(a.g.dtable) + row[u] * a.g.n, c[u], a.g.n, v);
+            if (absent[u] == FULL_UNIT) {
+                u32x4* const to = reinterpret_cast<u32x4*>(table + e[u]);
+                if (PAST) __builtin_nontemporal_store(base[u], to);
+                else *to = base[u];
+            } else if (absent[u] != 0) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (absent[u] >> i & 1)
+                        table[e[u] + i] =
+                            a.g.base == nullptr ? TP(0) : static_cast<const TP*>(a.g.base)[e[u] + i];
+            }
         }
     }
 }
@@ -793,7 +823,8 @@ hipError_t embed_grad(const EmbedGradArgs& g, void* ws, hipStream_t s) {
     }
     if (g.rows > kRun)
         e.heavy = (int)std::min<int64_t>(div_up(div_up(g.rows, kRun) * e.blocks, 4), kRestGroups);
-    const int64_t rest = g.base == g.dtable ? 0 : div_up((int64_t)g.classes * e.units, 256 * kLoads);
+    const int64_t rest =
+        g.base == g.dtable ? 0 : div_up((int64_t)g.classes * g.n / kVec<TP> + 2, 256 * kLoads);
     const int groups = e.heavy + (int)std::min<int64_t>(rest, kRestGroups);
     if (groups == 0) return hipSuccess;
     const bool past = (int64_t)g.classes * g.n * (int64_t)sizeof(TP) >= kPastCaches;

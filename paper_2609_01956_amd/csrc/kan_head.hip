@@ -209,6 +209,55 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_tile_kernel(HeadTileArgs 
     });
 }
 
+// ------------------------------------------------------------ the gradient's rows
+
+struct HeadGradTileArgs {
+    LogitArgs z;
+    const float *stats, *dlogp;
+    int64_t ignore;
+    int all;          // classes
+    void* dz;         // [rows][zstride], 0 past the classes; of fp32 as terms, kDzTerms of them
+    int64_t zstride;  // elements, a multiple of 16 bytes
+    int64_t zplane;   // elements from term to term
+};
+constexpr int kDzTerms = 3;
+
+// What a row's dz is made of: dz = d ([v = target] - exp(z - m - logs)).
+struct RowGrad {
+    float m, logs, d;
+    int target;  // from the launch's first class on
+    // what is subtracted from the logit with its scale's rounding (in bf16 p's own rounding hides
+    // that of the exponential's argument)
+    template <bool EXACT>
+    __device__ __forceinline__ float offset() const {
+        return EXACT ? m : m + logs;
+    }
+};
+__device__ __forceinline__ RowGrad row_grad(const HeadGradTileArgs& g, int64_t row) {
+    // (rows that have no gradient: p = 0, whatever their logits are)
+    RowGrad r = {__builtin_huge_valf(), 0.0f, 0.0f, -1};
+    if (row >= g.z.rows) return r;
+    const int64_t c = g.z.targets[row];
+    const float m = g.stats[2 * row], logs = g.stats[2 * row + 1], d = g.dlogp[row];
+    if (c == g.ignore) return r;
+    // (a target that is no class, NaN and infinite logits show in the row's gradient)
+    r.d = c < 0 || c >= g.all || m != m || logs != logs ? __builtin_nanf("") : d;
+    if (m == kNegInf && logs == kNegInf && r.d == r.d) {
+        r.d = 0.0f;
+        return r;
+    }
+    r.m = m;
+    r.logs = logs;
+    r.target = (int)c - g.z.first;
+    return r;
+}
+// -d p for the logit less its offset.
+template <bool EXACT>
+__device__ __forceinline__ float dz_of(const RowGrad& r, float t) {
+    return -r.d * (EXACT ? exp_exact(__builtin_fmaxf(t - r.logs, -1e4f))
+                         : exp_of(__builtin_fmaxf(t, -1e4f)));
+}
+
 // ------------------------------------------------------------ few rows
 
 // Elements [k, k + 16 bytes) of a row of n, 0 past its end.
@@ -239,12 +288,16 @@ constexpr int kThinWaves = 8;
 constexpr int kThinLds = 64 << 10;  // bytes of x in LDS at a time (128 KB: one workgroup a CU, slower)
 
 // Rows of weights straight from memory into the matrix instruction, x from LDS: bound by the reads of
-// the weights.  NT: groups of 16 rows.  SPLIT: the waves share one group of
-// 16 classes and split k.
-template <typename T, int NT, bool BEST, bool SPLIT>
-__global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs a) {
+// the weights.  NT: groups of 16 rows.  WHAT: the rows' parts, with the best class, or dz in fp32,
+// [classes][16 NT].  SPLIT: the waves share one group of 16 classes and split k.
+enum { kLogp, kBest, kDz };
+template <typename T, int NT, int WHAT, bool SPLIT>
+__global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs a,
+                                                                    HeadGradTileArgs grad,
+                                                                    float* dz) {
+    constexpr bool BEST = WHAT == kBest;
     constexpr int V = kVec<T>, ROWS = 16 * NT;
-    constexpr int SLICE = kThinLds / ROWS / 16;  // chunks of a row in LDS at a time
+    constexpr int SLICE = kThinLds / ROWS / 16 & ~7;  // chunks of a row in LDS at a time
     constexpr int TURN = SPLIT ? 1 : kThinWaves;  // groups of 16 classes of a workgroup at a time
     extern __shared__ __attribute__((aligned(128))) char lds[];
     __shared__ Best red[kThinWaves][ROWS];
@@ -265,10 +318,12 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
     };
     Best best[NT];
     int64_t target[NT];
+    RowGrad of[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         best[t] = Best{kNegInf, 0.0f, kNoIndex};
-        target[t] = t * 16 + r16 < a.rows ? a.targets[t * 16 + r16] : -1;
+        target[t] = WHAT != kDz && t * 16 + r16 < a.rows ? a.targets[t * 16 + r16] : -1;
+        if (WHAT == kDz) of[t] = row_grad(grad, t * 16 + r16);
     }
     const bool once = chunks <= width;
     if (once) {
@@ -338,6 +393,16 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+            if constexpr (WHAT == kDz) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int p = p0 + quad * 4 + i;
+                    const float v = __builtin_fmaf(acc[t][i], a.scale, -of[t].template offset<true>());
+                    const float y = dz_of<true>(of[t], v) + (p == of[t].target ? of[t].d : 0.0f);
+                    if (p < a.classes) dz[((int64_t)p * NT + t) * 16 + r16] = y;
+                }
+                continue;
+            }
             float m = best[t].m;
             int at = best[t].at;
 #pragma unroll
@@ -356,6 +421,7 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
             best[t] = Best{m, s, at};
         }
     }
+    if (WHAT == kDz) return;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         best[t] = join(best[t], from_lane(best[t], 16));
@@ -434,53 +500,6 @@ __device__ __forceinline__ void store_four(T* at, int64_t left, const T (&v)[4])
 #pragma unroll
     for (int i = 0; i < 3; ++i)
         if (i < left) at[i] = v[i];
-}
-
-struct HeadGradTileArgs {
-    LogitArgs z;
-    const float *stats, *dlogp;
-    int64_t ignore;
-    int all;          // classes
-    void* dz;         // [rows][zstride], 0 past the classes; of fp32 as terms, kDzTerms of them
-    int64_t zstride;  // elements, a multiple of 16 bytes
-    int64_t zplane;   // elements from term to term
-};
-constexpr int kDzTerms = 3;
-
-// What a row's dz is made of: dz = d ([v = target] - exp(z - m - logs)).
-struct RowGrad {
-    float m, logs, d;
-    int target;  // from the launch's first class on
-    // what is subtracted from the logit with its scale's rounding (in bf16 p's own rounding hides
-    // that of the exponential's argument)
-    template <bool EXACT>
-    __device__ __forceinline__ float offset() const {
-        return EXACT ? m : m + logs;
-    }
-};
-__device__ __forceinline__ RowGrad row_grad(const HeadGradTileArgs& g, int64_t row) {
-    // (rows that have no gradient: p = 0, whatever their logits are)
-    RowGrad r = {__builtin_huge_valf(), 0.0f, 0.0f, -1};
-    if (row >= g.z.rows) return r;
-    const int64_t c = g.z.targets[row];
-    const float m = g.stats[2 * row], logs = g.stats[2 * row + 1], d = g.dlogp[row];
-    if (c == g.ignore) return r;
-    // (a target that is no class, NaN and infinite logits show in the row's gradient)
-    r.d = c < 0 || c >= g.all || m != m || logs != logs ? __builtin_nanf("") : d;
-    if (m == kNegInf && logs == kNegInf && r.d == r.d) {
-        r.d = 0.0f;
-        return r;
-    }
-    r.m = m;
-    r.logs = logs;
-    r.target = (int)c - g.z.first;
-    return r;
-}
-// -d p for the logit less its offset.
-template <bool EXACT>
-__device__ __forceinline__ float dz_of(const RowGrad& r, float t) {
-    return -r.d * (EXACT ? exp_exact(__builtin_fmaxf(t - r.logs, -1e4f))
-                         : exp_of(__builtin_fmaxf(t, -1e4f)));
 }
 
 // dz of the tiles in bf16, or in bf16 terms of fp32 (TERMS): the operand of the products that follow.
@@ -621,6 +640,138 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_product_kernel(ProductArg
             store_four(static_cast<O*>(a.out) + row * a.np + p0 + c, left, w);
         }
         Tl::meet();
+    }
+}
+
+// Few rows: both products at once, each weight read and each of its gradients written once, on the
+// vector ALUs (two fused multiply-adds per weight and row).  A lane holds four columns of x and of
+// dx, R rows of them; a wave goes through its classes, the dz of four of them in a lane each, and
+// the waves of a workgroup add their dx through LDS.
+constexpr int kOuterRows = 16, kOuterWaves = 4;
+struct HeadOuterArgs {
+    const void *x, *w;
+    const float* dz;           // [classes][kOuterRows]
+    int64_t xstride, wstride;  // elements
+    int rows, classes, n;
+    int each;                  // classes of a wave
+    const int64_t* targets;
+    int64_t ignore;
+    float scale;
+    float* part;               // [workgroups of a column block][rows][n], or null
+    void* dw;                  // or null
+};
+// Four columns of a row (0 past its end), at any alignment.
+template <typename T>
+struct Four {
+    typedef T any __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    any v;
+    __device__ __forceinline__ void load(const T* row, int left) {
+        v = any{};
+        if (left >= 4) {
+            v = *reinterpret_cast<const any*>(row);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < left) v[i] = row[i];
+        }
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 2) return bf16_to_f32(v[i]);
+        else return v[i];
+    }
+};
+
+template <typename T, int R>
+__global__ void __launch_bounds__(64 * kOuterWaves) head_outer_kernel(HeadOuterArgs a, int blocks) {
+    constexpr int U = R == 16 ? 4 : 8;  // classes in flight
+    __shared__ float sums[kOuterWaves][R][256];
+    static_assert(kOuterRows == 16, "four classes' dz a wave");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int block = blockIdx.x % blocks, slice = blockIdx.x / blocks;
+    const int c = (block * 64 + lane) * 4, left = a.n - c;
+    float x[R][4], dx[R][4] = {};
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        Four<T> v;
+        // (nothing of what ignored rows hold)
+        const bool live = r < a.rows && a.targets[r] != a.ignore;
+        v.load(static_cast<const T*>(a.x) + (live ? r * a.xstride + c : 0), live ? left : 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[r][i] = v.get(i);
+    }
+    const int64_t first = ((int64_t)slice * kOuterWaves + wave) * a.each;
+    const int64_t last = first + a.each < a.classes ? first + a.each : a.classes;
+    for (int64_t p = first; p < last; p += U) {
+        Four<T> w[U];
+        float dz[U / 4];
+#pragma unroll
+        for (int q = 0; q < U / 4; ++q) {
+            const int64_t at = p + 4 * q + (lane >> 4);
+            dz[q] = a.dz[(at < last ? at : p) * kOuterRows + (lane & 15)];
+        }
+        if (a.part != nullptr) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                w[u].load(static_cast<const T*>(a.w) + (p + u < last ? p + u : p) * a.wstride + c,
+                          left);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p + u >= last) break;
+            float g[4] = {};
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float d = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(
+                    (int)__float_as_uint(dz[u / 4]), (u % 4) * 16 + r));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (a.part != nullptr) dx[r][i] = __builtin_fmaf(d, w[u].get(i), dx[r][i]);
+                    g[i] = __builtin_fmaf(d, x[r][i], g[i]);
+                }
+            }
+            if (a.dw != nullptr && left > 0) {
+                T o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = rounded<T>(g[i] * a.scale);
+                store_four(static_cast<T*>(a.dw) + (p + u) * a.n + c, left, o);
+            }
+        }
+    }
+    if (a.part == nullptr) return;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        *reinterpret_cast<floatx4*>(&sums[wave][r][lane * 4]) =
+            floatx4{dx[r][0], dx[r][1], dx[r][2], dx[r][3]};
+    __syncthreads();
+    const int at = block * 256 + threadIdx.x;
+    if (at >= a.n) return;
+    for (int r = 0; r < a.rows; ++r) {
+        float s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kOuterWaves; ++k) s += sums[k][r][threadIdx.x];
+        a.part[((int64_t)slice * a.rows + r) * a.n + at] = s;
+    }
+}
+
+// out = scale times the sum of many parts of few values: 16 lanes a value, each a sixteenth of the
+// parts.
+template <typename T>
+__global__ void __launch_bounds__(256) head_gather_kernel(const float* part, int parts, int64_t n,
+                                                          float scale, T* out) {
+    __shared__ float sums[16][17];
+    const int v = threadIdx.x & 15, strand = threadIdx.x >> 4;
+    for (int64_t first = (int64_t)blockIdx.x * 16; first < n; first += (int64_t)gridDim.x * 16) {
+        float s = 0.0f;
+        if (first + v < n)
+            for (int k = strand; k < parts; k += 16) s += part[k * n + first + v];
+        __syncthreads();
+        sums[strand][v] = s;
+        __syncthreads();
+        if (threadIdx.x < 16 && first + v < n) {
+            s = 0.0f;
+            for (int k = 0; k < 16; ++k) s += sums[k][v];
+            out[first + v] = rounded<T>(s * scale);
+        }
     }
 }
 
@@ -916,8 +1067,6 @@ ProductPlan sums_plan(int64_t rows, int64_t classes, int64_t k, int es, bool ter
 
 struct HeadPlan {
     bool thin, big, terms;
-    bool split;         // thin: a group's k over the waves
-    int groups;         // thin: workgroups
     int64_t parts;
     int64_t piece;      // classes
     int to;             // elements of a packed row
@@ -928,6 +1077,14 @@ struct HeadPlan {
     size_t bytes;
 };
 
+// Few classes and a long k: a workgroup for each 16 classes.
+bool thin_split(const HeadShape& s) {
+    return div_up(s.classes, 16) <= 2 * kFillTiles && div_up(s.n, 16 / s.es) >= 64;
+}
+int thin_groups(const HeadShape& s) {
+    return (int)std::min<int64_t>(div_up(div_up(s.classes, 16), thin_split(s) ? 1 : kThinWaves),
+                                  2 * kFillTiles);
+}
 HeadPlan head_plan(const HeadShape& s, void* ws) {
     HeadPlan p = {};
     Arena arena = {static_cast<char*>(ws)};
@@ -937,12 +1094,7 @@ HeadPlan head_plan(const HeadShape& s, void* ws) {
     const int64_t packed = (int64_t)p.to * (p.terms ? kTerms * 2 : s.es);  // bytes of a row
     const bool xp = p.terms || !s.xs, wp = p.terms || !s.ws;
     if (p.thin) {
-        const int64_t groups = div_up(s.classes, 16);
-        // few classes and a long k: a workgroup for each 16 classes
-        p.split = groups <= 2 * kFillTiles && div_up(s.n, 16 / s.es) >= 64;
-        p.groups = (int)std::min<int64_t>(div_up(groups, p.split ? 1 : kThinWaves),
-                                          2 * kFillTiles);
-        p.parts = p.groups;
+        p.parts = thin_groups(s);
     } else {
         p.big = big_tiles(s.rows, s.classes, s.n, p.terms ? 2 : s.es, p.terms);
         const int b = p.big ? kBig : kSmall;
@@ -990,22 +1142,40 @@ hipError_t pack(bool terms, const void* x, int64_t stride, int64_t rows, int n, 
         if (e_ != hipSuccess) return e_;      \
     } while (0)
 
-template <typename T, int NT, bool BEST>
-hipError_t thin(const HeadPlan& p, const HeadThinArgs& a, hipStream_t st) {
-    const int chunks = (int)div_up(a.n, kVec<T>), slice = kThinLds / (16 * NT) / 16;
+template <typename T, int NT, int WHAT>
+hipError_t thin(const HeadShape& s, const HeadThinArgs& a, const HeadGradTileArgs& g, float* dz,
+                hipStream_t st) {
+    const bool split = thin_split(s);
+    const int chunks = (int)div_up(a.n, kVec<T>), slice = kThinLds / (16 * NT) / 16 & ~7;
     // (x, and the waves' sums after it)
     const size_t lds = std::max((size_t)16 * NT * std::min((chunks + 7) & ~7, slice) * 16,
-                                (size_t)(p.split ? kThinWaves * NT * 1024 : 0));
+                                (size_t)(split ? kThinWaves * NT * 1024 : 0));
     const auto kernel =
-        p.split ? head_thin_kernel<T, NT, BEST, true> : head_thin_kernel<T, NT, BEST, false>;
-    kernel<<<p.groups, 64 * kThinWaves, lds, st>>>(a);
+        split ? head_thin_kernel<T, NT, WHAT, true> : head_thin_kernel<T, NT, WHAT, false>;
+    kernel<<<thin_groups(s), 64 * kThinWaves, lds, st>>>(a, g, dz);
     return hipGetLastError();
 }
-template <typename T, bool BEST>
-hipError_t thin(const HeadPlan& p, const HeadThinArgs& a, hipStream_t st) {
-    return a.rows <= 16   ? thin<T, 1, BEST>(p, a, st)
-           : a.rows <= 32 ? thin<T, 2, BEST>(p, a, st)
-                          : thin<T, 4, BEST>(p, a, st);
+template <typename T, int WHAT>
+hipError_t thin(const HeadShape& s, const HeadThinArgs& a, hipStream_t st) {
+    const HeadGradTileArgs none = {};
+    return a.rows <= 16   ? thin<T, 1, WHAT>(s, a, none, nullptr, st)
+           : a.rows <= 32 ? thin<T, 2, WHAT>(s, a, none, nullptr, st)
+           : a.rows <= 48 ? thin<T, 3, WHAT>(s, a, none, nullptr, st)
+                          : thin<T, 4, WHAT>(s, a, none, nullptr, st);
+}
+HeadThinArgs thin_args(const HeadShape& s, const void* x, const void* w, float scale,
+                       const int64_t* targets) {
+    HeadThinArgs t = {};
+    t.x = x;
+    t.w = w;
+    t.rows = (int)s.rows;
+    t.xstride = s.xstride;
+    t.wstride = s.wstride;
+    t.classes = s.classes;
+    t.n = s.n;
+    t.scale = scale;
+    t.targets = targets;
+    return t;
 }
 
 // Workgroups that are resident together: one of a big tile on a CU, or two of a small one.
@@ -1057,18 +1227,9 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
     HeadPlan p = head_plan(s, ws);
     if (a.best == nullptr) p.out.best = nullptr;
     if (p.thin) {
-        HeadThinArgs t = {};
-        t.x = a.x;
-        t.w = a.w;
-        t.rows = (int)s.rows;
-        t.xstride = s.xstride;
-        t.wstride = s.wstride;
-        t.classes = s.classes;
-        t.n = s.n;
-        t.scale = a.scale;
-        t.targets = a.targets;
+        HeadThinArgs t = thin_args(s, a.x, a.w, a.scale, a.targets);
         t.out = p.out;
-        KAN_TRY(a.best != nullptr ? thin<T, true>(p, t, st) : thin<T, false>(p, t, st));
+        KAN_TRY(a.best != nullptr ? thin<T, kBest>(s, t, st) : thin<T, kLogp>(s, t, st));
     } else {
         HeadTileArgs t = {};
         const int es = p.terms ? 2 : s.es;
@@ -1122,7 +1283,8 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
 }
 
 struct HeadGradPlan {
-    bool terms;
+    bool few, terms;
+    int blocks, slices, each;  // few rows: column blocks, workgroups of each, classes of a wave
     int64_t piece, zstride;  // classes; elements
     int to;
     void *xp, *wp;           // packed rows, or null
@@ -1135,6 +1297,19 @@ struct HeadGradPlan {
 HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
     HeadGradPlan p = {};
     Arena arena = {static_cast<char*>(ws)};
+    // (16 rows of bf16: 326 us against the tiles' 252 at 1024 -> 131072, bound by the multiply-adds)
+    p.few = s.rows <= (s.es == 2 ? kOuterRows / 2 : kOuterRows);
+    if (p.few) {
+        // (about 1024 workgroups, each wave at least 16 classes)
+        p.blocks = (int)div_up(s.n, 256);
+        const int64_t most = std::max<int64_t>(1, 4 * kFillTiles / p.blocks);
+        p.each = (int)std::max<int64_t>(16, div_up(s.classes, most * kOuterWaves));
+        p.slices = (int)div_up(s.classes, (int64_t)p.each * kOuterWaves);
+        p.z = arena.take<float>((int64_t)s.classes * kOuterRows * 4);
+        if (dx) p.dx = arena.take<float>((int64_t)p.slices * s.rows * s.n * 4);
+        p.bytes = arena.at;
+        return p;
+    }
     p.terms = s.es == 4;  // (three products of each)
     p.to = (int)up(s.n, p.terms ? 8 : 16 / s.es);
     const int64_t packed = (int64_t)p.to * (p.terms ? kTerms * 2 : s.es);  // bytes of a row
@@ -1186,6 +1361,31 @@ hipError_t sum(const float* acc, int splits, int64_t n, float scale, void* out, 
 }
 
 template <typename T>
+hipError_t head_grad_few(const HeadShape& s, const HeadGradArgs& a, const HeadGradPlan& p,
+                         hipStream_t st) {
+    HeadGradTileArgs g = {};
+    g.z.rows = s.rows;
+    g.z.targets = a.targets;
+    g.stats = a.stats;
+    g.dlogp = a.dlogp;
+    g.ignore = a.ignore;
+    g.all = s.classes;
+    KAN_TRY(thin<T, 1, kDz>(s, thin_args(s, a.x, a.w, a.scale, a.targets), g, p.z, st));
+    const HeadOuterArgs o = {a.x, a.w, p.z, s.xstride, s.wstride, (int)s.rows, s.classes, s.n, p.each,
+                             a.targets, a.ignore, a.scale, p.dx, a.dw};
+    auto kernel = s.rows <= 4 ? head_outer_kernel<T, 4> : head_outer_kernel<T, 8>;
+    if constexpr (sizeof(T) == 4)
+        if (s.rows > 8) kernel = head_outer_kernel<T, kOuterRows>;
+    kernel<<<p.blocks * p.slices, 64 * kOuterWaves, 0, st>>>(o, p.blocks);
+    KAN_TRY(hipGetLastError());
+    if (p.dx == nullptr) return hipSuccess;
+    const int64_t n = s.rows * s.n;
+    head_gather_kernel<T><<<grid_of(n, 16), 256, 0, st>>>(p.dx, p.slices, n, a.scale,
+                                                          static_cast<T*>(a.dx));
+    return hipGetLastError();
+}
+
+template <typename T>
 hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStream_t st) {
     if (s.rows == 0) {
         if (a.dw == nullptr) return hipSuccess;
@@ -1194,6 +1394,7 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
         return hipGetLastError();
     }
     const HeadGradPlan p = head_grad_plan(s, a.dx != nullptr, a.dw != nullptr, ws);
+    if (p.few) return head_grad_few<T>(s, a, p, st);
     const bool terms = p.terms;
     const int es = terms ? 2 : s.es;
     HeadGradTileArgs g = {};

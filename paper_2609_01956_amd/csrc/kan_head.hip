@@ -822,21 +822,44 @@ struct HeadRowsArgs {
     int64_t* best;
 };
 
-// Few tiles: the logits' sums, which were made in parts of k, to what is asked; a wave per row.
+// Few tiles: the logits' sums, which were made in parts of k, to what is asked; a row per wave, or
+// per workgroup (WHOLE), four classes of a lane at a time.
+template <bool WHOLE>
 __global__ void __launch_bounds__(256) head_rows_kernel(HeadRowsArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int U = 4, LANES = WHOLE ? 256 : 64;
+    __shared__ Best waves[4];
+    const int lane = threadIdx.x & (LANES - 1);
+    const int64_t row = WHOLE ? (int64_t)blockIdx.x
+                              : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= a.rows) return;
     const float* const z = a.z + row * a.classes;
     const int64_t step = a.rows * a.classes;
     Best b = {kNegInf, 0.0f, kNoIndex};
-    for (int c = lane; c < a.classes; c += 64) {
-        const float v = sum_of(z + c, a.splits, step) * a.scale;
+    for (int c = lane; c < a.classes; c += U * LANES) {
+        float v[U] = {};
+        for (int k = 0; k < a.splits; ++k)
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] += z[k * step + min(c + u * LANES, a.classes - 1)];
         // (a NaN adds to the sum alone)
-        b = join(b, Best{v == v ? v : kNegInf, 0.0f, v == v ? c : kNoIndex});
-        b.s += exp_of(v - anchor(b.m));
+        Best here = {kNegInf, 0.0f, kNoIndex};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool in = c + u * LANES < a.classes;
+            v[u] = in ? v[u] * a.scale : kNegInf;
+            if (in && (v[u] > here.m || (v[u] == here.m && here.at == kNoIndex)))
+                here.at = c + u * LANES;
+            here.m = __builtin_fmaxf(here.m, v[u]);
+        }
+        b = join(b, here);
+#pragma unroll
+        for (int u = 0; u < U; ++u) b.s += exp_of(v[u] - anchor(b.m));
     }
     for (int o = 1; o < 64; o *= 2) b = join(b, from_lane(b, o));
+    if (WHOLE) {
+        if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = b;
+        __syncthreads();
+        b = join(join(waves[0], waves[1]), join(waves[2], waves[3]));
+    }
     if (lane != 0) return;
     const float logs = logf(b.s);
     const int64_t t = a.targets[row];
@@ -1030,7 +1053,7 @@ ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, int es, bool terms) 
     double least = 0.0;
     for (const bool big : {true, false}) {
         const int64_t tiles = tiles_of(np, nq, big);
-        for (int64_t splits = 1; splits == 1 || (splits <= 64 && splits <= steps / 4 &&
+        for (int64_t splits = 1; splits == 1 || (splits <= 2 * kFillTiles && splits <= steps / 4 &&
                                                  tiles * splits <= 8 * kFillTiles);
              ++splits) {
             const double time =
@@ -1262,7 +1285,8 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
                 KAN_TRY(sums<T>(p.pz, t.z, p.z, st));
                 const HeadRowsArgs r = {p.z, p.pz.splits, s.rows, s.classes, a.scale, a.targets,
                                         a.ignore, a.logp, a.stats, a.best};
-                head_rows_kernel<<<(int)div_up(s.rows, 4), 256, 0, st>>>(r);
+                if (s.classes >= 512) head_rows_kernel<true><<<(int)s.rows, 256, 0, st>>>(r);
+                else head_rows_kernel<false><<<(int)div_up(s.rows, 4), 256, 0, st>>>(r);
                 return hipGetLastError();
             }
             const bool best = a.best != nullptr;
@@ -1353,10 +1377,15 @@ hipError_t gradient_tiles(const HeadGradTileArgs& g, bool big, hipStream_t st) {
     return hipGetLastError();
 }
 
+// (many parts go over 16 lanes a value: 62 parts of 1442 values 37 us in one lane each)
 template <typename T>
 hipError_t sum(const float* acc, int splits, int64_t n, float scale, void* out, hipStream_t st) {
-    head_sum_kernel<T><<<grid_of(n, 1024), 256, 0, st>>>(acc, splits, n, scale,
-                                                         static_cast<T*>(out));
+    if (splits >= 12)
+        head_gather_kernel<T><<<grid_of(n, 16), 256, 0, st>>>(acc, splits, n, scale,
+                                                              static_cast<T*>(out));
+    else
+        head_sum_kernel<T><<<grid_of(n, 1024), 256, 0, st>>>(acc, splits, n, scale,
+                                                             static_cast<T*>(out));
     return hipGetLastError();
 }
 
@@ -1379,10 +1408,7 @@ hipError_t head_grad_few(const HeadShape& s, const HeadGradArgs& a, const HeadGr
     kernel<<<p.blocks * p.slices, 64 * kOuterWaves, 0, st>>>(o, p.blocks);
     KAN_TRY(hipGetLastError());
     if (p.dx == nullptr) return hipSuccess;
-    const int64_t n = s.rows * s.n;
-    head_gather_kernel<T><<<grid_of(n, 16), 256, 0, st>>>(p.dx, p.slices, n, a.scale,
-                                                          static_cast<T*>(a.dx));
-    return hipGetLastError();
+    return sum<T>(p.dx, p.slices, s.rows * s.n, a.scale, a.dx, st);
 }
 
 template <typename T>

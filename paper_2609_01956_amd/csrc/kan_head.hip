@@ -1053,9 +1053,10 @@ ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, int es, bool terms) 
     double least = 0.0;
     for (const bool big : {true, false}) {
         const int64_t tiles = tiles_of(np, nq, big);
-        for (int64_t splits = 1; splits == 1 || (splits <= 2 * kFillTiles && splits <= steps / 4 &&
-                                                 tiles * splits <= 8 * kFillTiles);
-             ++splits) {
+        // (1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 15, ..: a few are enough)
+        const int64_t most = std::min(steps / 4, 8 * kFillTiles / std::max<int64_t>(1, tiles));
+        for (int64_t splits = 1; splits == 1 || splits <= std::min<int64_t>(most, 2 * kFillTiles);
+             splits += std::max<int64_t>(1, splits / 4)) {
             const double time =
                 tile_time(big, tiles * splits, steps_of(div_up(k, splits), es, terms), es) +
                 (splits > 1 ? 4.0 + 2.0 * splits * np * nq * 4 / 4.5e6 : 0.0);

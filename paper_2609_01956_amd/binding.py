@@ -1127,6 +1127,9 @@ def clip_grad_norm(grads: Iterable, max_norm: float, eps: float = 1e-6, out=None
 
 # ------------------------------------------------- the two ends of a token model
 
+_MOST = 2 ** 31 - 1  # what a call's 32-bit sizes hold
+
+
 def _tokens(tokens) -> int:
     if not tokens.is_cuda:
         raise ValueError("tensors must live on the GPU")
@@ -1143,6 +1146,8 @@ def _matrix(what: str, t, device) -> Tuple[int, int, int]:
     if len(shape) != 2 or shape[1] < 1:
         raise ValueError(f"{what} must be [rows, n] with n >= 1")
     rows, n = shape
+    if rows > _MOST or n > _MOST:
+        raise ValueError(f"{what} has more than 2^31 - 1 rows or columns")
     stride, inner = t.stride()
     if rows <= 1:
         stride = n
@@ -1180,6 +1185,8 @@ def embedding_backward(tokens, dy, classes: int, scale: float = 1.0, ignore_inde
     device tensor) is used when large enough, else a fresh one is taken."""
     torch = _torch()
     rows, device, classes = _tokens(tokens), tokens.device, int(classes)
+    if not 1 <= classes <= _MOST:
+        raise ValueError("classes must be from 1 to 2^31 - 1")
     if dy.shape[:-1] != tokens.shape or dy.dim() != tokens.dim() + 1:
         raise ValueError("dy must be [..., n] for tokens [...]")
     if dy.dim() != 2:

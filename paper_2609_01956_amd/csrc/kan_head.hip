@@ -154,7 +154,8 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_tile_kernel(HeadTileArgs 
 #pragma unroll
         for (int j = 0; j < Tl::RQ; ++j) {
             const int64_t row = q0 + Tl::q_of(tid, j);
-            target[j] = row < a.rows ? a.targets[row] - a.first : -1;
+            target[j] = row < a.rows ? a.targets[row] : -1;
+            target[j] = target[j] < a.first ? -1 : target[j] - a.first;
         }
         ahead();
         const float scale = settle(t, a, p0, tid, kNegInf);
@@ -1047,8 +1048,9 @@ struct ProductPlan {
 };
 // The least of the time for the tiles and, with k in splits, for their sums (written and read at
 // about 4.5 TB/s, one more launch).
-ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, int es, bool terms) {
+ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, bool terms) {
     ProductPlan p;
+    const int es = 2;
     const int64_t step = 128 / es, steps = div_up(k, step);
     double least = 0.0;
     for (const bool big : {true, false}) {
@@ -1078,13 +1080,14 @@ ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, int es, bool terms) 
 // Few tiles with a long k: the logits' sums over parts of k, in memory, rather than the tiles' own
 // logits (8 us: the launch that reads them).  0: no.
 constexpr int64_t kSumsBytes = INT64_C(64) << 20;
-ProductPlan sums_plan(int64_t rows, int64_t classes, int64_t k, int es, bool terms) {
+ProductPlan sums_plan(int64_t rows, int64_t classes, int64_t k, bool terms) {
     ProductPlan p = {};
+    const int es = 2;
     const int64_t steps = steps_of(k, es, terms);
-    if (es != 2 || tiles_of(rows, classes, true) > kFillTiles) return p;
+    if (tiles_of(rows, classes, true) > kFillTiles) return p;
     const double own = std::min(tile_time(true, tiles_of(rows, classes, true), steps, es),
                                 tile_time(false, tiles_of(rows, classes, false), steps, es));
-    p = product_plan(classes, rows, k, es, terms);
+    p = product_plan(classes, rows, k, terms);
     if (p.time + 8.0 >= own || p.splits * rows * classes * 4 > kSumsBytes) p.splits = 0;
     return p;
 }
@@ -1128,8 +1131,8 @@ HeadPlan head_plan(const HeadShape& s, void* ws) {
         p.piece = std::min<int64_t>(p.piece * b, up(s.classes, b));
         if (xp) p.xp = arena.take(s.rows * packed);
         if (wp) p.wp = arena.take(p.piece * packed);
-        if (p.piece >= s.classes)
-            p.pz = sums_plan(s.rows, s.classes, s.n, p.terms ? 2 : s.es, p.terms);
+        if (p.piece >= s.classes && (p.terms || s.es == 2))
+            p.pz = sums_plan(s.rows, s.classes, s.n, p.terms);
         if (p.pz.splits > 0) {
             p.z = arena.take<float>((int64_t)p.pz.splits * s.rows * s.classes * 4);
             p.bytes = arena.at;
@@ -1336,9 +1339,9 @@ HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
         return p;
     }
     p.terms = s.es == 4;  // (three products of each)
-    p.to = (int)up(s.n, p.terms ? 8 : 16 / s.es);
-    const int64_t packed = (int64_t)p.to * (p.terms ? kTerms * 2 : s.es);  // bytes of a row
-    const int zes = p.terms ? kDzTerms * 2 : s.es;                         // and of a logit
+    p.to = (int)up(s.n, 8);
+    const int64_t packed = (int64_t)p.to * (p.terms ? kTerms : 1) * 2;  // bytes of a row
+    const int zes = (p.terms ? kDzTerms : 1) * 2;                       // and of a logit
     const bool wp = p.terms || !s.ws;
     // as few pieces as their dz (and packed weights) and launches allow, of one size
     const int64_t row = zes * s.rows + (wp ? packed : 0);
@@ -1351,16 +1354,15 @@ HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
     if (p.terms || !s.xs || dw) p.xp = arena.take(s.rows * packed);
     if (wp) p.wp = arena.take(p.piece * packed);
     p.dz = arena.take(s.rows * p.zstride * zes);
-    const int es = p.terms ? 2 : s.es;
-    if (p.piece >= s.classes) p.pz = sums_plan(s.rows, s.classes, s.n, es, p.terms);
+    if (p.piece >= s.classes) p.pz = sums_plan(s.rows, s.classes, s.n, p.terms);
     if (p.pz.splits > 0) p.z = arena.take<float>((int64_t)p.pz.splits * s.rows * s.classes * 4);
     if (dx) {
-        p.px = product_plan(s.n, s.rows, p.zstride, es, p.terms);
+        p.px = product_plan(s.n, s.rows, p.zstride, p.terms);
         if (p.px.splits > 1 || p.piece < s.classes)
             p.dx = arena.take<float>((int64_t)p.px.splits * s.rows * s.n * 4);
     }
     if (dw) {
-        p.pw = product_plan(s.n, here, s.rows, es, p.terms);
+        p.pw = product_plan(s.n, here, s.rows, p.terms);
         if (p.pw.splits > 1) p.dw = arena.take<float>((int64_t)p.pw.splits * here * s.n * 4);
     }
     p.bytes = arena.at;
@@ -1423,7 +1425,7 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
     const HeadGradPlan p = head_grad_plan(s, a.dx != nullptr, a.dw != nullptr, ws);
     if (p.few) return head_grad_few<T>(s, a, p, st);
     const bool terms = p.terms;
-    const int es = terms ? 2 : s.es;
+    const int es = 2;  // bytes of an operand's element
     HeadGradTileArgs g = {};
     g.z.x = p.xp != nullptr ? p.xp : a.x;
     g.z.xstride = (p.xp != nullptr ? p.to : s.xstride) * es;

@@ -219,3 +219,52 @@ def test_refusals():
                  lambda: kb.embedding_backward(t, x, 30, dtype=BF16)):
         with pytest.raises(NotImplementedError):
             call()
+
+
+def test_sizes_past_32_bits():
+    """Sizes that a call's 32 bits do not hold are refused, not wrapped to small ones."""
+    t = torch.zeros(4, dtype=torch.int64, device=device())
+    dy = torch.ones(4, 1, dtype=BF16, device=device())
+    say("token operators past 32 bits")
+    for classes in (2 ** 32 + 3, 2 ** 31, 0, -1):
+        with pytest.raises(ValueError):
+            kb.embedding_backward(t, dy, classes)
+    table = torch.empty(2 ** 32 + 3, 1, dtype=BF16, device=device())
+    with pytest.raises(ValueError):
+        kb.embedding(t, table)
+    with pytest.raises(ValueError):
+        kb.linear_logprobs(dy, table, t)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("rows,classes,n", [(1 << 20, 300, 16), (3, (1 << 24) + 5, 8),
+                                            (70, (1 << 22) + 5, 8), (5, 21, 1 << 20),
+                                            (100, 21, 1 << 20)])
+def test_longest(rows, classes, n, dt):
+    """The most rows and columns, and many classes."""
+    x, w, t, d = make(rows, classes, n, 0, 0, 0, dt, 26)
+    scale = 0.5 * n ** -0.5
+    say(f"linear head of the longest {rows} {classes} {n} {dt}")
+    logp, stats, best = kb.linear_logprobs(x, w, t, scale=scale, best=True)
+    z, lp, m, _, _ = forward64(x, w, t, scale)
+    tol = ztol(z, n)
+    below((logp.double() - lp).abs(), 2 * tol + 4e-6 + 4 * U * lp.abs())
+    below(m - z.gather(1, best[:, None])[:, 0], 2 * tol)
+    del z
+    dx, dw = kb.linear_logprobs_backward(x, w, t, stats, d, scale=scale)
+    z, dz = gradient64(x, w, t, stats, d, scale)
+    check_gradients(x, w, dx, dw, z, dz, d, scale, dt)
+
+
+def test_rows_past_32_bits():
+    """Rows of more than 2^32 elements in all, and their sums, which are whole numbers."""
+    rows, V, n = 300000, 1000, 16384
+    say("embedding rows past 2^32 elements")
+    table = (torch.arange(V, device=device())[:, None] % 7 +
+             torch.arange(n, device=device()) % 11).to(BF16)
+    t = torch.arange(rows, device=device()) * 7 % V
+    y = kb.embedding(t, table)
+    for first in (0, rows // 2, rows - 100):
+        assert torch.equal(y[first:first + 100], table[t[first:first + 100]])
+    grad = kb.embedding_backward(t, y, V, dtype=F32)
+    assert torch.equal(grad, table.float() * (rows // V))

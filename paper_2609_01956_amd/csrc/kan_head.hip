@@ -219,6 +219,7 @@ struct HeadGradTileArgs {
     int all;          // classes
     void* dz;         // [rows][zstride], 0 past the classes; of fp32 as terms, kDzTerms of them
     int64_t zstride;  // elements, a multiple of 16 bytes
+    int64_t zwidth;   // of a row that may be written
     int64_t zplane;   // elements from term to term
 };
 constexpr int kDzTerms = 3;
@@ -554,7 +555,7 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileA
                 for (int u = tid; u < Tl::ROWS * U; u += Tl::THREADS) {
                     const int r = u / U, p = (u % U) * V;
                     const int64_t q = q0 + Tl::q_of_row(r, j);
-                    if (q < a.rows && p0 + p < g.zstride)
+                    if (q < a.rows && p0 + p < g.zwidth)
                         *reinterpret_cast<u32x4*>(dz + q * g.zstride + p0 + p) =
                             *reinterpret_cast<const u32x4*>(lds + AT + r * PITCH +
                                                             p * (int)sizeof(T));
@@ -1023,11 +1024,29 @@ int64_t tiles_of(int64_t a, int64_t b, bool big) {
 int64_t steps_of(int64_t k, int es, bool terms) {
     return div_up(k, 128 / es) * (terms ? kSegments : 1);
 }
-bool big_tiles(int64_t rows, int64_t classes, int64_t k, int es, bool terms) {
-    const int64_t steps = steps_of(k, es, terms);
-    return tile_time(true, tiles_of(rows, classes, true), steps, es) <=
-           tile_time(false, tiles_of(rows, classes, false), steps, es);
+
+// How many of `wide` (classes) by `rows` products big tiles make: all, none, or as many as fill the
+// GPU some whole turns, with small tiles for the rest in a second launch.
+struct Mix {
+    int64_t big;  // of wide: a multiple of kBig, or all
+    double time;
+};
+constexpr double kSecondLaunch = 4.0;
+Mix mix_of(int64_t rows, int64_t wide, int64_t k, int es, bool terms) {
+    const int64_t steps = steps_of(k, es, terms), tiles = tiles_of(rows, wide, true);
+    Mix m = {wide, tile_time(true, tiles, steps, es)};
+    const auto offer = [&](int64_t big, double time) {
+        if (time < m.time) m = {big, time};
+    };
+    offer(0, tile_time(false, tiles_of(rows, wide, false), steps, es));
+    const int64_t high = div_up(rows, kBig), big = tiles / kFillTiles * kFillTiles / high * kBig;
+    if (big > 0 && big < wide)
+        offer(big, tile_time(true, big / kBig * high, steps, es) + kSecondLaunch +
+                       tile_time(false, tiles_of(rows, wide - big, false), steps, es));
+    return m;
 }
+// The tiles along `wide`.
+int64_t parts_of(int64_t big, int64_t wide) { return div_up(big, kBig) + div_up(wide - big, kSmall); }
 
 constexpr int64_t kTermRows = 384;
 // fp32 operands as bf16 terms: what making them costs (12 bytes of memory traffic an element) is
@@ -1043,13 +1062,14 @@ bool by_terms(const HeadShape& s) {
 struct ProductPlan {
     bool big;
     double time;
-    int tp, tq, splits;
+    int tp, splits;
     int64_t k_split;
+    int64_t rest;  // of nq: the first row that small tiles make in a second launch, or nq
 };
 // The least of the time for the tiles and, with k in splits, for their sums (written and read at
 // about 4.5 TB/s, one more launch).
 ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, bool terms) {
-    ProductPlan p;
+    ProductPlan p = {};
     const int es = 2;
     const int64_t step = 128 / es, steps = div_up(k, step);
     double least = 0.0;
@@ -1068,10 +1088,17 @@ ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, bool terms) {
             p.splits = (int)splits;
         }
     }
+    const Mix mix = mix_of(np, nq, k, es, terms);
+    p.rest = nq;
+    if (mix.big > 0 && mix.big < nq && mix.time < least) {
+        least = mix.time;
+        p.big = true;
+        p.splits = 1;
+        p.rest = mix.big;
+    }
     p.time = least;
     const int b = p.big ? kBig : kSmall;
     p.tp = (int)div_up(np, b);
-    p.tq = (int)div_up(nq, b);
     p.k_split = div_up(steps, p.splits) * step;
     p.splits = (int)div_up(k, p.k_split);
     return p;
@@ -1083,17 +1110,15 @@ constexpr int64_t kSumsBytes = INT64_C(64) << 20;
 ProductPlan sums_plan(int64_t rows, int64_t classes, int64_t k, bool terms) {
     ProductPlan p = {};
     const int es = 2;
-    const int64_t steps = steps_of(k, es, terms);
     if (tiles_of(rows, classes, true) > kFillTiles) return p;
-    const double own = std::min(tile_time(true, tiles_of(rows, classes, true), steps, es),
-                                tile_time(false, tiles_of(rows, classes, false), steps, es));
+    const double own = mix_of(rows, classes, k, es, terms).time;
     p = product_plan(classes, rows, k, terms);
     if (p.time + 8.0 >= own || p.splits * rows * classes * 4 > kSumsBytes) p.splits = 0;
     return p;
 }
 
 struct HeadPlan {
-    bool thin, big, terms;
+    bool thin, terms;
     int64_t parts;
     int64_t piece;      // classes
     int to;             // elements of a packed row
@@ -1123,12 +1148,13 @@ HeadPlan head_plan(const HeadShape& s, void* ws) {
     if (p.thin) {
         p.parts = thin_groups(s);
     } else {
-        p.big = big_tiles(s.rows, s.classes, s.n, p.terms ? 2 : s.es, p.terms);
-        const int b = p.big ? kBig : kSmall;
-        p.parts = div_up(s.classes, b);
-        p.piece = kPieceTiles / div_up(s.rows, b);
-        if (wp) p.piece = std::min(p.piece, std::max<int64_t>(1, kPieceBytes / packed / b));
-        p.piece = std::min<int64_t>(p.piece * b, up(s.classes, b));
+        int64_t most = kPieceTiles / div_up(s.rows, kSmall) * kSmall / kBig * kBig;
+        if (wp) most = std::min(most, std::max<int64_t>(kPieceBytes / packed / kBig * kBig, kBig));
+        p.piece = up(div_up(s.classes, div_up(s.classes, most)), kBig);
+        for (int64_t first = 0; first < s.classes; first += p.piece) {
+            const int64_t here = std::min<int64_t>(s.classes - first, p.piece);
+            p.parts += parts_of(mix_of(s.rows, here, s.n, p.terms ? 2 : s.es, p.terms).big, here);
+        }
         if (xp) p.xp = arena.take(s.rows * packed);
         if (wp) p.wp = arena.take(p.piece * packed);
         if (p.piece >= s.classes && (p.terms || s.es == 2))
@@ -1208,23 +1234,61 @@ HeadThinArgs thin_args(const HeadShape& s, const void* x, const void* w, float s
 // Workgroups that are resident together: one of a big tile on a CU, or two of a small one.
 int resident(int tiles, bool big) { return std::min(tiles, big ? kFillTiles : 2 * kFillTiles); }
 
+// launch(z, classes before, are its tiles big) for the first `big` classes, and for the rest.
+template <typename F>
+hipError_t by_tiles(const LogitArgs& all, int64_t big, F&& launch) {
+    for (const bool first : {true, false}) {
+        const int64_t from = first ? 0 : big, here = first ? big : all.classes - big;
+        if (here == 0) continue;
+        const int side = first ? kBig : kSmall;
+        LogitArgs z = all;
+        z.w = static_cast<const char*>(all.w) + from * all.wstride;
+        z.first = (int)(all.first + from);
+        z.classes = (int)here;
+        z.tp = (int)div_up(here, side);
+        z.tq = (int)div_up(all.rows, side);
+        KAN_TRY(launch(z, from, first));
+    }
+    return hipSuccess;
+}
+
 template <typename T, typename Tl>
-hipError_t tiles(const HeadTileArgs& a, bool best, bool big, hipStream_t st) {
+hipError_t logit_tiles(const HeadTileArgs& a, bool best, bool big, hipStream_t st) {
     const int groups = resident(a.z.tp * a.z.tq, big);
     if (best) head_tile_kernel<T, Tl, true><<<groups, Tl::THREADS, 0, st>>>(a);
     else head_tile_kernel<T, Tl, false><<<groups, Tl::THREADS, 0, st>>>(a);
     return hipGetLastError();
 }
+template <typename T, int S>
+hipError_t logit_tiles(const HeadTileArgs& a, const void* best, bool big, hipStream_t st) {
+    return big ? logit_tiles<T, BigLogits<T, S>>(a, best != nullptr, true, st)
+               : logit_tiles<T, SmallLogits<T, S>>(a, best != nullptr, false, st);
+}
 
 // O: the type of the call (of its operands, in fp32 as bf16 terms, and its results).
 template <typename O, int MP, int MQ>
-hipError_t product(const ProductPlan& p, const ProductArgs& a, hipStream_t st) {
+hipError_t product(const ProductPlan& p, const ProductArgs& all, hipStream_t st) {
     constexpr int S = sizeof(O) == 4 ? kSegments : 1;
     typedef Tile<uint16_t, 2, 4, 4, 2, MP, MQ, S> Big;
     typedef Tile<uint16_t, 2, 2, 2, 2, MP, MQ, S> Small;
-    const int groups = p.tp * p.tq * p.splits;
+    const int64_t rest = std::min(p.rest, all.nq);
+    ProductArgs a = all;
+    a.nq = rest;
+    a.k_split = p.k_split;
+    a.tp = p.tp;
+    a.tq = (int)div_up(rest, p.big ? kBig : kSmall);
+    const int groups = a.tp * a.tq * p.splits;
     if (p.big) head_product_kernel<O, Big, MP, MQ><<<groups, Big::THREADS, 0, st>>>(a);
     else head_product_kernel<O, Small, MP, MQ><<<groups, Small::THREADS, 0, st>>>(a);
+    KAN_TRY(hipGetLastError());
+    if (rest == all.nq) return hipSuccess;
+    a.q = static_cast<const char*>(all.q) + rest * (MQ == kByRows ? all.qstride : 2);
+    a.nq = all.nq - rest;
+    a.tp = (int)div_up(all.np, kSmall);
+    a.tq = (int)div_up(a.nq, kSmall);
+    if (all.out != nullptr) a.out = static_cast<O*>(all.out) + rest * all.np;
+    if (all.acc != nullptr) a.acc = all.acc + rest * all.np;
+    head_product_kernel<O, Small, MP, MQ><<<a.tp * a.tq, Small::THREADS, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -1242,9 +1306,6 @@ hipError_t sums(const ProductPlan& p, const LogitArgs& z, float* out, hipStream_
     r.np = z.classes;
     r.nq = z.rows;
     r.k = z.k;
-    r.k_split = p.k_split;
-    r.tp = p.tp;
-    r.tq = p.tq;
     r.acc = out;
     return product<O, kByRows, kByRows>(p, r, st);
 }
@@ -1269,21 +1330,17 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
         t.z.scale = a.scale;
         t.z.targets = a.targets;
         t.out = p.out;
-        const int b = p.big ? kBig : kSmall;
-        t.z.tq = (int)div_up(s.rows, b);
         if (p.xp != nullptr)
             KAN_TRY(pack<T>(p.terms, a.x, s.xstride, s.rows, s.n, p.xp, p.to, nullptr, 0, st));
         for (int64_t first = 0; first < s.classes; first += p.piece) {
+            const int64_t here = std::min<int64_t>(s.classes - first, p.piece);
             t.z.first = (int)first;
-            t.z.classes = (int)std::min<int64_t>(s.classes - first, p.piece);
-            t.z.tp = (int)div_up(t.z.classes, b);
-            t.part = first / b;
+            t.z.classes = (int)here;
             t.z.w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
             if (p.wp != nullptr) {
-                KAN_TRY(pack<T>(p.terms, t.z.w, s.wstride, t.z.classes, s.n, p.wp, p.to, nullptr, 0,
-                                st));
+                KAN_TRY(pack<T>(p.terms, t.z.w, s.wstride, here, s.n, p.wp, p.to, nullptr, 0, st));
                 t.z.w = p.wp;
-                t.z.wplane = p.terms ? (int64_t)t.z.classes * p.to * es : 0;
+                t.z.wplane = p.terms ? here * p.to * es : 0;
             }
             if (p.pz.splits > 0) {
                 KAN_TRY(sums<T>(p.pz, t.z, p.z, st));
@@ -1293,14 +1350,14 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
                 else head_rows_kernel<false><<<(int)div_up(s.rows, 4), 256, 0, st>>>(r);
                 return hipGetLastError();
             }
-            const bool best = a.best != nullptr;
-            if (p.terms)
-                KAN_TRY(p.big ? tiles<uint16_t, BigLogits<uint16_t, kSegments>>(t, best, true, st)
-                              : tiles<uint16_t, SmallLogits<uint16_t, kSegments>>(t, best, false,
-                                                                                  st));
-            else
-                KAN_TRY(p.big ? tiles<T, BigLogits<T, 1>>(t, best, true, st)
-                              : tiles<T, SmallLogits<T, 1>>(t, best, false, st));
+            KAN_TRY(by_tiles(t.z, mix_of(s.rows, here, s.n, es, p.terms).big,
+                             [&](const LogitArgs& z, int64_t, bool big) {
+                                 const HeadTileArgs part = {z, t.out, t.part};
+                                 t.part += z.tp;
+                                 return p.terms
+                                            ? logit_tiles<uint16_t, kSegments>(part, a.best, big, st)
+                                            : logit_tiles<T, 1>(part, a.best, big, st);
+                             }));
         }
     }
     HeadJoinArgs j = {p.out, s.rows, (int)p.parts, s.classes, 1, a.targets, a.ignore, a.logp, a.stats,
@@ -1455,17 +1512,20 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
             g.z.w = p.wp;
             g.z.wplane = terms ? here * p.to * es : 0;
         }
-        const bool big = big_tiles(s.rows, here, s.n, es, terms);
-        const int b = big ? kBig : kSmall;
-        g.z.tp = (int)div_up(here, b);
-        g.z.tq = (int)div_up(s.rows, b);
         if (p.pz.splits > 0) {
             KAN_TRY(sums<T>(p.pz, g.z, p.z, st));
             head_dz_kernel<sizeof(T) == 4>
                 <<<grid_of(s.rows * (p.zstride / 8), 256), 256, 0, st>>>(g, p.z, p.pz.splits);
             KAN_TRY(hipGetLastError());
         } else {
-            KAN_TRY(gradient_tiles<T>(g, big, st));
+            KAN_TRY(by_tiles(g.z, mix_of(s.rows, here, s.n, es, terms).big,
+                             [&](const LogitArgs& z, int64_t from, bool big) {
+                                 HeadGradTileArgs part = g;
+                                 part.z = z;
+                                 part.dz = static_cast<uint16_t*>(p.dz) + from;
+                                 part.zwidth = p.zstride - from;
+                                 return gradient_tiles<T>(part, big, st);
+                             }));
         }
         ProductArgs r = {};
         r.q = p.dz;
@@ -1482,9 +1542,6 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
             r.nq = s.rows;
             r.k = up(here, 16 / es);  // (whole chunks of dz's rows, which are 0 past the classes)
             r.pk = here;
-            r.k_split = p.px.k_split;
-            r.tp = p.px.tp;
-            r.tq = p.px.tq;
             r.acc = p.dx;
             r.add = first > 0;
             r.out = whole ? a.dx : nullptr;
@@ -1494,21 +1551,16 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
         }
         if (a.dw != nullptr) {
             char* const out = static_cast<char*>(a.dw) + first * s.n * s.es;
-            ProductPlan pw = p.pw;
-            pw.tq = (int)div_up(here, pw.big ? kBig : kSmall);
             r.p = p.xp;
             r.pstride = g.z.xstride;
             r.pplane = g.z.xplane;
             r.nq = here;
             r.k = r.pk = r.qk = s.rows;
-            r.k_split = pw.k_split;
-            r.tp = pw.tp;
-            r.tq = pw.tq;
             r.acc = p.dw;
             r.add = false;
-            r.out = pw.splits == 1 ? out : nullptr;
-            KAN_TRY(product<T, kByK, kByK>(pw, r, st));
-            if (pw.splits > 1) KAN_TRY(sum<T>(p.dw, pw.splits, here * s.n, a.scale, out, st));
+            r.out = p.pw.splits == 1 ? out : nullptr;
+            KAN_TRY(product<T, kByK, kByK>(p.pw, r, st));
+            if (p.pw.splits > 1) KAN_TRY(sum<T>(p.dw, p.pw.splits, here * s.n, a.scale, out, st));
         }
     }
     return hipSuccess;

@@ -200,6 +200,47 @@ __device__ __forceinline__ void digits_before(const uint32_t* count, uint32_t* f
     __syncthreads();
 }
 
+// The first rows of the table, as they are where their tokens do not occur (base, or 0): written by
+// workgroups beside those that sort, which leave most of the GPU and its memory idle.  In 16-byte
+// units of memory, whatever the rows are.
+struct Fill {
+    const char* base;  // or null: 0
+    char* to;
+    int64_t bytes;        // of the table
+    int64_t first, last;  // units: the one that holds the first byte is 0
+    int groups;           // workgroups, the last ones of the launch
+};
+constexpr int kFillTurn = kLoads * kSortThreads;
+__device__ __forceinline__ void fill_units(const Fill& f, int group) {
+    const int head = (int)(reinterpret_cast<uintptr_t>(f.to) & 15);
+    for (int64_t first = f.first + (int64_t)group * kFillTurn; first < f.last;
+         first += (int64_t)f.groups * kFillTurn) {
+        int64_t at[kLoads];
+        bool whole[kLoads];
+        u32x4 v[kLoads];
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const int64_t u = first + k * kSortThreads + threadIdx.x;
+            at[k] = u < f.last ? u * 16 - head : f.bytes;
+            whole[k] = at[k] >= 0 && at[k] + 16 <= f.bytes;
+            v[k] = u32x4{0, 0, 0, 0};
+            if (f.base != nullptr && whole[k])
+                v[k] = *unit_at(reinterpret_cast<const uint16_t*>(f.base + at[k]), 0);
+        }
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            if (whole[k]) {
+                *reinterpret_cast<u32x4*>(f.to + at[k]) = v[k];
+                continue;
+            }
+            for (int64_t b = at[k] < 0 ? 0 : at[k]; b < at[k] + 16 && b < f.bytes; b += 2)
+                *reinterpret_cast<uint16_t*>(f.to + b) =
+                    f.base == nullptr ? (uint16_t)0
+                                      : *reinterpret_cast<const uint16_t*>(f.base + b);
+        }
+    }
+}
+
 struct SortArgs {
     const int64_t* tokens;  // the first pass's input, or null:
     const Entry* in;
@@ -213,6 +254,7 @@ struct SortArgs {
     int tiles;
     int2* span;        // [classes + 1], to be cleared, and the later passes' hists
     int64_t later;     // (from `next` on)
+    Fill fill;
 };
 
 __device__ __forceinline__ Entry entry_of(const SortArgs& a, int64_t i) {
@@ -274,6 +316,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortArgs a) 
     __shared__ uint32_t all[kDigits], first[kDigits];
     __shared__ uint32_t next[kCountTiles * kDigits];
     constexpr int kBatches = kSortTile / kSortThreads;
+    if ((int)blockIdx.x >= a.tiles) {
+        fill_units(a.fill, blockIdx.x - a.tiles);
+        return;
+    }
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, digits = 1 << a.bits;
     if (a.next != nullptr)
         for (int i = threadIdx.x; i < a.tiles << a.next_bits; i += kSortThreads) next[i] = 0;
@@ -332,16 +378,21 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortArgs a) 
                       next[i]);
 }
 
-// At most kSortFew entries: all passes in LDS by the first workgroup; the others clear the spans.
+// At most kSortFew entries: all passes in LDS by the first workgroup; others clear the spans.
 __global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortArgs a, int passes) {
     __shared__ uint32_t count[kSortWaves][kDigits];
     __shared__ uint32_t all[kDigits], first[kDigits];
     __shared__ Entry hold[kSortFew];
     constexpr int kBatches = kSortFew / kSortThreads;
-    if (blockIdx.x > 0 || gridDim.x == 1)
+    const int groups = (int)gridDim.x - a.fill.groups;
+    if ((int)blockIdx.x >= groups) {
+        fill_units(a.fill, blockIdx.x - groups);
+        return;
+    }
+    if (blockIdx.x > 0 || groups == 1)
         clear_spans(a.span, (int64_t)a.classes + 1,
-                    (int64_t)(gridDim.x == 1 ? 0 : blockIdx.x - 1) * kSortThreads + threadIdx.x,
-                    (int64_t)(gridDim.x == 1 ? 1 : gridDim.x - 1) * kSortThreads);
+                    (int64_t)(groups == 1 ? 0 : blockIdx.x - 1) * kSortThreads + threadIdx.x,
+                    (int64_t)(groups == 1 ? 1 : groups - 1) * kSortThreads);
     if (blockIdx.x > 0) return;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     Entry e[kBatches];
@@ -400,6 +451,7 @@ struct EmbedSumArgs {
     int lanes;             // of a chunk: 64, 128 or 256
     int blocks;            // of 64 units, a row
     int heavy;             // the last launch: workgroups for tokens of more than kRun entries
+    int64_t filled;        // 16-byte units of the table that have been filled
 };
 
 // The sums of a level's chunks c0 .. c1 of the token that starts at entry `start`, added in order.
@@ -633,7 +685,7 @@ __global__ void __launch_bounds__(256) embed_rest_kernel(EmbedSumArgs a) {
     const int64_t total = (int64_t)a.g.classes * a.g.n;
     const int head = (int)((reinterpret_cast<uintptr_t>(table) & 15) / sizeof(TP));
     const int64_t units = (total + head + V - 1) / V, groups = gridDim.x - a.heavy;
-    for (int64_t first = (int64_t)(blockIdx.x - a.heavy) * 256 * kLoads; first < units;
+    for (int64_t first = a.filled + (int64_t)(blockIdx.x - a.heavy) * 256 * kLoads; first < units;
          first += groups * 256 * kLoads) {
         // rows of the workgroup's elements, from that of the first one on
         const int64_t e0 = first * V - head, origin = e0 < 0 ? 0 : e0;
@@ -697,6 +749,12 @@ int groups_of(int64_t n) { return (int)std::min<int64_t>(n, kMaxGroups); }
 
 // Workgroups of each kind in the last launch: they go on by strides.
 constexpr int kRestGroups = 1 << 13;
+// Bytes (read and written) of the table that a pass of sorting may fill beside it, what one launch
+// sorts taking about two passes' time; workgroups of such a launch.  4096 x 1024 bf16 of 131072 tokens:
+// without 71 us, 32 MB 67, 64 MB 61, 96 MB 55; 65536 x 256 fp32 of 50001 62, 59, 59, 59; with a base,
+// 30001 x 1001 of 50001, 122, 120, 124, 127.
+constexpr int64_t kFillBytes = INT64_C(48) << 20;
+constexpr int kFillGroups = 256;
 
 struct EmbedGradPlan {
     Entry* list[2];
@@ -762,9 +820,23 @@ hipError_t embed_grad(const EmbedGradArgs& g, void* ws, hipStream_t s) {
     a.bits = a.next_bits = p.bits;
     a.tiles = p.tiles;
     a.span = p.span;
+    // (in place, rows of tokens that do not occur stay as they are)
+    const int64_t bytes = (int64_t)g.classes * g.n * (int64_t)sizeof(TP);
+    const int64_t units =
+        g.base == g.dtable ? 0 : div_up(bytes + (reinterpret_cast<uintptr_t>(g.dtable) & 15), 16);
+    a.fill = Fill{static_cast<const char*>(g.base), static_cast<char*>(g.dtable), bytes, 0, 0, 0};
+    const auto fill_next = [&](int sorting, int passes) {
+        a.fill.first = a.fill.last;
+        a.fill.last =
+            std::min(units, a.fill.first + passes * kFillBytes / (g.base == nullptr ? 16 : 32));
+        a.fill.groups = (int)std::min<int64_t>(div_up(a.fill.last - a.fill.first, kFillTurn),
+                                               kFillGroups - sorting);
+    };
     const int clear = (int)std::min<int64_t>(div_up((int64_t)g.classes + 1, 4 * kSortThreads), 1024);
     if (g.rows <= kSortFew) {
-        sort_few_kernel<<<clear == 1 ? 1 : clear + 1, kSortThreads, 0, s>>>(a, p.passes);
+        const int groups = clear == 1 ? 1 : clear + 1;
+        fill_next(1, 2);
+        sort_few_kernel<<<groups + a.fill.groups, kSortThreads, 0, s>>>(a, p.passes);
         KAN_TRY(hipGetLastError());
     } else {
         const int64_t hist = (int64_t)p.tiles * kDigits;
@@ -783,7 +855,8 @@ hipError_t embed_grad(const EmbedGradArgs& g, void* ws, hipStream_t s) {
                 sort_scan_kernel<<<kDigits / 64, 64, 0, s>>>(a);
                 KAN_TRY(hipGetLastError());
             }
-            sort_scatter_kernel<<<p.tiles, kSortThreads, 0, s>>>(a);
+            if (p.tiles <= kCountTiles) fill_next(p.tiles, 1);
+            sort_scatter_kernel<<<p.tiles + a.fill.groups, kSortThreads, 0, s>>>(a);
             KAN_TRY(hipGetLastError());
             a.tokens = nullptr;
             a.span = nullptr;
@@ -823,8 +896,8 @@ hipError_t embed_grad(const EmbedGradArgs& g, void* ws, hipStream_t s) {
     }
     if (g.rows > kRun)
         e.heavy = (int)std::min<int64_t>(div_up(div_up(g.rows, kRun) * e.blocks, 4), kRestGroups);
-    const int64_t rest =
-        g.base == g.dtable ? 0 : div_up((int64_t)g.classes * g.n / kVec<TP> + 2, 256 * kLoads);
+    e.filled = a.fill.last;
+    const int64_t rest = div_up(units - e.filled, 256 * kLoads);
     const int groups = e.heavy + (int)std::min<int64_t>(rest, kRestGroups);
     if (groups == 0) return hipSuccess;
     const bool past = (int64_t)g.classes * g.n * (int64_t)sizeof(TP) >= kPastCaches;

@@ -29,6 +29,15 @@ __device__ __forceinline__ float exp_exact(float t) {
     const float h = t * kLog2e, e = __builtin_amdgcn_exp2f(h);
     return __builtin_fmaf(e, __builtin_fmaf(-h, kLn2Low, __builtin_fmaf(-h, kLn2, t)), e);
 }
+// 1 - exp(t), to 2^-22 of it near t = 0, where the difference would lose what p nearly 1 leaves (nine
+// terms of the series: the tenth is below 2^-29 of the sum).
+__device__ __forceinline__ float one_less_exp(float t) {
+    if (!(__builtin_fabsf(t) <= 0.5f)) return 1.0f - exp_exact(__builtin_fmaxf(t, -1e4f));
+    float s = 1.0f;
+#pragma unroll
+    for (int k = 9; k >= 2; --k) s = __builtin_fmaf(s, t * (1.0f / k), 1.0f);
+    return -t * s;
+}
 // What a maximum is subtracted as: rows (so far) without any class stay at 0.
 __device__ __forceinline__ float anchor(float m) { return m == kNegInf ? 0.0f : m; }
 
@@ -260,6 +269,12 @@ __device__ __forceinline__ float dz_of(const RowGrad& r, float t) {
                          : exp_of(__builtin_fmaxf(t, -1e4f)));
 }
 
+// dz of the target for the logit less its offset.
+template <bool EXACT>
+__device__ __forceinline__ float target_of(const RowGrad& r, float t) {
+    return EXACT ? r.d * one_less_exp(t - r.logs) : dz_of<false>(r, t) + r.d;
+}
+
 // ------------------------------------------------------------ few rows
 
 // Elements [k, k + 16 bytes) of a row of n, 0 past its end.
@@ -337,7 +352,9 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
     for (int g0 = blockIdx.x * TURN; g0 < groups; g0 += gridDim.x * TURN) {
         const int p0 = (SPLIT ? g0 : g0 + wave) * 16;
         const T* const row = w + (int64_t)min(p0 + r16, a.classes - 1) * a.wstride;
-        floatx4 acc[NT] = {};
+        // (fp32: several sums, each of a part of the products, so that roundings add up less)
+        constexpr int SUMS = sizeof(T) == 2 ? 1 : NT <= 2 ? 4 : 2;
+        floatx4 all[NT][SUMS] = {};
         for (int c0 = 0; c0 < chunks; c0 += width) {
             if (!once) {
                 __syncthreads();
@@ -351,14 +368,15 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
                     const u32x4 xv = *reinterpret_cast<const u32x4*>(
                         lds + ((size_t)r * width + ((c + quad) ^ (r & 7))) * 16);
                     if constexpr (sizeof(T) == 2) {
-                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(bf16x8, wv), __builtin_bit_cast(bf16x8, xv), acc[t],
-                            0, 0, 0);
+                        all[t][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8, wv), __builtin_bit_cast(bf16x8, xv),
+                            all[t][0], 0, 0, 0);
                     } else {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                                __uint_as_float(wv[i]), __uint_as_float(xv[i]), acc[t], 0, 0, 0);
+                            all[t][i % SUMS] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                                __uint_as_float(wv[i]), __uint_as_float(xv[i]), all[t][i % SUMS], 0,
+                                0, 0);
                     }
                 }
             };
@@ -381,6 +399,13 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
                 product(c, at < chunks ? chunk_of(row, at * V, a.n) : u32x4{0, 0, 0, 0});
             }
         }
+        floatx4 acc[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            acc[t] = all[t][0];
+            if constexpr (SUMS > 1) acc[t] += all[t][1];
+            if constexpr (SUMS > 2) acc[t] += all[t][2] + all[t][3];
+        }
         if constexpr (SPLIT) {
             // (the only group of the workgroup: its sums may stand where x did)
             floatx4* const sums = reinterpret_cast<floatx4*>(lds);
@@ -400,7 +425,8 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
                 for (int i = 0; i < 4; ++i) {
                     const int p = p0 + quad * 4 + i;
                     const float v = __builtin_fmaf(acc[t][i], a.scale, -of[t].template offset<true>());
-                    const float y = dz_of<true>(of[t], v) + (p == of[t].target ? of[t].d : 0.0f);
+                    float y = dz_of<true>(of[t], v);
+                    if (p == of[t].target) y = target_of<true>(of[t], v);
                     if (p < a.classes) dz[((int64_t)p * NT + t) * 16 + r16] = y;
                 }
                 continue;
@@ -526,18 +552,28 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileA
         for (int j = 0; j < Tl::RQ; ++j) {
             const RowGrad& r = row[j];
             const float o = -r.offset<TERMS>();
+            const bool here = r.target >= p0 && r.target < p0 + Tl::BP;
+            const int target = r.target - p1;
+            float own = 0.0f;  // the target's logit, then its dz
+            if (here) {
+#pragma unroll
+                for (int i = 0; i < Tl::RP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        own = target == Tl::p_step(i, e) ? t.acc[i][j][e] : own;
+                own = target_of<TERMS>(r, __builtin_fmaf(own, scale, o));
+            }
 #pragma unroll
             for (int i = 0; i < Tl::RP; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     t.acc[i][j][e] = dz_of<TERMS>(r, __builtin_fmaf(t.acc[i][j][e], scale, o));
-            if (r.target >= p0 && r.target < p0 + Tl::BP) {
-                const int p = r.target - p1;
+            if (here) {
 #pragma unroll
                 for (int i = 0; i < Tl::RP; ++i)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        t.acc[i][j][e] += p == Tl::p_step(i, e) ? r.d : 0.0f;
+                        t.acc[i][j][e] = target == Tl::p_step(i, e) ? own : t.acc[i][j][e];
             }
             if (p0 + Tl::BP > a.classes) {
                 const int classes = a.classes - p1;
@@ -897,8 +933,8 @@ __global__ void __launch_bounds__(256) head_dz_kernel(HeadGradTileArgs g, const 
             y[k] = 0.0f;
             if (c >= a.classes) continue;
             const float v = sum_of(z + row * a.classes + c, splits, step);
-            y[k] = dz_of<TERMS>(r, __builtin_fmaf(v, a.scale, -r.offset<TERMS>()));
-            if (c == r.target) y[k] += r.d;
+            const float t = __builtin_fmaf(v, a.scale, -r.offset<TERMS>());
+            y[k] = c == r.target ? target_of<TERMS>(r, t) : dz_of<TERMS>(r, t);
         }
         uint16_t* out = static_cast<uint16_t*>(g.dz) + row * g.zstride + c0;
         for (int term = 0; term < (TERMS ? kDzTerms : 1); ++term, out += g.zplane) {

@@ -268,3 +268,27 @@ def test_rows_past_32_bits():
         assert torch.equal(y[first:first + 100], table[t[first:first + 100]])
     grad = kb.embedding_backward(t, y, V, dtype=F32)
     assert torch.equal(grad, table.float() * (rows // V))
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("rows,V,n", [(7, 5, 3), (100, 90001, 700), (5000, 2000, 33),
+                                      (9000, 90001, 701)])
+def test_gradients_at_odd_places(rows, V, n, dt):
+    """The gradient and its base one element past an aligned place: as at aligned ones, and nothing
+    around it; a row without tokens is its base or 0 wherever in the table it is."""
+    g = torch.Generator(device=device())
+    g.manual_seed(27)
+    t = torch.randint(0, V, (rows,), device=device(), generator=g)
+    dy = torch.randn(rows, n, device=device(), generator=g).to(dt)
+    base = torch.randn(V, n, device=device(), generator=g).to(dt)
+    odd = torch.full((V * n + 2,), 9.0, dtype=dt, device=device())
+    odd_base = torch.empty(V * n + 3, dtype=dt, device=device())[3:].view(V, n).copy_(base)
+    say(f"embedding_backward at odd places {rows} {V} {n} {dt}")
+    absent = torch.ones(V, dtype=torch.bool, device=device())
+    absent[t] = False
+    for b, ob in ((None, None), (base, odd_base)):
+        want = kb.embedding_backward(t, dy, V, base=b)
+        assert torch.equal(want[absent], (torch.zeros_like(base) if b is None else b)[absent])
+        kb.embedding_backward(t, dy, V, base=ob, out=odd[1:-1].view(V, n))
+        assert torch.equal(odd[1:-1].view(V, n), want)
+        assert float(odd[0]) == 9.0 and float(odd[-1]) == 9.0

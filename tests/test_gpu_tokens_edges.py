@@ -292,3 +292,22 @@ def test_gradients_at_odd_places(rows, V, n, dt):
         kb.embedding_backward(t, dy, V, base=ob, out=odd[1:-1].view(V, n))
         assert torch.equal(odd[1:-1].view(V, n), want)
         assert float(odd[0]) == 9.0 and float(odd[-1]) == 9.0
+
+
+@pytest.mark.parametrize("rows,V", [(6, 10), (16, 3000), (40, 300), (600, 4000)])
+def test_targets_nearly_certain(rows, V):
+    """1 - p of a target with p nearly 1, in fp32, for given stats: to its own size (2^-22 of the series,
+    two roundings of dz and as many of its terms and sum), not to that of p.  Rows of the identity make
+    the logits the weights, and dz the weights' gradient."""
+    x = torch.eye(rows, device=device())
+    t = torch.randperm(V, device=device())[:rows]
+    w = torch.zeros(V, rows, device=device())
+    w[t, torch.arange(rows, device=device())] = 14.0
+    logs = torch.log1p(torch.tensor((V - 1) * math.exp(-14.0), dtype=torch.float64)).float()
+    stats = torch.stack([torch.full((rows,), 14.0), logs.expand(rows)], 1).to(device())
+    d = -torch.rand(rows, device=device()) - 0.1
+    say(f"linear head targets nearly certain {rows} {V}")
+    _, dw = kb.linear_logprobs_backward(x, w, t, stats, d, need_dx=False)
+    want = -torch.expm1(-logs.double()).to(device()) * d.double()
+    got = dw[t, torch.arange(rows, device=device())].double()
+    below((got - want).abs(), want.abs() * (2.0 ** -22 + 6 * U))

@@ -703,14 +703,14 @@ kan_status kan_embedding_backward_workspace_bytes(int64_t rows, int32_t classes,
 
 /*
  * kan_linear_logprobs -- log probabilities of given classes (tokens) under the softmax of a linear
- * head, whose logits are never in memory:
+ * head, whose logits are not kept:
  *
  *   z[b, v] = scale sum_i x[b, i] weight[v, i]
  *   m[b] = max_v z[b, v],  logs[b] = log sum_v exp(z[b, v] - m[b])
  *   logp[b] = z[b, targets[b]] - m[b] - logs[b]
  *   best[b] = the lowest v with z[b, v] = m[b]
  *
- *   x            [rows, n], rows x_stride >= n elements apart (what lies between is not read)
+ *   x            [rows, n], rows x_stride >= n elements apart (what lies between has no effect)
  *   weight       [classes, n], rows weight_stride >= n elements apart
  *   scale        finite
  *   targets      [rows] int64; ignore_index gives logp 0, another value outside [0, classes)
@@ -724,11 +724,15 @@ kan_status kan_embedding_backward_workspace_bytes(int64_t rows, int32_t classes,
  * x and weight are of dtype; products and sums are binary32 (the sum before the scale, too, has
  * to stay in its range).  Large fp32 products take both operands as three bf16 terms, which hold
  * all 24 bits of values from 2^-109 on; products of their smallest terms, below 2^-25 of the whole,
- * are left out.  Rows of 16-byte aligned x and weight
- * of whole 16-byte units are read as they stand; others are copied to the workspace (weights in
- * pieces), except in calls of at most 64 rows.  A NaN or +infinity among a row's logits makes its
- * logp and logs NaN (best then ranks NaN after every number); a row whose logits are all -infinity
- * has logp -infinity.  Results of a row do not depend on what other rows hold.
+ * are left out.  Up to 32 rows (64 in fp32, or where the weights would have to be copied) x and the
+ * weights are read as they stand.  With more, tensors whose rows are whole 16-byte units, 16-byte
+ * aligned and at most 4 MiB apart are; others, and those that are taken as terms, are copied to the
+ * workspace (weights in pieces).  Where few rows and classes leave the GPU idle, sums over parts of n
+ * go to the workspace, at most 64 MiB.  The logits of one call differ from those of a call of
+ * another size by their sums' roundings; best is the lowest of classes whose logits round alike, or one
+ * as good to within that.  A NaN or +infinity among a row's logits makes its logp and logs NaN (best
+ * then ranks NaN after every number); a row whose logits are all -infinity has logp -infinity.
+ * Results of a row do not depend on what other rows hold.
  *
  * Outputs must not overlap each other or an input.  Returns KAN_OK, KAN_ERR_INVALID_ARG (rows < 0
  * or > 2^20, classes < 1 or > 2^30, n < 1 or > 2^20, a stride below n, rows * x_stride or classes *
@@ -762,9 +766,10 @@ kan_status kan_linear_logprobs_workspace_bytes(kan_dtype dtype, int64_t rows, in
  *                (...), 16-byte aligned, overlapping no other argument; overwritten.  May be NULL
  *                with rows == 0.
  *
- * The logits are formed again, a piece of the vocabulary at a time.  dz is rounded to dtype between
- * the products (at most 2^-8 of it in bf16, the precision of the products' operands), everything else is
- * binary32, summed in a fixed order (deterministic).  An ignored row gives 0 to dx and nothing to
+ * The logits are formed again, a piece of the vocabulary at a time (of up to 8 rows, 16 in fp32, all
+ * at once).  With more than 8 rows of bf16, dz is rounded to bf16 between the products (half a step,
+ * 2^-8 of it: the precision of the products' operands); of fp32 rows it goes on as three bf16 terms,
+ * which hold it.  Everything else is binary32, summed in a fixed order (deterministic).  An ignored row gives 0 to dx and nothing to
  * dweight, whatever x holds there.  A target that is neither a class nor ignore_index makes its
  * row of dx and all of dweight NaN, and so does a row whose logp is NaN.  Infinite weights and
  * inputs give NaN where 0 multiplies them.

@@ -5,6 +5,21 @@
 //   logp_b = z_bt - m - log s,  best_b = the lowest v with z_bv = m
 //   dz_bv = dlogp_b ([v = t_b] - p_bv),  p = exp(z - m - log s)
 //   dx = scale dz W,  dW = scale dz^T X
+//
+// Forward.  Many rows: tiles of 256 x 256 logits (kan_tile.h) on the matrix cores, each reduced in
+// registers to its rows' maximum, sum and best class, 8 bytes (and 4) a row and tile; a second kernel
+// joins a row's parts.  The workgroups stay, one a CU, and begin a tile's loads before the tile
+// ahead of it is reduced.  8192 x 2048 -> 131072 bf16 3.6 ms, 1.22 PFLOP/s; 2001 x 1001 -> 50001, whose
+// rows have to be copied first (37 us), 250 us, six turns of the GPU by big tiles and a seventh by
+// small ones.  Up to 32 (64) rows: weights straight from memory into 16 x 16 products, x in LDS, bound
+// by the reads (1 x 1024 -> 131072 bf16 45 us, 6.0 TB/s).  Few tiles: sums over parts of k in memory.
+//
+// Gradient.  The logits' tiles again, as dz in memory, 512 MB of it (and of copied weights) at a
+// time, of which the two products are made: dx over the classes, dW over the rows, in the same
+// tiles, where too few fill the GPU over parts of k that are added after it.  That dz is written once
+// and read twice takes less than to make the logits twice: at 8192 x 2048 -> 131072 bf16 the three
+// products take 1.05, 0.89 and 0.89 ms for each quarter of the classes, 11.3 ms in all, 1.17 PFLOP/s.
+// Few rows: both products in one pass over the weights on the vector ALUs.
 #include "kan_head.h"
 
 #include <algorithm>

@@ -1,5 +1,5 @@
 // kan_rows.h -- device helpers of the kernels that work on rows (layer norm, log
-// probabilities): 16-byte loads and stores at any alignment, and sums and maxima over
+// probabilities, embedding): 16-byte loads and stores at any alignment, and sums and maxima over
 // groups of lanes.
 #pragma once
 

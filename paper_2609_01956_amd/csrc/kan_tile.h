@@ -6,7 +6,10 @@
 // (16 bytes per lane, no registers between), into one of two buffers; a step is 64 KB for a tile of
 // 256 x 256.  One barrier a step, before the last quarter of its products, tells that the next
 // step has arrived and that all waves have read this one, whose buffer then takes the loads of
-// the step after the next.  Fragments are read a quarter ahead of their products.
+// the step after the next.  Fragments are read a quarter ahead of their products, each read (and load)
+// between two of them: in front of all, the reads keep the matrix cores waiting (8192 x 8192 x 8192
+// 1.31 against 1.35 PFLOP/s).  A wave that waits at the barrier has a lower priority than one that
+// goes on (2%).
 //
 // In LDS:
 //   by rows  128 bytes a row, its eight 16-byte chunks at chunk ^ (row >> 1 & 7): sixteen lanes that
@@ -15,16 +18,23 @@
 //            for 16 lanes), whose four rows stand in different quarters of the banks, 64-byte
 //            blocks at block ^ (k & 3)
 // What lies past an operand's end is 0 (the buffer's bounds).  By rows, k must be a whole number of
-// 16-byte chunks; rows are 16-byte aligned in both, and end with a chunk.  By k, columns past the end hold what follows:
-// they reach outputs past the end only.
+// 16-byte chunks; rows are 16-byte aligned in both, and end with a chunk.  By k, columns past the end
+// hold what follows: they reach outputs past the end only.
 //
 // Each wave holds RP x RQ tiles of 32 x 32: a lane's accumulators are 16 values of p (in fours of
 // neighbours) for one q, so that sums over p stay in the lane.
 //
-// Measured on MI355X, 8192 x 8192, bf16, 256 x 256 tiles: k = 8192 1.21 PFLOP/s, 2048 1.06; without
-// any loads, in LDS or to it, 1.61: the products alone hold the card at its power limit.  Steps of
-// half the size in a ring of five, four in flight: 1.18 and 1.00.  Four waves of 128 x 128: 1.17
-// and 0.99; tiles of 128 x 128, two workgroups a CU: 1.03 and 0.94.
+// Measured on MI355X, random bf16, 256 x 256 tiles, with the head's sums of exponentials (PFLOP/s;
+// of zeros, which take less power; a library's product of the same shape):
+//   8192 x 8192 x k = 8192     1.32-1.35 (1.82; 1.61-1.64, of zeros 2.27)
+//   8192 x 131072 x k = 2048   1.23-1.25 (1.59; 1.35-1.40, 1.61)
+//   8192 x 32768 x k = 1024    1.13-1.17 (1.45; 1.29, 1.65)
+// Random operands hold the card at its power limit, zeros show the waits that are left.  Per step the
+// LDS gives 192 KB of fragments and takes 64 KB of loads, as many of its clocks as the matrix cores need.
+// Tried: a ring of five steps of half the size, four in flight, 2-6% slower; four waves of 128 x 128,
+// which read a third less, 7% slower in the products (their one wave a SIMD waits alone), and their
+// accumulators leave the logits' sums no registers; the barrier after two or four products of its
+// quarter 2 and 3% slower; tiles of 128 x 128, two workgroups a CU, 15%.
 #pragma once
 
 #include "kan_device.h"
@@ -107,47 +117,50 @@ struct Side {
         }
     }
 
-    // The loads of the step of segment `seg` that begins at k (of `end`; none past it: zeros) to LDS
-    // byte dst.
-    __device__ __forceinline__ void issue(const Operand& o, int seg, int64_t k, int64_t end, int wave,
-                                          uint32_t dst) const {
+    // The loads of the step of segment `seg` that begins at k (of `end`; none past it: zeros): what
+    // they have in common, and each, to the step at LDS byte dst.
+    struct Loads {
+        u32x4 rsrc;
+        uint32_t at;
+        int bytes;  // of the step's k
+    };
+    __device__ __forceinline__ Loads loads(const Operand& o, int seg, int64_t k, int64_t end) const {
         const char* at = o.at + (MODE == kByRows ? 0 : k * o.stride) +
                          (int64_t)(o.terms >> 4 * seg & 15) * o.plane;
         const int64_t there = end < o.k ? end : o.k;
-        const int rows = MODE == kByRows ? o.left : (int)(there - k < K ? there - k : K);
+        const int rows = MODE == kByRows ? (k < end ? o.left : 0) : (int)(there - k < K ? there - k : K);
         // (bounds are kept by 4 bytes: by k, the last row to the end of its last chunk)
         const int64_t width = MODE == kByRows ? end * ES : ((int64_t)o.left * ES + 15) & ~15;
         const uint64_t base = reinterpret_cast<uint64_t>(at);
-        const u32x4 rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu,
-                            rows > 0 ? (uint32_t)((int64_t)(rows - 1) * o.stride + width) : 0u,
-                            (uint32_t)kBufferWord3};
-        const int bytes = (int)(end - k < K ? end - k : K) * ES;  // of the step's k
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            uint32_t v = from[i];
-            if constexpr (MODE == kByRows) {
-                const int c = tail ^ (((wave * LOADS + i) & 1) * 64);
-                v = c >= bytes ? 0x80000000u : v;
-            }
-            dma16(rsrc, v, MODE == kByRows ? (uint32_t)(k * ES) : 0u, dst + (wave * LOADS + i) * 1024);
+        Loads l;
+        l.rsrc = u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu,
+                       rows > 0 ? (uint32_t)((int64_t)(rows - 1) * o.stride + width) : 0u,
+                       (uint32_t)kBufferWord3};
+        l.at = MODE == kByRows && k < end ? (uint32_t)(k * ES) : 0u;
+        l.bytes = (int)(end - k < K ? end - k : K) * ES;
+        return l;
+    }
+    __device__ __forceinline__ void issue(const Loads& l, int i, int wave, uint32_t dst) const {
+        uint32_t v = from[i];
+        if constexpr (MODE == kByRows) {
+            const int c = tail ^ (((wave * LOADS + i) & 1) * 64);
+            v = c >= l.bytes ? 0x80000000u : v;
         }
+        dma16(l.rsrc, v, l.at, dst + (wave * LOADS + i) * 1024);
     }
 
-    // The fragments of a quarter of a step at src.
-    __device__ __forceinline__ void fetch(const char KAN_LDS* src, int quarter, u32x4 (&f)[R]) const {
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            if constexpr (MODE == kByRows) {
-                f[i] = *(const u32x4 KAN_LDS*)(src + read[0] + chunk[quarter] + i * 32 * 128);
-            } else {
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                const char KAN_LDS* p = src + read[i] + quarter * 16 * ROW;
-                const u32x2 lo = __builtin_bit_cast(
-                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KAN_LDS*)p));
-                const u32x2 hi = __builtin_bit_cast(
-                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KAN_LDS*)(p + 4 * ROW)));
-                f[i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
-            }
+    // Fragment i of a quarter of a step at src.
+    __device__ __forceinline__ u32x4 fetch(const char KAN_LDS* src, int quarter, int i) const {
+        if constexpr (MODE == kByRows) {
+            return *(const u32x4 KAN_LDS*)(src + read[0] + chunk[quarter] + i * 32 * 128);
+        } else {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            const char KAN_LDS* p = src + read[i] + quarter * 16 * ROW;
+            const u32x2 lo = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KAN_LDS*)p));
+            const u32x2 hi = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 KAN_LDS*)(p + 4 * ROW)));
+            return u32x4{lo[0], lo[1], hi[0], hi[1]};
         }
     }
 
@@ -195,13 +208,6 @@ struct Tile {
                                                          __uint_as_float(b[i]), c, 0, 0, 0);
         }
     }
-    __device__ __forceinline__ void products(const u32x4 (&a)[RP], const u32x4 (&b)[RQ]) {
-#pragma unroll
-        for (int i = 0; i < RP; ++i)
-#pragma unroll
-            for (int j = 0; j < RQ; ++j) multiply(a[i], b[j], acc[i][j]);
-    }
-
     // The loads of the first step of a tile over k from `at` to `end`, to the first STEP bytes of
     // lds (which no wave reads any more), ahead of `run`.
     __device__ __forceinline__ void start(char KAN_LDS* lds, const Operand& p, const Operand& q,
@@ -209,8 +215,12 @@ struct Tile {
         const int lane = threadIdx.x & 63, wave = wave_of();
         sp.place(lane, wave, wave % WP, p.stride);
         sq.place(lane, wave, wave / WP, q.stride);
-        sp.issue(p, 0, at, end, wave, byte_of(lds));
-        sq.issue(q, 0, at, end, wave, byte_of(lds) + SideP::BYTES);
+        const auto lp = sp.loads(p, 0, at, end);
+        const auto lq = sq.loads(q, 0, at, end);
+#pragma unroll
+        for (int i = 0; i < SideP::LOADS; ++i) sp.issue(lp, i, wave, byte_of(lds));
+#pragma unroll
+        for (int i = 0; i < SideQ::LOADS; ++i) sq.issue(lq, i, wave, byte_of(lds) + SideP::BYTES);
     }
 
     // The sum over k from `at` to `end`, after `start` with the same arguments.  lds: BYTES.
@@ -226,38 +236,68 @@ struct Tile {
         // (the segments of a step's k follow one another: their terms are read from L2 again)
         int64_t k = SEGS > 1 ? at : at + K;
         int seg = SEGS > 1 ? 1 : 0;
-        const auto issue = [&](uint32_t dst) {
-            if (k >= end) return;
-            sp.issue(p, seg, k, end, wave, dst);
-            sq.issue(q, seg, k, end, wave, dst + SideP::BYTES);
+        typename SideP::Loads lp;
+        typename SideQ::Loads lq;
+        const auto next = [&] {
+            lp = sp.loads(p, seg, k, end);
+            lq = sq.loads(q, seg, k, end);
             if (++seg >= SEGS) seg = 0, k += K;
         };
-        issue(base + STEP);
+        constexpr int LOADS = SideP::LOADS + SideQ::LOADS;
+        const auto issue = [&](int i, uint32_t dst) {
+            if (i < SideP::LOADS) sp.issue(lp, i, wave, dst);
+            else sq.issue(lq, i - SideP::LOADS, wave, dst + SideP::BYTES);
+        };
+        next();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) issue(i, base + STEP);
         u32x4 a[2][RP], b[2][RQ];
-        const auto fetch = [&](const char KAN_LDS* src, int quarter, int to) {
-            sp.fetch(src, quarter, a[to]);
-            sq.fetch(src + SideP::BYTES, quarter, b[to]);
+        const auto fetch = [&](const char KAN_LDS* src, int quarter, int to, int i) {
+            if (i < RP) a[to][i] = sp.fetch(src, quarter, i);
+            else b[to][i - RP] = sq.fetch(src + SideP::BYTES, quarter, i - RP);
         };
         arrive();
-        fetch(lds, 0, 0);
+#pragma unroll
+        for (int i = 0; i < RP + RQ; ++i) fetch(lds, 0, 0, i);
         int cur = 0;
+        // (between the matrix instructions, which one after the other keep the matrix cores busy: the
+        // reads of the next quarter, and the loads)
+        constexpr int PRODUCTS = RP * RQ;
         for (int steps = SEGS * (int)((end - at + K - 1) / K); steps > 0; --steps) {
 #pragma unroll
-            for (int c = 0; c < 3; ++c) {
-                fetch(lds + cur, c + 1, (c + 1) & 1);
-                products(a[c & 1], b[c & 1]);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int c = 0; c < 4; ++c) {
+                if (c == 3) {
+                    next();
+                    __builtin_amdgcn_sched_barrier(0);
+                    __builtin_amdgcn_s_setprio(0);
+                    arrive();
+                    __builtin_amdgcn_s_setprio(1);
+                }
+#pragma unroll
+                for (int m = 0; m < PRODUCTS; ++m) {
+                    // (after the last step: of what the buffer held before, for nothing)
+#pragma unroll
+                    for (int i = 0; i < RP + RQ; ++i)
+                        if (turn_of(i, RP + RQ, PRODUCTS) == m)
+                            fetch(c < 3 ? lds + cur : lds + STEP - cur, (c + 1) & 3, (c + 1) & 1, i);
+                    if (c == 3) {
+#pragma unroll
+                        for (int i = 0; i < LOADS; ++i)
+                            if (turn_of(i, LOADS, PRODUCTS) == m) issue(i, base + cur);
+                    }
+                    multiply(a[c & 1][m / RQ], b[c & 1][m % RQ], acc[m / RQ][m % RQ]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-            arrive();
-            __builtin_amdgcn_sched_barrier(0);
-            issue(base + cur);
-            // (after the last step: of what the buffer held before, for nothing)
-            fetch(lds + STEP - cur, 0, 0);
-            products(a[1], b[1]);
-            __builtin_amdgcn_sched_barrier(0);
             cur = STEP - cur;
         }
+        __builtin_amdgcn_s_setprio(0);
         arrive();
+    }
+
+    // Of n reads or loads between products, the product before which number i goes.
+    static constexpr int turn_of(int i, int n, int products) {
+        return n <= products ? i : i * products / n;
     }
 
     // This thread, computed anew after the loop (so that nothing derived from it lives across it).

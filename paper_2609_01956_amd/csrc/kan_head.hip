@@ -1433,7 +1433,7 @@ struct HeadGradPlan {
 HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
     HeadGradPlan p = {};
     Arena arena = {static_cast<char*>(ws)};
-    // (16 rows of bf16: 326 us against the tiles' 252 at 1024 -> 131072, bound by the multiply-adds)
+    // (16 rows of bf16: 326 us against the tiles' 240 at 1024 -> 131072, bound by the multiply-adds)
     p.few = s.rows <= (s.es == 2 ? kOuterRows / 2 : kOuterRows);
     if (p.few) {
         // (about 1024 workgroups, each wave at least 16 classes)

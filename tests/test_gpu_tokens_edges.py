@@ -311,3 +311,21 @@ def test_targets_nearly_certain(rows, V):
     want = -torch.expm1(-logs.double()).to(device()) * d.double()
     got = dw[t, torch.arange(rows, device=device())].double()
     below((got - want).abs(), want.abs() * (2.0 ** -22 + 6 * U))
+
+
+@pytest.mark.parametrize("rows,classes,n,dt",
+                         [(200, 45000, 40, F32),  # big tiles on the fp32 instruction
+                          (300, 20000, 1000, F32), (300, 20000, 1000, BF16),  # dW by both tiles
+                          (17000, 200, 1000, F32), (17000, 200, 1000, BF16),  # dx by both
+                          (17000, 40000, 1000, BF16)])  # added up over pieces
+def test_both_tiles(rows, classes, n, dt):
+    """More big tiles than fill the GPU a whole number of turns: the rest by small ones."""
+    x, w, t, d = make(rows, classes, n, 0, 0, 0, dt, 28)
+    scale = 0.5 * n ** -0.5
+    say(f"linear head by both tiles {rows} {classes} {n} {dt}")
+    logp, stats, _ = kb.linear_logprobs(x, w, t, scale=scale)
+    _, lp, _, _, _ = forward64(x, w, t, scale)
+    z, dz = gradient64(x, w, t, stats, d, scale)
+    below((logp.double() - lp).abs(), 2 * ztol(z, n) + 4e-6 + 4 * U * lp.abs())
+    dx, dw = kb.linear_logprobs_backward(x, w, t, stats, d, scale=scale)
+    check_gradients(x, w, dx, dw, z, dz, d, scale, dt)

@@ -10,9 +10,9 @@
 //
 // All of it is bound by the memory where it is large.  65536 x 1024 bf16 rows of 50001 tokens: 32 us,
 // 134 MB written at 4.2 TB/s while the table's rows come from it once and from the caches after.  The
-// gradient of 65536 x 4096 bf16 for 131072 tokens, 377 us: 0.54 GB read and the rows that occur written
-// in 160 us, the others in 170 (6.3 TB/s), sorting 30.  65536 x 256 fp32 for 50001, 61 us, is bound by
-// what its six launches wait for: 25 us sort, 18 sum chunks, 8 + 8 join and write the rest.
+// gradient of 65536 x 4096 bf16 for 131072 tokens, 367 us: 0.54 GB read and the rows that occur written
+// in 160 us, the others in 170 (6.3 TB/s), sorting 30.  65536 x 256 fp32 for 50001, 58 us, is bound by
+// what its six launches wait for: 25 us sort, 18 sum chunks, 5 + 7 join and write the rest.
 #include <algorithm>
 
 #include "kan_head.h"
@@ -618,37 +618,59 @@ __global__ void __launch_bounds__(256) embed_chunk_kernel(EmbedSumArgs a) {
     }
 }
 
-// The sums of a later level's chunks from those of the level before, a wave for each 64 units.
+// The sums of a later level's chunks from those of the level before, a workgroup for each 64 units: of
+// either token (the one at the chunk's first entry, the one at its last) in four waves, a quarter of
+// the sums in each.  (All in one wave: 8.4 us, so 4.9, for 64 chunks of 256 fp32; 17.9 and 8.6 for 64
+// of 4096 bf16.)
+constexpr int kJoinWaves = 4;  // of a token
 template <int V>
-__global__ void __launch_bounds__(256) embed_join_kernel(EmbedSumArgs a, int level) {
+__global__ void __launch_bounds__(128 * kJoinWaves) embed_join_kernel(EmbedSumArgs a, int level) {
+    __shared__ float sums[2][kJoinWaves - 1][V][64];
     const int64_t rows = a.g.rows, size = chunk_size(level), fine = chunk_size(level - 1);
     const int64_t items = (rows + size - 1) / size * a.blocks;
     const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int slot = wave / kJoinWaves, share = wave % kJoinWaves;
     // short rows leave lanes over: each strand of them takes a part of the sums
     int width = 64;
     while (width >= 2 * (int)a.units) width /= 2;
     const int strands = 64 / width;
-    for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items;
-         item += (int64_t)gridDim.x * 4) {
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t chunk = item / a.blocks;
         const uint32_t u = (uint32_t)(item - chunk * a.blocks) * 64 + (lane & (width - 1));
         const int64_t first = chunk * size, end = first + size < rows ? first + size : rows;
         const uint32_t head = a.sorted[first].key, last = a.sorted[end - 1].key;
-        for (int slot = 0; slot < 2; ++slot) {
-            const uint32_t k = slot == 0 ? head : last;
-            if (k >= (uint32_t)a.g.classes || (slot == 1 && k == head)) continue;
+        const uint32_t k = slot == 0 ? head : last;
+        bool live = k < (uint32_t)a.g.classes && !(slot == 1 && k == head);
+        float s[V] = {};
+        if (live) {
             const int2 span = a.span[k];
-            if (span.y - span.x <= size) continue;
-            const int64_t from = span.x > first ? span.x : first, to = span.y < end ? span.y : end;
-            const int c0 = (int)(from / fine), c1 = (int)((to - 1) / fine);
-            const int each = (c1 - c0 + strands) / strands, mine = c0 + lane / width * each;
-            float s[V] = {};
-            if (u < a.units) add_parts(a, level - 1, mine, min(mine + each - 1, c1), span.x, u, s);
-            for (int o = width; o < 64; o *= 2)
+            live = span.y - span.x > size;
+            if (live) {
+                const int64_t from = span.x > first ? span.x : first, to = span.y < end ? span.y : end;
+                const int c0 = (int)(from / fine), c1 = (int)((to - 1) / fine);
+                const int all = (c1 - c0 + kJoinWaves) / kJoinWaves, q0 = c0 + share * all;
+                const int q1 = min(q0 + all - 1, c1);
+                const int each = (q1 - q0 + strands) / strands, mine = q0 + lane / width * each;
+                if (u < a.units)
+                    add_parts(a, level - 1, mine, min(mine + each - 1, q1), span.x, u, s);
+                for (int o = width; o < 64; o *= 2)
 #pragma unroll
-                for (int i = 0; i < V; ++i) s[i] += __shfl_xor(s[i], o);
-            if (u < a.units && lane < width) store_part(a, level, 2 * chunk + slot, u, s);
+                    for (int i = 0; i < V; ++i) s[i] += __shfl_xor(s[i], o);
+            }
         }
+        __syncthreads();  // (the sums of the item before are read)
+        if (share > 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) sums[slot][share - 1][i][lane] = s[i];
+        }
+        __syncthreads();
+        if (share > 0 || !live || u >= a.units || lane >= width) continue;
+#pragma unroll
+        for (int q = 0; q < kJoinWaves - 1; ++q)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[i] += sums[slot][q][i][lane];
+        store_part(a, level, 2 * chunk + slot, u, s);
     }
 }
 
@@ -755,6 +777,7 @@ int groups_of(int64_t n) { return (int)std::min<int64_t>(n, kMaxGroups); }
 
 // Workgroups of each kind in the last launch: they go on by strides.
 constexpr int kRestGroups = 1 << 13;
+constexpr int kJoinGroups = 1 << 16;
 // Bytes (read and written) of the table that a pass of sorting may fill beside it, what one launch
 // sorts taking about two passes' time; workgroups of such a launch.  4096 x 1024 bf16 of 131072 tokens:
 // without 71 us, 32 MB 67, 64 MB 61, 96 MB 55; 65536 x 256 fp32 of 50001 62, 59, 59, 59; with a base,
@@ -897,7 +920,8 @@ hipError_t embed_grad(const EmbedGradArgs& g, void* ws, hipStream_t s) {
     }
     for (int l = 1; l < p.levels; ++l) {
         embed_join_kernel<kVec<TP>>
-            <<<groups_of(div_up(div_up(g.rows, chunk_size(l)) * e.blocks, 4)), 256, 0, s>>>(e, l);
+            <<<(int)std::min<int64_t>(div_up(g.rows, chunk_size(l)) * e.blocks, kJoinGroups),
+               128 * kJoinWaves, 0, s>>>(e, l);
         KAN_TRY(hipGetLastError());
     }
     if (g.rows > kRun)

@@ -971,44 +971,61 @@ __global__ void __launch_bounds__(256) head_zero_kernel(T* out, int64_t n) {
 
 // ------------------------------------------------------------ rows laid out for the tiles
 
-// Rows of n elements copied to rows of `to` elements (a multiple of 16 bytes), 0 past n; 0
-// throughout for rows whose target is `ignore` (targets null: none).
+// Rows of n elements to be laid out as rows of `to` elements (a multiple of 16 bytes), 0 past n; 0
+// throughout for rows whose target is `ignore` (targets null: none).  x null: no rows.
+struct Rows {
+    const void* x;
+    int64_t stride, rows;
+    int n, to;
+    void* out;
+    const int64_t* targets;
+    int64_t ignore;
+    int groups;  // workgroups that do it
+};
+// Of two in one launch the one that this workgroup does, and its place among those that do.
+__device__ __forceinline__ const Rows& rows_of(const Rows& a, const Rows& b, int* group) {
+    const bool first = (int)blockIdx.x < a.groups;
+    *group = first ? blockIdx.x : blockIdx.x - a.groups;
+    return first ? a : b;
+}
+
+// Copied.
 template <typename T>
-__global__ void __launch_bounds__(256) head_pack_kernel(const T* x, int64_t stride, int64_t rows,
-                                                        int n, T* out, int to,
-                                                        const int64_t* targets, int64_t ignore) {
+__global__ void __launch_bounds__(256) head_pack_kernel(Rows one, Rows two) {
     constexpr int V = kVec<T>;
-    const int units = to / V;
-    const int64_t all = rows * units;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
-         i += (int64_t)gridDim.x * 256) {
+    int group;
+    const Rows& r = rows_of(one, two, &group);
+    const int units = r.to / V;
+    const int64_t all = r.rows * units;
+    for (int64_t i = (int64_t)group * 256 + threadIdx.x; i < all; i += (int64_t)r.groups * 256) {
         const int64_t row = i / units;
         const int c = (int)(i - row * units) * V;
         u32x4 v = {0, 0, 0, 0};
-        if (targets == nullptr || targets[row] != ignore) v = chunk_of(x + row * stride, c, n);
-        *reinterpret_cast<u32x4*>(out + row * to + c) = v;
+        if (r.targets == nullptr || r.targets[row] != r.ignore)
+            v = chunk_of(static_cast<const T*>(r.x) + row * r.stride, c, r.n);
+        *reinterpret_cast<u32x4*>(static_cast<T*>(r.out) + row * r.to + c) = v;
     }
 }
 
-// fp32 rows of n elements as kTerms terms, rows of `to` elements (a multiple of 16 bytes), 0 past n; 0
-// throughout for rows whose target is `ignore` (targets null: none).
-__global__ void __launch_bounds__(256) head_terms_kernel(const float* x, int64_t stride, int64_t rows,
-                                                         int n, uint16_t* out, int to,
-                                                         const int64_t* targets, int64_t ignore) {
-    const int units = to / 8;
-    const int64_t all = rows * units;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
-         i += (int64_t)gridDim.x * 256) {
+// fp32 as kTerms terms.
+__global__ void __launch_bounds__(256) head_terms_kernel(Rows one, Rows two) {
+    int group;
+    const Rows& r = rows_of(one, two, &group);
+    const int units = r.to / 8;
+    const int64_t all = r.rows * units;
+    for (int64_t i = (int64_t)group * 256 + threadIdx.x; i < all; i += (int64_t)r.groups * 256) {
         const int64_t row = i / units;
         const int c = (int)(i - row * units) * 8;
         float v[8] = {}, finite[8];
-        if (targets == nullptr || targets[row] != ignore) {
-            const u32x4 a = chunk_of(x + row * stride, c, n), b = chunk_of(x + row * stride, c + 4, n);
+        if (r.targets == nullptr || r.targets[row] != r.ignore) {
+            const float* const x = static_cast<const float*>(r.x) + row * r.stride;
+            const u32x4 a = chunk_of(x, c, r.n), b = chunk_of(x, c + 4, r.n);
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(a[k]), v[4 + k] = __uint_as_float(b[k]);
         }
-        u32x4* const at = reinterpret_cast<u32x4*>(out + row * to + c);
-        const int64_t plane = rows * to / 8;
+        u32x4* const at =
+            reinterpret_cast<u32x4*>(static_cast<uint16_t*>(r.out) + row * r.to + c);
+        const int64_t plane = r.rows * r.to / 8;
         u32x4 h = narrow(v);
         float w[8];
         widen(h, w);
@@ -1127,7 +1144,8 @@ ProductPlan product_plan(int64_t np, int64_t nq, int64_t k, bool terms) {
     for (const bool big : {true, false}) {
         const int64_t tiles = tiles_of(np, nq, big);
         // (1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 15, ..: a few are enough)
-        const int64_t most = std::min(steps / 4, 8 * kFillTiles / std::max<int64_t>(1, tiles));
+        const int64_t most = std::min({steps, steps_of(k, es, terms) / 4,
+                                       8 * kFillTiles / std::max<int64_t>(1, tiles)});
         for (int64_t splits = 1; splits == 1 || splits <= std::min<int64_t>(most, 2 * kFillTiles);
              splits += std::max<int64_t>(1, splits / 4)) {
             const double time =
@@ -1225,18 +1243,15 @@ HeadPlan head_plan(const HeadShape& s, void* ws) {
 
 int grid_of(int64_t items, int per) { return (int)std::min<int64_t>(div_up(items, per), 1 << 16); }
 
-// Rows copied (T), or as terms of fp32 ones.
+// Rows copied (T), or as terms of fp32 ones, both in one launch.
 template <typename T>
-hipError_t pack(bool terms, const void* x, int64_t stride, int64_t rows, int n, void* out, int to,
-                const int64_t* targets, int64_t ignore, hipStream_t st) {
-    if (terms) {
-        head_terms_kernel<<<grid_of(rows * (to / 8), 256), 256, 0, st>>>(
-            static_cast<const float*>(x), stride, rows, n, static_cast<uint16_t*>(out), to, targets,
-            ignore);
-        return hipGetLastError();
-    }
-    head_pack_kernel<T><<<grid_of(rows * (to / kVec<T>), 256), 256, 0, st>>>(
-        static_cast<const T*>(x), stride, rows, n, static_cast<T*>(out), to, targets, ignore);
+hipError_t pack(bool terms, Rows one, Rows two, hipStream_t st) {
+    for (Rows* r : {&one, &two})
+        r->groups = r->x == nullptr ? 0 : grid_of(r->rows * (r->to / (terms ? 8 : kVec<T>)), 256);
+    const int groups = one.groups + two.groups;
+    if (groups == 0) return hipSuccess;
+    if (terms) head_terms_kernel<<<groups, 256, 0, st>>>(one, two);
+    else head_pack_kernel<T><<<groups, 256, 0, st>>>(one, two);
     return hipGetLastError();
 }
 
@@ -1381,18 +1396,19 @@ hipError_t head(const HeadShape& s, const HeadArgs& a, void* ws, hipStream_t st)
         t.z.scale = a.scale;
         t.z.targets = a.targets;
         t.out = p.out;
-        if (p.xp != nullptr)
-            KAN_TRY(pack<T>(p.terms, a.x, s.xstride, s.rows, s.n, p.xp, p.to, nullptr, 0, st));
         for (int64_t first = 0; first < s.classes; first += p.piece) {
             const int64_t here = std::min<int64_t>(s.classes - first, p.piece);
             t.z.first = (int)first;
             t.z.classes = (int)here;
             t.z.w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
+            Rows x = {}, w = {};
+            if (p.xp != nullptr && first == 0) x = {a.x, s.xstride, s.rows, s.n, p.to, p.xp};
             if (p.wp != nullptr) {
-                KAN_TRY(pack<T>(p.terms, t.z.w, s.wstride, here, s.n, p.wp, p.to, nullptr, 0, st));
+                w = {t.z.w, s.wstride, here, s.n, p.to, p.wp};
                 t.z.w = p.wp;
                 t.z.wplane = p.terms ? here * p.to * es : 0;
             }
+            KAN_TRY(pack<T>(p.terms, x, w, st));
             if (p.pz.splits > 0) {
                 KAN_TRY(sums<T>(p.pz, t.z, p.z, st));
                 const HeadRowsArgs r = {p.z, p.pz.splits, s.rows, s.classes, a.scale, a.targets,
@@ -1551,18 +1567,20 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
     g.zstride = p.zstride;
     g.zplane = s.rows * p.zstride;
     const int64_t zbytes = p.zstride * es;
-    if (p.xp != nullptr)
-        KAN_TRY(pack<T>(terms, a.x, s.xstride, s.rows, s.n, p.xp, p.to, a.targets, a.ignore, st));
     for (int64_t first = 0; first < s.classes; first += p.piece) {
         const int64_t here = std::min<int64_t>(s.classes - first, p.piece);
         g.z.w = static_cast<const char*>(a.w) + first * s.wstride * s.es;
         g.z.first = (int)first;
         g.z.classes = (int)here;
+        Rows x = {}, w = {};
+        if (p.xp != nullptr && first == 0)
+            x = {a.x, s.xstride, s.rows, s.n, p.to, p.xp, a.targets, a.ignore};
         if (p.wp != nullptr) {
-            KAN_TRY(pack<T>(terms, g.z.w, s.wstride, here, s.n, p.wp, p.to, nullptr, 0, st));
+            w = {g.z.w, s.wstride, here, s.n, p.to, p.wp};
             g.z.w = p.wp;
             g.z.wplane = terms ? here * p.to * es : 0;
         }
+        KAN_TRY(pack<T>(terms, x, w, st));
         if (p.pz.splits > 0) {
             KAN_TRY(sums<T>(p.pz, g.z, p.z, st));
             head_dz_kernel<sizeof(T) == 4>

@@ -1504,10 +1504,11 @@ hipError_t gradient_tiles(const HeadGradTileArgs& g, bool big, hipStream_t st) {
     return hipGetLastError();
 }
 
-// (many parts go over 16 lanes a value: 62 parts of 1442 values 37 us in one lane each)
+// (many parts of few values go over 16 lanes a value: 62 parts of 1442 values 37 us in one lane each; 15
+// of a million 26 us, so 10)
 template <typename T>
 hipError_t sum(const float* acc, int splits, int64_t n, float scale, void* out, hipStream_t st) {
-    if (splits >= 12)
+    if (splits >= 12 && n < kFillTiles * 1024)
         head_gather_kernel<T><<<grid_of(n, 16), 256, 0, st>>>(acc, splits, n, scale,
                                                               static_cast<T*>(out));
     else

@@ -19,7 +19,8 @@
 // tiles, where too few fill the GPU over parts of k that are added after it.  That dz is written once
 // and read twice takes less than to make the logits twice: at 8192 x 2048 -> 131072 bf16 the three
 // products take 1.05, 0.89 and 0.89 ms for each quarter of the classes, 11.3 ms in all, 1.17 PFLOP/s.
-// Few rows: both products in one pass over the weights on the vector ALUs.
+// Few rows: both products in one pass over the weights on the vector ALUs; up to 64 in fp32: dz by the
+// forward's kernel of few rows.
 #include "kan_head.h"
 
 #include <algorithm>
@@ -930,6 +931,20 @@ __global__ void __launch_bounds__(256) head_rows_kernel(HeadRowsArgs a) {
     if (a.best != nullptr) a.best[row] = b.at == kNoIndex ? 0 : b.at;
 }
 
+// dz of eight classes of a row from c0 on, as head_grad_kernel leaves it.
+template <bool TERMS>
+__device__ __forceinline__ void leave_dz(const HeadGradTileArgs& g, int64_t row, int c0, float (&y)[8]) {
+    uint16_t* out = static_cast<uint16_t*>(g.dz) + row * g.zstride + c0;
+    for (int term = 0; term < (TERMS ? kDzTerms : 1); ++term, out += g.zplane) {
+        const u32x4 h = narrow(y);
+        *reinterpret_cast<u32x4*>(out) = h;
+        float w[8];
+        widen(h, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] -= w[k];
+    }
+}
+
 // The same for the gradient: dz as head_grad_kernel leaves it, 16 bytes a lane.
 template <bool TERMS>
 __global__ void __launch_bounds__(256) head_dz_kernel(HeadGradTileArgs g, const float* z, int splits) {
@@ -951,15 +966,23 @@ __global__ void __launch_bounds__(256) head_dz_kernel(HeadGradTileArgs g, const 
             const float t = __builtin_fmaf(v, a.scale, -r.offset<TERMS>());
             y[k] = c == r.target ? target_of<TERMS>(r, t) : dz_of<TERMS>(r, t);
         }
-        uint16_t* out = static_cast<uint16_t*>(g.dz) + row * g.zstride + c0;
-        for (int term = 0; term < (TERMS ? kDzTerms : 1); ++term, out += g.zplane) {
-            const u32x4 h = narrow(y);
-            *reinterpret_cast<u32x4*>(out) = h;
-            float w[8];
-            widen(h, w);
+        leave_dz<TERMS>(g, row, c0, y);
+    }
+}
+
+// Up to 64 rows' dz in fp32, [classes][pitch], as terms by rows.
+__global__ void __launch_bounds__(256) head_turn_kernel(HeadGradTileArgs g, const float* dz, int pitch) {
+    const int64_t all = g.zstride / 8 * pitch;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t unit = i / pitch;
+        const int row = (int)(i - unit * pitch), c0 = (int)unit * 8;
+        if (row >= g.z.rows) continue;
+        float y[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] -= w[k];
-        }
+        for (int k = 0; k < 8; ++k)
+            y[k] = c0 + k < g.z.classes ? dz[(int64_t)(c0 + k) * pitch + row] : 0.0f;
+        leave_dz<true>(g, row, c0, y);
     }
 }
 
@@ -1441,6 +1464,7 @@ struct HeadGradPlan {
     int to;
     void *xp, *wp;           // packed rows, or null
     void* dz;
+    int thin;                // groups of 16 rows whose dz are made in fp32 first, at z; or 0
     float *dx, *dw, *z;      // sums over k in parts, or null
     ProductPlan px, pw, pz;  // (pz.splits > 0: the logits')
     size_t bytes;
@@ -1478,7 +1502,14 @@ HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
     if (p.terms || !s.xs || dw) p.xp = arena.take(s.rows * packed);
     if (wp) p.wp = arena.take(p.piece * packed);
     p.dz = arena.take(s.rows * p.zstride * zes);
-    if (p.piece >= s.classes) p.pz = sums_plan(s.rows, s.classes, s.n, p.terms);
+    // (weights read once in fp32, not six times as terms: 22 x 1004 -> 44307 149 us, so
+    // 70 and 5)
+    if (p.terms && s.rows <= kThinMost) {
+        p.thin = (int)div_up(s.rows, 16);
+        p.z = arena.take<float>(p.piece * p.thin * 16 * 4);
+    } else if (p.piece >= s.classes) {
+        p.pz = sums_plan(s.rows, s.classes, s.n, p.terms);
+    }
     if (p.pz.splits > 0) p.z = arena.take<float>((int64_t)p.pz.splits * s.rows * s.classes * 4);
     if (dx) {
         p.px = product_plan(s.n, s.rows, p.zstride, p.terms);
@@ -1582,7 +1613,21 @@ hipError_t head_grad(const HeadShape& s, const HeadGradArgs& a, void* ws, hipStr
             g.z.wplane = terms ? here * p.to * es : 0;
         }
         KAN_TRY(pack<T>(terms, x, w, st));
-        if (p.pz.splits > 0) {
+        if (p.thin > 0) {
+            if constexpr (sizeof(T) == 4) {
+                HeadShape part = s;
+                part.classes = (int)here;
+                const HeadThinArgs t =
+                    thin_args(part, a.x, static_cast<const char*>(a.w) + first * s.wstride * s.es,
+                              a.scale, a.targets);
+                KAN_TRY(p.thin == 2   ? thin<T, 2, kDz>(part, t, g, p.z, st)
+                        : p.thin == 3 ? thin<T, 3, kDz>(part, t, g, p.z, st)
+                                      : thin<T, 4, kDz>(part, t, g, p.z, st));
+                head_turn_kernel<<<grid_of(p.zstride / 8 * p.thin * 16, 256), 256, 0, st>>>(
+                    g, p.z, p.thin * 16);
+                KAN_TRY(hipGetLastError());
+            }
+        } else if (p.pz.splits > 0) {
             KAN_TRY(sums<T>(p.pz, g.z, p.z, st));
             head_dz_kernel<sizeof(T) == 4>
                 <<<grid_of(s.rows * (p.zstride / 8), 256), 256, 0, st>>>(g, p.z, p.pz.splits);

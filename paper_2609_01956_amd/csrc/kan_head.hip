@@ -336,7 +336,8 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
     __shared__ Best red[kThinWaves][ROWS];
     static_assert(kThinLds + sizeof(red) <= 160 << 10, "LDS of a CU");
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r16 = lane & 15, quad = lane >> 4;
-    const T* const x = static_cast<const T*>(a.x);
+    const int row0 = blockIdx.y * ROWS, rows = min(a.rows - row0, ROWS);
+    const T* const x = static_cast<const T*>(a.x) + row0 * a.xstride;
     const T* const w = static_cast<const T*>(a.w);
     const int chunks = (a.n + V - 1) / V;
     const int width = min((chunks + 7) & ~7, SLICE);  // chunks per row in LDS, a multiple of 8
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
         for (int i = threadIdx.x; i < ROWS * width; i += 64 * kThinWaves) {
             const int row = i / width, c = i - row * width;
             u32x4 v = {0, 0, 0, 0};
-            if (row < a.rows && (c0 + c) < chunks)
+            if (row < rows && (c0 + c) < chunks)
                 v = chunk_of(x + row * a.xstride, (c0 + c) * V, a.n);
             *reinterpret_cast<u32x4*>(lds + ((size_t)row * width + (c ^ (row & 7))) * 16) = v;
         }
@@ -355,8 +356,8 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         best[t] = Best{kNegInf, 0.0f, kNoIndex};
-        target[t] = WHAT != kDz && t * 16 + r16 < a.rows ? a.targets[t * 16 + r16] : -1;
-        if (WHAT == kDz) of[t] = row_grad(grad, t * 16 + r16);
+        target[t] = WHAT != kDz && t * 16 + r16 < rows ? a.targets[row0 + t * 16 + r16] : -1;
+        if (WHAT == kDz) of[t] = row_grad(grad, row0 + t * 16 + r16);
     }
     const bool once = chunks <= width;
     if (once) {
@@ -453,7 +454,7 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
             for (int i = 0; i < 4; ++i) {
                 const int p = p0 + quad * 4 + i;
                 const float z = p < a.classes ? acc[t][i] * a.scale : kNegInf;
-                if (p == target[t] && p < a.classes) a.out.target[t * 16 + r16] = z;
+                if (p == target[t] && p < a.classes) a.out.target[row0 + t * 16 + r16] = z;
                 if (BEST && (z > m || (z == kNegInf && at == kNoIndex && p < a.classes))) at = p;
                 m = __builtin_fmaxf(m, z);
                 acc[t][i] = z;
@@ -474,10 +475,10 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
     }
     __syncthreads();
     const int row = threadIdx.x;
-    if (row < a.rows) {
+    if (row < rows) {
         Best b = red[0][row];
         for (int i = 1; i < kThinWaves; ++i) b = join(b, red[i][row]);
-        leave(a.out, blockIdx.x, a.rows, row, b);
+        leave(a.out, blockIdx.x, a.rows, row0 + row, b);
     }
 }
 
@@ -1095,6 +1096,10 @@ constexpr int kBig = 256, kSmall = 128;  // a tile's sides
 // copy of the weights or, in fp32, multiply 128 rows (64 x 1024 -> 131072 bf16 61 us, by tiles 50;
 // 64 x 1024 -> 50001 fp32 91, by tiles 131).
 constexpr int kThinRows = 32, kThinMost = 64;
+// fp32 rows up to which that is done in groups of kThinMost where the tiles would need a copy of the
+// weights and terms do not pay: 156 x 935 -> 35856 169 us, by tiles 277; without a copy tiles are
+// as fast at 65 rows and faster above (256 x 1024 -> 50001 252 us against 302).
+constexpr int kThinGroups = 256;
 // Bytes of a piece's intermediate tensors.
 constexpr int64_t kPieceBytes = INT64_C(512) << 20;
 constexpr int64_t kPieceClasses = 1 << 20, kPieceTiles = 1 << 20;
@@ -1232,7 +1237,8 @@ int thin_groups(const HeadShape& s) {
 HeadPlan head_plan(const HeadShape& s, void* ws) {
     HeadPlan p = {};
     Arena arena = {static_cast<char*>(ws)};
-    p.thin = s.rows <= (s.es == 2 && s.ws ? kThinRows : kThinMost);
+    p.thin = s.rows <= (s.es == 2 && s.ws ? kThinRows : kThinMost) ||
+             (s.es == 4 && !s.ws && s.rows <= kThinGroups && !by_terms(s));
     p.terms = !p.thin && by_terms(s);
     p.to = (int)up(s.n, p.terms ? 8 : 16 / s.es);
     const int64_t packed = (int64_t)p.to * (p.terms ? kTerms * 2 : s.es);  // bytes of a row
@@ -1294,16 +1300,18 @@ hipError_t thin(const HeadShape& s, const HeadThinArgs& a, const HeadGradTileArg
                                 (size_t)(split ? kThinWaves * NT * 1024 : 0));
     const auto kernel =
         split ? head_thin_kernel<T, NT, WHAT, true> : head_thin_kernel<T, NT, WHAT, false>;
-    kernel<<<thin_groups(s), 64 * kThinWaves, lds, st>>>(a, g, dz);
+    const dim3 groups(thin_groups(s), (unsigned)div_up(a.rows, 16 * NT));
+    kernel<<<groups, 64 * kThinWaves, lds, st>>>(a, g, dz);
     return hipGetLastError();
 }
 template <typename T, int WHAT>
 hipError_t thin(const HeadShape& s, const HeadThinArgs& a, hipStream_t st) {
     const HeadGradTileArgs none = {};
-    return a.rows <= 16   ? thin<T, 1, WHAT>(s, a, none, nullptr, st)
-           : a.rows <= 32 ? thin<T, 2, WHAT>(s, a, none, nullptr, st)
-           : a.rows <= 48 ? thin<T, 3, WHAT>(s, a, none, nullptr, st)
-                          : thin<T, 4, WHAT>(s, a, none, nullptr, st);
+    const int64_t rows = div_up(a.rows, div_up(a.rows, kThinMost));  // of workgroups' own
+    return rows <= 16   ? thin<T, 1, WHAT>(s, a, none, nullptr, st)
+           : rows <= 32 ? thin<T, 2, WHAT>(s, a, none, nullptr, st)
+           : rows <= 48 ? thin<T, 3, WHAT>(s, a, none, nullptr, st)
+                        : thin<T, 4, WHAT>(s, a, none, nullptr, st);
 }
 HeadThinArgs thin_args(const HeadShape& s, const void* x, const void* w, float scale,
                        const int64_t* targets) {

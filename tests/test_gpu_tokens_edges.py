@@ -329,3 +329,18 @@ def test_both_tiles(rows, classes, n, dt):
     below((logp.double() - lp).abs(), 2 * ztol(z, n) + 4e-6 + 4 * U * lp.abs())
     dx, dw = kb.linear_logprobs_backward(x, w, t, stats, d, scale=scale)
     check_gradients(x, w, dx, dw, z, dz, d, scale, dt)
+
+
+@pytest.mark.parametrize("rows,classes,n", [(65, 3001, 33), (156, 9001, 135), (250, 700, 1001)])
+def test_few_rows_in_groups(rows, classes, n):
+    """fp32 rows past one group of 64 with weights at odd addresses."""
+    x, w, t, _ = make(rows, classes, n, 0, 0, 0, F32, 29)
+    scale = n ** -0.5
+    say(f"linear head in groups of rows {rows} {classes} {n}")
+    logp, stats, best = kb.linear_logprobs(x, w, t, scale=scale, best=True)
+    z, lp, m, logs, _ = forward64(x, w, t, scale)
+    tol = ztol(z, n)
+    below((logp.double() - lp).abs(), 2 * tol + 4e-6 + 4 * U * lp.abs())
+    below((stats[:, 0].double() - m).abs(), tol + U * m.abs())
+    below((stats[:, 1].double() - logs).abs(), 2 * tol + 4e-6 + 4 * U * logs.abs())
+    below(m - z.gather(1, best[:, None])[:, 0], 2 * tol)

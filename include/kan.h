@@ -724,14 +724,15 @@ kan_status kan_embedding_backward_workspace_bytes(int64_t rows, int32_t classes,
  * x and weight are of dtype; products and sums are binary32 (the sum before the scale, too, has
  * to stay in its range).  Large fp32 products take both operands as three bf16 terms, which hold
  * all 24 bits of values from 2^-109 on; products of their smallest terms, below 2^-25 of the whole,
- * are left out.  Up to 32 rows (64 in fp32, or where the weights would have to be copied, 256
- * in fp32 where they would) x and the weights are read as they stand.  With more, tensors whose rows are whole 16-byte units, 16-byte
- * aligned and at most 4 MiB apart are; others, and those that are taken as terms, are copied to the
- * workspace (weights in pieces).  Where few rows and classes leave the GPU idle, sums over parts of n
- * go to the workspace, at most 64 MiB.  The logits of one call differ from those of a call of
- * another size by their sums' roundings; best is the lowest of classes whose logits round alike, or one
- * as good to within that.  A NaN or +infinity among a row's logits makes its logp and logs NaN (best
- * then ranks NaN after every number); a row whose logits are all -infinity has logp -infinity.
+ * are left out.  Up to 32 rows (64 in fp32, or where the weights would have to be copied, 256 in
+ * fp32 where they would) x and the weights are read as they stand.  With more, tensors whose
+ * rows are whole 16-byte units, 16-byte aligned and at most 4 MiB apart are; others, and those
+ * that are taken as terms, are copied to the workspace (weights in pieces).  Where few rows and
+ * classes leave the GPU idle, sums over parts of n go to the workspace, at most 64 MiB.  The
+ * logits of one call differ from those of a call of another size by their sums' roundings; best
+ * is the lowest of classes whose logits round alike, or one as good to within that.  A NaN or
+ * +infinity among a row's logits makes its logp and logs NaN (best then ranks NaN after every
+ * number); a row whose logits are all -infinity has logp -infinity.
  * Results of a row do not depend on what other rows hold.
  *
  * Outputs must not overlap each other or an input.  Returns KAN_OK, KAN_ERR_INVALID_ARG (rows < 0

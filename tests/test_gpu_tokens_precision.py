@@ -1,0 +1,53 @@
+"""Token operators where values are far from each other, on the GPU against the formulas in float64:
+targets nearly certain.
+
+Rows of the identity make the logits the weights, and dz the weights' gradient; the logits are exact
+in either type, and so are the stats' m.  u = 2^-24; bf16 rounds a gradient once (2^-8 of it)."""
+import math
+
+import pytest
+
+from paper_2609_01956_amd import binding as kb
+from gpu_common import device, say, torch
+from test_gpu_head import below, U
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 0.0, BF16: 2.0 ** -8}
+
+
+def head_of(rows, V, n, dt, m, other):
+    """x, weight, targets, stats and dlogp of logits m for the targets and `other` elsewhere, and logs."""
+    g = torch.Generator(device=device())
+    g.manual_seed(rows + V)
+    at = torch.arange(rows, device=device())
+    x = torch.zeros(rows, n, dtype=dt, device=device())
+    x[at, at] = 1.0
+    t = torch.randperm(V, device=device(), generator=g)[:rows]
+    w = torch.zeros(V, n, dtype=dt, device=device())
+    w[:, :rows] = other
+    w[t, at] = m
+    logs = float(torch.tensor(math.log1p((V - 1) * math.exp(other - m)), dtype=F32))
+    stats = torch.tensor([[m, logs]], device=device()).expand(rows, 2).contiguous()
+    d = -torch.rand(rows, device=device(), generator=g) - 0.1
+    return x, w, t, stats, d, logs
+
+
+# few rows, tiles of both sizes, sums over parts of n
+SIZES = [(6, 10, 7), (16, 20, 17), (40, 300, 41), (16, 1000, 4096), (600, 4000, 601),
+         (2000, 20000, 2001)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("m,other", [(14.0, 0.0), (30.0, 10.0), (30.0, 9.0)])
+@pytest.mark.parametrize("rows,V,n", SIZES)
+def test_targets_nearly_certain(rows, V, n, m, other, dt):
+    """1 - p of a target with p nearly 1, for given stats, to its own size (2^-22 of the series, two
+    roundings of dz and as many of its terms and sum; in bf16 the gradient's), not to that of p."""
+    x, w, t, stats, d, logs = head_of(rows, V, n, dt, m, other)
+    say(f"linear head targets nearly certain {rows} {V} {n} {m} {other} {dt}")
+    _, dw = kb.linear_logprobs_backward(x, w, t, stats, d, need_dx=False)
+    want = -math.expm1(-logs) * d.double()
+    got = dw[t, torch.arange(rows, device=device())].double()
+    below((got - want).abs(), want.abs() * (HALF[dt] + 2.0 ** -22 + 6 * U))

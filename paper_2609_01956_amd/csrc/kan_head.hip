@@ -253,12 +253,6 @@ constexpr int kDzTerms = 3;
 struct RowGrad {
     float m, logs, d;
     int target;  // from the launch's first class on
-    // what is subtracted from the logit with its scale's rounding (in bf16 p's own rounding hides
-    // that of the exponential's argument)
-    template <bool EXACT>
-    __device__ __forceinline__ float offset() const {
-        return EXACT ? m : m + logs;
-    }
 };
 __device__ __forceinline__ RowGrad row_grad(const HeadGradTileArgs& g, int64_t row) {
     // (rows that have no gradient: p = 0, whatever their logits are)
@@ -278,11 +272,14 @@ __device__ __forceinline__ RowGrad row_grad(const HeadGradTileArgs& g, int64_t r
     r.target = (int)c - g.z.first;
     return r;
 }
-// -d p for the logit less its offset.
+// -d p for the logit less m (of which its scale's rounding is the only one: m + logs taken off at once
+// would cost p |m| 2^-24 of it).  Where bf16 follows, which hides the rounding of the exponential's
+// argument, log2 e and logs are in that argument's one operation.
 template <bool EXACT>
 __device__ __forceinline__ float dz_of(const RowGrad& r, float t) {
     return -r.d * (EXACT ? exp_exact(__builtin_fmaxf(t - r.logs, -1e4f))
-                         : exp_of(__builtin_fmaxf(t, -1e4f)));
+                         : __builtin_amdgcn_exp2f(__builtin_fmaxf(
+                               __builtin_fmaf(t, kLog2e, -r.logs * kLog2e), -1e4f)));
 }
 
 // dz of the target for the logit less m.  (By the series in bf16 too: with p near 1, d - d p keeps few
@@ -441,7 +438,7 @@ __global__ void __launch_bounds__(64 * kThinWaves) head_thin_kernel(HeadThinArgs
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int p = p0 + quad * 4 + i;
-                    const float v = __builtin_fmaf(acc[t][i], a.scale, -of[t].template offset<true>());
+                    const float v = __builtin_fmaf(acc[t][i], a.scale, -of[t].m);
                     float y = dz_of<true>(of[t], v);
                     if (p == of[t].target) y = target_of(of[t], v);
                     if (p < a.classes) dz[((int64_t)p * NT + t) * 16 + r16] = y;
@@ -568,7 +565,7 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileA
 #pragma unroll
         for (int j = 0; j < Tl::RQ; ++j) {
             const RowGrad& r = row[j];
-            const float o = -r.offset<TERMS>();
+            const float o = -r.m;
             const bool here = r.target >= p0 && r.target < p0 + Tl::BP;
             const int target = r.target - p1;
             float own = 0.0f;  // the target's logit, then its dz
@@ -578,7 +575,7 @@ __global__ void __launch_bounds__(Tl::THREADS, 2) head_grad_kernel(HeadGradTileA
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
                         own = target == Tl::p_step(i, e) ? t.acc[i][j][e] : own;
-                own = target_of(r, __builtin_fmaf(own, scale, -r.m));
+                own = target_of(r, __builtin_fmaf(own, scale, o));
             }
 #pragma unroll
             for (int i = 0; i < Tl::RP; ++i)
@@ -964,8 +961,8 @@ __global__ void __launch_bounds__(256) head_dz_kernel(HeadGradTileArgs g, const 
             y[k] = 0.0f;
             if (c >= a.classes) continue;
             const float v = sum_of(z + row * a.classes + c, splits, step);
-            y[k] = c == r.target ? target_of(r, __builtin_fmaf(v, a.scale, -r.m))
-                                 : dz_of<TERMS>(r, __builtin_fmaf(v, a.scale, -r.offset<TERMS>()));
+            const float t = __builtin_fmaf(v, a.scale, -r.m);
+            y[k] = c == r.target ? target_of(r, t) : dz_of<TERMS>(r, t);
         }
         leave_dz<TERMS>(g, row, c0, y);
     }

@@ -1,5 +1,5 @@
 """Token operators where values are far from each other, on the GPU against the formulas in float64:
-targets nearly certain.
+targets nearly certain, logits far from 0.
 
 Rows of the identity make the logits the weights, and dz the weights' gradient; the logits are exact
 in either type, and so are the stats' m.  u = 2^-24; bf16 rounds a gradient once (2^-8 of it)."""
@@ -17,21 +17,24 @@ F32, BF16 = torch.float32, torch.bfloat16
 HALF = {F32: 0.0, BF16: 2.0 ** -8}
 
 
-def head_of(rows, V, n, dt, m, other):
-    """x, weight, targets, stats and dlogp of logits m for the targets and `other` elsewhere, and logs."""
+def head_of(rows, V, n, dt, m, other, base=0.0):
+    """x, weight, targets, stats and dlogp of logits `base` + m for the targets and + other elsewhere,
+    the logits' distance from m, and logs."""
     g = torch.Generator(device=device())
     g.manual_seed(rows + V)
     at = torch.arange(rows, device=device())
     x = torch.zeros(rows, n, dtype=dt, device=device())
     x[at, at] = 1.0
+    x[:, rows] = 1.0
     t = torch.randperm(V, device=device(), generator=g)[:rows]
     w = torch.zeros(V, n, dtype=dt, device=device())
     w[:, :rows] = other
     w[t, at] = m
+    w[:, rows] = base
     logs = float(torch.tensor(math.log1p((V - 1) * math.exp(other - m)), dtype=F32))
-    stats = torch.tensor([[m, logs]], device=device()).expand(rows, 2).contiguous()
+    stats = torch.tensor([[base + m, logs]], device=device()).expand(rows, 2).contiguous()
     d = -torch.rand(rows, device=device(), generator=g) - 0.1
-    return x, w, t, stats, d, logs
+    return x, w, t, stats, d, other - m, logs
 
 
 # few rows, tiles of both sizes, sums over parts of n
@@ -45,9 +48,26 @@ SIZES = [(6, 10, 7), (16, 20, 17), (40, 300, 41), (16, 1000, 4096), (600, 4000, 
 def test_targets_nearly_certain(rows, V, n, m, other, dt):
     """1 - p of a target with p nearly 1, for given stats, to its own size (2^-22 of the series, two
     roundings of dz and as many of its terms and sum; in bf16 the gradient's), not to that of p."""
-    x, w, t, stats, d, logs = head_of(rows, V, n, dt, m, other)
+    x, w, t, stats, d, _, logs = head_of(rows, V, n, dt, m, other)
     say(f"linear head targets nearly certain {rows} {V} {n} {m} {other} {dt}")
     _, dw = kb.linear_logprobs_backward(x, w, t, stats, d, need_dx=False)
     want = -math.expm1(-logs) * d.double()
     got = dw[t, torch.arange(rows, device=device())].double()
     below((got - want).abs(), want.abs() * (HALF[dt] + 2.0 ** -22 + 6 * U))
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("base", [0.0, 2.0 ** 20, -(2.0 ** 20)])
+@pytest.mark.parametrize("rows,V,n", SIZES)
+def test_logits_far_from_zero(rows, V, n, base, dt):
+    """p of logits near a large m: it depends on their distances t alone.  t is exact; t - logs, its
+    product with log2 e and the exponential are off by 3 u (|t| + logs) + 4 u; 2^-22 for the fp32 form's,
+    and 6 roundings of dz, its terms and their sums."""
+    x, w, t, stats, d, far, logs = head_of(rows, V, n, dt, 14.0, 12.0, base)
+    say(f"linear head far from zero {rows} {V} {n} {base} {dt}")
+    _, dw = kb.linear_logprobs_backward(x, w, t, stats, d, need_dx=False)
+    at = torch.arange(rows, device=device())
+    want = (-math.exp(far - logs) * d.double()).expand(V, rows).clone()
+    want[t, at] = -math.expm1(-logs) * d.double()
+    below((dw[:, :rows].double() - want).abs(),
+          want.abs() * (HALF[dt] + 2.0 ** -22 + (3 * (abs(far) + logs) + 10) * U))

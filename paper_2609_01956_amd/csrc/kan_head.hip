@@ -509,7 +509,8 @@ __global__ void __launch_bounds__(256) head_join_kernel(HeadJoinArgs a) {
     }
     if (strand != 0 || row >= a.rows) return;
     b = red[r];
-    const float logs = logf(b.s);
+    // (a tile takes m = +infinity from sums that are finite before the scale, which leaves it an s of 0)
+    const float logs = b.m == -kNegInf ? __builtin_nanf("") : logf(b.s);
     const int64_t t = a.targets[row];
     float lp = 0.0f;
     if (t != a.ignore) {

@@ -1,8 +1,9 @@
 """Token operators where values are far from each other, on the GPU against the formulas in float64:
-targets nearly certain, logits far from 0.
+targets nearly certain, logits far from 0 and out of range.
 
-Rows of the identity make the logits the weights, and dz the weights' gradient; the logits are exact
-in either type, and so are the stats' m.  u = 2^-24; bf16 rounds a gradient once (2^-8 of it)."""
+In the first two, rows of the identity make the logits the weights, and dz the weights' gradient;
+the logits are exact in either type, and so are the stats' m.  u = 2^-24; bf16 rounds a gradient once
+(2^-8 of it)."""
 import math
 
 import pytest
@@ -71,3 +72,35 @@ def test_logits_far_from_zero(rows, V, n, base, dt):
     want[t, at] = -math.expm1(-logs) * d.double()
     below((dw[:, :rows].double() - want).abs(),
           want.abs() * (HALF[dt] + 2.0 ** -22 + (3 * (abs(far) + logs) + 10) * U))
+
+
+# tiles of both sizes throughout (whole ones), sums over parts of n, few rows
+WHOLE = [(2048, 16384, 16), (100, 1024, 16), (600, 4096, 16), (64, 256, 4096), (128, 512, 2048),
+         (5, 1024, 16), (40, 1024, 16)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("rows,V,n", WHOLE)
+def test_logits_that_the_scale_takes_out_of_range(rows, V, n, dt):
+    """Finite sums whose scaled logits overflow: +infinity among them makes a row's logp and logs NaN,
+    and its dx and all of dweight; -infinity takes no part."""
+    g = torch.Generator(device=device())
+    g.manual_seed(31)
+    x = torch.zeros(rows, n, dtype=dt, device=device())
+    x[:, 1] = 1.0
+    x[2, 0], x[3, 0] = 2.0 ** 63, -(2.0 ** 63)
+    w = torch.zeros(V, n, dtype=dt, device=device())
+    w[:, 1] = torch.randint(-8, 9, (V,), device=device(), generator=g) / 8
+    w[V - 1, 0] = 2.0 ** 63
+    t = torch.randint(0, V - 1, (rows,), device=device(), generator=g)
+    say(f"linear head out of range {rows} {V} {n} {dt}")
+    logp, stats, _ = kb.linear_logprobs(x, w, t, scale=8.0)
+    assert bool(logp[2].isnan()) and bool(stats[2, 1].isnan())
+    keep = torch.arange(rows, device=device()) != 2
+    z = x.double() @ w.double().t() * 8.0
+    z[3, V - 1] = -math.inf
+    lp = torch.log_softmax(z, 1).gather(1, t[:, None])[:, 0]
+    # (the logits are exact: the sum of exponentials and its logarithm)
+    below((logp.double() - lp)[keep].abs(), 4e-6 + 4 * U * lp[keep].abs())
+    dx, dw = kb.linear_logprobs_backward(x, w, t, stats, -torch.ones_like(logp), scale=8.0)
+    assert bool(dx[2].isnan().all()) and bool(dw.isnan().all()) and not bool(dx[keep].isnan().any())

@@ -262,7 +262,7 @@ __device__ __forceinline__ RowGrad row_grad(const HeadGradTileArgs& g, int64_t r
     const float m = g.stats[2 * row], logs = g.stats[2 * row + 1], d = g.dlogp[row];
     if (c == g.ignore) return r;
     // (a target that is no class, NaN and infinite logits show in the row's gradient)
-    r.d = c < 0 || c >= g.all || m != m || logs != logs ? __builtin_nanf("") : d;
+    r.d = c < 0 || c >= g.all || m != m || m == -kNegInf || logs != logs ? __builtin_nanf("") : d;
     if (m == kNegInf && logs == kNegInf && r.d == r.d) {
         r.d = 0.0f;
         return r;

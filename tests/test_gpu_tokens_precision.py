@@ -104,3 +104,24 @@ def test_logits_that_the_scale_takes_out_of_range(rows, V, n, dt):
     below((logp.double() - lp)[keep].abs(), 4e-6 + 4 * U * lp[keep].abs())
     dx, dw = kb.linear_logprobs_backward(x, w, t, stats, -torch.ones_like(logp), scale=8.0)
     assert bool(dx[2].isnan().all()) and bool(dw.isnan().all()) and not bool(dx[keep].isnan().any())
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("logs", [-math.inf, 0.0, 1.0, math.nan])
+@pytest.mark.parametrize("rows,V,n", WHOLE)
+def test_stats_of_infinite_logits(rows, V, n, logs, dt):
+    """m = +infinity in the stats, whatever logs is beside it: the row's dx and all of dweight are NaN,
+    the other rows' dx as without it."""
+    g = torch.Generator(device=device())
+    g.manual_seed(32)
+    x = torch.randn(rows, n, device=device(), generator=g).to(dt)
+    w = torch.randn(V, n, device=device(), generator=g).to(dt)
+    t = torch.randint(0, V, (rows,), device=device(), generator=g)
+    say(f"linear head stats of infinite logits {rows} {V} {n} {logs} {dt}")
+    logp, stats, _ = kb.linear_logprobs(x, w, t, scale=0.1)
+    d = -torch.ones_like(logp)
+    want, _ = kb.linear_logprobs_backward(x, w, t, stats, d, scale=0.1)
+    stats[2, 0], stats[2, 1] = math.inf, logs
+    dx, dw = kb.linear_logprobs_backward(x, w, t, stats, d, scale=0.1)
+    keep = torch.arange(rows, device=device()) != 2
+    assert bool(dx[2].isnan().all()) and bool(dw.isnan().all()) and torch.equal(dx[keep], want[keep])

@@ -1506,12 +1506,12 @@ HeadGradPlan head_grad_plan(const HeadShape& s, bool dx, bool dw, void* ws) {
     const int64_t here = std::min<int64_t>(p.piece, s.classes);
     // (a copy without what ignored rows hold: 0 times it need not be 0)
     if (p.terms || !s.xs || dw) p.xp = arena.take(s.rows * packed);
-    if (wp) p.wp = arena.take(p.piece * packed);
-    p.dz = arena.take(s.rows * p.zstride * zes);
     // (weights read once in fp32, not six times as terms: 22 x 1004 -> 44307 149 us, so
-    // 70 and 5)
-    if (p.terms && s.rows <= kThinMost) {
-        p.thin = (int)div_up(s.rows, 16);
+    // 70 and 5; their terms are dx's alone then)
+    if (p.terms && s.rows <= kThinMost) p.thin = (int)div_up(s.rows, 16);
+    if (wp && (dx || p.thin == 0)) p.wp = arena.take(p.piece * packed);
+    p.dz = arena.take(s.rows * p.zstride * zes);
+    if (p.thin > 0) {
         p.z = arena.take<float>(p.piece * p.thin * 16 * 4);
     } else if (p.piece >= s.classes) {
         p.pz = sums_plan(s.rows, s.classes, s.n, p.terms);

@@ -1,5 +1,6 @@
 """Token operators at the sizes at which their kernels go another way, on the GPU against the formulas
-in float64: fp32 gradients of few rows over a vocabulary in several pieces."""
+in float64: runs of tokens around a chunk of sorted entries and around a group of chunks, and fp32
+gradients of few rows over a vocabulary in several pieces."""
 import pytest
 
 from paper_2609_01956_amd import binding as kb
@@ -8,8 +9,58 @@ from test_gpu_head import check_gradients, gradient64
 
 pytestmark = pytest.mark.gpu
 
-F32 = torch.float32
+F32, BF16 = torch.float32, torch.bfloat16
+TYPES = [(F32, F32), (BF16, BF16), (BF16, F32)]  # of the rows, of the table
 
+
+def check_runs(counts, n, dt, tt, seed):
+    """Tokens 0, 1, .. so many times each, shuffled, with whole numbers, which fp32 adds exactly in any
+    order: equal to the definition's, rounded once; with a base, in place too."""
+    g = torch.Generator(device=device())
+    g.manual_seed(seed)
+    counts = torch.tensor(counts, device=device())
+    t = torch.repeat_interleave(torch.arange(counts.numel(), device=device()), counts)
+    t = t[torch.randperm(t.numel(), device=device(), generator=g)]
+    dy = torch.randint(-4, 5, (t.numel(), n), device=device(), generator=g).to(dt)
+    base = torch.randint(-4, 5, (counts.numel(), n), device=device(), generator=g).to(tt)
+    want = torch.zeros(counts.numel(), n, dtype=torch.float64, device=device())
+    want.index_add_(0, t, dy.double())
+    got = kb.embedding_backward(t, dy, counts.numel(), dtype=tt)
+    assert torch.equal(got, want.to(tt))
+    total = (want + base.double()).to(tt)
+    assert torch.equal(kb.embedding_backward(t, dy, counts.numel(), base=base), total)
+    inside = base.clone()
+    kb.embedding_backward(t, dy, counts.numel(), base=inside, out=inside)
+    assert torch.equal(inside, total)
+
+
+@pytest.mark.parametrize("dt,tt", TYPES)
+@pytest.mark.parametrize("n", [1, 5, 8, 40])
+def test_runs_around_a_chunk(dt, tt, n):
+    """Runs of 15, 16 and 17 entries (the most that one chunk sums, and the fewest that it does not)
+    and of about two chunks, at every offset from a chunk's first entry."""
+    say(f"embedding_backward runs around a chunk {dt} {tt} {n}")
+    for lead in range(17):
+        check_runs([lead, 15, 16, 17, 1, 31, 32, 33, 0, 16, 17, 15, 2, 48, 17, 17, 16, 16, 15], n, dt,
+                   tt, lead)
+
+
+@pytest.mark.parametrize("dt,tt", TYPES)
+@pytest.mark.parametrize("n", [3, 264])
+def test_runs_around_a_group_of_chunks(dt, tt, n):
+    """The same around 1024 entries, from which on a token's sums are themselves summed."""
+    say(f"embedding_backward runs around a group of chunks {dt} {tt} {n}")
+    for lead in (0, 1, 15, 16, 17, 1023):
+        check_runs([lead, 1023, 1024, 1025, 1, 1024, 2047, 2048, 2049, 16, 1024], n, dt, tt, lead)
+
+
+@pytest.mark.parametrize("dt,tt", TYPES)
+@pytest.mark.parametrize("rows", [15, 16, 17])
+def test_batches_around_a_chunk(dt, tt, rows):
+    """A batch of a chunk, and one token less and more: all of one token, and of two."""
+    say(f"embedding_backward batches around a chunk {dt} {tt} {rows}")
+    for first in (rows, 1, rows - 1, rows // 2):
+        check_runs([0, first, 0, rows - first], 9, dt, tt, first)
 
 
 def head_inputs(rows, classes, n, seed):

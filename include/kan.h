@@ -688,8 +688,8 @@ kan_status kan_embedding(kan_dtype dtype, kan_dtype table_dtype, int64_t rows, i
  *   workspace    caller-owned, workspace_bytes >= kan_embedding_backward_workspace_bytes(...),
  *                16-byte aligned, overlapping no other argument; overwritten
  *
- * Tokens are sorted; each row's sum is binary32, in an order that depends on the tokens alone
- * (deterministic), and rounded once with the base.  Returns as kan_embedding.
+ * Tokens are sorted; each row's sum is binary32, in an order that depends on the tokens, n and the
+ * dtypes alone (deterministic), and rounded once with the base.  Returns as kan_embedding.
  */
 kan_status kan_embedding_backward(kan_dtype dtype, kan_dtype table_dtype, int64_t rows,
                                   int32_t classes, int32_t n, const int64_t* tokens,

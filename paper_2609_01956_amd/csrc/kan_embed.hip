@@ -1,12 +1,13 @@
 // kan_embed.hip -- rows of a table for tokens, scaled, and the gradient of the table.
 //
 //   y_b = scale table[t_b]
-//   dtable_v = base_v + scale sum_{b: t_b = v} dy_b   (in rising order of b)
+//   dtable_v = base_v + scale sum_{b: t_b = v} dy_b
 //
 // The gradient sorts the tokens (stable, by digits of up to nine bits), so that a row's sum has
-// one order whatever runs when.  Tokens that occur often are summed in chunks of kRun sorted
-// entries first, each to a row of fp32 partial sums; then every row of the table is written once,
-// from its own few entries or from its chunks' sums.
+// one order whatever runs when: for the same tokens, n and types the same bits.  Up to kRun entries
+// are summed in rising order of b.  Tokens that occur more often are summed in chunks of kRun sorted
+// entries first, each to a row of fp32 partial sums, which are then added in a fixed order; every
+// row of the table is written once, from its own few entries or from its chunks' sums.
 //
 // All of it is bound by the memory where it is large.  65536 x 1024 bf16 rows of 50001 tokens: 32 us,
 // 134 MB written at 4.2 TB/s while the table's rows come from it once and from the caches after.  The
@@ -45,12 +46,6 @@ struct Piece {
             for (int i = 0; i < U; ++i) v[k * U + i] = u[i];
         }
     }
-    __device__ __forceinline__ void add(int c, int n, float (&s)[V]) {
-        float v[V];
-        value(c, n, v);
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[i] += v[i];
-    }
 };
 
 // Four bf16: 8 bytes, so that a lane's columns fill 16 bytes of an fp32 row.
@@ -72,12 +67,6 @@ struct Piece<uint16_t, 4> {
         const uint64_t r = raw >> (16 * past);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = __uint_as_float((uint32_t)(r >> (16 * i)) << 16);
-    }
-    __device__ __forceinline__ void add(int c, int n, float (&s)[4]) {
-        float v[4];
-        value(c, n, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] += v[i];
     }
 };
 
@@ -884,6 +873,7 @@ hipError_t embed_grad(const EmbedGradArgs& g, void* ws, hipStream_t s) {
                 sort_scan_kernel<<<kDigits / 64, 64, 0, s>>>(a);
                 KAN_TRY(hipGetLastError());
             }
+            // (beside the sort of more tiles it has not been tried: the last launch writes those rows)
             if (p.tiles <= kCountTiles) fill_next(p.tiles, 1);
             sort_scatter_kernel<<<p.tiles + a.fill.groups, kSortThreads, 0, s>>>(a);
             KAN_TRY(hipGetLastError());

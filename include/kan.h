@@ -768,12 +768,13 @@ kan_status kan_linear_logprobs_workspace_bytes(kan_dtype dtype, int64_t rows, in
  *                with rows == 0.
  *
  * The logits are formed again, a piece of the vocabulary at a time (of up to 8 rows, 16 in fp32, all
- * at once).  With more than 8 rows of bf16, dz is rounded to bf16 between the products (half a step,
- * 2^-8 of it: the precision of the products' operands); of fp32 rows it goes on as three bf16 terms,
- * which hold it.  Everything else is binary32, summed in a fixed order (deterministic).  An ignored row gives 0 to dx and nothing to
- * dweight, whatever x holds there.  A target that is neither a class nor ignore_index makes its
- * row of dx and all of dweight NaN, and so does a row whose logp is NaN.  Infinite weights and
- * inputs give NaN where 0 multiplies them.
+ * at once); dz of a target is formed from 1 - p, not from p.  With more than 8 rows of bf16, dz is
+ * rounded to bf16 between the products (half a step, 2^-8 of it: the precision of the products'
+ * operands); of more than 16 fp32 rows it goes on as three bf16 terms, which hold values from 2^-109
+ * to 2^127 in full.  Everything else is binary32, summed in a fixed order (deterministic).  An ignored
+ * row gives 0 to dx and nothing to dweight, whatever x holds there.  A target that is neither a class
+ * nor ignore_index makes its row of dx and all of dweight NaN, and so does a row whose logp is NaN or
+ * whose m is +infinity.  Infinite weights and inputs give NaN where 0 multiplies them.
  *
  * Outputs must not overlap each other or an input.  Returns as kan_linear_logprobs;
  * KAN_ERR_INVALID_ARG also without any output.
